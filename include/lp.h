@@ -65,6 +65,7 @@ typedef enum {
 } lp_status;
 
 enum { LP_F32 = 0, LP_F64 = 1 };                       /* dtype */
+enum { LP_BF16 = 2, LP_F16 = 3 };                      /* dtypes of layer steps, checkpoints and label heads only */
 enum { LP_DENSE = 0, LP_CONV3X3 = 1 };                 /* layer */
 enum { LP_TANH = 0, LP_RELU = 1, LP_SMOOTHRELU = 2, LP_IDENTITY = 3 }; /* activation sigma */
 enum { LP_RELAX_F = 0, LP_RELAX_FCF = 1, LP_RELAX_FCFCF = 2 }; /* MGRIT relaxation */
@@ -336,6 +337,96 @@ int32_t lp_vec_dot(int32_t dtype, size_t n, const void* x, const void* y, double
  * double. ws: device workspace of at least lp_workspace_bytes(prob, NULL) bytes. */
 int32_t lp_accuracy(const lp_problem* prob, int32_t nc, const void* uN, const void* W, const void* mu,
                     const void* c, double* acc, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- layer steps of any width, 8-bit checkpoints, heads over large vocabularies ----
+ * The layer of Section 2.2 for wide networks in 16-bit or fp32 types, one step per
+ * call, the network head for integer labels over a vocabulary whose logits are
+ * never stored, and activations kept in 8 bits for the way back. Arrays of
+ * floating-point values have the call's dtype (LP_F32, LP_BF16 or LP_F16; LP_F64
+ * returns LP_EUNSUPPORTED) unless stated; every sum is held in fp32 or more and
+ * rounded to the dtype once. Products run on the matrix cores. No call waits for
+ * the stream or reads anything back, so all can be captured into a graph; two
+ * calls or graphs that may overlap in time need workspaces of their own. Arrays
+ * must not overlap except where stated. Results are bitwise reproducible. Limits
+ * (LP_EUNSUPPORTED above them): B <= 2^24, widths <= 2^20, nc <= 2^24, and 2^35
+ * values per array. */
+
+/* One step y = r + h sigma(x W^T + b): x [B][ni], W [no][ni] (W[i][j] maps input
+ * j to output i), b [no], r and y [B][no]. */
+typedef struct {
+  int32_t abi_version;   /* must equal LP_ABI_VERSION */
+  int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16 */
+  int32_t act;           /* LP_TANH | LP_RELU | LP_SMOOTHRELU | LP_IDENTITY */
+  int32_t B;             /* rows, >= 0 (0: nothing to do; weight gradients are zero) */
+  int32_t ni, no;        /* input and output width, >= 1 */
+  double h;              /* factor of the activation, finite */
+} lp_step;
+
+/* Workspace bytes of lp_step_forward and lp_step_backward; 0 for an invalid step. */
+size_t lp_step_workspace_bytes(const lp_step* step);
+
+/* The step. b, r nullable. r may be x (the residual layer of Section 2.2, ni = no),
+ * another array, or y itself (updated in place); y must not be x. y8, ye
+ * (nullable, together): the 8-bit checkpoint of y is written too, the one that
+ * lp_checkpoint_store gives for it. A NaN pre-activation gives NaN under every
+ * activation. */
+int32_t lp_step_forward(const lp_step* step, const void* x, const void* W, const void* b, const void* r, void* y,
+                        int8_t* y8, uint8_t* ye, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of the step for dy [B][no]:
+ *   g  = sigma'(x W^T + b) dy      (the pre-activation is formed again, from x or its checkpoint;
+ *                                   g is rounded to the dtype for the next two products)
+ *   dx = h g W (+ dy with residual = 1, where r was x; needs ni = no)   [B][ni]
+ *   dW = h g^T x   [no][ni],   db = h sum_k g_k   [no]   (db from g before its rounding)
+ * The gradient of another r is dy itself. Exactly one of x and (x8, xe) is given,
+ * the other NULL. dx, dW, db nullable: not wanted. Outputs must not alias inputs. */
+int32_t lp_step_backward(const lp_step* step, const void* x, const int8_t* x8, const uint8_t* xe, const void* W,
+                         const void* b, const void* dy, int32_t residual, void* dx, void* dW, void* db, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* 8-bit checkpoint of activations x [B][q] (compare LP_STORE_CPOINTS, which keeps
+ * fewer rows): x8 [B][q] int8 and xe [B][ceil(q / 32)], one byte per 32 features
+ * of a row. With m the block's largest magnitude,
+ *   e = max(emin, floor(log2 m) - 6),  xe = e + 127,
+ *   x8 = the nearest whole number to x / 2^e (ties to even), at most 127 in magnitude;
+ * emin = -24 for LP_F16 and -126 otherwise. The values x8 2^e that lp_checkpoint_load
+ * gives are exact in every dtype; they differ from x by at most half of 2^e (by at
+ * most 2^e where |x| > 127.5 2^e). A block with an infinity or a NaN has xe = 255 and x8 = 0
+ * and reads back as NaN. */
+int32_t lp_checkpoint_store(int32_t dtype, int32_t B, int32_t q, const void* x, int8_t* x8, uint8_t* xe, void* stream);
+int32_t lp_checkpoint_load(int32_t dtype, int32_t B, int32_t q, const int8_t* x8, const uint8_t* xe, void* x,
+                           void* stream);
+
+/* Head of a network over a large vocabulary (compare lp_loss_terminal). */
+typedef struct {
+  int32_t abi_version;   /* must equal LP_ABI_VERSION */
+  int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16 */
+  int32_t B;             /* rows, >= 0 */
+  int32_t q;             /* features of a row, >= 1 */
+  int32_t nc;            /* classes, >= 1 */
+} lp_label_head;
+
+/* Workspace bytes of lp_loss_labels, with grad != 0 when any gradient is asked
+ * for; 0 for an invalid head. It grows with B nc / 16 at most, and holds the
+ * probabilities of one piece of the vocabulary at a time. */
+size_t lp_loss_labels_workspace_bytes(const lp_label_head* head, int32_t grad);
+
+/* Softmax cross-entropy of integer labels: z_k = W u_k + mu, u [B][q], W [nc][q],
+ * mu [nc] (nullable), labels [B] (int64). A row whose label lies outside
+ * 0..nc-1 has none and does not count; n is the number of rows that have one.
+ *   row[k] = log sum_j exp(z_kj) - z_k[label]   (fp32, 0 for a row without a label; nullable)
+ *   J[0]   = (1/n) sum_k row[k]                  (fp32 on the device; 0 if n = 0)
+ * and, each if not NULL (dmu needs mu), the gradients of gscale J (gscale: a loss
+ * scale, 1 otherwise):
+ *   du = (gscale/n) P W  [B][q],  dW = (gscale/n) P^T u  [nc][q],  dmu = (gscale/n) sum_k P_k  [nc],
+ * P = softmax(z) - onehot(label), rounded to the dtype for the two products (times
+ * 2^14 for LP_F16). Rows without a label have du = 0 and add nothing to dW and dmu,
+ * whatever u holds there (infinities and NaN too). A class with mu = -infinity has
+ * probability 0 and takes no part (a label on it: row = +infinity); with every class
+ * so the row is NaN. */
+int32_t lp_loss_labels(const lp_label_head* head, const void* u, const void* W, const void* mu, const int64_t* labels,
+                       double gscale, float* J, float* row, void* du, void* dW, void* dmu, void* ws, size_t ws_bytes,
+                       void* stream);
 
 /* ---- tracing (a profiling aid, not part of the method) ----
  * When enabled for a kernel kind, every launch of that kind records a pair of

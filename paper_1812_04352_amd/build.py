@@ -19,7 +19,7 @@ OBJ = os.path.join(HERE, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["lp_host.cpp", "lp_common.hip", "lp_loss.hip", "lp_dense_f32.hip", "lp_dense_narrow.hip",
+SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_step_host.cpp", "lp_host.cpp", "lp_common.hip", "lp_loss.hip", "lp_dense_f32.hip", "lp_dense_narrow.hip",
            "lp_dense_mfma.hip", "lp_dense_resid.hip", "lp_dense_serial.hip",
            "lp_dense_wide.hip", "lp_conv.hip", "lp_noalloc.hip"]
 
@@ -46,7 +46,7 @@ def _compile(src: str) -> str:
 SAN_FLAGS = ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer",
              "-Xarch_host", "-shared-libasan"]
-SAN_SOURCES = ["lp_host.cpp", "lp_noalloc.hip"]  # the translation units with host logic beyond launches
+SAN_SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_step_host.cpp", "lp_host.cpp", "lp_noalloc.hip"]  # the translation units with host logic beyond launches
 SAN_OUT = os.path.join(OBJ, "liblp_san.so")
 
 

@@ -20,7 +20,9 @@ namespace {
 
 thread_local std::string g_err;
 
-int fail(int code, const char* fmt, ...) {
+}  // namespace
+
+int lp::fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -30,10 +32,18 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-int hip_fail(hipError_t e, const char* what) {
+int lp::hip_fail(hipError_t e, const char* what) {
   if (e == hipErrorNotSupported) return fail(LP_EUNSUPPORTED, "%s: no kernel for this shape", what);
   return fail(LP_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+void lp::clear_error() { g_err.clear(); }
+
+namespace {
+
+using lp::check_ws;
+using lp::fail;
+using lp::hip_fail;
 
 #define LP_TRY(expr, what)                       \
   do {                                           \
@@ -238,13 +248,17 @@ size_t resid_bytes(const lp_problem* p) {
   return up((size_t)partial_capacity(p) * sizeof(double)) + up(sizeof(double));
 }
 
-int check_ws(const void* ws, size_t have, size_t need) {
+}  // namespace
+
+int lp::check_ws(const void* ws, size_t have, size_t need) {
   if (need == 0) return LP_OK;
   if (!ws) return fail(LP_EWORKSPACE, "workspace is NULL (%zu bytes needed)", need);
   if ((uintptr_t)ws % kAlign) return fail(LP_EWORKSPACE, "workspace is not %zu-byte aligned", kAlign);
   if (have < need) return fail(LP_EWORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
   return LP_OK;
 }
+
+namespace {
 
 // One MGRIT solve (state or adjoint) over the hierarchy.
 struct Solver {

@@ -215,4 +215,78 @@ hipError_t launch_dot(int dtype, size_t n, const void* x, const void* y, double*
 hipError_t launch_accuracy(int dtype, int B, int q, int nc, const void* uN, const void* Wc, const void* mu,
                            const void* c, double* acc, void* ws, hipStream_t st);  // lp_loss.hip
 
+// ---- layer steps of any width, 8-bit checkpoints and heads over large vocabularies ----
+// (one translation unit per element type: lp_step_bf16.hip, lp_step_f16.hip, lp_step_f32.hip)
+struct StepArgs {
+  int dtype;           // LP_F32 | LP_BF16 | LP_F16
+  int act;
+  int B, ni, no;
+  double h;
+  const void* x;       // [B][ni] (backward: nullptr with a checkpoint)
+  const int8_t* x8;    // backward: checkpoint of x
+  const uint8_t* xe;
+  const void* W;       // [no][ni]
+  const void* b;       // [no], nullable
+  const void* r;       // forward: [B][no], nullable
+  void* y;
+  int8_t* y8;          // forward: checkpoint of y (nullable)
+  uint8_t* ye;
+  const void* dy;      // backward: [B][no]
+  int residual;        // backward: dx gets dy added
+  void* dx;            // nullable
+  void* dW;            // nullable
+  void* db;            // nullable
+  void* ws;
+};
+
+// Workspace of a backward call: offsets of g, the values of x's checkpoint, the column
+// partials of db and the partial products of dW.
+struct StepLayout {
+  size_t g, x, col, part, total;
+  int splits;
+};
+StepLayout step_layout(int dtype, int B, int ni, int no);
+
+struct LabelArgs {
+  int dtype;
+  int B, q, nc;
+  const void* u;       // [B][q]
+  const void* W;       // [nc][q]
+  const void* mu;      // [nc], nullable
+  const int64_t* labels;
+  double gscale;
+  float* J;
+  float* row;          // [B], nullable
+  void* du;            // nullable
+  void* dW;            // nullable
+  void* dmu;           // nullable
+  void* ws;
+};
+
+struct LabelLayout {
+  size_t part, zl, row;                                           // losses
+  size_t from, to, lab, count, scale, lse, u, P, du, col, wpart;  // gradients
+  size_t total;
+  int piece;  // classes whose probabilities are held at a time
+};
+LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad);
+
+#define LP_STEP_LAUNCHERS(T)                                                                                  \
+  hipError_t step_forward_##T(const StepArgs& a, hipStream_t st);                                             \
+  hipError_t step_backward_##T(const StepArgs& a, hipStream_t st);                                            \
+  hipError_t ck_store_##T(const void* x, int8_t* x8, uint8_t* xe, long B, int q, hipStream_t st);             \
+  hipError_t ck_load_##T(const int8_t* x8, const uint8_t* xe, void* x, long B, int q, hipStream_t st);        \
+  hipError_t loss_labels_##T(const LabelArgs& a, hipStream_t st);
+LP_STEP_LAUNCHERS(bf16)
+LP_STEP_LAUNCHERS(f16)
+LP_STEP_LAUNCHERS(f32)
+#undef LP_STEP_LAUNCHERS
+
+// Error reporting shared by the host translation units (lp_host.cpp): sets the thread's
+// last error and returns the code.
+int fail(int code, const char* fmt, ...);
+int hip_fail(hipError_t e, const char* what);
+void clear_error();
+int check_ws(const void* ws, size_t have, size_t need);
+
 }  // namespace lp

@@ -1,0 +1,347 @@
+// Softmax cross-entropy of integer labels over a large vocabulary, for one element type
+// (included by one translation unit per type). With z_k = W u_k + mu and the rows k that have
+// a label c_k in 0..nc-1 (n of them):
+//   lse_k = log sum_j exp z_kj,  loss_k = lse_k - z_k[c_k],  J = (1/n) sum loss_k,
+//   P = softmax(z) - onehot,  du = (s/n) P W,  dW = (s/n) P^T u,  dmu = (s/n) sum_k P_k.
+// The logits are never stored. A product over all classes leaves, per tile of classes, each
+// row's maximum and sum of exponentials (8 bytes where the tile had 128 logits); they are
+// joined in order into lse. For the gradients the logits are formed a second time, a piece of
+// the vocabulary after the other; a piece of P is kept in the workspace in the element type (the
+// type of the next products' operands), as P times PSCALE: 2^14 for f16, whose range would
+// otherwise lose the small probabilities of a large vocabulary (the least normal value then
+// stands for 3.7e-9), a power of two that the epilogues take back exactly.
+// Rows without a label take no part in the gradients, whatever they hold: the labelled rows are
+// first copied together, so a product runs over n rows.
+#pragma once
+
+#include "lp_internal.h"
+#include "lp_mm.h"
+
+namespace lp {
+namespace {
+
+using mm::f32x16;
+using mm::f32x4;
+using mm::Place;
+
+template <typename T> constexpr float PSCALE = 1.f;
+template <> constexpr float PSCALE<_Float16> = 16384.f;
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(1.4426950408889634f * x); }
+
+struct MaxSum {
+  float m, s;  // maximum and sum of exp(z - m); m = -inf, s = 0 where no class is left
+};
+
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
+  const float m = fmaxf(a.m, b.m);
+  if (m == -INFINITY) return MaxSum{m, a.s + b.s};  // (a NaN's sum stays one)
+  return MaxSum{m, a.s * exp_of(a.m - m) + b.s * exp_of(b.m - m)};
+}
+
+// Per row: maximum and sum of exponentials over the tile's classes, and the label's logit.
+template <typename T>
+struct EpLse {
+  struct Args {
+    const T* mu;            // nullable
+    const int64_t* labels;  // of D's rows
+    MaxSum* part;           // [class tiles][rows]
+    float* zl;              // [rows]: logit of the label
+    long rows;              // row stride of part
+  };
+  template <int FM, int FN, int WGM, int WGN>
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
+    MaxSum* red = reinterpret_cast<MaxSum*>(lds);  // [WGN][rows of the tile]
+    constexpr int BM = WGM * FM * 32;
+    const int half = 4 * (c.lane >> 5);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int m = c.mw + 32 * i + (c.lane & 31);
+      const int64_t lab = m < c.M ? a.labels[m] : -1;
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = c.nw + 32 * j + 8 * q + half;
+          f32x4 z = mm::quad(acc[i][j], q);
+          if (a.mu && n < c.N) z += mm::load4(a.mu, n, c.N);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (n + k < c.N) {
+              if (lab == n + k) a.zl[m] = z[k];
+            } else {
+              z[k] = -INFINITY;
+            }
+            acc[i][j][4 * q + k] = z[k];
+            top = fmaxf(top, z[k]);
+          }
+        }
+      // a NaN is no maximum; it comes back through the sum (exp of NaN)
+      const float ref = top == -INFINITY ? 0.f : top;
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += exp_of(acc[i][j][r] - ref);
+      MaxSum v{top, s};
+      v = join(v, MaxSum{__shfl_xor(v.m, 32, 64), __shfl_xor(v.s, 32, 64)});
+      if (c.lane < 32) red[c.wn * BM + c.wm * FM * 32 + 32 * i + c.lane] = v;
+    }
+    __syncthreads();
+    for (int r = threadIdx.x; r < BM; r += 64 * WGM * WGN) {
+      MaxSum v = red[r];
+#pragma unroll
+      for (int w = 1; w < WGN; ++w) v = join(v, red[w * BM + r]);
+      if (c.m0 + r < c.M) a.part[(size_t)c.nt * a.rows + c.m0 + r] = v;
+    }
+  }
+};
+
+// A piece of P (times PSCALE), and its column sums over the tile's rows (fp32, before rounding).
+template <typename T>
+struct EpProb {
+  struct Args {
+    const T* mu;            // nullable, of the piece
+    const int64_t* labels;  // of D's rows
+    const float* lse;
+    T* P;                   // [rows][N]
+    float* part;            // [tile rows][part_ld], from the piece's first class on (nullable)
+    long part_ld;
+    int j0;                 // first class of the piece
+  };
+  template <int FM, int FN, int WGM, int WGN>
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
+    const int half = 4 * (c.lane >> 5);
+    f32x16 sums[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) sums[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int m = c.mw + 32 * i + (c.lane & 31);
+      if (m >= c.M) continue;
+      const int64_t lab = a.labels[m] - a.j0;
+      const float lse = a.lse[m];
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = c.nw + 32 * j + 8 * q + half;
+          if (n >= c.N) continue;
+          f32x4 z = mm::quad(acc[i][j], q);
+          if (a.mu) z += mm::load4(a.mu, n, c.N);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            z[k] = exp_of(z[k] - lse) - (lab == n + k ? 1.f : 0.f);
+            sums[j][4 * q + k] += z[k];
+          }
+          mm::store4(a.P + (size_t)m * c.N, n, c.N, z * PSCALE<T>);
+        }
+    }
+    if (a.part) mm::column_sums<FN, WGM, WGN>(sums, c, lds, a.part + (size_t)c.mt * a.part_ld);
+  }
+};
+
+// du of a piece: added to the earlier pieces' sum in fp32, or, with the last piece, scaled,
+// rounded and written to the row that the labelled row came from.
+template <typename T>
+struct EpDu {
+  struct Args {
+    float* acc32;      // [rows][N]: sum over the pieces
+    T* du;
+    const int* from;   // row of u that a labelled row came from
+    const float* scale;
+    float f;
+    int first, last;
+  };
+  template <int FM, int FN, int WGM, int WGN>
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
+    const float f = a.f * a.scale[0];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int m = c.mw + 32 * i + (c.lane & 31);
+      if (m >= c.M) continue;
+      float* row = a.acc32 + (size_t)m * c.N;
+      T* out = a.du + (size_t)a.from[m] * c.N;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = c.nw + 32 * j + 8 * q + 4 * (c.lane >> 5);
+          if (n >= c.N) continue;
+          f32x4 v = mm::quad(acc[i][j], q);
+          if (!a.first) v += mm::load4(row, n, c.N);
+          if (a.last) mm::store4(out, n, c.N, v * f);
+          else mm::store4(row, n, c.N, v);
+        }
+    }
+  }
+};
+
+// Lists the rows that have a label (in order): from[r] = row, to[row] = r or -1, lab[r], their
+// number, and gs / max(1, number). One workgroup.
+__global__ __launch_bounds__(1024) void k_rows(const int64_t* labels, int B, int nc, double gs, int* from, int* to,
+                                               int64_t* lab, int* count, float* scale) {
+  __shared__ int wave_n[16];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  int base = 0;
+  for (int b0 = 0; b0 < B; b0 += 1024) {
+    const int b = b0 + t;
+    const int64_t l = b < B ? labels[b] : -1;
+    const bool on = l >= 0 && l < nc;
+    const uint64_t mask = __ballot(on);
+    if (lane == 0) wave_n[w] = __popcll(mask);
+    __syncthreads();
+    int at = base, all = 0;
+    for (int k = 0; k < 16; ++k) {
+      if (k < w) at += wave_n[k];
+      all += wave_n[k];
+    }
+    at += __popcll(mask & ((1ull << lane) - 1));
+    if (on) {
+      from[at] = b;
+      lab[at] = l;
+    }
+    if (b < B) to[b] = on ? at : -1;
+    base += all;
+    __syncthreads();
+  }
+  if (t == 0) {
+    count[0] = base;
+    scale[0] = (float)(gs / (double)(base > 0 ? base : 1));
+  }
+}
+
+// Copies the labelled rows together; the other rows' loss and gradient are zero. A wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gather(const T* u, const int* to, int B, int q, T* uc, T* du, float* row) {
+  const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (b >= B) return;
+  const int r = to[b];
+  if (r < 0) {
+    if (lane == 0) row[b] = 0.f;
+    if (du)
+      for (int i = 4 * lane; i < q; i += 256) mm::store4(du + (size_t)b * q, i, q, f32x4{0.f, 0.f, 0.f, 0.f});
+    return;
+  }
+  for (int i = 4 * lane; i < q; i += 256) mm::store4(uc + (size_t)r * q, i, q, mm::load4(u + (size_t)b * q, i, q));
+}
+
+// Joins the class tiles of a row: lse and the loss. 16 rows per workgroup, 16 threads a row.
+// labels as in EpLse; a row without one has loss 0. from (nullable): where row r's loss goes.
+__global__ __launch_bounds__(256) void k_lse(const MaxSum* part, int tiles, long rows, const int64_t* labels, int nc,
+                                             const float* zl, const int* count, int M, const int* from, float* lse,
+                                             float* loss) {
+  __shared__ MaxSum red[16][17];
+  if (count) M = min(M, *count);
+  const int r = threadIdx.x & 15, g = threadIdx.x >> 4, m = blockIdx.x * 16 + r;
+  MaxSum v{-INFINITY, 0.f};
+  if (m < M)
+    for (int t = g; t < tiles; t += 16) v = join(v, part[(size_t)t * rows + m]);
+  red[g][r] = v;
+  __syncthreads();
+  if (g || m >= M) return;
+  for (int k = 1; k < 16; ++k) v = join(v, red[k][r]);
+  const float l = v.m + logf(v.s);
+  if (lse) lse[m] = l;
+  const int64_t lab = labels[m];
+  loss[from ? from[m] : m] = lab >= 0 && lab < nc ? l - zl[m] : 0.f;
+}
+
+// J = sum of the rows' losses / number of labelled rows, in fp64 and in a fixed order.
+__global__ __launch_bounds__(1024) void k_mean_loss(const float* loss, const int64_t* labels, int B, int nc, float* J) {
+  __shared__ double sh[1024];
+  double s = 0.0, n = 0.0;
+  for (int b = threadIdx.x; b < B; b += 1024) {
+    s += (double)loss[b];
+    n += labels[b] >= 0 && labels[b] < nc ? 1.0 : 0.0;
+  }
+  s = block_sum<1024>(s, sh);
+  n = block_sum<1024>(n, sh);
+  if (threadIdx.x == 0) J[0] = (float)(s / (n > 0.0 ? n : 1.0));
+}
+
+template <typename T>
+hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
+  const bool grad = a.du || a.dW || a.dmu;
+  const LabelLayout l = label_layout(a.dtype, a.B, a.q, a.nc, grad);
+  char* w = static_cast<char*>(a.ws);
+  MaxSum* part = reinterpret_cast<MaxSum*>(w + l.part);
+  float* zl = reinterpret_cast<float*>(w + l.zl);
+  float* row = a.row ? a.row : reinterpret_cast<float*>(w + l.row);
+  const int tiles = mm::ceil_div(a.nc, mm::TILE);
+  const T* W = static_cast<const T*>(a.W);
+  const T* mu = static_cast<const T*>(a.mu);
+  hipError_t e = hipSuccess;
+  if (!grad && a.B == 0) {
+    k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, 0, a.nc, a.J);
+    return hipGetLastError();
+  }
+  if (!grad) {
+    typename EpLse<T>::Args ea{mu, a.labels, part, zl, a.B};
+    const mm::Prob p{a.u, W, a.q, a.q, a.B, a.nc, a.q, nullptr, 0, 0, 0, 0, 0};
+    if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, 1, st)) != hipSuccess) return e;
+    k_lse<<<(unsigned)mm::ceil_div(a.B, 16), 256, 0, st>>>(part, tiles, a.B, a.labels, a.nc, zl, nullptr, a.B, nullptr,
+                                                           nullptr, row);
+    k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
+    return hipGetLastError();
+  }
+  int* from = reinterpret_cast<int*>(w + l.from);
+  int* to = reinterpret_cast<int*>(w + l.to);
+  int64_t* lab = reinterpret_cast<int64_t*>(w + l.lab);
+  int* count = reinterpret_cast<int*>(w + l.count);
+  float* scale = reinterpret_cast<float*>(w + l.scale);
+  float* lse = reinterpret_cast<float*>(w + l.lse);
+  T* uc = reinterpret_cast<T*>(w + l.u);
+  T* P = reinterpret_cast<T*>(w + l.P);
+  float* acc32 = reinterpret_cast<float*>(w + l.du);
+  float* col = reinterpret_cast<float*>(w + l.col);
+  float* wpart = reinterpret_cast<float*>(w + l.wpart);
+  k_rows<<<1, 1024, 0, st>>>(a.labels, a.B, a.nc, a.gscale, from, to, lab, count, scale);
+  if (a.B) {  // (an empty batch leaves a zero loss and zero sums)
+    k_gather<T><<<(unsigned)mm::ceil_div(a.B, 4), 256, 0, st>>>((const T*)a.u, to, a.B, a.q, uc, (T*)a.du, row);
+    typename EpLse<T>::Args ea{mu, lab, part, zl, a.B};
+    const mm::Prob p{uc, W, a.q, a.q, a.B, a.nc, a.q, count, 1, 0, 0, 0, 0};
+    if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, 1, st)) != hipSuccess) return e;
+    k_lse<<<(unsigned)mm::ceil_div(a.B, 16), 256, 0, st>>>(part, tiles, a.B, lab, a.nc, zl, count, a.B, from, lse, row);
+  }
+  k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
+  for (int j0 = 0; j0 < a.nc; j0 += l.piece) {
+    const int n = std::min(l.piece, a.nc - j0);
+    if (a.B) {
+      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, a.dmu ? col + j0 : nullptr, a.nc, j0};
+      const mm::Prob pp{uc, W + (size_t)j0 * a.q, a.q, a.q, a.B, n, a.q, count, 1, 0, 0, 0, 0};
+      if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, 1, st)) != hipSuccess) return e;
+    }
+    if (a.du && a.B) {
+      typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
+      const mm::Prob pd{P, W + (size_t)j0 * a.q, n, a.q, a.B, a.q, n, count, 1, 0, 0, 0, 0};
+      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, 1, st)) != hipSuccess) return e;
+    }
+    if (a.dW) {
+      T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
+      const mm::Prob pw{P, uc, n, a.q, n, a.q, a.B, count, 0, 1, 0, 0, 0};
+      const int splits = mm::splits_of(sizeof(T), n, a.q, a.B);
+      if (splits > 1) {
+        if ((e = mm::launch_mm<T, true, true, mm::EpPart>(pw, mm::EpPart::Args{wpart}, splits, st)) != hipSuccess) return e;
+        const size_t nw = (size_t)n * a.q;
+        mm::k_join<T><<<(unsigned)std::min<size_t>((nw + 1023) / 1024, 4096), 256, 0, st>>>(wpart, splits, nw, dW,
+                                                                                            1.f / PSCALE<T>, scale);
+        e = hipGetLastError();
+      } else {
+        e = mm::launch_mm<T, true, true, mm::EpScale<T>>(
+            pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale}, 1, st);
+      }
+      if (e != hipSuccess) return e;
+    }
+  }
+  if (a.dmu) {
+    mm::k_colsum<T><<<(unsigned)mm::ceil_div(a.nc, 256), 256, 0, st>>>(col, mm::ceil_div(a.B, mm::TILE), mm::TILE, count, a.nc,
+                                                                     (T*)a.dmu, 1.f, scale);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+}  // namespace lp

@@ -20,6 +20,7 @@ LIB_PATH = os.environ.get("LP_LIBRARY") or os.path.join(os.path.dirname(os.path.
 LP_ABI_VERSION = 4
 LP_OK, LP_EINVAL, LP_EUNSUPPORTED, LP_EWORKSPACE, LP_EHIP, LP_ENONFINITE = range(6)
 LP_F32, LP_F64 = 0, 1
+LP_BF16, LP_F16 = 2, 3  # layer steps, checkpoints and label heads only
 LP_DENSE, LP_CONV3X3 = 0, 1
 LP_TANH, LP_RELU, LP_SMOOTHRELU, LP_IDENTITY = 0, 1, 2, 3
 LP_RELAX_F, LP_RELAX_FCF, LP_RELAX_FCFCF = 0, 1, 2
@@ -41,6 +42,8 @@ EXPORTS = (
     "lp_gradient", "lp_gradient_cpoints", "lp_residual_norm", "lp_residual_norm_noalloc", "lp_check_finite", "lp_open_forward", "lp_open_grad",
     "lp_loss_terminal", "lp_sgd_update", "lp_vec_axpby", "lp_vec_dot", "lp_accuracy",
     "lp_trace_enable", "lp_trace_read",
+    "lp_step_workspace_bytes", "lp_step_forward", "lp_step_backward", "lp_checkpoint_store", "lp_checkpoint_load",
+    "lp_loss_labels_workspace_bytes", "lp_loss_labels",
 )
 
 
@@ -62,6 +65,16 @@ class LpMgrit(ctypes.Structure):
                 ("storage", ctypes.c_int32)]
 
 
+class LpStep(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("B", ctypes.c_int32), ("ni", ctypes.c_int32), ("no", ctypes.c_int32), ("h", ctypes.c_double)]
+
+
+class LpLabelHead(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_int32), ("dtype", ctypes.c_int32), ("B", ctypes.c_int32),
+                ("q", ctypes.c_int32), ("nc", ctypes.c_int32)]
+
+
 class LpError(RuntimeError):
     def __init__(self, status: int, call: str, detail: str):
         super().__init__(f"{call}: status {status} ({detail})")
@@ -72,6 +85,8 @@ _lib: Optional[ctypes.CDLL] = None
 
 _P = ctypes.POINTER(LpProblem)
 _M = ctypes.POINTER(LpMgrit)
+_S = ctypes.POINTER(LpStep)
+_H = ctypes.POINTER(LpLabelHead)
 _v = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _sz = ctypes.c_size_t
@@ -102,6 +117,13 @@ _SIGS = {
     "lp_accuracy": ([_P, _i32, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
     "lp_trace_enable": ([ctypes.c_uint32], _i32),
     "lp_trace_read": ([_i32, _i32, _ip, _dp], _i32),
+    "lp_step_workspace_bytes": ([_S], _sz),
+    "lp_step_forward": ([_S, _v, _v, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
+    "lp_step_backward": ([_S, _v, _v, _v, _v, _v, _v, _i32, _v, _v, _v, _v, _sz, _v], _i32),
+    "lp_checkpoint_store": ([_i32, _i32, _i32, _v, _v, _v, _v], _i32),
+    "lp_checkpoint_load": ([_i32, _i32, _i32, _v, _v, _v, _v], _i32),
+    "lp_loss_labels_workspace_bytes": ([_H, _i32], _sz),
+    "lp_loss_labels": ([_H, _v, _v, _v, _v, ctypes.c_double, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
 }
 
 
@@ -427,3 +449,147 @@ def lp_accuracy(p: LpProblem, nc: int, uN, W, mu, c, acc, ws) -> None:
     _check(load().lp_accuracy(ctypes.byref(p), nc, _arr(uN, p.B * p.q, "uN", dt), _arr(W, nc * p.q, "W", dt),
                               _arr(mu, nc, "mu", dt), _arr(c, p.B * nc, "c", dt), _arr(acc, 1, "acc", torch.float64),
                               wp, wn, _stream()), "lp_accuracy")
+
+
+# ---------------------------------------------------------------- layer steps, checkpoints, label heads
+
+WIDE_DTYPE = {"f32": LP_F32, "f64": LP_F64, "bf16": LP_BF16, "f16": LP_F16}
+CHECKPOINT_BLOCK = 32  # features of a row that share a scale
+
+
+def step(dtype: str, act: str, B: int, ni: int, no: int, h: float = 1.0) -> LpStep:
+    """One layer step y = r + h sigma(x W^T + b), x [B][ni], W [no][ni]; dtype "f32", "bf16" or "f16"."""
+    return LpStep(LP_ABI_VERSION, WIDE_DTYPE[dtype], ACT[act], B, ni, no, h)
+
+
+def label_head(dtype: str, B: int, q: int, nc: int) -> LpLabelHead:
+    """Softmax head over nc classes for B rows of q features; dtype "f32", "bf16" or "f16"."""
+    return LpLabelHead(LP_ABI_VERSION, WIDE_DTYPE[dtype], B, q, nc)
+
+
+def _wide_dtype(kind: int):
+    import torch
+    return {LP_F32: torch.float32, LP_F64: torch.float64, LP_BF16: torch.bfloat16, LP_F16: torch.float16}[kind]
+
+
+def _dev(t, numel: int, name: str, dtype, optional: bool = False):
+    """_arr for a tensor on the current device (whose current stream the call uses); NULL for an
+    optional one that is not given."""
+    if t is None and optional:
+        return None
+    p = _arr(t, numel, name, dtype)
+    import torch
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return p
+
+
+def _dev_ws(ws):
+    if ws is None:
+        raise ValueError("a workspace is required")
+    import torch
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    if ws.device.index != torch.cuda.current_device():
+        raise ValueError(f"workspace is on {ws.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size()
+
+
+def _blocks(q: int) -> int:
+    return -(-q // CHECKPOINT_BLOCK)
+
+
+def lp_step_workspace_bytes(st: LpStep) -> int:
+    n = load().lp_step_workspace_bytes(ctypes.byref(st))
+    if n == 0:
+        raise LpError(LP_EINVAL, "lp_step_workspace_bytes", load().lp_last_error().decode())
+    return int(n)
+
+
+def alloc_step_workspace(st: LpStep, device="cuda"):
+    import torch
+    return torch.empty(lp_step_workspace_bytes(st), dtype=torch.uint8, device=device)
+
+
+def lp_step_forward(st: LpStep, x, W, b, r, y, ws, y8=None, ye=None) -> None:
+    """y = r + h sigma(x W^T + b). b and r may be None; r may be x, another tensor, or y itself.
+    y8 [B][no] int8 and ye [B][ceil(no / 32)] uint8 receive the checkpoint of y."""
+    import torch
+    dt = _wide_dtype(st.dtype)
+    wp, wn = _dev_ws(ws)
+    _check(load().lp_step_forward(
+        ctypes.byref(st), _dev(x, st.B * st.ni, "x", dt), _dev(W, st.no * st.ni, "W", dt),
+        _dev(b, st.no, "b", dt, True), _dev(r, st.B * st.no, "r", dt, True), _dev(y, st.B * st.no, "y", dt),
+        _dev(y8, st.B * st.no, "y8", torch.int8, True), _dev(ye, st.B * _blocks(st.no), "ye", torch.uint8, True),
+        wp, wn, _stream()), "lp_step_forward")
+
+
+def lp_step_backward(st: LpStep, x, W, b, dy, dx, dW, db, ws, residual: bool = False) -> None:
+    """Gradients of lp_step_forward for dy. x: the step's input, or its checkpoint as a pair
+    (x8, xe). residual: r was x, so dx gets dy added. dx, dW, db may be None (not wanted)."""
+    import torch
+    dt = _wide_dtype(st.dtype)
+    if isinstance(x, (tuple, list)):
+        xp = None
+        x8p = _dev(x[0], st.B * st.ni, "x8", torch.int8)
+        xep = _dev(x[1], st.B * _blocks(st.ni), "xe", torch.uint8)
+    else:
+        xp, x8p, xep = _dev(x, st.B * st.ni, "x", dt), None, None
+    wp, wn = _dev_ws(ws)
+    _check(load().lp_step_backward(
+        ctypes.byref(st), xp, x8p, xep, _dev(W, st.no * st.ni, "W", dt), _dev(b, st.no, "b", dt, True),
+        _dev(dy, st.B * st.no, "dy", dt), int(bool(residual)), _dev(dx, st.B * st.ni, "dx", dt, True),
+        _dev(dW, st.no * st.ni, "dW", dt, True), _dev(db, st.no, "db", dt, True), wp, wn, _stream()),
+        "lp_step_backward")
+
+
+def _ck_args(x, x8, xe):
+    import torch
+    kinds = {torch.float32: LP_F32, torch.bfloat16: LP_BF16, torch.float16: LP_F16, torch.float64: LP_F64}
+    if x is None or x.dtype not in kinds or x.dim() < 1:
+        raise ValueError("x must be a float32, bfloat16 or float16 tensor of rows")
+    q = x.shape[-1]
+    B = x.numel() // q if q else 0
+    return (kinds[x.dtype], B, q, _dev(x, B * q, "x", x.dtype), _dev(x8, B * q, "x8", torch.int8),
+            _dev(xe, B * _blocks(q), "xe", torch.uint8))
+
+
+def lp_checkpoint_store(x, x8, xe) -> None:
+    """8-bit checkpoint of the rows of x [..., q]: x8 int8 like x, xe uint8 [..., ceil(q / 32)]."""
+    kind, B, q, xp, x8p, xep = _ck_args(x, x8, xe)
+    _check(load().lp_checkpoint_store(kind, B, q, xp, x8p, xep, _stream()), "lp_checkpoint_store")
+
+
+def lp_checkpoint_load(x8, xe, x) -> None:
+    """The values of a checkpoint, written to the rows of x [..., q]."""
+    kind, B, q, xp, x8p, xep = _ck_args(x, x8, xe)
+    _check(load().lp_checkpoint_load(kind, B, q, x8p, xep, xp, _stream()), "lp_checkpoint_load")
+
+
+def lp_loss_labels_workspace_bytes(hd: LpLabelHead, grad: bool) -> int:
+    n = load().lp_loss_labels_workspace_bytes(ctypes.byref(hd), int(bool(grad)))
+    if n == 0:
+        raise LpError(LP_EINVAL, "lp_loss_labels_workspace_bytes", load().lp_last_error().decode())
+    return int(n)
+
+
+def alloc_loss_labels_workspace(hd: LpLabelHead, grad: bool = True, device="cuda"):
+    """grad: whether gradients will be asked for (losses alone need far less)."""
+    import torch
+    return torch.empty(lp_loss_labels_workspace_bytes(hd, grad), dtype=torch.uint8, device=device)
+
+
+def lp_loss_labels(hd: LpLabelHead, u, W, mu, labels, J, ws, row=None, du=None, dW=None, dmu=None,
+                   gscale: float = 1.0) -> None:
+    """Softmax cross-entropy of int64 labels over the logits u W^T + mu (mu may be None): J[0] (a device
+    float32) <- the mean loss of the rows whose label lies in 0..nc-1, row (float32 [B]) <- every row's
+    loss, and the gradients of gscale J for those of du, dW, dmu that are given."""
+    import torch
+    dt = _wide_dtype(hd.dtype)
+    wp, wn = _dev_ws(ws)
+    _check(load().lp_loss_labels(
+        ctypes.byref(hd), _dev(u, hd.B * hd.q, "u", dt), _dev(W, hd.nc * hd.q, "W", dt),
+        _dev(mu, hd.nc, "mu", dt, True), _dev(labels, hd.B, "labels", torch.int64), gscale,
+        _dev(J, 1, "J", torch.float32), _dev(row, hd.B, "row", torch.float32, True),
+        _dev(du, hd.B * hd.q, "du", dt, True), _dev(dW, hd.nc * hd.q, "dW", dt, True),
+        _dev(dmu, hd.nc, "dmu", dt, True), wp, wn, _stream()), "lp_loss_labels")

@@ -1,0 +1,318 @@
+"""Layer steps of any width, their gradients and 8-bit checkpoints against 64-bit plain forms, at
+the sizes, types and values where they can go wrong. Bounds: tests/wide_testutil.py."""
+import math
+
+import pytest
+import torch
+
+import wide_testutil as T
+from paper_1812_04352_amd import lp as L
+
+pytestmark = pytest.mark.gpu
+
+ACTS = ("tanh", "relu", "smoothrelu", "identity")
+# one row to ragged tiles; widths of one value, odd ones, below, at and above tiles and stages
+SHAPES = [(1, 1, 1), (1, 64, 64), (2, 7, 5), (1, 4096, 200), (5, 33, 1000), (16, 512, 48), (31, 256, 96), (64, 64, 128),
+          (129, 130, 131), (200, 63, 257), (256, 192, 320), (300, 220, 220), (17, 1000, 33), (40, 8, 2050),
+          (513, 96, 64), (1000, 24, 40)]
+
+
+def inputs(seed, dtype, B, ni, no, res):
+    g = torch.Generator().manual_seed(seed)
+    x = T.draw(g, (B, ni), dtype)
+    W = T.draw(g, (no, ni), dtype, 1 / math.sqrt(ni))
+    b = T.draw(g, (no,), dtype, 0.3)
+    r = {"none": None, "self": x, "other": T.draw(g, (B, no), dtype)}[res]
+    return x, W, b, r, T.draw(g, (B, no), dtype, 0.1)
+
+
+def residual_kind(i, ni, no):
+    return "self" if ni == no and i % 2 == 0 else ("none", "other")[i % 2]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("i", range(len(SHAPES)))
+def test_forward(dtype, i):
+    B, ni, no = SHAPES[i]
+    act = ACTS[i % 4]
+    h = (1.0, 0.125, -0.5)[i % 3]
+    x, W, b, r, _ = inputs(i, dtype, B, ni, no, residual_kind(i, ni, no))
+    if i % 5 == 4:
+        b = None
+    xg = T.gpu(x)
+    rg = xg if r is x else T.gpu(r)
+    s = T.Step(dtype, act, B, ni, no, h)
+    y, y8, ye = s.forward(xg, T.gpu(W), T.gpu(b), rg, ck=True)
+    ref, bound = T.forward(x, W, b, r, act, h, dtype)
+    T.check(y, ref, bound, "y")
+    # the checkpoint is that of y as it was stored
+    e8, ee = T.pack(y.cpu())
+    assert torch.equal(y8.cpu(), e8) and torch.equal(ye.cpu(), ee)
+    # the same bits without the checkpoint
+    assert torch.equal(s.forward(xg, T.gpu(W), T.gpu(b), rg), y)
+
+
+@pytest.mark.parametrize("ck", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("i", range(len(SHAPES)))
+def test_backward(dtype, i, ck):
+    B, ni, no = SHAPES[i]
+    act = ACTS[(i + 1) % 4]
+    h = (0.125, 1.0, -2.0)[i % 3]
+    x, W, b, _, dy = inputs(100 + i, dtype, B, ni, no, "none")
+    residual = ni == no
+    if i % 5 == 3:
+        b = None
+    xin = T.gpu(x)
+    if ck:
+        x8, xe = T.pack(x)
+        x = T.unpack(x8, xe)
+        xin = (T.gpu(x8), T.gpu(xe))
+    s = T.Step(dtype, act, B, ni, no, h)
+    got = s.backward(xin, T.gpu(W), T.gpu(b), T.gpu(dy), residual)
+    ref = T.backward(x, W, b, dy, act, h, residual, dtype)
+    for name, a, (r, e) in zip(("dx", "dW", "db"), got, ref):
+        T.check(a, r, e, name)
+
+
+def test_aligned_arrays():
+    """Rows on 16-byte boundaries (whole vectors) next to the views of the other tests."""
+    for dtype in ("bf16", "f16", "f32"):
+        for B, ni, no in ((130, 256, 384), (257, 128, 128), (1, 512, 256), (300, 72, 520)):
+            x, W, b, _, dy = inputs(7, dtype, B, ni, no, "none")
+            s = T.Step(dtype, "tanh", B, ni, no, 0.5)
+            dev = [t.cuda() for t in (x, W, b, dy)]
+            y = torch.empty((B, no), dtype=T.DT[dtype], device="cuda")
+            L.lp_step_forward(s.st, dev[0], dev[1], dev[2], None, y, s.ws)
+            T.check(y, *T.forward(x, W, b, None, "tanh", 0.5, dtype), "y")
+            o = [torch.empty_like(t) for t in dev[:3]]
+            L.lp_step_backward(s.st, dev[0], dev[1], dev[2], dev[3], *o, s.ws)
+            for name, a, (r, e) in zip(("dx", "dW", "db"), o, T.backward(x, W, b, dy, "tanh", 0.5, False, dtype)):
+                T.check(a, r, e, f"{name} {dtype} {B} {ni} {no}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_long_contraction_and_tall_batch(dtype):
+    """Lengths where the contraction is split and joined: a long width for few rows, a tall batch for
+    a small weight."""
+    for B, ni, no in ((3, 8192, 40), (5000, 40, 24), (70, 6000, 72)):
+        x, W, b, _, dy = inputs(9, dtype, B, ni, no, "none")
+        s = T.Step(dtype, "smoothrelu", B, ni, no, 0.25)
+        y = s.forward(T.gpu(x), T.gpu(W), T.gpu(b), None)
+        T.check(y, *T.forward(x, W, b, None, "smoothrelu", 0.25, dtype), "y")
+        got = s.backward(T.gpu(x), T.gpu(W), T.gpu(b), T.gpu(dy), False)
+        for name, a, (r, e) in zip(("dx", "dW", "db"), got, T.backward(x, W, b, dy, "smoothrelu", 0.25, False, dtype)):
+            T.check(a, r, e, f"{name} {B} {ni} {no}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_in_place_residual(dtype):
+    B, ni, no = 70, 65, 130
+    x, W, b, r, _ = inputs(11, dtype, B, ni, no, "other")
+    s = T.Step(dtype, "tanh", B, ni, no, 0.5)
+    y = T.gpu(r)
+    L.lp_step_forward(s.st, T.gpu(x), T.gpu(W), T.gpu(b), y, y, s.ws)
+    T.check(y, *T.forward(x, W, b, r, "tanh", 0.5, dtype), "y")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_wanted_gradients_alone(dtype):
+    B, ni, no = 90, 70, 100
+    x, W, b, _, dy = inputs(13, dtype, B, ni, no, "none")
+    s = T.Step(dtype, "tanh", B, ni, no, 0.5)
+    args = (T.gpu(x), T.gpu(W), T.gpu(b), T.gpu(dy), False)
+    full = s.backward(*args)
+    for want in ((True, False, False), (False, True, False), (False, False, True), (False, False, False)):
+        for a, f, w in zip(s.backward(*args, want=want), full, want):
+            assert (a is None) if not w else torch.equal(a, f)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_empty_batch(dtype):
+    ni, no = 33, 65
+    g = torch.Generator().manual_seed(1)
+    W, b = T.gpu(T.draw(g, (no, ni), dtype)), T.gpu(T.draw(g, (no,), dtype))
+    s = T.Step(dtype, "relu", 0, ni, no, 1.0)
+    e = torch.empty((0, ni), dtype=T.DT[dtype], device="cuda")
+    o = torch.empty((0, no), dtype=T.DT[dtype], device="cuda")
+    L.lp_step_forward(s.st, e, W, b, None, o, s.ws)
+    dx, dW, db = s.backward(e, W, b, o, False)
+    assert dx.numel() == 0 and not dW.any() and not db.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_values_that_are_not_finite_stay_in_their_row(dtype):
+    B, ni, no = 140, 96, 72
+    x, W, b, _, dy = inputs(17, dtype, B, ni, no, "none")
+    clean = x.clone()
+    x[3, 5], x[64, 0], x[139, 95] = math.nan, math.inf, -math.inf
+    bad = torch.zeros(B, dtype=torch.bool)
+    bad[[3, 64, 139]] = True
+    for act in ACTS:
+        s = T.Step(dtype, act, B, ni, no, 0.5)
+        y, y8, ye = s.forward(T.gpu(x), T.gpu(W), T.gpu(b), None, ck=True)
+        ref = T.forward(clean, W, b, None, act, 0.5, dtype)
+        T.check(y.cpu()[~bad], ref[0][~bad], ref[1][~bad], act)
+        yc = y.cpu()
+        assert yc[3].isnan().all()
+        # an infinite input: what the activation makes of an infinite pre-activation of its sign
+        sign = torch.sign(W[:, 0].double())
+        lim = {"tanh": 0.5 * sign, "relu": torch.where(sign > 0, math.inf, 0.0), "smoothrelu":
+               torch.where(sign > 0, math.inf, 0.0), "identity": sign * math.inf}[act].double()
+        sure = sign != 0
+        assert torch.equal(yc[64].double()[sure], lim[sure])
+        assert torch.equal(ye.cpu()[3], torch.full((3,), 255, dtype=torch.uint8)) and not y8.cpu()[3].any()
+        dx = s.backward(T.gpu(x), T.gpu(W), T.gpu(b), T.gpu(dy), False)[0].cpu()
+        rdx, edx = T.backward(clean, W, b, dy, act, 0.5, False, dtype)[0]
+        T.check(dx[~bad], rdx[~bad], edx[~bad], act)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("q", [1, 4, 31, 32, 33, 64, 220, 1000])
+def test_checkpoint_values(dtype, q):
+    g = torch.Generator().manual_seed(q)
+    B = 37
+    x = T.draw(g, (B, q), dtype) * torch.exp(2 * torch.randn((B, 1), generator=g)).to(T.DT[dtype])
+    fi = torch.finfo(T.DT[dtype])
+    x[0] = 0
+    x[1] = fi.max
+    x[2] = -fi.max
+    x[3] = fi.smallest_normal * fi.eps  # the smallest subnormal
+    x[4] *= fi.smallest_normal
+    x[5, q // 2] = math.nan
+    x[6, 0] = math.inf
+    x[7, q - 1] = -math.inf
+    x[8] = torch.linspace(-127.5, 127.5, q).to(x.dtype) if q > 1 else 127.5  # beyond 127 steps, ties
+    x[9] = (torch.arange(q) % 129 - 64).to(x.dtype) * 0.5 + 0.25
+    x[10] = 2.0 ** (torch.arange(q) % 20 - 10).to(x.dtype)
+    x[11] = -0.0
+    e8, ee = T.pack(x)
+    xg = T.gpu(x)
+    x8, f8 = T.out((B, q), torch.int8)
+    xe, fe = T.out(tuple(ee.shape), torch.uint8)
+    L.lp_checkpoint_store(xg, x8, xe)
+    back, fb = T.out((B, q), T.DT[dtype])
+    L.lp_checkpoint_load(x8, xe, back)
+    torch.cuda.synchronize()
+    assert torch.equal(x8.cpu(), e8) and torch.equal(xe.cpu(), ee)
+    assert T.guarded(f8, x8.numel()) and T.guarded(fe, xe.numel()) and T.guarded(fb, back.numel())
+    ref = T.unpack(e8, ee)
+    got = back.cpu().double()
+    assert torch.equal(got.isnan(), ref.isnan())
+    assert torch.equal(got.nan_to_num(), ref.nan_to_num())  # exact in every type
+    # off by at most half a step, a step where 127 is exceeded
+    unit = torch.ldexp(torch.ones(ee.shape, dtype=torch.float64), ee.long() - 127).repeat_interleave(32, 1)[:, :q]
+    ok = (ee != 255).repeat_interleave(32, 1)[:, :q]
+    xd = x.double()
+    lim = torch.where(xd.abs() > 127.5 * unit, unit, unit / 2)
+    assert ((got - xd).abs() <= lim)[ok].all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_arrays_beyond_32_bit_offsets(dtype):
+    """More than 2^31 values: the last rows of a step and of a checkpoint."""
+    B, ni, no = 70000, 32768, 40
+    g = torch.Generator().manual_seed(3)
+    x = torch.zeros((B, ni), dtype=T.DT[dtype], device="cuda")
+    tail = T.draw(g, (200, ni), dtype)
+    x[-200:] = tail.cuda()
+    W, b = T.draw(g, (no, ni), dtype, 1 / math.sqrt(ni)), T.draw(g, (no,), dtype)
+    s = T.Step(dtype, "tanh", B, ni, no, 1.0)
+    y = s.forward(x, W.cuda(), b.cuda(), None)
+    ref, bound = T.forward(tail, W, b, None, "tanh", 1.0, dtype)
+    T.check(y[-200:], ref, bound, "y")
+    del s
+    x8 = torch.empty((B, ni), dtype=torch.int8, device="cuda")
+    xe = torch.empty((B, ni // 32), dtype=torch.uint8, device="cuda")
+    L.lp_checkpoint_store(x, x8, xe)
+    e8, ee = T.pack(tail[-3:])
+    assert torch.equal(x8[-3:].cpu(), e8) and torch.equal(xe[-3:].cpu(), ee)
+    x.fill_(5)
+    L.lp_checkpoint_load(x8, xe, x)
+    assert torch.equal(x[-3:].cpu().double(), T.unpack(e8, ee)) and not x[0].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_another_stream_and_graphs(dtype):
+    """Captured forward and backward calls, replayed with eager work in between, equal the eager
+    results; two graphs with workspaces of their own; calls on a stream other than the default."""
+    B, ni, no = 300, 136, 200
+    x, W, b, r, dy = (T.gpu(t) for t in inputs(23, dtype, B, ni, no, "other"))
+    dt = T.DT[dtype]
+    st = L.step(dtype, "tanh", B, ni, no, 0.5)
+
+    def bufs():
+        return dict(y=torch.zeros((B, no), dtype=dt, device="cuda"),
+                    y8=torch.zeros((B, no), dtype=torch.int8, device="cuda"),
+                    ye=torch.zeros((B, 7), dtype=torch.uint8, device="cuda"),
+                    dx=torch.zeros((B, ni), dtype=dt, device="cuda"),
+                    dW=torch.zeros((no, ni), dtype=dt, device="cuda"), db=torch.zeros(no, dtype=dt, device="cuda"),
+                    ws=L.alloc_step_workspace(st))
+
+    def call(o):
+        L.lp_step_forward(st, x, W, b, r, o["y"], o["ws"], o["y8"], o["ye"])
+        L.lp_step_backward(st, x, W, b, dy, o["dx"], o["dW"], o["db"], o["ws"])
+
+    eager = bufs()
+    call(eager)
+    side = torch.cuda.Stream()
+    other = bufs()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(other)
+    side.synchronize()
+    graphs = []
+    for _ in range(2):
+        o = bufs()
+        gr = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(gr):
+            call(o)
+        graphs.append((gr, o))
+    names = ("y", "y8", "ye", "dx", "dW", "db")
+    assert all(torch.equal(eager[k], other[k]) for k in names)
+    for it in range(4):
+        x.copy_(torch.randn((B, ni), generator=torch.Generator("cuda").manual_seed(it), device="cuda").to(dt))
+        call(eager)
+        torch.cuda.synchronize()
+        for gr, o in graphs:
+            for k in names:
+                o[k].zero_()
+            gr.replay()
+        torch.cuda.synchronize()
+        for gr, o in graphs:
+            assert all(torch.equal(eager[k], o[k]) for k in names), it
+
+
+def test_same_bits_every_time():
+    for dtype in ("bf16", "f32"):
+        x, W, b, r, dy = (T.gpu(t) for t in inputs(29, dtype, 700, 300, 90, "other"))
+        s = T.Step(dtype, "tanh", 700, 300, 90, 0.5)
+        first = [s.forward(x, W, b, r)] + s.backward(x, W, b, dy, False)
+        for _ in range(3):
+            for a, c in zip(first, [s.forward(x, W, b, r)] + s.backward(x, W, b, dy, False)):
+                assert torch.equal(a, c)
+
+
+def test_gradients_against_differences():
+    """The gradients of sum(c * y) against central differences of the 64-bit form along random
+    directions of x, W and b."""
+    B, ni, no, h = 40, 50, 60, 0.5
+    for act in ("tanh", "smoothrelu", "identity"):
+        x, W, b, _, dy = inputs(31, "f32", B, ni, no, "none")
+        s = T.Step("f32", act, B, ni, no, h)
+        dx, dW, db = (t.double().cpu() for t in s.backward(T.gpu(x), T.gpu(W), T.gpu(b), T.gpu(dy), False))
+        g = torch.Generator().manual_seed(5)
+        dirs = [torch.randn(t.shape, generator=g, dtype=torch.float64) for t in (x, W, b)]
+
+        def f(e):
+            z = (x.double() + e * dirs[0]) @ (W.double() + e * dirs[1]).t() + b.double() + e * dirs[2]
+            return float((dy.double() * h * T.sigma(z, act)).sum())
+
+        eps = 1e-5
+        num = (f(eps) - f(-eps)) / (2 * eps)
+        ana = float((dx * dirs[0]).sum() + (dW * dirs[1]).sum() + (db * dirs[2]).sum())
+        # fp32 gradients: 2^-20 of the terms' magnitudes; differences: second order in eps, and the
+        # smoothed ReLU's kinks in its slope
+        mag = float((dx * dirs[0]).abs().sum() + (dW * dirs[1]).abs().sum() + (db * dirs[2]).abs().sum())
+        assert abs(num - ana) <= 1e-6 * mag + 1e-4 * abs(num), (act, num, ana)
