@@ -11,12 +11,16 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace lp {
 
 constexpr int CK_BLOCK = 32;
 
-template <typename T> constexpr uint32_t ck_min_byte() { return 1; }
-template <> constexpr uint32_t ck_min_byte<_Float16>() { return 127 - 24; }
+template <typename T>
+constexpr uint32_t ck_min_byte() {
+  return std::is_same<T, _Float16>::value ? 127 - 24 : 1;
+}
 
 // The scale byte of a block whose largest magnitude has these float bits (an infinity or a
 // NaN has larger bits than every finite value).

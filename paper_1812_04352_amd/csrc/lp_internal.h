@@ -239,10 +239,10 @@ struct StepArgs {
   void* ws;
 };
 
-// Workspace of a backward call: offsets of g, the values of x's checkpoint, the column
-// partials of db and the partial products of dW.
+// Workspace of a step: offsets of g, of copies of x (or its checkpoint's values) and W whose
+// rows start on 16 bytes, the column partials of db and the partial products of dW.
 struct StepLayout {
-  size_t g, x, col, part, total;
+  size_t g, x, W, col, part, total;
   int splits;
 };
 StepLayout step_layout(int dtype, int B, int ni, int no);
@@ -265,9 +265,10 @@ struct LabelArgs {
 
 struct LabelLayout {
   size_t part, zl, row;                                           // losses
-  size_t from, to, lab, count, scale, lse, u, P, du, col, wpart;  // gradients
+  size_t u, W;                                                    // copies with rows on 16 bytes
+  size_t from, to, lab, count, scale, lse, P, du, col, wpart;     // gradients
   size_t total;
-  int piece;  // classes whose probabilities are held at a time
+  int piece;  // classes taken at a time
 };
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad);
 

@@ -14,18 +14,20 @@
 // first copied together, so a product runs over n rows.
 #pragma once
 
+#include <type_traits>
+
 #include "lp_internal.h"
 #include "lp_mm.h"
 
 namespace lp {
-namespace {
+namespace wide {
 
 using mm::f32x16;
 using mm::f32x4;
 using mm::Place;
 
-template <typename T> constexpr float PSCALE = 1.f;
-template <> constexpr float PSCALE<_Float16> = 16384.f;
+template <typename T>
+constexpr float PSCALE = std::is_same<T, _Float16>::value ? 16384.f : 1.f;
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(1.4426950408889634f * x); }
 
@@ -43,40 +45,48 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
 template <typename T>
 struct EpLse {
   struct Args {
-    const T* mu;            // nullable
+    const T* mu;            // nullable, of the product's first class
     const int64_t* labels;  // of D's rows
     MaxSum* part;           // [class tiles][rows]
     float* zl;              // [rows]: logit of the label
     long rows;              // row stride of part
+    int j0;                 // first class of the product
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     MaxSum* red = reinterpret_cast<MaxSum*>(lds);  // [WGN][rows of the tile]
     constexpr int BM = WGM * FM * 32;
-    const int half = 4 * (c.lane >> 5);
-#pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = c.mw + 32 * i + (c.lane & 31);
-      const int64_t lab = m < c.M ? a.labels[m] : -1;
-      float top = -INFINITY;
+    if (a.mu) {
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int n = c.nw + 32 * j + 8 * q + half;
-          f32x4 z = mm::quad(acc[i][j], q);
-          if (a.mu && n < c.N) z += mm::load4(a.mu, n, c.N);
+          const f32x4 b = mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (n + k < c.N) {
-              if (lab == n + k) a.zl[m] = z[k];
-            } else {
-              z[k] = -INFINITY;
-            }
-            acc[i][j][4 * q + k] = z[k];
-            top = fmaxf(top, z[k]);
-          }
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] += b[k];
         }
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const int m = c.row(i);
+      // the label's place among the lane's values: class nw + 32 j + 8 q + 4 (lane / 32) + k
+      const int64_t l = (m < c.M ? a.labels[m] : -1) - a.j0;
+      const int at = l >= 0 && l < c.N ? (int)l - c.nw : -1;
+      float top = -INFINITY, zl = 0.f;
+      bool mine = false;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int n = c.feature(j, r >> 2) - c.nw + (r & 3);
+          if (!WHOLE && c.nw + n >= c.N) acc[i][j][r] = -INFINITY;
+          const float z = acc[i][j][r];
+          if (at == n) zl = z, mine = true;
+          top = fmaxf(top, z);
+        }
+      if (mine) a.zl[m] = zl;
       // a NaN is no maximum; it comes back through the sum (exp of NaN)
       const float ref = top == -INFINITY ? 0.f : top;
       float s = 0.f;
@@ -98,44 +108,57 @@ struct EpLse {
   }
 };
 
-// A piece of P (times PSCALE), and its column sums over the tile's rows (fp32, before rounding).
+// A piece of P (times PSCALE; rows of ld values, zeros behind the N that count), and its column
+// sums over the tile's rows (fp32, before rounding).
 template <typename T>
 struct EpProb {
   struct Args {
     const T* mu;            // nullable, of the piece
     const int64_t* labels;  // of D's rows
     const float* lse;
-    T* P;                   // [rows][N]
+    T* P;
+    int ld;
     float* part;            // [tile rows][part_ld], from the piece's first class on (nullable)
     long part_ld;
     int j0;                 // first class of the piece
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
-    const int half = 4 * (c.lane >> 5);
     f32x16 sums[FN];
+    if (a.mu) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 b = mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N);
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] += b[k];
+        }
+    }
 #pragma unroll
     for (int j = 0; j < FN; ++j) sums[j] = 0.f;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      const int m = c.mw + 32 * i + (c.lane & 31);
+      const int m = c.row(i);
       if (m >= c.M) continue;
-      const int64_t lab = a.labels[m] - a.j0;
+      const int64_t l = a.labels[m] - a.j0;
+      const int at = l >= 0 && l < c.N ? (int)l - c.nw : -1;
       const float lse = a.lse[m];
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int n = c.nw + 32 * j + 8 * q + half;
-          if (n >= c.N) continue;
           f32x4 z = mm::quad(acc[i][j], q);
-          if (a.mu) z += mm::load4(a.mu, n, c.N);
+          const int n = c.feature(j, q) - c.nw;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            z[k] = exp_of(z[k] - lse) - (lab == n + k ? 1.f : 0.f);
+            z[k] = exp_of(z[k] - lse) - (at == n + k ? 1.f : 0.f);
+            if (!WHOLE && c.nw + n + k >= c.N) z[k] = 0.f;
             sums[j][4 * q + k] += z[k];
           }
-          mm::store4(a.P + (size_t)m * c.N, n, c.N, z * PSCALE<T>);
+          mm::store4<WHOLE>(a.P + (size_t)m * a.ld, c.nw + n, a.ld, z * PSCALE<T>);
         }
     }
     if (a.part) mm::column_sums<FN, WGM, WGN>(sums, c, lds, a.part + (size_t)c.mt * a.part_ld);
@@ -154,33 +177,35 @@ struct EpDu {
     float f;
     int first, last;
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
     const float f = a.f * a.scale[0];
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      const int m = c.mw + 32 * i + (c.lane & 31);
+      const int m = c.row(i);
       if (m >= c.M) continue;
       float* row = a.acc32 + (size_t)m * c.N;
       T* out = a.du + (size_t)a.from[m] * c.N;
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
+      for (int j = 0; j < FN; ++j) {
+        f32x4 v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          v[q] = a.first ? f32x4{0.f, 0.f, 0.f, 0.f} : mm::load4<WHOLE>(row, c.feature(j, q), c.N);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int n = c.nw + 32 * j + 8 * q + 4 * (c.lane >> 5);
-          if (n >= c.N) continue;
-          f32x4 v = mm::quad(acc[i][j], q);
-          if (!a.first) v += mm::load4(row, n, c.N);
-          if (a.last) mm::store4(out, n, c.N, v * f);
-          else mm::store4(row, n, c.N, v);
+          v[q] += mm::quad(acc[i][j], q);
+          if (a.last) mm::store4<WHOLE>(out, c.feature(j, q), c.N, v[q] * f);
+          else mm::store4<WHOLE>(row, c.feature(j, q), c.N, v[q]);
         }
+      }
     }
   }
 };
 
 // Lists the rows that have a label (in order): from[r] = row, to[row] = r or -1, lab[r], their
 // number, and gs / max(1, number). One workgroup.
-__global__ __launch_bounds__(1024) void k_rows(const int64_t* labels, int B, int nc, double gs, int* from, int* to,
+static __global__ __launch_bounds__(1024) void k_rows(const int64_t* labels, int B, int nc, double gs, int* from, int* to,
                                                int64_t* lab, int* count, float* scale) {
   __shared__ int wave_n[16];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -212,9 +237,10 @@ __global__ __launch_bounds__(1024) void k_rows(const int64_t* labels, int B, int
   }
 }
 
-// Copies the labelled rows together; the other rows' loss and gradient are zero. A wave per row.
+// Copies the labelled rows together (rows of ld values, zeros behind the q that count); the other rows' loss and gradient are zero. A wave per row.
 template <typename T>
-__global__ __launch_bounds__(256) void k_gather(const T* u, const int* to, int B, int q, T* uc, T* du, float* row) {
+__global__ __launch_bounds__(256) void k_gather(const T* u, const int* to, int B, int q, T* uc, int ld, T* du,
+                                                float* row) {
   const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (b >= B) return;
   const int r = to[b];
@@ -224,12 +250,12 @@ __global__ __launch_bounds__(256) void k_gather(const T* u, const int* to, int B
       for (int i = 4 * lane; i < q; i += 256) mm::store4(du + (size_t)b * q, i, q, f32x4{0.f, 0.f, 0.f, 0.f});
     return;
   }
-  for (int i = 4 * lane; i < q; i += 256) mm::store4(uc + (size_t)r * q, i, q, mm::load4(u + (size_t)b * q, i, q));
+  for (int i = 4 * lane; i < ld; i += 256) mm::store4(uc + (size_t)r * ld, i, ld, mm::load4(u + (size_t)b * q, i, q));
 }
 
 // Joins the class tiles of a row: lse and the loss. 16 rows per workgroup, 16 threads a row.
 // labels as in EpLse; a row without one has loss 0. from (nullable): where row r's loss goes.
-__global__ __launch_bounds__(256) void k_lse(const MaxSum* part, int tiles, long rows, const int64_t* labels, int nc,
+static __global__ __launch_bounds__(256) void k_lse(const MaxSum* part, int tiles, long rows, const int64_t* labels, int nc,
                                              const float* zl, const int* count, int M, const int* from, float* lse,
                                              float* loss) {
   __shared__ MaxSum red[16][17];
@@ -249,7 +275,7 @@ __global__ __launch_bounds__(256) void k_lse(const MaxSum* part, int tiles, long
 }
 
 // J = sum of the rows' losses / number of labelled rows, in fp64 and in a fixed order.
-__global__ __launch_bounds__(1024) void k_mean_loss(const float* loss, const int64_t* labels, int B, int nc, float* J) {
+static __global__ __launch_bounds__(1024) void k_mean_loss(const float* loss, const int64_t* labels, int B, int nc, float* J) {
   __shared__ double sh[1024];
   double s = 0.0, n = 0.0;
   for (int b = threadIdx.x; b < B; b += 1024) {
@@ -269,23 +295,9 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   MaxSum* part = reinterpret_cast<MaxSum*>(w + l.part);
   float* zl = reinterpret_cast<float*>(w + l.zl);
   float* row = a.row ? a.row : reinterpret_cast<float*>(w + l.row);
-  const int tiles = mm::ceil_div(a.nc, mm::TILE);
+  const int tiles = mm::ceil_div(a.nc, mm::TILE), ldu = mm::padded(sizeof(T), a.q);
   const T* W = static_cast<const T*>(a.W);
   const T* mu = static_cast<const T*>(a.mu);
-  hipError_t e = hipSuccess;
-  if (!grad && a.B == 0) {
-    k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, 0, a.nc, a.J);
-    return hipGetLastError();
-  }
-  if (!grad) {
-    typename EpLse<T>::Args ea{mu, a.labels, part, zl, a.B};
-    const mm::Prob p{a.u, W, a.q, a.q, a.B, a.nc, a.q, nullptr, 0, 0, 0, 0, 0};
-    if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, 1, st)) != hipSuccess) return e;
-    k_lse<<<(unsigned)mm::ceil_div(a.B, 16), 256, 0, st>>>(part, tiles, a.B, a.labels, a.nc, zl, nullptr, a.B, nullptr,
-                                                           nullptr, row);
-    k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
-    return hipGetLastError();
-  }
   int* from = reinterpret_cast<int*>(w + l.from);
   int* to = reinterpret_cast<int*>(w + l.to);
   int64_t* lab = reinterpret_cast<int64_t*>(w + l.lab);
@@ -297,30 +309,53 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   float* acc32 = reinterpret_cast<float*>(w + l.du);
   float* col = reinterpret_cast<float*>(w + l.col);
   float* wpart = reinterpret_cast<float*>(w + l.wpart);
-  k_rows<<<1, 1024, 0, st>>>(a.labels, a.B, a.nc, a.gscale, from, to, lab, count, scale);
-  if (a.B) {  // (an empty batch leaves a zero loss and zero sums)
-    k_gather<T><<<(unsigned)mm::ceil_div(a.B, 4), 256, 0, st>>>((const T*)a.u, to, a.B, a.q, uc, (T*)a.du, row);
-    typename EpLse<T>::Args ea{mu, lab, part, zl, a.B};
-    const mm::Prob p{uc, W, a.q, a.q, a.B, a.nc, a.q, count, 1, 0, 0, 0, 0};
-    if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, 1, st)) != hipSuccess) return e;
-    k_lse<<<(unsigned)mm::ceil_div(a.B, 16), 256, 0, st>>>(part, tiles, a.B, lab, a.nc, zl, count, a.B, from, lse, row);
+  hipError_t e = hipSuccess;
+  // rows of the products: u's own, or with gradients the labelled ones
+  const T* rows = uc;
+  long ldr = ldu;
+  if (grad) {
+    k_rows<<<1, 1024, 0, st>>>(a.labels, a.B, a.nc, a.gscale, from, to, lab, count, scale);
+    if (a.B) k_gather<T><<<(unsigned)mm::ceil_div(a.B, 4), 256, 0, st>>>((const T*)a.u, to, a.B, a.q, uc, ldu, (T*)a.du, row);
+    e = hipGetLastError();
+  } else {
+    const mm::Operand<T> u(a.u, a.B, a.q, uc, st);
+    rows = u.p;
+    ldr = u.ld;
+    e = u.e;
   }
-  k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
-  for (int j0 = 0; j0 < a.nc; j0 += l.piece) {
+  if (e != hipSuccess) return e;
+  const int* cnt = grad ? count : nullptr;
+  const int64_t* labels = grad ? lab : a.labels;
+  for (int j0 = 0; j0 < a.nc && a.B; j0 += l.piece) {
     const int n = std::min(l.piece, a.nc - j0);
+    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, n, a.q, w + l.W, st);
+    if (Wj.e != hipSuccess) return Wj.e;
+    typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)(j0 / mm::TILE) * a.B, zl, a.B, j0};
+    const mm::Prob p{rows, Wj.p, ldr, Wj.ld, a.B, n, a.q, cnt, 1, 0, 0, 0, 0};
+    if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, 1, st)) != hipSuccess) return e;
+  }
+  if (a.B)
+    k_lse<<<(unsigned)mm::ceil_div(a.B, 16), 256, 0, st>>>(part, tiles, a.B, labels, a.nc, zl, cnt, a.B, grad ? from : nullptr,
+                                                           grad ? lse : nullptr, row);
+  k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
+  if ((e = hipGetLastError()) != hipSuccess || !grad) return e;
+  for (int j0 = 0; j0 < a.nc; j0 += l.piece) {
+    const int n = std::min(l.piece, a.nc - j0), ldp = mm::padded(sizeof(T), n);
+    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, a.B ? n : 0, a.q, w + l.W, st);
+    if (Wj.e != hipSuccess) return Wj.e;
     if (a.B) {
-      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, a.dmu ? col + j0 : nullptr, a.nc, j0};
-      const mm::Prob pp{uc, W + (size_t)j0 * a.q, a.q, a.q, a.B, n, a.q, count, 1, 0, 0, 0, 0};
+      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, ldp, a.dmu ? col + j0 : nullptr, a.nc, j0};
+      const mm::Prob pp{uc, Wj.p, ldu, Wj.ld, a.B, n, a.q, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, 1, st)) != hipSuccess) return e;
     }
     if (a.du && a.B) {
       typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
-      const mm::Prob pd{P, W + (size_t)j0 * a.q, n, a.q, a.B, a.q, n, count, 1, 0, 0, 0, 0};
+      const mm::Prob pd{P, Wj.p, ldp, Wj.ld, a.B, a.q, n, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, 1, st)) != hipSuccess) return e;
     }
     if (a.dW) {
       T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
-      const mm::Prob pw{P, uc, n, a.q, n, a.q, a.B, count, 0, 1, 0, 0, 0};
+      const mm::Prob pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
       const int splits = mm::splits_of(sizeof(T), n, a.q, a.B);
       if (splits > 1) {
         if ((e = mm::launch_mm<T, true, true, mm::EpPart>(pw, mm::EpPart::Args{wpart}, splits, st)) != hipSuccess) return e;
@@ -343,5 +378,5 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   return e;
 }
 
-}  // namespace
+}  // namespace wide
 }  // namespace lp

@@ -29,6 +29,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "lp_device.h"
 
 namespace lp {
@@ -66,11 +68,12 @@ __device__ __forceinline__ f32x16 mma(f32x4 a, f32x4 b, f32x16 c) {
   return c;
 }
 
-// Four values of a row of N features from feature n on, as floats (0 past the row's end).
-template <typename T>
+// Four values of a row of N features from feature n on, as floats (0 past the row's end;
+// WHOLE: they are all there).
+template <bool WHOLE = false, typename T>
 __device__ __forceinline__ f32x4 load4(const T* row, int n, int N) {
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (n + 4 <= N) {
+  if (WHOLE || n + 4 <= N) {
     const auto x = *reinterpret_cast<const typename GVec<T, 4>::type*>(row + n);
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = (float)x[k];
@@ -82,9 +85,9 @@ __device__ __forceinline__ f32x4 load4(const T* row, int n, int N) {
   return v;
 }
 
-template <typename T>
+template <bool WHOLE = false, typename T>
 __device__ __forceinline__ void store4(T* row, int n, int N, f32x4 v) {
-  if (n + 4 <= N) {
+  if (WHOLE || n + 4 <= N) {
     typename GVec<T, 4>::type x;
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = (T)v[k];
@@ -96,22 +99,8 @@ __device__ __forceinline__ void store4(T* row, int n, int N, f32x4 v) {
   }
 }
 
-// 16 bytes of global memory of which the first n values count, the rest zero; nothing is
-// read past them.
-template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const T* p, long n) {
-  constexpr int V = 16 / sizeof(T);
-  typename GVec<T, V>::type v;
-  if (n >= V) {
-    v = *reinterpret_cast<const typename GVec<T, V>::type*>(p);
-  } else {
-#pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = k < n ? p[k] : (T)0.f;
-  }
-  return __builtin_bit_cast(u32x4, v);
-}
-
-// One operand's tile of R rows of D: from global memory to registers and on to LDS.
+// One operand's tile of R rows of D, straight from global memory to LDS. Arrays start on 16
+// bytes and so do their rows.
 template <typename T, int R, int NT, bool COLS>
 struct Stage {
   static constexpr int V = 16 / sizeof(T);           // values per chunk
@@ -120,41 +109,59 @@ struct Stage {
   static constexpr int CH = R / V;                   // columns: chunks per row of the stage
   static constexpr int SWZ = (sizeof(T) == 2 ? 12 : 8) & (CH - 1);
   static_assert(R * 8 % NT == 0, "whole chunks per thread");
-  u32x4 reg[PER];
+  static_assert(NT % 64 == 0 && (COLS ? NT / CH % 4 == 0 : true), "the exchange is the same for all of a thread's chunks");
 
   static __device__ __forceinline__ int swz(int k) {  // columns: chunk exchange of row k
     return (sizeof(T) == 2 ? k << 2 : k << 1) & SWZ;
   }
 
+  const unsigned char* base;  // of the next stage (uniform)
+  long left;                  // bytes from base to the end of the last row that counts
+  long step;                  // bytes per stage
+  uint32_t off[PER];
+  int kc;                     // rows: first contraction index of this thread's chunks
+  int k, k1;
+
   // rows r0.. of `rows`, contraction k0.. up to k1
-  __device__ __forceinline__ void load(const T* p, long ld, int r0, int rows, int k0, int k1) {
+  __device__ __forceinline__ void start(const void* p, long ld, int r0, int rows, int k0, int k1_) {
+    const int t = threadIdx.x;
+    k = k0;
+    k1 = k1_;
+    if constexpr (!COLS) {
+      const int c = (t & 7) ^ ((t >> 3) & 7);
+      kc = c * V;
+      base = static_cast<const unsigned char*>(p) + ((long)r0 * ld + k0) * (long)sizeof(T);
+      left = ((long)(rows - r0) * ld - k0) * (long)sizeof(T);
+      step = KB;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int id = threadIdx.x + i * NT;
-      if constexpr (!COLS) {
-        const int r = r0 + (id >> 3), k = k0 + (id & 7) * V;
-        reg[i] = load_chunk<T>(p + (long)r * ld + k, r < rows ? k1 - k : 0);
-      } else {
-        const int k = k0 + id / CH, r = r0 + (id % CH) * V;
-        reg[i] = load_chunk<T>(p + (long)k * ld + r, k < k1 ? rows - r : 0);
-      }
+      for (int i = 0; i < PER; ++i) off[i] = (uint32_t)((t + i * NT) >> 3) * (uint32_t)(ld * sizeof(T)) + c * 16;
+    } else {
+      const int c = (t % CH) ^ swz(t / CH);
+      kc = 0;
+      base = static_cast<const unsigned char*>(p) + ((long)k0 * ld + r0) * (long)sizeof(T);
+      left = ((long)(k1 - k0) * ld - r0) * (long)sizeof(T);
+      step = BK * ld * (long)sizeof(T);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) off[i] = (uint32_t)((t + i * NT) / CH) * (uint32_t)(ld * sizeof(T)) + c * 16;
     }
   }
 
-  __device__ __forceinline__ void store(unsigned char* lds) const {
+  // Requests the next stage. Loads past `left` give zeros: rows past the last (rows), contraction
+  // indices past the last (columns); so does an offset of 2^31 (rows: past the contraction's end).
+  __device__ __forceinline__ void load(unsigned char* lds) {
+#ifdef __HIP_DEVICE_COMPILE__  // (buffer resources are no type of the host compilation)
+    typedef __attribute__((address_space(3))) void lds_void;
+    const __amdgpu_buffer_rsrc_t r =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, left < 0x7fffffff ? (int)left : 0x7fffffff, 0x00020000);
+    const bool past = !COLS && k + kc >= k1;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int id = threadIdx.x + i * NT;
-      int at;
-      if constexpr (!COLS) {
-        const int r = id >> 3;
-        at = r * 8 + ((id & 7) ^ (r & 7));
-      } else {
-        const int k = id / CH;
-        at = k * CH + ((id % CH) ^ swz(k));
-      }
-      *reinterpret_cast<u32x4*>(lds + at * 16) = reg[i];
-    }
+    for (int i = 0; i < PER; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(lds + (i * NT + (threadIdx.x & ~63)) * 16), 16,
+                                               past ? 0x80000000u : off[i], 0, 0, 0);
+    base += step;
+    left -= step;
+    k += BK;
+#endif
   }
 
   // the fragment of rows r0..r0+31 and contraction step kk (two chunks) of a stage
@@ -208,6 +215,8 @@ struct Place {
   int mt, nt;      // tile indices
   int split;
   int lane;
+  __device__ __forceinline__ int row(int i) const { return mw + 32 * i + (lane & 31); }
+  __device__ __forceinline__ int feature(int j, int q) const { return nw + 32 * j + 8 * q + 4 * (lane >> 5); }
 };
 
 // Workgroups go to the eight XCDs in turn, each with its own L2: an XCD takes a run of
@@ -250,8 +259,6 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_mm(Prob p, typename E::Args 
   c.split = blockIdx.y;
   const int k0 = blockIdx.y * p.kper, k1 = min(K, k0 + p.kper);
   const int steps = k1 > k0 ? (k1 - k0 + SA::BK - 1) / SA::BK : 0;
-  const T* A = static_cast<const T*>(p.A);
-  const T* B = static_cast<const T*>(p.B);
   f32x16 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -259,19 +266,19 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_mm(Prob p, typename E::Args 
     for (int j = 0; j < FN; ++j) acc[i][j] = 0.f;
   SA sa;
   SB sb;
+  sa.start(p.A, p.lda, c.m0, c.M, k0, k1);
+  sb.start(p.B, p.ldb, c.n0, c.N, k0, k1);
   if (steps) {
-    sa.load(A, p.lda, c.m0, c.M, k0, k1);
-    sb.load(B, p.ldb, c.n0, c.N, k0, k1);
+    sa.load(lds[0]);
+    sb.load(lds[0] + BM * KB);
   }
   for (int s = 0; s < steps; ++s) {
     unsigned char* la = lds[s & 1];
     unsigned char* lb = la + BM * KB;
-    sa.store(la);
-    sb.store(lb);
     __syncthreads();
     if (s + 1 < steps) {
-      sa.load(A, p.lda, c.m0, c.M, k0 + (s + 1) * SA::BK, k1);
-      sb.load(B, p.ldb, c.n0, c.N, k0 + (s + 1) * SA::BK, k1);
+      sa.load(lds[(s + 1) & 1]);
+      sb.load(lds[(s + 1) & 1] + BM * KB);
     }
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -287,7 +294,10 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_mm(Prob p, typename E::Args 
     }
   }
   __syncthreads();  // the epilogue may use the stages' LDS
-  E::template run<FM, FN, WGM, WGN>(ea, c, acc, reinterpret_cast<float*>(&lds[0][0]));
+  float* el = reinterpret_cast<float*>(&lds[0][0]);
+  // whole quads of features everywhere: straight-line code, no test per quad
+  if (c.n0 + BN <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, el);
+  else E::template run<false, FM, FN, WGM, WGN>(ea, c, acc, el);
 }
 
 // The four values of quad q of a block
@@ -339,20 +349,17 @@ struct EpPart {
   struct Args {
     float* part;  // [splits][M][N]
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
     float* out = a.part + (size_t)c.split * c.M * c.N;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      const int m = c.mw + 32 * i + (c.lane & 31);
+      const int m = c.row(i);
       if (m >= c.M) continue;
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = c.nw + 32 * j + 8 * q + 4 * (c.lane >> 5);
-          if (n < c.N) store4(out + (size_t)m * c.N, n, c.N, quad(acc[i][j], q));
-        }
+        for (int q = 0; q < 4; ++q) store4<WHOLE>(out + (size_t)m * c.N, c.feature(j, q), c.N, quad(acc[i][j], q));
     }
   }
 };
@@ -365,20 +372,17 @@ struct EpScale {
     float f;
     const float* scale;
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
     const float f = a.scale ? a.f * a.scale[0] : a.f;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      const int m = c.mw + 32 * i + (c.lane & 31);
+      const int m = c.row(i);
       if (m >= c.M) continue;
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = c.nw + 32 * j + 8 * q + 4 * (c.lane >> 5);
-          if (n < c.N) store4(a.out + (size_t)m * c.N, n, c.N, quad(acc[i][j], q) * f);
-        }
+        for (int q = 0; q < 4; ++q) store4<WHOLE>(a.out + (size_t)m * c.N, c.feature(j, q), c.N, quad(acc[i][j], q) * f);
     }
   }
 };
@@ -409,12 +413,56 @@ __global__ __launch_bounds__(256) void k_colsum(const float* part, int tiles, in
   out[i] = (T)((float)s * (scale ? f * scale[0] : f));
 }
 
+// Rows of `cols` values to rows of ld values, zeros behind them (ld a multiple of a chunk): a
+// copy whose rows start on 16 bytes.
+template <typename T>
+__global__ __launch_bounds__(256) void k_repack(const T* in, T* out, size_t rows, int cols, int ld) {
+  constexpr int V = 16 / sizeof(T);
+  const int per = ld / V;
+  for (size_t id = (size_t)blockIdx.x * 256 + threadIdx.x; id < rows * per; id += (size_t)gridDim.x * 256) {
+    const size_t r = id / per;
+    const int c = (int)(id - r * per) * V;
+    const T* p = in + r * cols + c;
+    typename GVec<T, V>::type v;
+    if (c + V <= cols) {
+      v = *reinterpret_cast<const typename GVec<T, V>::type*>(p);
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = c + k < cols ? p[k] : (T)0.f;
+    }
+    *reinterpret_cast<typename GVec<T, V>::type*>(out + r * ld + c) = v;
+  }
+}
+
 // ---------------------------------------------------------------- launches
 
 // Tile sizes: 4 waves of 64 x 64.
 constexpr int TILE = 128;
 
 inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
+
+// The leading dimension of a row of n values that starts on 16 bytes.
+inline int padded(size_t esz, int n) { return ceil_div(n, 16 / (int)esz) * (16 / (int)esz); }
+
+// An operand as the products need it: the caller's array where its rows start on 16 bytes,
+// else a copy in the workspace.
+template <typename T>
+struct Operand {
+  const T* p;
+  long ld;
+  hipError_t e;
+  Operand(const void* in, size_t rows, int cols, void* copy, hipStream_t st)
+      : p(static_cast<const T*>(in)), ld(cols), e(hipSuccess) {
+    if (cols * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0) return;
+    ld = padded(sizeof(T), cols);
+    p = static_cast<const T*>(copy);
+    const size_t n = rows * (ld * sizeof(T) / 16);
+    if (n == 0) return;
+    k_repack<T><<<(unsigned)std::min<size_t>((n + 255) / 256, 1u << 20), 256, 0, st>>>(
+        static_cast<const T*>(in), static_cast<T*>(copy), rows, cols, (int)ld);
+    e = hipGetLastError();
+  }
+};
 
 template <typename T, bool AT, bool BT, class E>
 hipError_t launch_mm(Prob p, const typename E::Args& ea, int splits, hipStream_t st) {

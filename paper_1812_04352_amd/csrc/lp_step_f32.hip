@@ -6,14 +6,14 @@
 
 namespace lp {
 
-hipError_t step_forward_f32(const StepArgs& a, hipStream_t st) { return step_forward_t<float>(a, st); }
-hipError_t step_backward_f32(const StepArgs& a, hipStream_t st) { return step_backward_t<float>(a, st); }
+hipError_t step_forward_f32(const StepArgs& a, hipStream_t st) { return wide::step_forward_t<float>(a, st); }
+hipError_t step_backward_f32(const StepArgs& a, hipStream_t st) { return wide::step_backward_t<float>(a, st); }
 hipError_t ck_store_f32(const void* x, int8_t* x8, uint8_t* xe, long B, int q, hipStream_t st) {
-  return ck_store_t<float>(x, x8, xe, B, q, st);
+  return wide::ck_store_t<float>(x, x8, xe, B, q, st);
 }
 hipError_t ck_load_f32(const int8_t* x8, const uint8_t* xe, void* x, long B, int q, hipStream_t st) {
-  return ck_load_t<float>(x8, xe, x, B, q, st);
+  return wide::ck_load_t<float>(x8, xe, x, B, q, q, st);
 }
-hipError_t loss_labels_f32(const LabelArgs& a, hipStream_t st) { return loss_labels_t<float>(a, st); }
+hipError_t loss_labels_f32(const LabelArgs& a, hipStream_t st) { return wide::loss_labels_t<float>(a, st); }
 
 }  // namespace lp

@@ -94,20 +94,21 @@ StepLayout step_layout(int dtype, int B, int ni, int no) {
     at += up(bytes);
     return r;
   };
-  l.g = take((size_t)B * no * e);
-  l.x = take((size_t)B * ni * e);
+  l.g = take((size_t)B * mm::padded(e, no) * e);
+  l.x = take((size_t)B * mm::padded(e, ni) * e);
+  l.W = take((size_t)no * mm::padded(e, ni) * e);
   l.col = take((size_t)mm::ceil_div(B, mm::TILE) * no * 4);
   l.part = take(l.splits > 1 ? (size_t)l.splits * no * ni * 4 : 0);
   l.total = std::max<size_t>(at, 256);
   return l;
 }
 
-// A piece of the vocabulary holds at most PIECE_BYTES of probabilities, in whole tiles of
-// classes (at least one tile).
+// A piece of the vocabulary holds at most PIECE_BYTES of probabilities and of (copied) weights,
+// in whole tiles of classes (at least one tile).
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;
 
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
-  const size_t e = esize(dtype);
+  const size_t e = esize(dtype), ldq = mm::padded(e, q);
   LabelLayout l{};
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
@@ -115,20 +116,21 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     at += up(bytes);
     return r;
   };
+  const size_t fit = PIECE_BYTES / (std::max<size_t>(grad ? B : 0, ldq) * e) / mm::TILE * mm::TILE;
+  l.piece = (int)std::min<size_t>(nc, std::max<size_t>(fit, mm::TILE));
   l.part = take((size_t)mm::ceil_div(nc, mm::TILE) * B * 8);
   l.zl = take((size_t)B * 4);
   l.row = take((size_t)B * 4);
+  l.u = take((size_t)B * ldq * e);
+  l.W = take((size_t)l.piece * ldq * e);
   if (grad) {
-    const size_t fit = PIECE_BYTES / (std::max(B, 1) * e) / mm::TILE * mm::TILE;
-    l.piece = (int)std::min<size_t>(nc, std::max<size_t>(fit, mm::TILE));
     l.from = take((size_t)B * 4);
     l.to = take((size_t)B * 4);
     l.lab = take((size_t)B * 8);
     l.count = take(4);
     l.scale = take(4);
     l.lse = take((size_t)B * 4);
-    l.u = take((size_t)B * q * e);
-    l.P = take((size_t)B * l.piece * e);
+    l.P = take((size_t)B * mm::padded(e, l.piece) * e);
     l.du = take(l.piece < nc ? (size_t)B * q * 4 : 0);
     l.col = take((size_t)mm::ceil_div(B, mm::TILE) * nc * 4);
     // the last piece is smaller than the others: the most splits it may take

@@ -8,16 +8,33 @@
 //              dx = h g W (+ dy),  dW = h g^T x,  db = h sum g (from g before its rounding)
 #pragma once
 
+#include <type_traits>
+
 #include "lp_checkpoint.h"
 #include "lp_internal.h"
 #include "lp_mm.h"
 
 namespace lp {
-namespace {
+namespace wide {
 
 using mm::f32x16;
 using mm::f32x4;
 using mm::Place;
+
+// Four values of a checkpoint row of N features.
+template <bool WHOLE = false>
+__device__ __forceinline__ void store_ck(int8_t* row, int n, int N, f32x4 v, float inv) {
+  typename mm::GVec<int8_t, 4>::type w;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = (int8_t)ck_round(v[k], inv);
+  if (WHOLE || n + 4 <= N) {
+    *reinterpret_cast<typename mm::GVec<int8_t, 4>::type*>(row + n) = w;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (n + k < N) row[n + k] = w[k];
+  }
+}
 
 // tanh for the 16-bit types: (1 - t) / (1 + t) with t = exp(-2|x|) on the hardware's exp2 and
 // reciprocal (error below 2^-22 absolute); below 1/4, where the difference would cancel, the odd
@@ -41,24 +58,28 @@ __device__ __forceinline__ float dtanh(float x) {
   }
 }
 
-// sigma and sigma' of a run-time activation (uniform over the launch). A NaN stays one.
-template <typename T>
-__device__ __forceinline__ float sigma(float z, int act) {
-  switch (act) {
-    case ACT_TANH: return sizeof(T) == 2 ? tanh16(z) : tanhf(z);
-    case ACT_RELU: return z != z ? z : act_f<float, ACT_RELU>(z);
-    case ACT_SMOOTHRELU: return z != z ? z : act_f<float, ACT_SMOOTHRELU>(z);
-    default: return z;
-  }
+// sigma and sigma'. A NaN stays one.
+template <typename T, int ACT>
+__device__ __forceinline__ float sigma(float z) {
+  if constexpr (ACT == ACT_TANH) return sizeof(T) == 2 ? tanh16(z) : tanhf(z);
+  else return z != z ? z : act_f<float, ACT>(z);
 }
 
-template <typename T>
-__device__ __forceinline__ float dsigma(float z, int act) {
+template <typename T, int ACT>
+__device__ __forceinline__ float dsigma(float z) {
+  if constexpr (ACT == ACT_TANH) return dtanh<T>(z);
+  else if constexpr (ACT == ACT_IDENTITY) return 1.f;
+  else return z != z ? z : dact_f<float, ACT>(z);
+}
+
+// Calls f with the activation as a compile-time constant (uniform over the launch).
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
   switch (act) {
-    case ACT_TANH: return dtanh<T>(z);
-    case ACT_RELU: return z != z ? z : dact_f<float, ACT_RELU>(z);
-    case ACT_SMOOTHRELU: return z != z ? z : dact_f<float, ACT_SMOOTHRELU>(z);
-    default: return 1.f;
+    case ACT_TANH: return f(std::integral_constant<int, ACT_TANH>{});
+    case ACT_RELU: return f(std::integral_constant<int, ACT_RELU>{});
+    case ACT_SMOOTHRELU: return f(std::integral_constant<int, ACT_SMOOTHRELU>{});
+    default: return f(std::integral_constant<int, ACT_IDENTITY>{});
   }
 }
 
@@ -75,101 +96,104 @@ struct EpStep {
     float h;
     int act;
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
-    const int half = 4 * (c.lane >> 5);
+    const int nb = (c.N + CK_BLOCK - 1) / CK_BLOCK;
+    with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int n0 = c.nw + 32 * j;
-      if (n0 >= c.N) continue;
-      f32x4 bias[4];
+      for (int j = 0; j < FN; ++j) {
+        if (!WHOLE && c.nw + 32 * j >= c.N) continue;
+        f32x4 bias[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) bias[q] = a.b ? mm::load4(a.b, n0 + 8 * q + half, c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int q = 0; q < 4; ++q)
+          bias[q] = a.b ? mm::load4<WHOLE>(a.b, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const int m = c.mw + 32 * i + (c.lane & 31);
-        const bool on = m < c.M;
-        const size_t row = (size_t)(on ? m : 0) * c.N;
-        f32x4 v[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = n0 + 8 * q + half;
-          const f32x4 z = mm::quad(acc[i][j], q) + bias[q];
-          f32x4 r = {0.f, 0.f, 0.f, 0.f};
-          if (a.r && on && n < c.N) r = mm::load4(a.r + row, n, c.N);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[q][k] = (float)(T)(r[k] + a.h * sigma<T>(z[k], a.act));
-          if (on && n < c.N) mm::store4(a.y + row, n, c.N, v[q]);
-        }
-        if (a.y8) {  // uniform over the launch
-          uint32_t top = 0;
+        for (int i = 0; i < FM; ++i) {
+          const int m = c.row(i);
+          const bool on = m < c.M;
+          const size_t row = (size_t)(on ? m : c.M - 1) * c.N;
+          f32x4 v[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (n0 + 8 * q + half + k < c.N) top = max(top, abs_bits(v[q][k]));
-          top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-          const uint32_t byte = ck_byte<T>(top);
-          const float inv = ck_inv(byte);
-          if (!on) continue;
+            v[q] = a.r ? mm::load4<WHOLE>(a.r + row, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+          uint32_t top = 0;
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const int n = n0 + 8 * q + half;
-            typename mm::GVec<int8_t, 4>::type w;
+            const f32x4 z = mm::quad(acc[i][j], q) + bias[q];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = (int8_t)ck_round(v[q][k], inv);
-            if (n + 4 <= c.N) {
-              *reinterpret_cast<typename mm::GVec<int8_t, 4>::type*>(a.y8 + row + n) = w;
-            } else {
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                if (n + k < c.N) a.y8[row + n + k] = w[k];
+            for (int k = 0; k < 4; ++k) {
+              v[q][k] = (float)(T)(v[q][k] + a.h * sigma<T, decltype(act)::value>(z[k]));
+              if (WHOLE || c.feature(j, q) + k < c.N) top = max(top, abs_bits(v[q][k]));
             }
           }
-          if (half == 0) a.ye[(size_t)m * ((c.N + CK_BLOCK - 1) / CK_BLOCK) + n0 / CK_BLOCK] = (uint8_t)byte;
+          if (on) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mm::store4<WHOLE>(a.y + row, c.feature(j, q), c.N, v[q]);
+          }
+          if (a.y8) {
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+            const uint32_t byte = ck_byte<T>(top);
+            const float inv = ck_inv(byte);
+            if (on) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) store_ck<WHOLE>(a.y8 + row, c.feature(j, q), c.N, v[q], inv);
+              if (c.lane < 32) a.ye[(size_t)m * nb + (c.nw + 32 * j) / CK_BLOCK] = (uint8_t)byte;
+            }
+          }
         }
       }
-    }
+    });
   }
 };
 
-// g = sigma'(D + b) dy, and the sums of its columns over the tile's rows (fp32, before rounding)
+// g = sigma'(D + b) dy (rows of ld values, zeros behind the N that count), and the sums of its
+// columns over the tile's rows (fp32, before rounding)
 template <typename T>
 struct EpGrad {
   struct Args {
     const T* b;
     const T* dy;
     T* g;
+    int ld;
     float* part;  // [tile rows][N]
     int act;
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
-    const int half = 4 * (c.lane >> 5);
     f32x16 sums[FN];
+    with_act(a.act, [&](auto act) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int n0 = c.nw + 32 * j;
-      sums[j] = 0.f;
+      for (int j = 0; j < FN; ++j) {
+        sums[j] = 0.f;
+        if (!WHOLE && c.nw + 32 * j >= a.ld) continue;
+        f32x4 bias[4];
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const int m = c.mw + 32 * i + (c.lane & 31);
+        for (int q = 0; q < 4; ++q)
+          bias[q] = a.b ? mm::load4<WHOLE>(a.b, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = n0 + 8 * q + half;
-          if (m >= c.M || n >= c.N) continue;
-          f32x4 z = mm::quad(acc[i][j], q);
-          if (a.b) z += mm::load4(a.b, n, c.N);
-          f32x4 g = mm::load4(a.dy + (size_t)m * c.N, n, c.N);
+        for (int i = 0; i < FM; ++i) {
+          const int m = c.row(i);
+          const bool on = m < c.M;
+          const size_t row = on ? m : c.M - 1;
+          f32x4 g[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            g[k] *= dsigma<T>(z[k], a.act);
-            sums[j][4 * q + k] += g[k];
+          for (int q = 0; q < 4; ++q) g[q] = mm::load4<WHOLE>(a.dy + row * c.N, c.feature(j, q), c.N);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 z = mm::quad(acc[i][j], q) + bias[q];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              g[q][k] = on && (WHOLE || c.feature(j, q) + k < c.N) ? g[q][k] * dsigma<T, decltype(act)::value>(z[k]) : 0.f;
+              sums[j][4 * q + k] += g[q][k];
+            }
           }
-          mm::store4(a.g + (size_t)m * c.N, n, c.N, g);
+          if (on) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mm::store4<WHOLE>(a.g + row * a.ld, c.feature(j, q), a.ld, g[q]);
+          }
         }
       }
-    }
+    });
     mm::column_sums<FN, WGM, WGN>(sums, c, lds, a.part + (size_t)c.mt * c.N);
   }
 };
@@ -182,22 +206,22 @@ struct EpDx {
     T* dx;
     float h;
   };
-  template <int FM, int FN, int WGM, int WGN>
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      const int m = c.mw + 32 * i + (c.lane & 31);
+      const int m = c.row(i);
       if (m >= c.M) continue;
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
+      for (int j = 0; j < FN; ++j) {
+        f32x4 v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int n = c.nw + 32 * j + 8 * q + 4 * (c.lane >> 5);
-          if (n >= c.N) continue;
-          f32x4 v = mm::quad(acc[i][j], q) * a.h;
-          if (a.dy) v += mm::load4(a.dy + (size_t)m * c.N, n, c.N);
-          mm::store4(a.dx + (size_t)m * c.N, n, c.N, v);
-        }
+        for (int q = 0; q < 4; ++q)
+          v[q] = a.dy ? mm::load4<WHOLE>(a.dy + (size_t)m * c.N, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          mm::store4<WHOLE>(a.dx + (size_t)m * c.N, c.feature(j, q), c.N, v[q] + mm::quad(acc[i][j], q) * a.h);
+      }
     }
   }
 };
@@ -218,27 +242,23 @@ __global__ __launch_bounds__(256) void k_ck_store(const T* x, int8_t* x8, uint8_
     for (int o = 1; o < 8; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
     const uint32_t byte = ck_byte<T>(top);
     const float inv = ck_inv(byte);
-    typename mm::GVec<int8_t, 4>::type w;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = (int8_t)ck_round(v[k], inv);
-    int8_t* out = x8 + row * q + n;
-    if (n + 4 <= q) {
-      *reinterpret_cast<typename mm::GVec<int8_t, 4>::type*>(out) = w;
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (n + k < q) out[k] = w[k];
-    }
+    store_ck(x8 + row * q, n, q, v, inv);
     if (part == 0) xe[blk] = (uint8_t)byte;
   }
 }
 
+// Rows of ld >= q values, zeros behind the q that count (ld at most the next multiple of 32).
 template <typename T>
-__global__ __launch_bounds__(256) void k_ck_load(const int8_t* x8, const uint8_t* xe, T* x, size_t nblk, int q, int nb) {
+__global__ __launch_bounds__(256) void k_ck_load(const int8_t* x8, const uint8_t* xe, T* x, size_t nblk, int q, int nb,
+                                                 int ld) {
   for (size_t blk = (size_t)blockIdx.x * 32 + (threadIdx.x >> 3); blk < nblk; blk += (size_t)gridDim.x * 32) {
     const size_t row = blk / nb;
     const int n = (int)(blk - row * nb) * CK_BLOCK + 4 * (threadIdx.x & 7);
-    if (n < q) mm::store4(x + row * q, n, q, mm::load4(x8 + row * q, n, q) * ck_scale(xe[blk]));
+    // (a block that is not finite is NaN in the row's features only: the rest of ld is zero)
+    f32x4 v = mm::load4(x8 + row * q, n, q) * ck_scale(xe[blk]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = n + k < q ? v[k] : 0.f;
+    if (n < ld) mm::store4(x + row * ld, n, ld, v);
   }
 }
 
@@ -253,10 +273,10 @@ hipError_t ck_store_t(const void* x, int8_t* x8, uint8_t* xe, long B, int q, hip
 }
 
 template <typename T>
-hipError_t ck_load_t(const int8_t* x8, const uint8_t* xe, void* x, long B, int q, hipStream_t st) {
+hipError_t ck_load_t(const int8_t* x8, const uint8_t* xe, void* x, long B, int q, int ld, hipStream_t st) {
   const int nb = mm::ceil_div(q, CK_BLOCK);
   const size_t nblk = (size_t)B * nb;
-  k_ck_load<T><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb);
+  k_ck_load<T><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb, ld);
   return hipGetLastError();
 }
 
@@ -266,8 +286,13 @@ inline mm::Prob prob(const void* A, long lda, const void* B, long ldb, int M, in
 
 template <typename T>
 hipError_t step_forward_t(const StepArgs& a, hipStream_t st) {
+  const StepLayout l = step_layout(a.dtype, a.B, a.ni, a.no);
+  char* w = static_cast<char*>(a.ws);
+  const mm::Operand<T> x(a.x, a.B, a.ni, w + l.x, st), W(a.W, a.no, a.ni, w + l.W, st);
+  if (x.e != hipSuccess) return x.e;
+  if (W.e != hipSuccess) return W.e;
   typename EpStep<T>::Args e{(const T*)a.b, (const T*)a.r, (T*)a.y, a.y8, a.ye, (float)a.h, a.act};
-  return mm::launch_mm<T, false, false, EpStep<T>>(prob(a.x, a.ni, a.W, a.ni, a.B, a.no, a.ni), e, 1, st);
+  return mm::launch_mm<T, false, false, EpStep<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), e, 1, st);
 }
 
 template <typename T>
@@ -275,27 +300,28 @@ hipError_t step_backward_t(const StepArgs& a, hipStream_t st) {
   const StepLayout l = step_layout(a.dtype, a.B, a.ni, a.no);
   char* w = static_cast<char*>(a.ws);
   T* g = reinterpret_cast<T*>(w + l.g);
+  const int ldg = mm::padded(sizeof(T), a.no), ldx = mm::padded(sizeof(T), a.ni);
   float* colpart = reinterpret_cast<float*>(w + l.col);
   float* part = reinterpret_cast<float*>(w + l.part);
-  const void* x = a.x;
   hipError_t e = hipSuccess;
-  if (!x) {
-    x = w + l.x;
-    if (a.B && (e = ck_load_t<T>(a.x8, a.xe, w + l.x, a.B, a.ni, st)) != hipSuccess) return e;
-  }
+  if (!a.x && a.B && (e = ck_load_t<T>(a.x8, a.xe, w + l.x, a.B, a.ni, ldx, st)) != hipSuccess) return e;
+  mm::Operand<T> x(a.x ? a.x : w + l.x, a.x ? a.B : 0, a.ni, w + l.x, st);
+  const mm::Operand<T> W(a.W, a.no, a.ni, w + l.W, st);
+  if (x.e != hipSuccess) return x.e;
+  if (W.e != hipSuccess) return W.e;
   if (a.B) {  // (an empty batch leaves zero sums: products over no rows)
-    typename EpGrad<T>::Args eg{(const T*)a.b, (const T*)a.dy, g, colpart, a.act};
-    e = mm::launch_mm<T, false, false, EpGrad<T>>(prob(x, a.ni, a.W, a.ni, a.B, a.no, a.ni), eg, 1, st);
+    typename EpGrad<T>::Args eg{(const T*)a.b, (const T*)a.dy, g, ldg, colpart, a.act};
+    e = mm::launch_mm<T, false, false, EpGrad<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), eg, 1, st);
     if (e != hipSuccess) return e;
   }
   const float h = (float)a.h;
   if (a.dx && a.B) {
     typename EpDx<T>::Args ed{a.residual ? (const T*)a.dy : nullptr, (T*)a.dx, h};
-    e = mm::launch_mm<T, false, true, EpDx<T>>(prob(g, a.no, a.W, a.ni, a.B, a.ni, a.no), ed, 1, st);
+    e = mm::launch_mm<T, false, true, EpDx<T>>(prob(g, ldg, W.p, W.ld, a.B, a.ni, a.no), ed, 1, st);
     if (e != hipSuccess) return e;
   }
   if (a.dW) {
-    const mm::Prob p = prob(g, a.no, x, a.ni, a.no, a.ni, a.B);
+    const mm::Prob p = prob(g, ldg, x.p, x.ld, a.no, a.ni, a.B);
     if (l.splits > 1) {
       e = mm::launch_mm<T, true, true, mm::EpPart>(p, mm::EpPart::Args{part}, l.splits, st);
       if (e != hipSuccess) return e;
@@ -316,5 +342,5 @@ hipError_t step_backward_t(const StepArgs& a, hipStream_t st) {
   return e;
 }
 
-}  // namespace
+}  // namespace wide
 }  // namespace lp
