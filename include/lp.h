@@ -407,8 +407,9 @@ typedef struct {
 } lp_label_head;
 
 /* Workspace bytes of lp_loss_labels, with grad != 0 when any gradient is asked
- * for; 0 for an invalid head. It grows with B nc / 16 at most, and holds the
- * probabilities of one piece of the vocabulary at a time. */
+ * for; 0 for an invalid head. It holds 8 bytes per row and tile of 64 to 256
+ * classes, and with gradients the probabilities of one piece of the vocabulary at
+ * a time (256 MiB or 256 classes). */
 size_t lp_loss_labels_workspace_bytes(const lp_label_head* head, int32_t grad);
 
 /* Softmax cross-entropy of integer labels: z_k = W u_k + mu, u [B][q], W [nc][q],

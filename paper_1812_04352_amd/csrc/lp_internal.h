@@ -9,6 +9,15 @@
 
 namespace lp {
 
+namespace mm {
+// How a product of the wide operators runs (lp_mm.h): its tile size (256, 128 or 64, square)
+// and splits of the contraction.
+struct Plan {
+  int tile, splits, tm, tn;
+  size_t part_bytes() const { return splits > 1 ? (size_t)splits * tm * tn * tile * tile * 4 : 0; }
+};
+}  // namespace mm
+
 // Tracing hook. While a traced call runs, the kernels it launches record their
 // own start (the first launch) and end (every launch; the last one stands) into
 // these events on the dispatch itself, so tracing puts no marker packets into
@@ -240,10 +249,10 @@ struct StepArgs {
 };
 
 // Workspace of a step: offsets of g, of copies of x (or its checkpoint's values) and W whose
-// rows start on 16 bytes, the column partials of db and the partial products of dW.
+// rows start on 16 bytes, the column partials of db and the partial sums of split products.
 struct StepLayout {
   size_t g, x, W, col, part, total;
-  int splits;
+  mm::Plan z, zx, zw;  // the products x W^T, g W and g^T x
 };
 StepLayout step_layout(int dtype, int B, int ni, int no);
 
@@ -266,7 +275,8 @@ struct LabelArgs {
 struct LabelLayout {
   size_t part, zl, row;                                           // losses
   size_t u, W;                                                    // copies with rows on 16 bytes
-  size_t from, to, lab, count, scale, lse, P, du, col, wpart;     // gradients
+  size_t from, to, lab, count, scale, lse, P, du, col;            // gradients
+  size_t split;                                                   // partial sums of split products
   size_t total;
   int piece;  // classes taken at a time
 };

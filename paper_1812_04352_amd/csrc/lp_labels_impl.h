@@ -56,22 +56,16 @@ struct EpLse {
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     MaxSum* red = reinterpret_cast<MaxSum*>(lds);  // [WGN][rows of the tile]
     constexpr int BM = WGM * FM * 32;
-    if (a.mu) {
+    f32x4 mu[FN][4];
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 b = mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N);
-#pragma unroll
-          for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] += b[k];
-        }
-    }
+      for (int q = 0; q < 4; ++q)
+        mu[j][q] = a.mu ? mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       const int m = c.row(i);
-      // the label's place among the lane's values: class nw + 32 j + 8 q + 4 (lane / 32) + k
+      // the label's place among the wave's classes
       const int64_t l = (m < c.M ? a.labels[m] : -1) - a.j0;
       const int at = l >= 0 && l < c.N ? (int)l - c.nw : -1;
       float top = -INFINITY, zl = 0.f;
@@ -81,10 +75,9 @@ struct EpLse {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int n = c.feature(j, r >> 2) - c.nw + (r & 3);
-          if (!WHOLE && c.nw + n >= c.N) acc[i][j][r] = -INFINITY;
-          const float z = acc[i][j][r];
+          const float z = acc[i][j][r] + mu[j][r >> 2][r & 3];
           if (at == n) zl = z, mine = true;
-          top = fmaxf(top, z);
+          if (WHOLE || c.nw + n < c.N) top = fmaxf(top, z);
         }
       if (mine) a.zl[m] = zl;
       // a NaN is no maximum; it comes back through the sum (exp of NaN)
@@ -93,7 +86,8 @@ struct EpLse {
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s += exp_of(acc[i][j][r] - ref);
+        for (int r = 0; r < 16; ++r)
+          if (WHOLE || c.feature(j, r >> 2) + (r & 3) < c.N) s += exp_of((acc[i][j][r] + mu[j][r >> 2][r & 3]) - ref);
       MaxSum v{top, s};
       v = join(v, MaxSum{__shfl_xor(v.m, 32, 64), __shfl_xor(v.s, 32, 64)});
       if (c.lane < 32) red[c.wn * BM + c.wm * FM * 32 + 32 * i + c.lane] = v;
@@ -125,41 +119,40 @@ struct EpProb {
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     f32x16 sums[FN];
-    if (a.mu) {
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 b = mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N);
-#pragma unroll
-          for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[i][j][4 * q + k] += b[k];
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < FN; ++j) sums[j] = 0.f;
+    int at[FM];  // the label's place among the wave's classes
+    float lse[FM];
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-      const int m = c.row(i);
-      if (m >= c.M) continue;
+      const int m = min(c.row(i), c.M - 1);
       const int64_t l = a.labels[m] - a.j0;
-      const int at = l >= 0 && l < c.N ? (int)l - c.nw : -1;
-      const float lse = a.lse[m];
+      at[i] = l >= 0 && l < c.N ? (int)l - c.nw : -1;
+      lse[i] = a.lse[m];
+    }
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
+    for (int j = 0; j < FN; ++j) {
+      sums[j] = 0.f;
+      if (!WHOLE && c.nw + 32 * j >= a.ld) continue;
+      f32x4 mu[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        mu[q] = a.mu ? mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int m = c.row(i);
+        if (m >= c.M) continue;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          f32x4 z = mm::quad(acc[i][j], q);
+          f32x4 z = mm::quad(acc[i][j], q) + mu[q];
           const int n = c.feature(j, q) - c.nw;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            z[k] = exp_of(z[k] - lse) - (at == n + k ? 1.f : 0.f);
+            z[k] = exp_of(z[k] - lse[i]) - (at[i] == n + k ? 1.f : 0.f);
             if (!WHOLE && c.nw + n + k >= c.N) z[k] = 0.f;
             sums[j][4 * q + k] += z[k];
           }
           mm::store4<WHOLE>(a.P + (size_t)m * a.ld, c.nw + n, a.ld, z * PSCALE<T>);
         }
+      }
     }
     if (a.part) mm::column_sums<FN, WGM, WGN>(sums, c, lds, a.part + (size_t)c.mt * a.part_ld);
   }
@@ -253,21 +246,34 @@ __global__ __launch_bounds__(256) void k_gather(const T* u, const int* to, int B
   for (int i = 4 * lane; i < ld; i += 256) mm::store4(uc + (size_t)r * ld, i, ld, mm::load4(u + (size_t)b * q, i, q));
 }
 
-// Joins the class tiles of a row: lse and the loss. 16 rows per workgroup, 16 threads a row.
+// Joins the class tiles of a row: lse and the loss. `per` rows (a power of two) by 256 / per threads
+// a workgroup: many threads a row where there are few rows (16 rows of 1024 tiles: 33 us with 16
+// threads a row, 5 with 128).
 // labels as in EpLse; a row without one has loss 0. from (nullable): where row r's loss goes.
 static __global__ __launch_bounds__(256) void k_lse(const MaxSum* part, int tiles, long rows, const int64_t* labels, int nc,
-                                             const float* zl, const int* count, int M, const int* from, float* lse,
-                                             float* loss) {
-  __shared__ MaxSum red[16][17];
+                                                    const float* zl, const int* count, int M, const int* from, float* lse,
+                                                    float* loss, int per) {
+  __shared__ MaxSum red[256];
   if (count) M = min(M, *count);
-  const int r = threadIdx.x & 15, g = threadIdx.x >> 4, m = blockIdx.x * 16 + r;
+  const int r = threadIdx.x & (per - 1), g = threadIdx.x / per, groups = 256 / per, m = blockIdx.x * per + r;
   MaxSum v{-INFINITY, 0.f};
-  if (m < M)
-    for (int t = g; t < tiles; t += 16) v = join(v, part[(size_t)t * rows + m]);
-  red[g][r] = v;
-  __syncthreads();
+  if (m < M) {
+    int t = g;
+    for (; t + 3 * groups < tiles; t += 4 * groups) {
+      MaxSum w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = part[(size_t)(t + k * groups) * rows + m];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v = join(v, w[k]);
+    }
+    for (; t < tiles; t += groups) v = join(v, part[(size_t)t * rows + m]);
+  }
+  red[threadIdx.x] = v;
+  for (int half = groups / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (g < half) red[threadIdx.x] = v = join(v, red[threadIdx.x + half * per]);
+  }
   if (g || m >= M) return;
-  for (int k = 1; k < 16; ++k) v = join(v, red[k][r]);
   const float l = v.m + logf(v.s);
   if (lse) lse[m] = l;
   const int64_t lab = labels[m];
@@ -295,7 +301,7 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   MaxSum* part = reinterpret_cast<MaxSum*>(w + l.part);
   float* zl = reinterpret_cast<float*>(w + l.zl);
   float* row = a.row ? a.row : reinterpret_cast<float*>(w + l.row);
-  const int tiles = mm::ceil_div(a.nc, mm::TILE), ldu = mm::padded(sizeof(T), a.q);
+  const int ldu = mm::padded(sizeof(T), a.q);
   const T* W = static_cast<const T*>(a.W);
   const T* mu = static_cast<const T*>(a.mu);
   int* from = reinterpret_cast<int*>(w + l.from);
@@ -308,7 +314,7 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   T* P = reinterpret_cast<T*>(w + l.P);
   float* acc32 = reinterpret_cast<float*>(w + l.du);
   float* col = reinterpret_cast<float*>(w + l.col);
-  float* wpart = reinterpret_cast<float*>(w + l.wpart);
+  void* split = w + l.split;
   hipError_t e = hipSuccess;
   // rows of the products: u's own, or with gradients the labelled ones
   const T* rows = uc;
@@ -326,17 +332,22 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const int* cnt = grad ? count : nullptr;
   const int64_t* labels = grad ? lab : a.labels;
+  int tiles = 0;  // class tiles so far
   for (int j0 = 0; j0 < a.nc && a.B; j0 += l.piece) {
     const int n = std::min(l.piece, a.nc - j0);
+    const mm::Plan pl = mm::plan_of(sizeof(T), a.B, n, a.q);
     const mm::Operand<T> Wj(W + (size_t)j0 * a.q, n, a.q, w + l.W, st);
     if (Wj.e != hipSuccess) return Wj.e;
-    typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)(j0 / mm::TILE) * a.B, zl, a.B, j0};
+    typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)tiles * a.B, zl, a.B, j0};
     const mm::Prob p{rows, Wj.p, ldr, Wj.ld, a.B, n, a.q, cnt, 1, 0, 0, 0, 0};
-    if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, 1, st)) != hipSuccess) return e;
+    if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, pl, split, st)) != hipSuccess) return e;
+    tiles += pl.tn;
   }
-  if (a.B)
-    k_lse<<<(unsigned)mm::ceil_div(a.B, 16), 256, 0, st>>>(part, tiles, a.B, labels, a.nc, zl, cnt, a.B, grad ? from : nullptr,
-                                                           grad ? lse : nullptr, row);
+  if (a.B) {
+    const int per = a.B >= 2048 ? 16 : 2;
+    k_lse<<<(unsigned)mm::ceil_div(a.B, per), 256, 0, st>>>(part, tiles, a.B, labels, a.nc, zl, cnt, a.B,
+                                                            grad ? from : nullptr, grad ? lse : nullptr, row, per);
+  }
   k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
   if ((e = hipGetLastError()) != hipSuccess || !grad) return e;
   for (int j0 = 0; j0 < a.nc; j0 += l.piece) {
@@ -344,38 +355,30 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
     const mm::Operand<T> Wj(W + (size_t)j0 * a.q, a.B ? n : 0, a.q, w + l.W, st);
     if (Wj.e != hipSuccess) return Wj.e;
     if (a.B) {
-      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, ldp, a.dmu ? col + j0 : nullptr, a.nc, j0};
+      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, ldp, a.dmu ? col : nullptr, n, j0};
+      const mm::Plan pl = mm::plan_of(sizeof(T), a.B, n, a.q);
       const mm::Prob pp{uc, Wj.p, ldu, Wj.ld, a.B, n, a.q, count, 1, 0, 0, 0, 0};
-      if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, 1, st)) != hipSuccess) return e;
+      if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, pl, split, st)) != hipSuccess) return e;
+      if (a.dmu)
+        mm::k_colsum<T><<<(unsigned)mm::ceil_div(n, 64), 256, 0, st>>>(col, pl.tm, pl.tile, count, n, (T*)a.dmu + j0, 1.f, scale);
+    } else if (a.dmu) {
+      mm::k_colsum<T><<<(unsigned)mm::ceil_div(n, 64), 256, 0, st>>>(col, 0, 1, nullptr, n, (T*)a.dmu + j0, 1.f, scale);
     }
     if (a.du && a.B) {
       typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
       const mm::Prob pd{P, Wj.p, ldp, Wj.ld, a.B, a.q, n, count, 1, 0, 0, 0, 0};
-      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, 1, st)) != hipSuccess) return e;
+      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n), split, st)) != hipSuccess)
+        return e;
     }
     if (a.dW) {
       T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
       const mm::Prob pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
-      const int splits = mm::splits_of(sizeof(T), n, a.q, a.B);
-      if (splits > 1) {
-        if ((e = mm::launch_mm<T, true, true, mm::EpPart>(pw, mm::EpPart::Args{wpart}, splits, st)) != hipSuccess) return e;
-        const size_t nw = (size_t)n * a.q;
-        mm::k_join<T><<<(unsigned)std::min<size_t>((nw + 1023) / 1024, 4096), 256, 0, st>>>(wpart, splits, nw, dW,
-                                                                                            1.f / PSCALE<T>, scale);
-        e = hipGetLastError();
-      } else {
-        e = mm::launch_mm<T, true, true, mm::EpScale<T>>(
-            pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale}, 1, st);
-      }
+      e = mm::launch_mm<T, true, true, mm::EpScale<T>>(pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale},
+                                                       mm::plan_of(sizeof(T), n, a.q, a.B), split, st);
       if (e != hipSuccess) return e;
     }
   }
-  if (a.dmu) {
-    mm::k_colsum<T><<<(unsigned)mm::ceil_div(a.nc, 256), 256, 0, st>>>(col, mm::ceil_div(a.B, mm::TILE), mm::TILE, count, a.nc,
-                                                                     (T*)a.dmu, 1.f, scale);
-    e = hipGetLastError();
-  }
-  return e;
+  return hipGetLastError();
 }
 
 }  // namespace wide

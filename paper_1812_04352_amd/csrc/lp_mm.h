@@ -14,12 +14,11 @@
 // consecutive features at a time (vector loads and stores of rows), and sums over a row
 // need one exchange with lane l ^ 32.
 //
-// LDS holds KB = 128 bytes of the contraction (64 values of 16 bits, 32 floats) of every
-// row of the tile, twice (one stage is filled while the other is read; one barrier a
-// stage), in 16-byte chunks.
-//   rows:    chunk c of row r lies at r * 8 + (c ^ (r & 7)): the eight chunks of a bank
-//            cycle that a fragment read takes (eight rows, one chunk index) hit different
-//            banks, and so do the writes.
+// LDS holds several stages of KB bytes of the contraction of every row of the tile (some are
+// filled while one is read; one barrier a stage), in 16-byte chunks.
+//   rows:    the chunks of a row are exchanged by a part of the row's index, so that the eight
+//            chunks of a bank cycle that a fragment read takes (eight rows, one chunk index)
+//            lie in different banks.
 //   columns: row k of the stage holds its R columns; fragments of 16-bit types are read
 //            with the transposing LDS load, which hands lane i of 16 the values (k0..k0+3,
 //            column i) from four rows' 32-byte pieces. Chunks are exchanged by 64 bytes
@@ -30,8 +29,10 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lp_device.h"
+#include "lp_internal.h"
 
 namespace lp {
 namespace mm {
@@ -45,8 +46,6 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int KB = 128;  // bytes of the contraction per row and stage
 
 // N consecutive values in global memory, with their element's alignment
 template <typename T, int N> struct GVec { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
@@ -99,20 +98,25 @@ __device__ __forceinline__ void store4(T* row, int n, int N, f32x4 v) {
   }
 }
 
-// One operand's tile of R rows of D, straight from global memory to LDS. Arrays start on 16
-// bytes and so do their rows.
-template <typename T, int R, int NT, bool COLS>
+// One operand's tile of R rows of D, KB bytes of the contraction a row, straight from global
+// memory to LDS. Arrays start on 16 bytes and so do their rows.
+template <typename T, int R, int KB, int NT, bool COLS>
 struct Stage {
   static constexpr int V = 16 / sizeof(T);           // values per chunk
   static constexpr int BK = KB / (int)sizeof(T);     // contraction values per stage
-  static constexpr int PER = R * 8 / NT;             // chunks per thread
+  static constexpr int RC = KB / 16;                 // rows: chunks per row
+  static constexpr int PER = R * RC / NT;            // chunks per thread
   static constexpr int CH = R / V;                   // columns: chunks per row of the stage
   static constexpr int SWZ = (sizeof(T) == 2 ? 12 : 8) & (CH - 1);
-  static_assert(R * 8 % NT == 0, "whole chunks per thread");
-  static_assert(NT % 64 == 0 && (COLS ? NT / CH % 4 == 0 : true), "the exchange is the same for all of a thread's chunks");
+  static_assert(R * RC % NT == 0, "whole chunks per thread");
+  static_assert(!COLS || NT / CH % (sizeof(T) == 2 ? 4 : 8) == 0, "the exchange is the same for all of a thread's chunks");
+  static_assert(KB == 64 || KB == 128, "the rows' exchange");
 
   static __device__ __forceinline__ int swz(int k) {  // columns: chunk exchange of row k
     return (sizeof(T) == 2 ? k << 2 : k << 1) & SWZ;
+  }
+  static __device__ __forceinline__ int rswz(int r) {  // rows: chunk exchange of row r
+    return KB == 128 ? r & 7 : (r >> 1) & 3;
   }
 
   const unsigned char* base;  // of the next stage (uniform)
@@ -128,13 +132,13 @@ struct Stage {
     k = k0;
     k1 = k1_;
     if constexpr (!COLS) {
-      const int c = (t & 7) ^ ((t >> 3) & 7);
+      const int c = (t % RC) ^ rswz(t / RC);
       kc = c * V;
       base = static_cast<const unsigned char*>(p) + ((long)r0 * ld + k0) * (long)sizeof(T);
       left = ((long)(rows - r0) * ld - k0) * (long)sizeof(T);
       step = KB;
 #pragma unroll
-      for (int i = 0; i < PER; ++i) off[i] = (uint32_t)((t + i * NT) >> 3) * (uint32_t)(ld * sizeof(T)) + c * 16;
+      for (int i = 0; i < PER; ++i) off[i] = (uint32_t)((t + i * NT) / RC) * (uint32_t)(ld * sizeof(T)) + c * 16;
     } else {
       const int c = (t % CH) ^ swz(t / CH);
       kc = 0;
@@ -146,49 +150,69 @@ struct Stage {
     }
   }
 
-  // Requests the next stage. Loads past `left` give zeros: rows past the last (rows), contraction
-  // indices past the last (columns); so does an offset of 2^31 (rows: past the contraction's end).
-  __device__ __forceinline__ void load(unsigned char* lds) {
+  // Requests the next stage; wave: the wave's index in a scalar register. Loads past `left` give
+  // zeros: rows past the last (rows), contraction indices past the last (columns); so does an
+  // offset of 2^31 (rows: past the contraction's end, which only the last stage can hold).
+  __device__ __forceinline__ void load(unsigned char* lds, int wave) {
 #ifdef __HIP_DEVICE_COMPILE__  // (buffer resources are no type of the host compilation)
     typedef __attribute__((address_space(3))) void lds_void;
-    const __amdgpu_buffer_rsrc_t r =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, left < 0x7fffffff ? (int)left : 0x7fffffff, 0x00020000);
-    const bool past = !COLS && k + kc >= k1;
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<unsigned char*>(base), 0, (left >> 31) != 0 ? 0x7fffffff : (int)left, 0x00020000);
+    if (!COLS && k + BK > k1) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) off[i] = k + kc >= k1 ? 0x80000000u : off[i];
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(lds + (i * NT + (threadIdx.x & ~63)) * 16), 16,
-                                               past ? 0x80000000u : off[i], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(lds + (i * NT + wave * 64) * 16), 16, off[i], 0, 0, 0);
     base += step;
     left -= step;
     k += BK;
 #endif
   }
 
-  // the fragment of rows r0..r0+31 and contraction step kk (two chunks) of a stage
-  static __device__ __forceinline__ typename Frag<T>::type frag(const unsigned char* lds, int r0, int kk, int lane) {
-    typedef typename Frag<T>::type F;
+};
+
+// Reads a wave's fragments of one operand: NF blocks of 32 rows of D from row r0 of the tile on.
+// A lane's offsets into a stage are kept in registers as far as the exchange of chunks makes them
+// differ (rows: per contraction step; columns: per block), the rest is the load's own offset.
+template <typename T, class S, int KB, int NF, bool COLS>
+struct Reader {
+  typedef typename Frag<T>::type F;
+  static constexpr int N = COLS ? NF : KB / 32;
+  uint32_t at[N];
+
+  __device__ __forceinline__ Reader(int r0, int lane) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
+      if constexpr (!COLS) {
+        const int r = r0 + (lane & 31), c = 2 * x + (lane >> 5);
+        at[x] = (r * S::RC + (c ^ S::rswz(r))) * 16;
+      } else if constexpr (sizeof(T) == 2) {
+        const int col = r0 + 32 * x + 16 * ((lane >> 4) & 1) + 4 * (lane & 3), k = 8 * (lane >> 5) + ((lane >> 2) & 3);
+        at[x] = (k * S::CH + ((col / S::V) ^ S::swz(k))) * 16 + (col % S::V) * 2;
+      } else {
+        const int col = r0 + 32 * x + (lane & 31), k = 4 * (lane >> 5);
+        at[x] = (k * S::CH + ((col / S::V) ^ S::swz(k))) * 16 + (col % S::V) * 4;
+      }
+    }
+  }
+
+  // block i, contraction step kk (two chunks) of the stage at lds
+  __device__ __forceinline__ F operator()(const unsigned char* lds, int i, int kk) const {
     if constexpr (!COLS) {
-      const int r = r0 + (lane & 31), c = 2 * kk + (lane >> 5);
-      return *reinterpret_cast<const F*>(lds + (r * 8 + (c ^ (r & 7))) * 16);
+      return *reinterpret_cast<const F*>(lds + at[kk] + i * 32 * KB);
     } else if constexpr (sizeof(T) == 2) {
       typedef __attribute__((address_space(3))) s16x4 lds4;
-      const int col = r0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
       s16x4 h[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int k = 16 * kk + 8 * (lane >> 5) + 4 * j + ((lane >> 2) & 3);
-        const unsigned char* a = lds + (k * CH + ((col / V) ^ swz(k))) * 16 + (col % V) * 2;
-        h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)a);
-      }
+      for (int j = 0; j < 2; ++j)
+        h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + at[i] + (16 * kk + 4 * j) * S::CH * 16));
       return __builtin_bit_cast(F, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
       F v;
-      const int col = r0 + (lane & 31);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int k = 8 * kk + 4 * (lane >> 5) + j;
-        v[j] = *reinterpret_cast<const float*>(lds + (k * CH + ((col / V) ^ swz(k))) * 16 + (col % V) * 4);
-      }
+      for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(lds + at[i] + (8 * kk + j) * S::CH * 16);
       return v;
     }
   }
@@ -231,14 +255,26 @@ __device__ __forceinline__ void tile_of(int id, int tm, int tn, int& mt, int& nt
   nt = in / rows;
 }
 
-template <typename T, int BM, int BN, int WGM, int WGN, bool AT, bool BT, class E>
-__global__ __launch_bounds__(64 * WGM * WGN) void k_mm(Prob p, typename E::Args ea) {
-  constexpr int NT = 64 * WGM * WGN, FM = BM / WGM / 32, FN = BN / WGN / 32;
-  typedef Stage<T, BM, NT, AT> SA;
-  typedef Stage<T, BN, NT, BT> SB;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][(BM + BN) * KB];
+// Tile shapes: BM x BN values of D by WGM x WGN waves; NS stages of KB bytes in LDS; fragments
+// are read GK steps at a time, a group ahead of their products.
+template <int BM_, int BN_, int WGM_, int WGN_, int KB_, int NS_, int GK_>
+struct Shape {
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, KB = KB_, NS = NS_, GK = GK_, NT = 64 * WGM_ * WGN_;
+  static_assert((NS & (NS - 1)) == 0, "a stage's place is its index modulo NS");
+  static_assert(KB / 32 / GK % 2 == 0, "the fragment sets alternate within a stage");
+};
+
+// All but N of the wave's loads have landed, and every wave is here.
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  if constexpr (N == 0) __syncthreads();
+  else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+template <class S>
+__device__ __forceinline__ Place place(const Prob& p, int wave, int& K) {
   Place c;
-  int K = p.K;
+  K = p.K;
   c.M = p.M;
   c.N = p.N;
   if (p.count) {
@@ -247,16 +283,29 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_mm(Prob p, typename E::Args 
     if (p.count_k) K = min(K, n);
   }
   tile_of(blockIdx.x, p.tm, p.tn, c.mt, c.nt);
-  c.m0 = c.mt * BM;
-  c.n0 = c.nt * BN;
-  if (c.m0 >= c.M) return;
+  c.m0 = c.mt * S::BM;
+  c.n0 = c.nt * S::BN;
   c.lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
-  c.wm = wave / WGN;
-  c.wn = wave % WGN;
-  c.mw = c.m0 + c.wm * (BM / WGM);
-  c.nw = c.n0 + c.wn * (BN / WGN);
+  c.wm = wave / S::WGN;
+  c.wn = wave % S::WGN;
+  c.mw = c.m0 + c.wm * (S::BM / S::WGM);
+  c.nw = c.n0 + c.wn * (S::BN / S::WGN);
   c.split = blockIdx.y;
+  return c;
+}
+
+template <typename T, class S, bool AT, bool BT, class E>
+__global__ __launch_bounds__(S::NT) void k_mm(Prob p, typename E::Args ea) {
+  constexpr int BM = S::BM, BN = S::BN, WGM = S::WGM, WGN = S::WGN, KB = S::KB, NS = S::NS, NT = S::NT;
+  constexpr int FM = BM / WGM / 32, FN = BN / WGN / 32, GK = S::GK, NG = KB / 32 / GK;
+  typedef Stage<T, BM, KB, NT, AT> SA;
+  typedef Stage<T, BN, KB, NT, BT> SB;
+  constexpr int LOADS = SA::PER + SB::PER;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[NS][(BM + BN) * KB];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int K;
+  const Place c = place<S>(p, wave, K);
+  if (c.m0 >= c.M) return;
   const int k0 = blockIdx.y * p.kper, k1 = min(K, k0 + p.kper);
   const int steps = k1 > k0 ? (k1 - k0 + SA::BK - 1) / SA::BK : 0;
   f32x16 acc[FM][FN];
@@ -268,30 +317,59 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_mm(Prob p, typename E::Args 
   SB sb;
   sa.start(p.A, p.lda, c.m0, c.M, k0, k1);
   sb.start(p.B, p.ldb, c.n0, c.N, k0, k1);
+  // A group's fragments are read during the products of the group before; the last group of a
+  // stage reads the next stage's first fragments, behind the stage's one barrier: every wave has
+  // then read all of this stage, and the next one has landed, so the stage NS further on is
+  // requested into this one's place.
+  const Reader<T, SA, KB, FM, AT> ra(c.wm * (BM / WGM), c.lane);
+  const Reader<T, SB, KB, FN, BT> rb(c.wn * (BN / WGN), c.lane);
+  typename Frag<T>::type fa[2][GK][FM], fb[2][GK][FN];
+  const auto frags = [&](int s, int g, int to) {
+    const unsigned char* la = lds[s & (NS - 1)];
+#pragma unroll
+    for (int k = 0; k < GK; ++k) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[to][k][i] = ra(la, i, g * GK + k);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[to][k][j] = rb(la + BM * KB, j, g * GK + k);
+    }
+  };
+  const auto request = [&](int s) {
+    sa.load(lds[s & (NS - 1)], wave);
+    sb.load(lds[s & (NS - 1)] + BM * KB, wave);
+  };
+  // more: the stage NS further on exists; next: the next one does
+  const auto stage = [&](int s, auto more, auto next) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int at = g & 1;
+      if (g < NG - 1) {
+        frags(s, g + 1, at ^ 1);
+      } else if (decltype(next)::value) {
+        wait_and_meet<decltype(more)::value ? (NS - 2) * LOADS : 0>();
+        __builtin_amdgcn_sched_barrier(0);
+        if (decltype(more)::value) request(s + NS);
+        frags(s + 1, 0, at ^ 1);
+      }
+#pragma unroll
+      for (int k = 0; k < GK; ++k)
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = mma(fb[at][k][j], fa[at][k][i], acc[i][j]);
+    }
+  };
   if (steps) {
-    sa.load(lds[0]);
-    sb.load(lds[0] + BM * KB);
-  }
-  for (int s = 0; s < steps; ++s) {
-    unsigned char* la = lds[s & 1];
-    unsigned char* lb = la + BM * KB;
-    __syncthreads();
-    if (s + 1 < steps) {
-      sa.load(lds[(s + 1) & 1]);
-      sb.load(lds[(s + 1) & 1] + BM * KB);
-    }
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      typename Frag<T>::type fa[FM], fb[FN];
-#pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = SA::frag(la, c.wm * (BM / WGM) + 32 * i, kk, c.lane);
-#pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = SB::frag(lb, c.wn * (BN / WGN) + 32 * j, kk, c.lane);
-#pragma unroll
-      for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = mma(fb[j], fa[i], acc[i][j]);
-    }
+    for (int s = 0; s < NS; ++s)
+      if (s < steps) request(s);
+    if (steps >= NS) wait_and_meet<(NS - 1) * LOADS>();
+    else wait_and_meet<0>();
+    frags(0, 0, 0);
+    int s = 0;
+    for (; s + NS < steps; ++s) stage(s, std::true_type{}, std::true_type{});
+    for (; s + 1 < steps; ++s) stage(s, std::false_type{}, std::true_type{});
+    stage(s, std::false_type{}, std::false_type{});
   }
   __syncthreads();  // the epilogue may use the stages' LDS
   float* el = reinterpret_cast<float*>(&lds[0][0]);
@@ -344,23 +422,22 @@ __device__ __forceinline__ void column_sums(f32x16 (&v)[FN], const Place& c, flo
   }
 }
 
-// Partial sums of a split contraction, joined by k_join in the order of the splits.
-struct EpPart {
+// The partial sums of a split contraction as the lanes hold them; k_finish adds them in the order
+// of the splits and runs the product's epilogue.
+struct EpRaw {
   struct Args {
-    float* part;  // [splits][M][N]
+    f32x4* part;  // [splits][tiles][quads of a lane][threads]
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
-    float* out = a.part + (size_t)c.split * c.M * c.N;
+    constexpr int NT = 64 * WGM * WGN, Q = 4 * FM * FN;
+    f32x4* out = a.part + ((size_t)c.split * gridDim.x + blockIdx.x) * (Q * NT) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = c.row(i);
-      if (m >= c.M) continue;
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) store4<WHOLE>(out + (size_t)m * c.N, c.feature(j, q), c.N, quad(acc[i][j], q));
-    }
+        for (int q = 0; q < 4; ++q) out[((i * FN + j) * 4 + q) * NT] = quad(acc[i][j], q);
   }
 };
 
@@ -387,29 +464,63 @@ struct EpScale {
   }
 };
 
-// out[i] = f * scale[0] * sum over splits of part[split][i]
-template <typename T>
-__global__ __launch_bounds__(256) void k_join(const float* part, int splits, size_t n, T* out, float f,
-                                              const float* scale) {
-  const float g = scale ? f * scale[0] : f;
-  for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += (size_t)gridDim.x * 1024) {
-    const int left = (int)(n - i < 4 ? n - i : 4);
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < splits; ++k) s += load4(part + (size_t)k * n + i, 0, left);
-    store4(out + i, 0, left, s * g);
+// Adds the partial sums of a split contraction in order and runs the epilogue.
+template <class S, class E>
+__global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int splits, typename E::Args ea) {
+  constexpr int WGM = S::WGM, WGN = S::WGN, FM = S::BM / WGM / 32, FN = S::BN / WGN / 32, Q = 4 * FM * FN;
+  __shared__ float lds[4096];  // as much as an epilogue uses
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int K;
+  const Place c = place<S>(p, wave, K);
+  if (c.m0 >= c.M) return;
+  f32x16 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = 0.f;
+  for (int k = 0; k < splits; ++k) {
+    const f32x4* in = part + ((size_t)k * gridDim.x + blockIdx.x) * (Q * S::NT) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 v = in[((i * FN + j) * 4 + q) * S::NT];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[i][j][4 * q + r] += v[r];
+        }
   }
+  if (c.n0 + S::BN <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, lds);
+  else E::template run<false, FM, FN, WGM, WGN>(ea, c, acc, lds);
 }
 
-// out[n] = f * scale[0] * sum over tile rows of part[t][n], in fp64 and in order. With
-// `count` given, only the tile rows that hold rows below it were written.
+// out[n] = f * scale[0] * sum over tile rows of part[t][n], in fp64 and in order (64 columns by 4
+// runs of tile rows a workgroup). With `count` given, only the tile rows that hold rows below it
+// were written.
 template <typename T>
 __global__ __launch_bounds__(256) void k_colsum(const float* part, int tiles, int bm, const int* count, int n, T* out,
                                                 float f, const float* scale) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
+  __shared__ double sh[4][64];
+  const int i = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
   if (count) tiles = min(tiles, (*count + bm - 1) / bm);
+  const int per = (tiles + 3) / 4, t1 = min(tiles, (g + 1) * per);
   double s = 0.0;
-  for (int t = 0; t < tiles; ++t) s += (double)part[(size_t)t * n + i];
+  if (i < n) {
+    int t = g * per;
+    for (; t + 8 <= t1; t += 8) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = part[(size_t)(t + k) * n + i];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += (double)v[k];
+    }
+    for (; t < t1; ++t) s += (double)part[(size_t)t * n + i];
+  }
+  sh[g][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (g || i >= n) return;
+  s = ((sh[0][threadIdx.x] + sh[1][threadIdx.x]) + sh[2][threadIdx.x]) + sh[3][threadIdx.x];
   out[i] = (T)((float)s * (scale ? f * scale[0] : f));
 }
 
@@ -436,9 +547,6 @@ __global__ __launch_bounds__(256) void k_repack(const T* in, T* out, size_t rows
 
 // ---------------------------------------------------------------- launches
 
-// Tile sizes: 4 waves of 64 x 64.
-constexpr int TILE = 128;
-
 inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
 // The leading dimension of a row of n values that starts on 16 bytes.
@@ -464,24 +572,68 @@ struct Operand {
   }
 };
 
-template <typename T, bool AT, bool BT, class E>
-hipError_t launch_mm(Prob p, const typename E::Args& ea, int splits, hipStream_t st) {
-  constexpr int BK = KB / (int)sizeof(T);
-  p.tm = ceil_div(p.M, TILE);
-  p.tn = ceil_div(p.N, TILE);
-  p.kper = ceil_div(ceil_div(p.K, BK), splits) * BK;
-  if (p.kper == 0) p.kper = BK;
-  k_mm<T, TILE, TILE, 2, 2, AT, BT, E><<<dim3((unsigned)(p.tm * p.tn), (unsigned)splits), 256, 0, st>>>(p, ea);
+// Tile shapes. Large: a wave's 128 x 64 values reuse every LDS read most. Middle: two workgroups a
+// CU, one's epilogue beside the other's products. Small: four stages in flight for short grids.
+typedef Shape<256, 256, 2, 4, 128, 2, 2> Tile256;
+typedef Shape<128, 128, 2, 2, 128, 2, 2> Tile128;
+typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;
+constexpr int STAGE_BYTES = 128;
+
+// The plan with the least estimated time, from measured times of a stage (us) with one workgroup on
+// a CU and with all that fit there: 16 bits 256: 1.4 and 1.75, 128: 0.60 and 1.0 for two, 64: 0.28
+// and 0.45 for two; float (no large tile: its products are what counts there) 128: 1.75 and 3.4
+// for two, 64: 0.5 and 0.9 for two. A split writes and reads its partial sums (at 3 TB/s both ways)
+// and takes a second launch (3 us). Measured against the other choices: 1024 x 1024 x 4096 bf16, 21 us
+// by tiles of 64 (128: 35, 256: 89); 8192 x 1024 x 2048, 37 us by 128 (64: 53, 256: 57); 8192 x 4096 x
+// 4096, 230 us by 256 (128: 256, 64: over 370).
+inline Plan plan_of(size_t esz, long M, long N, long K) {
+  const bool f32 = esz == 4;
+  const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
+  Plan best{};
+  double least = 1e30;
+  for (int tile : {256, 128, 64}) {
+    if (f32 && tile == 256) continue;
+    const long tm = ceil_div(M, tile), tn = ceil_div(N, tile);
+    const double one = tile == 256 ? 1.4 : tile == 128 ? (f32 ? 1.75 : 0.60) : (f32 ? 0.5 : 0.28);
+    const double two = tile == 256 ? 3.5 : tile == 128 ? (f32 ? 3.4 : 1.0) : (f32 ? 0.9 : 0.45);
+    for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      if (splits > 1 && (steps < 4 * splits || tile == 256)) break;  // (a split large tile would be two middle ones)
+      const long n = ceil_div(tm * tn * splits, 256);
+      double t = ceil_div(steps, splits) * ((n / 2) * two + (n % 2) * (tile == 256 && n > 1 ? two / 2 : one));
+      if (splits > 1) t += 3.0 + 2.0 * splits * tm * tn * tile * tile * 4 / 3e6;
+      if (t < least) {
+        least = t;
+        best = Plan{tile, splits, (int)tm, (int)tn};
+      }
+    }
+  }
+  return best;
+}
+
+template <typename T, class S, bool AT, bool BT, class E>
+hipError_t launch_shape(Prob p, const typename E::Args& ea, const Plan& pl, void* part, hipStream_t st) {
+  constexpr int BK = S::KB / (int)sizeof(T);
+  p.tm = pl.tm;
+  p.tn = pl.tn;
+  p.kper = std::max(1, ceil_div(ceil_div(p.K, BK), pl.splits)) * BK;
+  const unsigned tiles = (unsigned)(p.tm * p.tn);
+  if (S::BM == 256 || pl.splits == 1) {
+    k_mm<T, S, AT, BT, E><<<dim3(tiles), S::NT, 0, st>>>(p, ea);
+  } else if constexpr (S::BM < 256) {
+    k_mm<T, S, AT, BT, EpRaw><<<dim3(tiles, (unsigned)pl.splits), S::NT, 0, st>>>(p, EpRaw::Args{static_cast<f32x4*>(part)});
+    k_finish<S, E><<<dim3(tiles), S::NT, 0, st>>>(p, static_cast<const f32x4*>(part), pl.splits, ea);
+  }
   return hipGetLastError();
 }
 
-// Splits of a contraction of K values for an M x N result: enough for two workgroups a
-// CU, each with at least four stages.
-inline int splits_of(size_t esz, int M, int N, long K) {
-  const long tiles = (long)ceil_div(M, TILE) * ceil_div(N, TILE), steps = ceil_div(K * (long)esz, KB);
-  long s = 512 / (tiles > 0 ? tiles : 1);
-  if (s > steps / 4) s = steps / 4;
-  return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+// part: pl.part_bytes() of workspace
+template <typename T, bool AT, bool BT, class E>
+hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, void* part, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (pl.tile == 256) return launch_shape<T, Tile256, AT, BT, E>(p, ea, pl, part, st);
+  }
+  if (pl.tile == 128) return launch_shape<T, Tile128, AT, BT, E>(p, ea, pl, part, st);
+  return launch_shape<T, Tile64, AT, BT, E>(p, ea, pl, part, st);
 }
 
 }  // namespace mm

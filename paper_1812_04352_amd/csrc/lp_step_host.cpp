@@ -87,7 +87,9 @@ namespace lp {
 StepLayout step_layout(int dtype, int B, int ni, int no) {
   const size_t e = esize(dtype);
   StepLayout l;
-  l.splits = mm::splits_of(e, no, ni, B);
+  l.z = mm::plan_of(e, B, no, ni);
+  l.zx = mm::plan_of(e, B, ni, no);
+  l.zw = mm::plan_of(e, no, ni, B);
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
     const size_t r = at;
@@ -97,14 +99,14 @@ StepLayout step_layout(int dtype, int B, int ni, int no) {
   l.g = take((size_t)B * mm::padded(e, no) * e);
   l.x = take((size_t)B * mm::padded(e, ni) * e);
   l.W = take((size_t)no * mm::padded(e, ni) * e);
-  l.col = take((size_t)mm::ceil_div(B, mm::TILE) * no * 4);
-  l.part = take(l.splits > 1 ? (size_t)l.splits * no * ni * 4 : 0);
+  l.col = take((size_t)l.z.tm * no * 4);
+  l.part = take(std::max({l.z.part_bytes(), l.zx.part_bytes(), l.zw.part_bytes()}));
   l.total = std::max<size_t>(at, 256);
   return l;
 }
 
 // A piece of the vocabulary holds at most PIECE_BYTES of probabilities and of (copied) weights,
-// in whole tiles of classes (at least one tile).
+// in whole tiles of classes (at least one).
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;
 
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
@@ -116,13 +118,30 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     at += up(bytes);
     return r;
   };
-  const size_t fit = PIECE_BYTES / (std::max<size_t>(grad ? B : 0, ldq) * e) / mm::TILE * mm::TILE;
-  l.piece = (int)std::min<size_t>(nc, std::max<size_t>(fit, mm::TILE));
-  l.part = take((size_t)mm::ceil_div(nc, mm::TILE) * B * 8);
+  const size_t fit = PIECE_BYTES / (std::max<size_t>(grad ? B : 0, ldq) * e) / 256 * 256;
+  l.piece = (int)std::min<size_t>(nc, std::max<size_t>(fit, 256));
+  // every piece but the last is alike
+  const int last = nc % l.piece ? nc % l.piece : l.piece, others = (nc - last) / l.piece;
+  size_t tiles = 0, split = 0, col = 0;
+  for (int n : {l.piece, last}) {
+    const mm::Plan z = mm::plan_of(e, B, n, q);
+    tiles += (size_t)z.tn * (n == last ? 1 : others);
+    split = std::max(split, z.part_bytes());
+    if (grad) {
+      split = std::max({split, mm::plan_of(e, B, q, n).part_bytes(), mm::plan_of(e, n, q, B).part_bytes()});
+      col = std::max(col, (size_t)z.tm * n * 4);
+    }
+    if (l.piece == last) {
+      tiles = (size_t)z.tn * (others + 1);
+      break;
+    }
+  }
+  l.part = take(tiles * B * 8);
   l.zl = take((size_t)B * 4);
   l.row = take((size_t)B * 4);
   l.u = take((size_t)B * ldq * e);
   l.W = take((size_t)l.piece * ldq * e);
+  l.split = take(split);
   if (grad) {
     l.from = take((size_t)B * 4);
     l.to = take((size_t)B * 4);
@@ -132,15 +151,7 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     l.lse = take((size_t)B * 4);
     l.P = take((size_t)B * mm::padded(e, l.piece) * e);
     l.du = take(l.piece < nc ? (size_t)B * q * 4 : 0);
-    l.col = take((size_t)mm::ceil_div(B, mm::TILE) * nc * 4);
-    // the last piece is smaller than the others: the most splits it may take
-    size_t wp = 0;
-    for (int n : {l.piece, nc % l.piece})
-      if (n) {
-        const size_t s = mm::splits_of(e, n, q, B);
-        if (s > 1) wp = std::max(wp, s * n * q * 4);
-      }
-    l.wpart = take(wp);
+    l.col = take(col);
   }
   l.total = std::max<size_t>(at, 256);
   return l;

@@ -292,7 +292,7 @@ hipError_t step_forward_t(const StepArgs& a, hipStream_t st) {
   if (x.e != hipSuccess) return x.e;
   if (W.e != hipSuccess) return W.e;
   typename EpStep<T>::Args e{(const T*)a.b, (const T*)a.r, (T*)a.y, a.y8, a.ye, (float)a.h, a.act};
-  return mm::launch_mm<T, false, false, EpStep<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), e, 1, st);
+  return mm::launch_mm<T, false, false, EpStep<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), e, l.z, w + l.part, st);
 }
 
 template <typename T>
@@ -302,7 +302,6 @@ hipError_t step_backward_t(const StepArgs& a, hipStream_t st) {
   T* g = reinterpret_cast<T*>(w + l.g);
   const int ldg = mm::padded(sizeof(T), a.no), ldx = mm::padded(sizeof(T), a.ni);
   float* colpart = reinterpret_cast<float*>(w + l.col);
-  float* part = reinterpret_cast<float*>(w + l.part);
   hipError_t e = hipSuccess;
   if (!a.x && a.B && (e = ck_load_t<T>(a.x8, a.xe, w + l.x, a.B, a.ni, ldx, st)) != hipSuccess) return e;
   mm::Operand<T> x(a.x ? a.x : w + l.x, a.x ? a.B : 0, a.ni, w + l.x, st);
@@ -311,32 +310,23 @@ hipError_t step_backward_t(const StepArgs& a, hipStream_t st) {
   if (W.e != hipSuccess) return W.e;
   if (a.B) {  // (an empty batch leaves zero sums: products over no rows)
     typename EpGrad<T>::Args eg{(const T*)a.b, (const T*)a.dy, g, ldg, colpart, a.act};
-    e = mm::launch_mm<T, false, false, EpGrad<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), eg, 1, st);
+    e = mm::launch_mm<T, false, false, EpGrad<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), eg, l.z, w + l.part, st);
     if (e != hipSuccess) return e;
   }
   const float h = (float)a.h;
   if (a.dx && a.B) {
     typename EpDx<T>::Args ed{a.residual ? (const T*)a.dy : nullptr, (T*)a.dx, h};
-    e = mm::launch_mm<T, false, true, EpDx<T>>(prob(g, ldg, W.p, W.ld, a.B, a.ni, a.no), ed, 1, st);
+    e = mm::launch_mm<T, false, true, EpDx<T>>(prob(g, ldg, W.p, W.ld, a.B, a.ni, a.no), ed, l.zx, w + l.part, st);
     if (e != hipSuccess) return e;
   }
   if (a.dW) {
-    const mm::Prob p = prob(g, ldg, x.p, x.ld, a.no, a.ni, a.B);
-    if (l.splits > 1) {
-      e = mm::launch_mm<T, true, true, mm::EpPart>(p, mm::EpPart::Args{part}, l.splits, st);
-      if (e != hipSuccess) return e;
-      const size_t n = (size_t)a.no * a.ni;
-      mm::k_join<T><<<(unsigned)std::min<size_t>((n + 1023) / 1024, 4096), 256, 0, st>>>(part, l.splits, n, (T*)a.dW, h,
-                                                                                          nullptr);
-      e = hipGetLastError();
-    } else {
-      e = mm::launch_mm<T, true, true, mm::EpScale<T>>(p, typename mm::EpScale<T>::Args{(T*)a.dW, h, nullptr}, 1, st);
-    }
+    e = mm::launch_mm<T, true, true, mm::EpScale<T>>(prob(g, ldg, x.p, x.ld, a.no, a.ni, a.B),
+                                                     typename mm::EpScale<T>::Args{(T*)a.dW, h, nullptr}, l.zw, w + l.part, st);
     if (e != hipSuccess) return e;
   }
   if (a.db) {
-    mm::k_colsum<T><<<(unsigned)mm::ceil_div(a.no, 256), 256, 0, st>>>(colpart, mm::ceil_div(a.B, mm::TILE), mm::TILE, nullptr,
-                                                                     a.no, (T*)a.db, h, nullptr);
+    mm::k_colsum<T><<<(unsigned)mm::ceil_div(a.no, 64), 256, 0, st>>>(colpart, a.B ? l.z.tm : 0, l.z.tile, nullptr, a.no,
+                                                                    (T*)a.db, h, nullptr);
     e = hipGetLastError();
   }
   return e;
