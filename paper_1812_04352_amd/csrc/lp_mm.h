@@ -8,7 +8,7 @@
 // three products of a layer (z = x W^T, dx = g W, dW = g^T x) read the caller's arrays as
 // they are.
 //
-// Matrix instructions: 32 x 32 x 16 (bf16, f16) and 32 x 32 x 2 (float), with n on the
+// Matrix instructions: 32 x 32 x 16 in bf16 or f16 (floats as split bf16 products), with n on the
 // instruction's rows and m on its columns. Lane l then holds, of each 32 x 32 block, the 16
 // values n = 8 (r / 4) + 4 (l / 32) + r % 4, r = 0..15, of the single row m = l % 32: four
 // consecutive features at a time (vector loads and stores of rows), and sums over a row
@@ -33,6 +33,7 @@
 
 #include "lp_device.h"
 #include "lp_internal.h"
+#include "lp_split.h"
 
 namespace lp {
 namespace mm {
@@ -42,6 +43,7 @@ typedef _Float16 f16;
 typedef __bf16 b16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+using lp::f32x8;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -50,10 +52,17 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // N consecutive values in global memory, with their element's alignment
 template <typename T, int N> struct GVec { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
 
-template <typename T> struct Frag;  // the 16 bytes a lane feeds to the matrix instructions
-template <> struct Frag<bf16> { typedef b16x8 type; };
-template <> struct Frag<f16> { typedef h16x8 type; };
-template <> struct Frag<float> { typedef f32x4 type; };
+// What a lane reads of one operand for a step of 16 contraction values (eight of them), and what
+// the matrix instructions take: floats are split into three bf16 parts (lp_split.h), six products
+// of which make one of floats: 2.4 times the float instructions' rate, with a smaller error.
+template <typename T> struct Frag;
+template <> struct Frag<bf16> { typedef b16x8 type; typedef b16x8 ready; };
+template <> struct Frag<f16> { typedef h16x8 type; typedef h16x8 ready; };
+template <> struct Frag<float> { typedef f32x8 type; typedef Split8 ready; };
+
+__device__ __forceinline__ b16x8 prepare(b16x8 x) { return x; }
+__device__ __forceinline__ h16x8 prepare(h16x8 x) { return x; }
+__device__ __forceinline__ Split8 prepare(f32x8 x) { return split8(x); }
 
 __device__ __forceinline__ f32x16 mma(b16x8 a, b16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -61,9 +70,19 @@ __device__ __forceinline__ f32x16 mma(b16x8 a, b16x8 b, f32x16 c) {
 __device__ __forceinline__ f32x16 mma(h16x8 a, h16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 mma(f32x4 a, f32x4 b, f32x16 c) {
+__device__ __forceinline__ f32x16 mma(const Split8& a, const Split8& b, f32x16 c) {
+  constexpr int ia[6] = {0, 2, 1, 0, 1, 0}, ib[6] = {2, 0, 1, 1, 0, 0};
 #pragma unroll
-  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+  for (int k = 0; k < 6; ++k) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.p[ia[k]], b.p[ib[k]], c, 0, 0, 0);
+  return c;
+}
+// the float instructions, for tiles whose split products are not finite
+template <typename F>
+__device__ __forceinline__ f32x16 mma_float(F a, F b, f32x16 c) {
+  if constexpr (std::is_same<F, f32x8>::value) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+  }
   return c;
 }
 
@@ -109,11 +128,10 @@ struct Stage {
   static constexpr int CH = R / V;                   // columns: chunks per row of the stage
   static constexpr int SWZ = (sizeof(T) == 2 ? 12 : 8) & (CH - 1);
   static_assert(R * RC % NT == 0, "whole chunks per thread");
-  static_assert(!COLS || NT / CH % (sizeof(T) == 2 ? 4 : 8) == 0, "the exchange is the same for all of a thread's chunks");
   static_assert(KB == 64 || KB == 128, "the rows' exchange");
 
   static __device__ __forceinline__ int swz(int k) {  // columns: chunk exchange of row k
-    return (sizeof(T) == 2 ? k << 2 : k << 1) & SWZ;
+    return (sizeof(T) == 2 ? k << 2 : k) & SWZ;
   }
   static __device__ __forceinline__ int rswz(int r) {  // rows: chunk exchange of row r
     return KB == 128 ? r & 7 : (r >> 1) & 3;
@@ -140,13 +158,15 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < PER; ++i) off[i] = (uint32_t)((t + i * NT) / RC) * (uint32_t)(ld * sizeof(T)) + c * 16;
     } else {
-      const int c = (t % CH) ^ swz(t / CH);
       kc = 0;
       base = static_cast<const unsigned char*>(p) + ((long)k0 * ld + r0) * (long)sizeof(T);
       left = ((long)(k1 - k0) * ld - r0) * (long)sizeof(T);
       step = BK * ld * (long)sizeof(T);
 #pragma unroll
-      for (int i = 0; i < PER; ++i) off[i] = (uint32_t)((t + i * NT) / CH) * (uint32_t)(ld * sizeof(T)) + c * 16;
+      for (int i = 0; i < PER; ++i) {
+        const int r = (t + i * NT) / CH;
+        off[i] = (uint32_t)r * (uint32_t)(ld * sizeof(T)) + ((t % CH) ^ swz(r)) * 16;
+      }
     }
   }
 
@@ -179,29 +199,35 @@ struct Stage {
 template <typename T, class S, int KB, int NF, bool COLS>
 struct Reader {
   typedef typename Frag<T>::type F;
-  static constexpr int N = COLS ? NF : KB / 32;
+  static constexpr int N = COLS ? NF : KB / (sizeof(T) == 2 ? 32 : 16);
   uint32_t at[N];
 
   __device__ __forceinline__ Reader(int r0, int lane) {
 #pragma unroll
     for (int x = 0; x < N; ++x) {
-      if constexpr (!COLS) {
-        const int r = r0 + (lane & 31), c = 2 * x + (lane >> 5);
+      if constexpr (!COLS) {  // 16 bits: step x; float: chunk x % 2 of step x / 2
+        const int r = r0 + (lane & 31), c = sizeof(T) == 2 ? 2 * x + (lane >> 5) : 4 * (x / 2) + 2 * (lane >> 5) + x % 2;
         at[x] = (r * S::RC + (c ^ S::rswz(r))) * 16;
       } else if constexpr (sizeof(T) == 2) {
         const int col = r0 + 32 * x + 16 * ((lane >> 4) & 1) + 4 * (lane & 3), k = 8 * (lane >> 5) + ((lane >> 2) & 3);
         at[x] = (k * S::CH + ((col / S::V) ^ S::swz(k))) * 16 + (col % S::V) * 2;
       } else {
-        const int col = r0 + 32 * x + (lane & 31), k = 4 * (lane >> 5);
+        const int col = r0 + 32 * x + (lane & 31), k = 8 * (lane >> 5);
         at[x] = (k * S::CH + ((col / S::V) ^ S::swz(k))) * 16 + (col % S::V) * 4;
       }
     }
   }
 
-  // block i, contraction step kk (two chunks) of the stage at lds
+  // block i, step kk (16 contraction values, eight of them this lane's) of the stage at lds
   __device__ __forceinline__ F operator()(const unsigned char* lds, int i, int kk) const {
     if constexpr (!COLS) {
-      return *reinterpret_cast<const F*>(lds + at[kk] + i * 32 * KB);
+      if constexpr (sizeof(T) == 2) {
+        return *reinterpret_cast<const F*>(lds + at[kk] + i * 32 * KB);
+      } else {
+        const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + at[2 * kk] + i * 32 * KB);
+        const f32x4 hi = *reinterpret_cast<const f32x4*>(lds + at[2 * kk + 1] + i * 32 * KB);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
     } else if constexpr (sizeof(T) == 2) {
       typedef __attribute__((address_space(3))) s16x4 lds4;
       s16x4 h[2];
@@ -212,7 +238,7 @@ struct Reader {
     } else {
       F v;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(lds + at[i] + (8 * kk + j) * S::CH * 16);
+      for (int j = 0; j < 8; ++j) v[j] = *reinterpret_cast<const float*>(lds + at[i] + (16 * kk + j) * S::CH * 16);
       return v;
     }
   }
@@ -261,7 +287,6 @@ template <int BM_, int BN_, int WGM_, int WGN_, int KB_, int NS_, int GK_>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, KB = KB_, NS = NS_, GK = GK_, NT = 64 * WGM_ * WGN_;
   static_assert((NS & (NS - 1)) == 0, "a stage's place is its index modulo NS");
-  static_assert(KB / 32 / GK % 2 == 0, "the fragment sets alternate within a stage");
 };
 
 // All but N of the wave's loads have landed, and every wave is here.
@@ -297,7 +322,9 @@ __device__ __forceinline__ Place place(const Prob& p, int wave, int& K) {
 template <typename T, class S, bool AT, bool BT, class E>
 __global__ __launch_bounds__(S::NT) void k_mm(Prob p, typename E::Args ea) {
   constexpr int BM = S::BM, BN = S::BN, WGM = S::WGM, WGN = S::WGN, KB = S::KB, NS = S::NS, NT = S::NT;
-  constexpr int FM = BM / WGM / 32, FN = BN / WGN / 32, GK = S::GK, NG = KB / 32 / GK;
+  constexpr int FM = BM / WGM / 32, FN = BN / WGN / 32, GK = S::GK;
+  constexpr int NG = KB / (16 * (int)sizeof(T)) / GK;
+  static_assert(NG % 2 == 0, "the fragment sets alternate within a stage");
   typedef Stage<T, BM, KB, NT, AT> SA;
   typedef Stage<T, BN, KB, NT, BT> SB;
   constexpr int LOADS = SA::PER + SB::PER;
@@ -308,68 +335,98 @@ __global__ __launch_bounds__(S::NT) void k_mm(Prob p, typename E::Args ea) {
   if (c.m0 >= c.M) return;
   const int k0 = blockIdx.y * p.kper, k1 = min(K, k0 + p.kper);
   const int steps = k1 > k0 ? (k1 - k0 + SA::BK - 1) / SA::BK : 0;
-  f32x16 acc[FM][FN];
-#pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = 0.f;
-  SA sa;
-  SB sb;
-  sa.start(p.A, p.lda, c.m0, c.M, k0, k1);
-  sb.start(p.B, p.ldb, c.n0, c.N, k0, k1);
-  // A group's fragments are read during the products of the group before; the last group of a
-  // stage reads the next stage's first fragments, behind the stage's one barrier: every wave has
-  // then read all of this stage, and the next one has landed, so the stage NS further on is
-  // requested into this one's place.
   const Reader<T, SA, KB, FM, AT> ra(c.wm * (BM / WGM), c.lane);
   const Reader<T, SB, KB, FN, BT> rb(c.wn * (BN / WGN), c.lane);
-  typename Frag<T>::type fa[2][GK][FM], fb[2][GK][FN];
-  const auto frags = [&](int s, int g, int to) {
-    const unsigned char* la = lds[s & (NS - 1)];
+  f32x16 acc[FM][FN];
+  // The contraction. A group's fragments are read during the products of the group before; the
+  // last group of a stage reads the next stage's first fragments, behind the stage's one barrier:
+  // every wave has then read all of this stage, and the next one has landed, so the stage NS
+  // further on is requested into this one's place.
+  const auto contract = [&](auto as_float) {
+    SA sa;
+    SB sb;
+    sa.start(p.A, p.lda, c.m0, c.M, k0, k1);
+    sb.start(p.B, p.ldb, c.n0, c.N, k0, k1);
 #pragma unroll
-    for (int k = 0; k < GK; ++k) {
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[to][k][i] = ra(la, i, g * GK + k);
+      for (int j = 0; j < FN; ++j) acc[i][j] = 0.f;
+    typename Frag<T>::type fa[2][GK][FM], fb[2][GK][FN];
+    const auto frags = [&](int s, int g, int to) {
+      const unsigned char* la = lds[s & (NS - 1)];
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[to][k][j] = rb(la + BM * KB, j, g * GK + k);
-    }
-  };
-  const auto request = [&](int s) {
-    sa.load(lds[s & (NS - 1)], wave);
-    sb.load(lds[s & (NS - 1)] + BM * KB, wave);
-  };
-  // more: the stage NS further on exists; next: the next one does
-  const auto stage = [&](int s, auto more, auto next) {
+      for (int k = 0; k < GK; ++k) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int at = g & 1;
-      if (g < NG - 1) {
-        frags(s, g + 1, at ^ 1);
-      } else if (decltype(next)::value) {
-        wait_and_meet<decltype(more)::value ? (NS - 2) * LOADS : 0>();
-        __builtin_amdgcn_sched_barrier(0);
-        if (decltype(more)::value) request(s + NS);
-        frags(s + 1, 0, at ^ 1);
+        for (int i = 0; i < FM; ++i) fa[to][k][i] = ra(la, i, g * GK + k);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fb[to][k][j] = rb(la + BM * KB, j, g * GK + k);
       }
-#pragma unroll
-      for (int k = 0; k < GK; ++k)
+    };
+    const auto request = [&](int s) {
+      sa.load(lds[s & (NS - 1)], wave);
+      sb.load(lds[s & (NS - 1)] + BM * KB, wave);
+    };
+    const auto products = [&](int at, int k) {
+      if constexpr (decltype(as_float)::value) {
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = mma(fb[at][k][j], fa[at][k][i], acc[i][j]);
+          for (int j = 0; j < FN; ++j) acc[i][j] = mma_float(fb[at][k][j], fa[at][k][i], acc[i][j]);
+      } else {
+        typename Frag<T>::ready ga[FM], gb[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) gb[j] = prepare(fb[at][k][j]);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) ga[i] = prepare(fa[at][k][i]);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = mma(gb[j], ga[i], acc[i][j]);
+      }
+    };
+    // more: the stage NS further on exists; next: the next one does
+    const auto stage = [&](int s, auto more, auto next) {
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const int at = g & 1;
+        if (g < NG - 1) {
+          frags(s, g + 1, at ^ 1);
+        } else if (decltype(next)::value) {
+          wait_and_meet<decltype(more)::value ? (NS - 2) * LOADS : 0>();
+          __builtin_amdgcn_sched_barrier(0);
+          if (decltype(more)::value) request(s + NS);
+          frags(s + 1, 0, at ^ 1);
+        }
+#pragma unroll
+        for (int k = 0; k < GK; ++k) products(at, k);
+      }
+    };
+    if (steps) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        if (s < steps) request(s);
+      if (steps >= NS) wait_and_meet<(NS - 1) * LOADS>();
+      else wait_and_meet<0>();
+      frags(0, 0, 0);
+      int s = 0;
+      for (; s + NS < steps; ++s) stage(s, std::true_type{}, std::true_type{});
+      for (; s + 1 < steps; ++s) stage(s, std::false_type{}, std::true_type{});
+      stage(s, std::false_type{}, std::false_type{});
     }
   };
-  if (steps) {
+  contract(std::false_type{});
+  if constexpr (sizeof(T) == 4) {
+    // An operand that is infinite or beyond the largest bf16 value makes split products NaN: a tile
+    // with a result that is not finite is formed again by the float instructions, which give
+    // infinities and overflow as fp32 has them.
+    bool finite = true;
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
-      if (s < steps) request(s);
-    if (steps >= NS) wait_and_meet<(NS - 1) * LOADS>();
-    else wait_and_meet<0>();
-    frags(0, 0, 0);
-    int s = 0;
-    for (; s + NS < steps; ++s) stage(s, std::true_type{}, std::true_type{});
-    for (; s + 1 < steps; ++s) stage(s, std::false_type{}, std::true_type{});
-    stage(s, std::false_type{}, std::false_type{});
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) finite = finite && fabsf(acc[i][j][r]) < INFINITY;
+    if (__syncthreads_or(!finite)) contract(std::true_type{});
   }
   __syncthreads();  // the epilogue may use the stages' LDS
   float* el = reinterpret_cast<float*>(&lds[0][0]);
@@ -577,25 +634,26 @@ struct Operand {
 typedef Shape<256, 256, 2, 4, 128, 2, 2> Tile256;
 typedef Shape<128, 128, 2, 2, 128, 2, 2> Tile128;
 typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;
+typedef Shape<256, 256, 2, 4, 128, 2, 1> Tile256f;  // float: two steps a stage
+typedef Shape<128, 128, 2, 2, 128, 2, 1> Tile128f;
+typedef Shape<64, 64, 2, 2, 128, 2, 1> Tile64f;
 constexpr int STAGE_BYTES = 128;
 
 // The plan with the least estimated time, from measured times of a stage (us) with one workgroup on
-// a CU and with all that fit there: 16 bits 256: 1.4 and 1.75, 128: 0.60 and 1.0 for two, 64: 0.28
-// and 0.45 for two; float (no large tile: its products are what counts there) 128: 1.75 and 3.4
-// for two, 64: 0.5 and 0.9 for two. A split writes and reads its partial sums (at 3 TB/s both ways)
-// and takes a second launch (3 us). Measured against the other choices: 1024 x 1024 x 4096 bf16, 21 us
-// by tiles of 64 (128: 35, 256: 89); 8192 x 1024 x 2048, 37 us by 128 (64: 53, 256: 57); 8192 x 4096 x
-// 4096, 230 us by 256 (128: 256, 64: over 370).
+// a CU and with two (of 256: two in turn). A split writes and reads its partial sums (3 TB/s both
+// ways) and takes a second launch (3 us). Measured against the other choices, bf16: 1024 x 1024 x
+// 4096 21 us by tiles of 64 (128: 35, 256: 89); 8192 x 1024 x 2048 37 us by 128 (64: 53, 256: 57);
+// 8192 x 4096 x 4096 230 us by 256 (128: 256, 64: over 370). float: 1024 x 1024 x 4096 95 us by 64 (128:
+// 185); 4096 x 2048 x 1024 85 by 128 (64: 110); 8192 x 4096 x 4096 1108 by 256 (128: 1272, 64: 1670).
 inline Plan plan_of(size_t esz, long M, long N, long K) {
-  const bool f32 = esz == 4;
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
+  const double stage[2][3][2] = {{{1.4, 3.5}, {0.60, 1.0}, {0.28, 0.45}}, {{3.9, 8.66}, {1.45, 2.48}, {0.74, 0.82}}};
   Plan best{};
   double least = 1e30;
-  for (int tile : {256, 128, 64}) {
-    if (f32 && tile == 256) continue;
+  for (int s = 0; s < 3; ++s) {
+    const int tile = 256 >> s;
     const long tm = ceil_div(M, tile), tn = ceil_div(N, tile);
-    const double one = tile == 256 ? 1.4 : tile == 128 ? (f32 ? 1.75 : 0.60) : (f32 ? 0.5 : 0.28);
-    const double two = tile == 256 ? 3.5 : tile == 128 ? (f32 ? 3.4 : 1.0) : (f32 ? 0.9 : 0.45);
+    const double one = stage[esz == 4][s][0], two = stage[esz == 4][s][1];
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (splits > 1 && (steps < 4 * splits || tile == 256)) break;  // (a split large tile would be two middle ones)
       const long n = ceil_div(tm * tn * splits, 256);
@@ -631,9 +689,13 @@ template <typename T, bool AT, bool BT, class E>
 hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, void* part, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
     if (pl.tile == 256) return launch_shape<T, Tile256, AT, BT, E>(p, ea, pl, part, st);
+    if (pl.tile == 128) return launch_shape<T, Tile128, AT, BT, E>(p, ea, pl, part, st);
+    return launch_shape<T, Tile64, AT, BT, E>(p, ea, pl, part, st);
+  } else {
+    if (pl.tile == 256) return launch_shape<T, Tile256f, AT, BT, E>(p, ea, pl, part, st);
+    if (pl.tile == 128) return launch_shape<T, Tile128f, AT, BT, E>(p, ea, pl, part, st);
+    return launch_shape<T, Tile64f, AT, BT, E>(p, ea, pl, part, st);
   }
-  if (pl.tile == 128) return launch_shape<T, Tile128, AT, BT, E>(p, ea, pl, part, st);
-  return launch_shape<T, Tile64, AT, BT, E>(p, ea, pl, part, st);
 }
 
 }  // namespace mm
