@@ -467,32 +467,57 @@ def label_head(dtype: str, B: int, q: int, nc: int) -> LpLabelHead:
     return LpLabelHead(LP_ABI_VERSION, WIDE_DTYPE[dtype], B, q, nc)
 
 
+_torch_dtypes: dict = {}  # library dtype -> torch dtype, and back
+
+
+def _kinds() -> dict:
+    if not _torch_dtypes:
+        import torch
+        for k, t in ((LP_F32, torch.float32), (LP_F64, torch.float64), (LP_BF16, torch.bfloat16),
+                     (LP_F16, torch.float16)):
+            _torch_dtypes[k], _torch_dtypes[t] = t, k
+    return _torch_dtypes
+
+
 def _wide_dtype(kind: int):
+    """torch's dtype of a descriptor's (an unknown one is the library's to refuse)."""
+    return _kinds().get(kind, _torch_dtypes[LP_F32])
+
+
+def _here(t, name: str) -> int:
+    """Index of the current device, on which every tensor of a call must be (the call uses its
+    current stream); t: any tensor of the call."""
     import torch
-    return {LP_F32: torch.float32, LP_F64: torch.float64, LP_BF16: torch.bfloat16, LP_F16: torch.float16}[kind]
+    if t is None or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    return torch.cuda.current_device()
 
 
-def _dev(t, numel: int, name: str, dtype, optional: bool = False):
-    """_arr for a tensor on the current device (whose current stream the call uses); NULL for an
-    optional one that is not given."""
+def _dev(t, numel: int, name: str, dtype, dev: int, optional: bool = False):
+    """Device pointer of a contiguous tensor on device dev holding at least numel elements, NULL for
+    an optional one that is not given. The checks that pass are few, since these calls run on small
+    batches too, where their host time counts; _arr words the refusals."""
     if t is None and optional:
         return None
-    p = _arr(t, numel, name, dtype)
-    import torch
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return p
+    if t is not None and t.dtype == dtype and t.get_device() == dev and t.is_contiguous() and t.numel() >= numel:
+        return t.data_ptr()
+    _arr(t, numel, name, dtype)
+    raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
 
 
-def _dev_ws(ws):
+def _dev_ws(ws, dev: int):
     if ws is None:
         raise ValueError("a workspace is required")
-    import torch
     if not ws.is_cuda or not ws.is_contiguous():
         raise ValueError("workspace must be a contiguous GPU tensor")
-    if ws.device.index != torch.cuda.current_device():
-        raise ValueError(f"workspace is on {ws.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size()
+    if ws.get_device() != dev:
+        raise ValueError(f"workspace is on {ws.device}, the current device is cuda:{dev}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _stream_of(dev: int):
+    import torch
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def _blocks(q: int) -> int:
@@ -516,12 +541,16 @@ def lp_step_forward(st: LpStep, x, W, b, r, y, ws, y8=None, ye=None) -> None:
     y8 [B][no] int8 and ye [B][ceil(no / 32)] uint8 receive the checkpoint of y."""
     import torch
     dt = _wide_dtype(st.dtype)
-    wp, wn = _dev_ws(ws)
-    _check(load().lp_step_forward(
-        ctypes.byref(st), _dev(x, st.B * st.ni, "x", dt), _dev(W, st.no * st.ni, "W", dt),
-        _dev(b, st.no, "b", dt, True), _dev(r, st.B * st.no, "r", dt, True), _dev(y, st.B * st.no, "y", dt),
-        _dev(y8, st.B * st.no, "y8", torch.int8, True), _dev(ye, st.B * _blocks(st.no), "ye", torch.uint8, True),
-        wp, wn, _stream()), "lp_step_forward")
+    dev = _here(W, "W")
+    B, ni, no = st.B, st.ni, st.no
+    wp, wn = _dev_ws(ws, dev)
+    rc = (_lib or load()).lp_step_forward(
+        ctypes.byref(st), _dev(x, B * ni, "x", dt, dev), _dev(W, no * ni, "W", dt, dev),
+        _dev(b, no, "b", dt, dev, True), _dev(r, B * no, "r", dt, dev, True), _dev(y, B * no, "y", dt, dev),
+        _dev(y8, B * no, "y8", torch.int8, dev, True), _dev(ye, B * _blocks(no), "ye", torch.uint8, dev, True),
+        wp, wn, _stream_of(dev))
+    if rc:
+        _check(rc, "lp_step_forward")
 
 
 def lp_step_backward(st: LpStep, x, W, b, dy, dx, dW, db, ws, residual: bool = False) -> None:
@@ -529,41 +558,49 @@ def lp_step_backward(st: LpStep, x, W, b, dy, dx, dW, db, ws, residual: bool = F
     (x8, xe). residual: r was x, so dx gets dy added. dx, dW, db may be None (not wanted)."""
     import torch
     dt = _wide_dtype(st.dtype)
+    dev = _here(W, "W")
+    B, ni, no = st.B, st.ni, st.no
     if isinstance(x, (tuple, list)):
         xp = None
-        x8p = _dev(x[0], st.B * st.ni, "x8", torch.int8)
-        xep = _dev(x[1], st.B * _blocks(st.ni), "xe", torch.uint8)
+        x8p = _dev(x[0], B * ni, "x8", torch.int8, dev)
+        xep = _dev(x[1], B * _blocks(ni), "xe", torch.uint8, dev)
     else:
-        xp, x8p, xep = _dev(x, st.B * st.ni, "x", dt), None, None
-    wp, wn = _dev_ws(ws)
-    _check(load().lp_step_backward(
-        ctypes.byref(st), xp, x8p, xep, _dev(W, st.no * st.ni, "W", dt), _dev(b, st.no, "b", dt, True),
-        _dev(dy, st.B * st.no, "dy", dt), int(bool(residual)), _dev(dx, st.B * st.ni, "dx", dt, True),
-        _dev(dW, st.no * st.ni, "dW", dt, True), _dev(db, st.no, "db", dt, True), wp, wn, _stream()),
-        "lp_step_backward")
+        xp, x8p, xep = _dev(x, B * ni, "x", dt, dev), None, None
+    wp, wn = _dev_ws(ws, dev)
+    rc = (_lib or load()).lp_step_backward(
+        ctypes.byref(st), xp, x8p, xep, _dev(W, no * ni, "W", dt, dev), _dev(b, no, "b", dt, dev, True),
+        _dev(dy, B * no, "dy", dt, dev), int(bool(residual)), _dev(dx, B * ni, "dx", dt, dev, True),
+        _dev(dW, no * ni, "dW", dt, dev, True), _dev(db, no, "db", dt, dev, True), wp, wn, _stream_of(dev))
+    if rc:
+        _check(rc, "lp_step_backward")
 
 
 def _ck_args(x, x8, xe):
-    import torch
-    kinds = {torch.float32: LP_F32, torch.bfloat16: LP_BF16, torch.float16: LP_F16, torch.float64: LP_F64}
-    if x is None or x.dtype not in kinds or x.dim() < 1:
+    dev = _here(x, "x")
+    kind = _kinds().get(x.dtype)
+    if kind is None or x.dim() < 1:
         raise ValueError("x must be a float32, bfloat16 or float16 tensor of rows")
+    import torch
     q = x.shape[-1]
     B = x.numel() // q if q else 0
-    return (kinds[x.dtype], B, q, _dev(x, B * q, "x", x.dtype), _dev(x8, B * q, "x8", torch.int8),
-            _dev(xe, B * _blocks(q), "xe", torch.uint8))
+    return (kind, B, q, _dev(x, B * q, "x", x.dtype, dev), _dev(x8, B * q, "x8", torch.int8, dev),
+            _dev(xe, B * _blocks(q), "xe", torch.uint8, dev), _stream_of(dev))
 
 
 def lp_checkpoint_store(x, x8, xe) -> None:
     """8-bit checkpoint of the rows of x [..., q]: x8 int8 like x, xe uint8 [..., ceil(q / 32)]."""
-    kind, B, q, xp, x8p, xep = _ck_args(x, x8, xe)
-    _check(load().lp_checkpoint_store(kind, B, q, xp, x8p, xep, _stream()), "lp_checkpoint_store")
+    kind, B, q, xp, x8p, xep, stream = _ck_args(x, x8, xe)
+    rc = (_lib or load()).lp_checkpoint_store(kind, B, q, xp, x8p, xep, stream)
+    if rc:
+        _check(rc, "lp_checkpoint_store")
 
 
 def lp_checkpoint_load(x8, xe, x) -> None:
     """The values of a checkpoint, written to the rows of x [..., q]."""
-    kind, B, q, xp, x8p, xep = _ck_args(x, x8, xe)
-    _check(load().lp_checkpoint_load(kind, B, q, x8p, xep, xp, _stream()), "lp_checkpoint_load")
+    kind, B, q, xp, x8p, xep, stream = _ck_args(x, x8, xe)
+    rc = (_lib or load()).lp_checkpoint_load(kind, B, q, x8p, xep, xp, stream)
+    if rc:
+        _check(rc, "lp_checkpoint_load")
 
 
 def lp_loss_labels_workspace_bytes(hd: LpLabelHead, grad: bool) -> int:
@@ -586,10 +623,14 @@ def lp_loss_labels(hd: LpLabelHead, u, W, mu, labels, J, ws, row=None, du=None, 
     loss, and the gradients of gscale J for those of du, dW, dmu that are given."""
     import torch
     dt = _wide_dtype(hd.dtype)
-    wp, wn = _dev_ws(ws)
-    _check(load().lp_loss_labels(
-        ctypes.byref(hd), _dev(u, hd.B * hd.q, "u", dt), _dev(W, hd.nc * hd.q, "W", dt),
-        _dev(mu, hd.nc, "mu", dt, True), _dev(labels, hd.B, "labels", torch.int64), gscale,
-        _dev(J, 1, "J", torch.float32), _dev(row, hd.B, "row", torch.float32, True),
-        _dev(du, hd.B * hd.q, "du", dt, True), _dev(dW, hd.nc * hd.q, "dW", dt, True),
-        _dev(dmu, hd.nc, "dmu", dt, True), wp, wn, _stream()), "lp_loss_labels")
+    dev = _here(W, "W")
+    B, q, nc = hd.B, hd.q, hd.nc
+    wp, wn = _dev_ws(ws, dev)
+    rc = (_lib or load()).lp_loss_labels(
+        ctypes.byref(hd), _dev(u, B * q, "u", dt, dev), _dev(W, nc * q, "W", dt, dev),
+        _dev(mu, nc, "mu", dt, dev, True), _dev(labels, B, "labels", torch.int64, dev), gscale,
+        _dev(J, 1, "J", torch.float32, dev), _dev(row, B, "row", torch.float32, dev, True),
+        _dev(du, B * q, "du", dt, dev, True), _dev(dW, nc * q, "dW", dt, dev, True),
+        _dev(dmu, nc, "dmu", dt, dev, True), wp, wn, _stream_of(dev))
+    if rc:
+        _check(rc, "lp_loss_labels")
