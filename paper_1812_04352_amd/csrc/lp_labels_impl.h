@@ -118,7 +118,8 @@ struct EpProb {
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
-    f32x16 sums[FN];
+    float col[FN];
+    unsigned char* buf = mm::wave_lds(lds, c, WGN);
     int at[FM];  // the label's place among the wave's classes
     float lse[FM];
 #pragma unroll
@@ -130,31 +131,32 @@ struct EpProb {
     }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
-      sums[j] = 0.f;
+      col[j] = 0.f;
       if (!WHOLE && c.nw + 32 * j >= a.ld) continue;
+      f32x16 sums = 0.f;
       f32x4 mu[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        mu[q] = a.mu ? mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+      mm::get_bias<WHOLE>(a.mu, c, j, mu);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        const int m = c.row(i);
-        if (m >= c.M) continue;
+        const bool on = c.row(i) < c.M;
+        f32x4 v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          f32x4 z = mm::quad(acc[i][j], q) + mu[q];
+          const f32x4 z = mm::quad(acc[i][j], q) + mu[q];
           const int n = c.feature(j, q) - c.nw;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            z[k] = exp_of(z[k] - lse[i]) - (at[i] == n + k ? 1.f : 0.f);
-            if (!WHOLE && c.nw + n + k >= c.N) z[k] = 0.f;
-            sums[j][4 * q + k] += z[k];
+            float p = exp_of(z[k] - lse[i]) - (at[i] == n + k ? 1.f : 0.f);
+            if (!on || (!WHOLE && c.nw + n + k >= c.N)) p = 0.f;
+            sums[4 * q + k] += p;
+            v[q][k] = p * PSCALE<T>;
           }
-          mm::store4<WHOLE>(a.P + (size_t)m * a.ld, c.nw + n, a.ld, z * PSCALE<T>);
         }
+        mm::put_rows<WHOLE>(a.P, a.ld, a.ld, c, i, j, buf, v);
       }
+      if (a.part) col[j] = mm::fold_columns(sums, c.lane);
     }
-    if (a.part) mm::column_sums<FN, WGM, WGN>(sums, c, lds, a.part + (size_t)c.mt * a.part_ld);
+    if (a.part) mm::column_sums<FN, WGM, WGN>(col, c, lds, a.part + (size_t)c.mt * a.part_ld);
   }
 };
 
@@ -171,28 +173,24 @@ struct EpDu {
     int first, last;
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
-  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     const float f = a.f * a.scale[0];
+    unsigned char* buf = mm::wave_lds(lds, c, WGN);
+    mm::Rows<WHOLE, float, FM, FN> sum(a.first ? nullptr : a.acc32, c.N, c);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = c.row(i);
-      if (m >= c.M) continue;
-      float* row = a.acc32 + (size_t)m * c.N;
-      T* out = a.du + (size_t)a.from[m] * c.N;
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
+      for (int i = 0; i < FM; ++i) {
         f32x4 v[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          v[q] = a.first ? f32x4{0.f, 0.f, 0.f, 0.f} : mm::load4<WHOLE>(row, c.feature(j, q), c.N);
+        sum.get(c, i, j, buf, v);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           v[q] += mm::quad(acc[i][j], q);
-          if (a.last) mm::store4<WHOLE>(out, c.feature(j, q), c.N, v[q] * f);
-          else mm::store4<WHOLE>(row, c.feature(j, q), c.N, v[q]);
+          if (a.last) v[q] *= f;
         }
+        if (a.last) mm::put_rows<WHOLE>(a.du, c.N, c.N, c, i, j, buf, v, [&](int m) { return a.from[m]; });
+        else mm::put_rows<WHOLE>(a.acc32, c.N, c.N, c, i, j, buf, v);
       }
-    }
   }
 };
 

@@ -443,39 +443,171 @@ __device__ __forceinline__ f32x4 quad(const f32x16& a, int q) {
   return v;
 }
 
-// Sums over the rows of a tile of one value per feature: v[j][r] holds a lane's sum over its
-// own block rows. Halving exchanges over the 32 lanes that share features leave one feature
-// block's value per lane, then the waves' sums are added in order. Result: out[n], n = n0.. .
-template <int FN, int WGM, int WGN>
-__device__ __forceinline__ void column_sums(f32x16 (&v)[FN], const Place& c, float* lds, float* out) {
-  const int BNW = 32 * FN;
+// A wave's 32 x 32 blocks of D between global memory, in rows of 16-byte pieces, and the quads that
+// the lanes hold, by way of the wave's own part of the LDS. Quads alone would be 8 bytes a lane from
+// 32 rows at a time.
+template <typename T>
+struct BlockIO {
+  static constexpr int W = 32 * (int)sizeof(T), PITCH = W + 16, CPR = W / 16, V = 16 / (int)sizeof(T);
+  static constexpr int ITER = (32 * CPR + 63) / 64, BYTES = 32 * PITCH;
+  typedef typename GVec<T, V>::type Piece;
+  typedef T LPiece __attribute__((ext_vector_type(V)));
+  typedef T Quad __attribute__((ext_vector_type(4)));
+  struct Block {
+    Piece p[ITER];
+  };
+
+  // pieces of block (i, j) of an array of rows of ld values (rows past the last are the last: not used)
+  static __device__ __forceinline__ Block fetch(const T* a, long ld, const Place& c, int i, int j) {
+    Block b;
 #pragma unroll
-  for (int j = 0; j < FN; ++j) {
-    // after the exchange over bit b the lane keeps the values r whose bit matches its own
-    float w[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) w[r] = v[j][r];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int half = 8 >> b, bit = 16 >> b;
-      const bool up = c.lane & bit;
-#pragma unroll
-      for (int r = 0; r < half; ++r) {
-        const float mine = up ? w[r + half] : w[r], other = up ? w[r] : w[r + half];
-        w[r] = mine + __shfl_xor(other, bit, 64);
-      }
+    for (int t = 0; t < ITER; ++t) {
+      const int id = c.lane + 64 * t, m = min(c.mw + 32 * i + id / CPR, c.M - 1);
+      b.p[t] = *reinterpret_cast<const Piece*>(a + (size_t)m * ld + c.nw + 32 * j + id % CPR * V);
     }
-    // lane bits 4..1 now name r (most significant first); bit 0 still to add
-    const float s = w[0] + __shfl_xor(w[0], 1, 64);
-    const int r = (c.lane >> 1) & 15;
-    if (!(c.lane & 1)) lds[c.wm * (WGN * BNW) + c.wn * BNW + 32 * j + 8 * (r >> 2) + 4 * (c.lane >> 5) + (r & 3)] = s;
+    return b;
+  }
+
+  static __device__ __forceinline__ void quads(const Block& b, unsigned char* buf, const Place& c, f32x4 (&v)[4]) {
+#pragma unroll
+    for (int t = 0; t < ITER; ++t) {
+      const int id = c.lane + 64 * t;
+      *reinterpret_cast<LPiece*>(buf + id / CPR * PITCH + id % CPR * 16) = b.p[t];
+    }
+    __builtin_amdgcn_wave_barrier();
+    const unsigned char* r = buf + (c.lane & 31) * PITCH + (c.lane >> 5) * 4 * sizeof(T);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const Quad x = *reinterpret_cast<const Quad*>(r + 8 * q * sizeof(T));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[q][k] = (float)x[k];
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // row(m): the index of row m in the array
+  template <typename F>
+  static __device__ __forceinline__ void store(T* a, long ld, const Place& c, int i, int j, unsigned char* buf,
+                                               const f32x4 (&v)[4], F row) {
+    unsigned char* w = buf + (c.lane & 31) * PITCH + (c.lane >> 5) * 4 * sizeof(T);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      Quad x;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = (T)v[q][k];
+      *reinterpret_cast<Quad*>(w + 8 * q * sizeof(T)) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int t = 0; t < ITER; ++t) {
+      const int id = c.lane + 64 * t, m = c.mw + 32 * i + id / CPR;
+      const Piece x = *reinterpret_cast<const LPiece*>(buf + id / CPR * PITCH + id % CPR * 16);
+      if (m < c.M) *reinterpret_cast<Piece*>(a + (size_t)row(m) * ld + c.nw + 32 * j + id % CPR * V) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
+// The LDS of an epilogue: a part per wave, as large as the largest type needs.
+constexpr int WAVE_LDS = BlockIO<float>::BYTES;
+__device__ __forceinline__ unsigned char* wave_lds(float* lds, const Place& c, int wgn) {
+  return reinterpret_cast<unsigned char*>(lds) + (c.wm * wgn + c.wn) * WAVE_LDS;
+}
+
+// An array of rows of ld values, c.N of which count (WHOLE: all of the tile's), as a lane's quads,
+// block by block in the order i = 0.. within j = 0..
+template <bool WHOLE, typename T, int FM, int FN>
+struct Rows {
+  typedef BlockIO<T> IO;
+  const T* a;
+  long ld;
+  typename IO::Block next;
+  __device__ __forceinline__ Rows(const T* a_, long ld_, const Place& c) : a(a_), ld(ld_) {
+    if constexpr (WHOLE) {
+      if (a) next = IO::fetch(a, ld, c, 0, 0);
+    }
+  }
+  // the quads of block (i, j) (zeros without an array); requests the next block's
+  __device__ __forceinline__ void get(const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
+    if (!a) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = 0.f;
+    } else if constexpr (WHOLE) {
+      const typename IO::Block b = next;
+      if (i + 1 < FM) next = IO::fetch(a, ld, c, i + 1, j);
+      else if (j + 1 < FN) next = IO::fetch(a, ld, c, 0, j + 1);
+      IO::quads(b, buf, c, v);
+    } else {
+      const T* row = a + (size_t)min(c.row(i), c.M - 1) * ld;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = load4(row, c.feature(j, q), c.N);
+    }
+  }
+};
+
+// The quads of block (i, j) to an array of rows of ld values, n of which are written.
+template <bool WHOLE, typename T, typename F>
+__device__ __forceinline__ void put_rows(T* a, long ld, int n, const Place& c, int i, int j, unsigned char* buf,
+                                         const f32x4 (&v)[4], F row) {
+  if constexpr (WHOLE) {
+    BlockIO<T>::store(a, ld, c, i, j, buf, v, row);
+  } else if (c.row(i) < c.M) {
+    T* r = a + (size_t)row(c.row(i)) * ld;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) store4(r, c.feature(j, q), n, v[q]);
+  }
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void put_rows(T* a, long ld, int n, const Place& c, int i, int j, unsigned char* buf,
+                                         const f32x4 (&v)[4]) {
+  put_rows<WHOLE>(a, ld, n, c, i, j, buf, v, [](int m) { return m; });
+}
+
+// Four features of a row vector (a bias) for each quad of block column j; zeros without one.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void get_bias(const T* b, const Place& c, int j, f32x4 (&v)[4]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) v[q] = b ? load4<WHOLE>(b, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+// Sums over a wave's rows of the features of a block column: v holds a lane's sums over its own
+// rows. Halving exchanges over the 32 lanes that share features leave one feature's sum per pair of
+// lanes: that of feature 8 (r / 4) + 4 (lane / 32) + r % 4, r = lane / 2 % 16.
+__device__ __forceinline__ float fold_columns(const f32x16& v, int lane) {
+  // after the exchange over a lane bit the lane keeps the values r whose bit matches its own
+  float w[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) w[r] = v[r];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const int half = 8 >> b, bit = 16 >> b;
+    const bool up = lane & bit;
+#pragma unroll
+    for (int r = 0; r < half; ++r) {
+      const float mine = up ? w[r + half] : w[r], other = up ? w[r] : w[r + half];
+      w[r] = mine + __shfl_xor(other, bit, 64);
+    }
+  }
+  return w[0] + __shfl_xor(w[0], 1, 64);
+}
+
+// The waves' folded sums of each block column, added in order: out[n], n = n0 ..
+template <int FN, int WGM, int WGN>
+__device__ __forceinline__ void column_sums(const float (&s)[FN], const Place& c, float* lds, float* out) {
+  constexpr int BNW = 32 * FN;
+  const int r = (c.lane >> 1) & 15;
+  __syncthreads();  // the waves' parts of the LDS are free
+  if (!(c.lane & 1)) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+      lds[c.wm * (WGN * BNW) + c.wn * BNW + 32 * j + 8 * (r >> 2) + 4 * (c.lane >> 5) + (r & 3)] = s[j];
   }
   __syncthreads();
   for (int n = threadIdx.x; n < WGN * BNW; n += 64 * WGM * WGN) {
-    float s = 0.f;
+    float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < WGM; ++w) s += lds[w * (WGN * BNW) + n];
-    if (c.n0 + n < c.N) out[c.n0 + n] = s;
+    for (int w = 0; w < WGM; ++w) t += lds[w * (WGN * BNW) + n];
+    if (c.n0 + n < c.N) out[c.n0 + n] = t;
   }
 }
 
@@ -507,17 +639,18 @@ struct EpScale {
     const float* scale;
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
-  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     const float f = a.scale ? a.f * a.scale[0] : a.f;
+    unsigned char* buf = wave_lds(lds, c, WGN);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = c.row(i);
-      if (m >= c.M) continue;
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
+      for (int i = 0; i < FM; ++i) {
+        f32x4 v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) store4<WHOLE>(a.out + (size_t)m * c.N, c.feature(j, q), c.N, quad(acc[i][j], q) * f);
-    }
+        for (int q = 0; q < 4; ++q) v[q] = quad(acc[i][j], q) * f;
+        put_rows<WHOLE>(a.out, c.N, c.N, c, i, j, buf, v);
+      }
   }
 };
 
@@ -525,7 +658,7 @@ struct EpScale {
 template <class S, class E>
 __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int splits, typename E::Args ea) {
   constexpr int WGM = S::WGM, WGN = S::WGN, FM = S::BM / WGM / 32, FN = S::BN / WGN / 32, Q = 4 * FM * FN;
-  __shared__ float lds[4096];  // as much as an epilogue uses
+  __shared__ __attribute__((aligned(16))) float lds[WGM * WGN * WAVE_LDS / 4];  // as much as an epilogue uses
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int K;
   const Place c = place<S>(p, wave, K);

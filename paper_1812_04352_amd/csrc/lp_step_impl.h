@@ -97,48 +97,46 @@ struct EpStep {
     int act;
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
-  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     const int nb = (c.N + CK_BLOCK - 1) / CK_BLOCK;
+    unsigned char* buf = mm::wave_lds(lds, c, WGN);
+    mm::Rows<WHOLE, T, FM, FN> res(a.r, c.N, c);
     with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         if (!WHOLE && c.nw + 32 * j >= c.N) continue;
         f32x4 bias[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          bias[q] = a.b ? mm::load4<WHOLE>(a.b, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+        mm::get_bias<WHOLE>(a.b, c, j, bias);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-          const int m = c.row(i);
-          const bool on = m < c.M;
-          const size_t row = (size_t)(on ? m : c.M - 1) * c.N;
           f32x4 v[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            v[q] = a.r ? mm::load4<WHOLE>(a.r + row, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
-          uint32_t top = 0;
+          res.get(c, i, j, buf, v);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const f32x4 z = mm::quad(acc[i][j], q) + bias[q];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              v[q][k] = (float)(T)(v[q][k] + a.h * sigma<T, decltype(act)::value>(z[k]));
-              if (WHOLE || c.feature(j, q) + k < c.N) top = max(top, abs_bits(v[q][k]));
-            }
+            for (int k = 0; k < 4; ++k) v[q][k] += a.h * sigma<T, decltype(act)::value>(z[k]);
           }
-          if (on) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) mm::store4<WHOLE>(a.y + row, c.feature(j, q), c.N, v[q]);
-          }
+          mm::put_rows<WHOLE>(a.y, c.N, c.N, c, i, j, buf, v);
           if (a.y8) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                v[q][k] = (float)(T)v[q][k];
+                if (WHOLE || c.feature(j, q) + k < c.N) top = max(top, abs_bits(v[q][k]));
+              }
             top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
             const uint32_t byte = ck_byte<T>(top);
             const float inv = ck_inv(byte);
-            if (on) {
 #pragma unroll
-              for (int q = 0; q < 4; ++q) store_ck<WHOLE>(a.y8 + row, c.feature(j, q), c.N, v[q], inv);
-              if (c.lane < 32) a.ye[(size_t)m * nb + (c.nw + 32 * j) / CK_BLOCK] = (uint8_t)byte;
-            }
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[q][k] = (float)ck_round(v[q][k], inv);
+            mm::put_rows<WHOLE>(a.y8, c.N, c.N, c, i, j, buf, v);
+            const int m = c.row(i);
+            if (m < c.M && c.lane < 32) a.ye[(size_t)m * nb + (c.nw + 32 * j) / CK_BLOCK] = (uint8_t)byte;
           }
         }
       }
@@ -160,41 +158,38 @@ struct EpGrad {
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
-    f32x16 sums[FN];
+    float col[FN];
+    unsigned char* buf = mm::wave_lds(lds, c, WGN);
+    mm::Rows<WHOLE, T, FM, FN> dy(a.dy, c.N, c);
     with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
-        sums[j] = 0.f;
+        col[j] = 0.f;
         if (!WHOLE && c.nw + 32 * j >= a.ld) continue;
+        f32x16 sums = 0.f;
         f32x4 bias[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          bias[q] = a.b ? mm::load4<WHOLE>(a.b, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+        mm::get_bias<WHOLE>(a.b, c, j, bias);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-          const int m = c.row(i);
-          const bool on = m < c.M;
-          const size_t row = on ? m : c.M - 1;
+          const bool on = c.row(i) < c.M;
           f32x4 g[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) g[q] = mm::load4<WHOLE>(a.dy + row * c.N, c.feature(j, q), c.N);
+          dy.get(c, i, j, buf, g);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const f32x4 z = mm::quad(acc[i][j], q) + bias[q];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              g[q][k] = on && (WHOLE || c.feature(j, q) + k < c.N) ? g[q][k] * dsigma<T, decltype(act)::value>(z[k]) : 0.f;
-              sums[j][4 * q + k] += g[q][k];
+              const bool in = on && (WHOLE || c.feature(j, q) + k < c.N);
+              g[q][k] = in ? g[q][k] * dsigma<T, decltype(act)::value>(z[k]) : 0.f;
+              sums[4 * q + k] += g[q][k];
             }
           }
-          if (on) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) mm::store4<WHOLE>(a.g + row * a.ld, c.feature(j, q), a.ld, g[q]);
-          }
+          mm::put_rows<WHOLE>(a.g, a.ld, a.ld, c, i, j, buf, g);
         }
+        col[j] = mm::fold_columns(sums, c.lane);
       }
     });
-    mm::column_sums<FN, WGM, WGN>(sums, c, lds, a.part + (size_t)c.mt * c.N);
+    mm::column_sums<FN, WGM, WGN>(col, c, lds, a.part + (size_t)c.mt * c.N);
   }
 };
 
@@ -207,22 +202,19 @@ struct EpDx {
     float h;
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
-  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
+    unsigned char* buf = mm::wave_lds(lds, c, WGN);
+    mm::Rows<WHOLE, T, FM, FN> dy(a.dy, c.N, c);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int m = c.row(i);
-      if (m >= c.M) continue;
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
+      for (int i = 0; i < FM; ++i) {
         f32x4 v[4];
+        dy.get(c, i, j, buf, v);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          v[q] = a.dy ? mm::load4<WHOLE>(a.dy + (size_t)m * c.N, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          mm::store4<WHOLE>(a.dx + (size_t)m * c.N, c.feature(j, q), c.N, v[q] + mm::quad(acc[i][j], q) * a.h);
+        for (int q = 0; q < 4; ++q) v[q] += mm::quad(acc[i][j], q) * a.h;
+        mm::put_rows<WHOLE>(a.dx, c.N, c.N, c, i, j, buf, v);
       }
-    }
   }
 };
 
