@@ -10,8 +10,8 @@
 namespace lp {
 
 namespace mm {
-// How a product of the wide operators runs (lp_mm.h): its tile size (256, 128 or 64, square)
-// and splits of the contraction.
+// How a product of the wide operators runs (lp_mm.h): its tile size (256, 128 or 64, square; 1:
+// the kernel of one row, one_features() features a tile) and splits of the contraction.
 struct Plan {
   int tile, splits, tm, tn;
   size_t part_bytes() const { return splits > 1 ? (size_t)splits * tm * tn * tile * tile * 4 : 0; }

@@ -51,6 +51,7 @@ struct EpLse {
     float* zl;              // [rows]: logit of the label
     long rows;              // row stride of part
     int j0;                 // first class of the product
+    bool blocks_of_32() const { return false; }
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
@@ -61,13 +62,13 @@ struct EpLse {
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        mu[j][q] = a.mu ? mm::load4<WHOLE>(a.mu, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+        mu[j][q] = a.mu ? mm::load4<WHOLE>(a.mu, c.feature(j, q), c.lim) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       const int m = c.row(i);
       // the label's place among the wave's classes
       const int64_t l = (m < c.M ? a.labels[m] : -1) - a.j0;
-      const int at = l >= 0 && l < c.N ? (int)l - c.nw : -1;
+      const int at = l >= 0 && l < c.lim ? (int)l - c.nw : -1;
       float top = -INFINITY, zl = 0.f;
       bool mine = false;
 #pragma unroll
@@ -77,7 +78,7 @@ struct EpLse {
           const int n = c.feature(j, r >> 2) - c.nw + (r & 3);
           const float z = acc[i][j][r] + mu[j][r >> 2][r & 3];
           if (at == n) zl = z, mine = true;
-          if (WHOLE || c.nw + n < c.N) top = fmaxf(top, z);
+          if (WHOLE || c.nw + n < c.lim) top = fmaxf(top, z);
         }
       if (mine) a.zl[m] = zl;
       // a NaN is no maximum; it comes back through the sum (exp of NaN)
@@ -87,12 +88,12 @@ struct EpLse {
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (WHOLE || c.feature(j, r >> 2) + (r & 3) < c.N) s += exp_of((acc[i][j][r] + mu[j][r >> 2][r & 3]) - ref);
+          if (WHOLE || c.feature(j, r >> 2) + (r & 3) < c.lim) s += exp_of((acc[i][j][r] + mu[j][r >> 2][r & 3]) - ref);
       MaxSum v{top, s};
       v = join(v, MaxSum{__shfl_xor(v.m, 32, 64), __shfl_xor(v.s, 32, 64)});
       if (c.lane < 32) red[c.wn * BM + c.wm * FM * 32 + 32 * i + c.lane] = v;
     }
-    __syncthreads();
+    c.meet<WGM * WGN>();
     for (int r = threadIdx.x; r < BM; r += 64 * WGM * WGN) {
       MaxSum v = red[r];
 #pragma unroll
@@ -115,6 +116,7 @@ struct EpProb {
     float* part;            // [tile rows][part_ld], from the piece's first class on (nullable)
     long part_ld;
     int j0;                 // first class of the piece
+    bool blocks_of_32() const { return false; }
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
@@ -126,7 +128,7 @@ struct EpProb {
     for (int i = 0; i < FM; ++i) {
       const int m = min(c.row(i), c.M - 1);
       const int64_t l = a.labels[m] - a.j0;
-      at[i] = l >= 0 && l < c.N ? (int)l - c.nw : -1;
+      at[i] = l >= 0 && l < c.lim ? (int)l - c.nw : -1;
       lse[i] = a.lse[m];
     }
 #pragma unroll
@@ -147,12 +149,12 @@ struct EpProb {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             float p = exp_of(z[k] - lse[i]) - (at[i] == n + k ? 1.f : 0.f);
-            if (!on || (!WHOLE && c.nw + n + k >= c.N)) p = 0.f;
+            if (!on || (!WHOLE && c.nw + n + k >= c.lim)) p = 0.f;
             sums[4 * q + k] += p;
             v[q][k] = p * PSCALE<T>;
           }
         }
-        mm::put_rows<WHOLE>(a.P, a.ld, a.ld, c, i, j, buf, v);
+        mm::put_rows<WHOLE>(a.P, a.ld, c.upto(a.ld), c, i, j, buf, v);
       }
       if (a.part) col[j] = mm::fold_columns(sums, c.lane);
     }
@@ -188,8 +190,8 @@ struct EpDu {
           v[q] += mm::quad(acc[i][j], q);
           if (a.last) v[q] *= f;
         }
-        if (a.last) mm::put_rows<WHOLE>(a.du, c.N, c.N, c, i, j, buf, v, [&](int m) { return a.from[m]; });
-        else mm::put_rows<WHOLE>(a.acc32, c.N, c.N, c, i, j, buf, v);
+        if (a.last) mm::put_rows<WHOLE>(a.du, c.N, c.lim, c, i, j, buf, v, [&](int m) { return a.from[m]; });
+        else mm::put_rows<WHOLE>(a.acc32, c.N, c.lim, c, i, j, buf, v);
       }
   }
 };
@@ -322,7 +324,7 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
     if (a.B) k_gather<T><<<(unsigned)mm::ceil_div(a.B, 4), 256, 0, st>>>((const T*)a.u, to, a.B, a.q, uc, ldu, (T*)a.du, row);
     e = hipGetLastError();
   } else {
-    const mm::Operand<T> u(a.u, a.B, a.q, uc, st);
+    const mm::Operand<T> u(a.u, a.B, a.q, uc, a.B == 1, st);
     rows = u.p;
     ldr = u.ld;
     e = u.e;
@@ -333,8 +335,8 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   int tiles = 0;  // class tiles so far
   for (int j0 = 0; j0 < a.nc && a.B; j0 += l.piece) {
     const int n = std::min(l.piece, a.nc - j0);
-    const mm::Plan pl = mm::plan_of(sizeof(T), a.B, n, a.q);
-    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, n, a.q, w + l.W, st);
+    const mm::Plan pl = mm::plan_rows(sizeof(T), a.B, n, a.q);
+    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, n, a.q, w + l.W, pl.tile == 1, st);
     if (Wj.e != hipSuccess) return Wj.e;
     typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)tiles * a.B, zl, a.B, j0};
     const mm::Prob p{rows, Wj.p, ldr, Wj.ld, a.B, n, a.q, cnt, 1, 0, 0, 0, 0};
@@ -350,11 +352,11 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   if ((e = hipGetLastError()) != hipSuccess || !grad) return e;
   for (int j0 = 0; j0 < a.nc; j0 += l.piece) {
     const int n = std::min(l.piece, a.nc - j0), ldp = mm::padded(sizeof(T), n);
-    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, a.B ? n : 0, a.q, w + l.W, st);
+    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, a.B ? n : 0, a.q, w + l.W, false, st);
     if (Wj.e != hipSuccess) return Wj.e;
     if (a.B) {
       typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, ldp, a.dmu ? col : nullptr, n, j0};
-      const mm::Plan pl = mm::plan_of(sizeof(T), a.B, n, a.q);
+      const mm::Plan pl = mm::plan_rows(sizeof(T), a.B, n, a.q);
       const mm::Prob pp{uc, Wj.p, ldu, Wj.ld, a.B, n, a.q, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, pl, split, st)) != hipSuccess) return e;
       if (a.dmu)
@@ -365,14 +367,14 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
     if (a.du && a.B) {
       typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
       const mm::Prob pd{P, Wj.p, ldp, Wj.ld, a.B, a.q, n, count, 1, 0, 0, 0, 0};
-      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n), split, st)) != hipSuccess)
+      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n, true), split, st)) != hipSuccess)
         return e;
     }
     if (a.dW) {
       T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
       const mm::Prob pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
       e = mm::launch_mm<T, true, true, mm::EpScale<T>>(pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale},
-                                                       mm::plan_of(sizeof(T), n, a.q, a.B), split, st);
+                                                       mm::plan_of(sizeof(T), n, a.q, a.B, true), split, st);
       if (e != hipSuccess) return e;
     }
   }

@@ -259,12 +259,21 @@ struct Prob {
 // feature n = nw + 32 j + 8 q + 4 (lane / 32) of quad q of block column j.
 struct Place {
   int M, N;
+  int lim;         // end of the workgroup's features
   int m0, n0;      // the workgroup's tile
   int mw, nw;      // the wave's part of it
   int wm, wn;      // the wave's place in the workgroup
   int mt, nt;      // tile indices
   int split;
   int lane;
+  // the end of what is written of rows of ld >= N values (the last tile also writes what is behind N)
+  __device__ __forceinline__ int upto(int ld) const { return lim == N ? ld : lim; }
+  // the workgroup's waves meet (a single wave's LDS accesses are in order by themselves)
+  template <int WAVES>
+  __device__ __forceinline__ void meet() const {
+    if constexpr (WAVES == 1) __builtin_amdgcn_wave_barrier();
+    else __syncthreads();
+  }
   __device__ __forceinline__ int row(int i) const { return mw + 32 * i + (lane & 31); }
   __device__ __forceinline__ int feature(int j, int q) const { return nw + 32 * j + 8 * q + 4 * (lane >> 5); }
 };
@@ -310,6 +319,7 @@ __device__ __forceinline__ Place place(const Prob& p, int wave, int& K) {
   tile_of(blockIdx.x, p.tm, p.tn, c.mt, c.nt);
   c.m0 = c.mt * S::BM;
   c.n0 = c.nt * S::BN;
+  c.lim = min(c.N, c.n0 + S::BN);
   c.lane = threadIdx.x & 63;
   c.wm = wave / S::WGN;
   c.wn = wave % S::WGN;
@@ -514,7 +524,7 @@ __device__ __forceinline__ unsigned char* wave_lds(float* lds, const Place& c, i
   return reinterpret_cast<unsigned char*>(lds) + (c.wm * wgn + c.wn) * WAVE_LDS;
 }
 
-// An array of rows of ld values, c.N of which count (WHOLE: all of the tile's), as a lane's quads,
+// An array of rows of ld values, those below c.lim of which count (WHOLE: all of the tile's), as a lane's quads,
 // block by block in the order i = 0.. within j = 0..
 template <bool WHOLE, typename T, int FM, int FN>
 struct Rows {
@@ -540,7 +550,7 @@ struct Rows {
     } else {
       const T* row = a + (size_t)min(c.row(i), c.M - 1) * ld;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = load4(row, c.feature(j, q), c.N);
+      for (int q = 0; q < 4; ++q) v[q] = load4(row, c.feature(j, q), c.lim);
     }
   }
 };
@@ -567,7 +577,7 @@ __device__ __forceinline__ void put_rows(T* a, long ld, int n, const Place& c, i
 template <bool WHOLE, typename T>
 __device__ __forceinline__ void get_bias(const T* b, const Place& c, int j, f32x4 (&v)[4]) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] = b ? load4<WHOLE>(b, c.feature(j, q), c.N) : f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int q = 0; q < 4; ++q) v[q] = b ? load4<WHOLE>(b, c.feature(j, q), c.lim) : f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
 // Sums over a wave's rows of the features of a block column: v holds a lane's sums over its own
@@ -596,18 +606,18 @@ template <int FN, int WGM, int WGN>
 __device__ __forceinline__ void column_sums(const float (&s)[FN], const Place& c, float* lds, float* out) {
   constexpr int BNW = 32 * FN;
   const int r = (c.lane >> 1) & 15;
-  __syncthreads();  // the waves' parts of the LDS are free
+  c.meet<WGM * WGN>();  // the waves' parts of the LDS are free
   if (!(c.lane & 1)) {
 #pragma unroll
     for (int j = 0; j < FN; ++j)
       lds[c.wm * (WGN * BNW) + c.wn * BNW + 32 * j + 8 * (r >> 2) + 4 * (c.lane >> 5) + (r & 3)] = s[j];
   }
-  __syncthreads();
+  c.meet<WGM * WGN>();
   for (int n = threadIdx.x; n < WGN * BNW; n += 64 * WGM * WGN) {
     float t = 0.f;
 #pragma unroll
     for (int w = 0; w < WGM; ++w) t += lds[w * (WGN * BNW) + n];
-    if (c.n0 + n < c.N) out[c.n0 + n] = t;
+    if (c.n0 + n < c.lim) out[c.n0 + n] = t;
   }
 }
 
@@ -622,11 +632,13 @@ struct EpRaw {
     constexpr int NT = 64 * WGM * WGN, Q = 4 * FM * FN;
     f32x4* out = a.part + ((size_t)c.split * gridDim.x + blockIdx.x) * (Q * NT) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < FM; ++i) {
+      if (c.row(i) >= c.M) continue;
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) out[((i * FN + j) * 4 + q) * NT] = quad(acc[i][j], q);
+    }
   }
 };
 
@@ -637,6 +649,7 @@ struct EpScale {
     T* out;  // [M][N]
     float f;
     const float* scale;
+    bool blocks_of_32() const { return false; }
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
@@ -649,7 +662,7 @@ struct EpScale {
         f32x4 v[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = quad(acc[i][j], q) * f;
-        put_rows<WHOLE>(a.out, c.N, c.N, c, i, j, buf, v);
+        put_rows<WHOLE>(a.out, c.N, c.lim, c, i, j, buf, v);
       }
   }
 };
@@ -668,10 +681,12 @@ __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = 0.f;
+#pragma unroll 2
   for (int k = 0; k < splits; ++k) {
     const f32x4* in = part + ((size_t)k * gridDim.x + blockIdx.x) * (Q * S::NT) + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < FM; ++i) {
+      if (c.row(i) >= c.M) continue;
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -680,9 +695,91 @@ __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int
 #pragma unroll
           for (int r = 0; r < 4; ++r) acc[i][j][4 * q + r] += v[r];
         }
+    }
   }
   if (c.n0 + S::BN <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, lds);
   else E::template run<false, FM, FN, WGM, WGN>(ea, c, acc, lds);
+}
+
+// A product of one row of A (both operands in rows): bound by reading B once. A workgroup takes NF
+// features, a wave R of them: it reads whole runs of their rows (64 lanes, 16 bytes each, one after the
+// other, U of them in flight), multiplies in fp32 on the vector ALU, and adds over its lanes in a fixed
+// order; the sums go through the LDS into the layout that an epilogue expects of one wave. Any alignment.
+// NF (one_features): a CU reads about 23 GB/s from memory, so few features a workgroup where there are
+// few in all: 1024 x 8192 bf16 7.5 us with 8, 9.5 with 16, 14.2 with 32; 4096 x 4096 8.9 with 16, 11.4 with
+// 32; 65536 x 4096 90 with 8, 87.5 with 16 (6.1 TB/s), 98 with 32. A checkpoint's blocks need 32.
+// (Matrix instructions fed from 16 rows' 64-byte pieces took 13 to 15 us there, split tiles 12 in two launches;
+// two to four rows on the vector ALU 21, where split tiles still take 12.)
+inline int one_features(long N) { return N <= 16384 ? 8 : 16; }
+
+template <typename T, int NF, class E>
+__global__ __launch_bounds__(32 * NF) void k_one(Prob p, typename E::Args ea) {
+  constexpr int V = 16 / (int)sizeof(T), RUN = 64 * V, R = 2, U = 4;
+  typedef typename GVec<T, V>::type GChunk;
+  __shared__ __attribute__((aligned(16))) float lds[WAVE_LDS / 4];
+  __shared__ float sums[32];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (p.count && *p.count == 0) return;
+  const int n0 = blockIdx.x * NF;
+  const T* a = static_cast<const T*>(p.A);
+  const T* b[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) b[j] = static_cast<const T*>(p.B) + (long)min(n0 + wave * R + j, p.N - 1) * p.ldb;
+  float acc[R] = {};
+  const auto add = [&](const GChunk (&w)[R], const GChunk& x) {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+#pragma unroll
+      for (int j = 0; j < R; ++j) acc[j] = fmaf((float)w[j][k], (float)x[k], acc[j]);
+  };
+  int k = lane * V;
+  for (; k - lane * V + U * RUN <= p.K; k += U * RUN) {  // U whole runs
+    GChunk w[U][R], x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) w[u][j] = *reinterpret_cast<const GChunk*>(b[j] + k + u * RUN);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = *reinterpret_cast<const GChunk*>(a + k + u * RUN);
+#pragma unroll
+    for (int u = 0; u < U; ++u) add(w[u], x[u]);
+  }
+  for (; k < p.K; k += RUN) {  // this lane's chunks of the rest
+    GChunk w[R], x;
+    if (k + V <= p.K) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) w[j] = *reinterpret_cast<const GChunk*>(b[j] + k);
+      x = *reinterpret_cast<const GChunk*>(a + k);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) w[j][e] = k + e < p.K ? b[j][k + e] : (T)0.f;
+        x[e] = k + e < p.K ? a[k + e] : (T)0.f;
+      }
+    }
+    add(w, x);
+  }
+  if (threadIdx.x < 32) sums[threadIdx.x] = 0.f;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc[j] += __shfl_xor(acc[j], o, 64);
+    if (lane == 0) sums[wave * R + j] = acc[j];
+  }
+  __syncthreads();
+  if (wave) return;
+  // lane l's quad q: row m = l % 32 (of which there is one), features 8 q + 4 (l / 32) ..
+  f32x16 d[1][1];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) d[0][0][r] = sums[8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)];
+  Place c;
+  c.M = 1, c.N = p.N, c.lim = min(p.N, n0 + NF), c.m0 = 0, c.n0 = n0, c.mw = 0, c.nw = n0, c.wm = 0, c.wn = 0;
+  c.mt = 0, c.nt = blockIdx.x, c.split = 0, c.lane = lane;
+  if (n0 + 32 <= c.lim) E::template run<true, 1, 1, 1, 1>(ea, c, d, lds);
+  else E::template run<false, 1, 1, 1, 1>(ea, c, d, lds);
 }
 
 // out[n] = f * scale[0] * sum over tile rows of part[t][n], in fp64 and in order (64 columns by 4
@@ -749,9 +846,10 @@ struct Operand {
   const T* p;
   long ld;
   hipError_t e;
-  Operand(const void* in, size_t rows, int cols, void* copy, hipStream_t st)
+  // as_is: any alignment will do
+  Operand(const void* in, size_t rows, int cols, void* copy, bool as_is, hipStream_t st)
       : p(static_cast<const T*>(in)), ld(cols), e(hipSuccess) {
-    if (cols * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0) return;
+    if (as_is || (cols * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0)) return;
     ld = padded(sizeof(T), cols);
     p = static_cast<const T*>(copy);
     const size_t n = rows * (ld * sizeof(T) / 16);
@@ -773,24 +871,28 @@ typedef Shape<64, 64, 2, 2, 128, 2, 1> Tile64f;
 constexpr int STAGE_BYTES = 128;
 
 // The plan with the least estimated time, from measured times of a stage (us) with one workgroup on
-// a CU and with two (of 256: two in turn). A split writes and reads its partial sums (3 TB/s both
+// a CU and with two (of 256: two in turn; one on every CU takes 1.85); cols: an operand in columns,
+// whose fragments take twice the LDS reads. A split writes and reads its partial sums (3 TB/s both
 // ways) and takes a second launch (3 us). Measured against the other choices, bf16: 1024 x 1024 x
 // 4096 21 us by tiles of 64 (128: 35, 256: 89); 8192 x 1024 x 2048 37 us by 128 (64: 53, 256: 57);
 // 8192 x 4096 x 4096 230 us by 256 (128: 256, 64: over 370). float: 1024 x 1024 x 4096 95 us by 64 (128:
 // 185); 4096 x 2048 x 1024 85 by 128 (64: 110); 8192 x 4096 x 4096 1108 by 256 (128: 1272, 64: 1670).
-inline Plan plan_of(size_t esz, long M, long N, long K) {
+inline Plan plan_of(size_t esz, long M, long N, long K, bool cols) {
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
-  const double stage[2][3][2] = {{{1.4, 3.5}, {0.60, 1.0}, {0.28, 0.45}}, {{3.9, 8.66}, {1.45, 2.48}, {0.74, 0.82}}};
+  const double stage[3][3][2] = {{{1.4, 3.6}, {0.65, 1.0}, {0.30, 0.45}},    // 16 bits, rows
+                                 {{1.4, 3.6}, {0.85, 1.1}, {0.59, 0.62}},    // 16 bits, columns
+                                 {{3.95, 8.7}, {1.55, 2.6}, {0.82, 1.0}}};  // float
+  const auto& us = stage[esz == 4 ? 2 : cols];
   Plan best{};
   double least = 1e30;
   for (int s = 0; s < 3; ++s) {
     const int tile = 256 >> s;
     const long tm = ceil_div(M, tile), tn = ceil_div(N, tile);
-    const double one = stage[esz == 4][s][0], two = stage[esz == 4][s][1];
+    const double two = us[s][1], one = tile == 256 && tm * tn > 128 ? two / 2 : us[s][0];
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (splits > 1 && (steps < 4 * splits || tile == 256)) break;  // (a split large tile would be two middle ones)
       const long n = ceil_div(tm * tn * splits, 256);
-      double t = ceil_div(steps, splits) * ((n / 2) * two + (n % 2) * (tile == 256 && n > 1 ? two / 2 : one));
+      double t = ceil_div(steps, splits) * ((n / 2) * two + (n % 2) * one);
       if (splits > 1) t += 3.0 + 2.0 * splits * tm * tn * tile * tile * 4 / 3e6;
       if (t < least) {
         least = t;
@@ -799,6 +901,12 @@ inline Plan plan_of(size_t esz, long M, long N, long K) {
     }
   }
   return best;
+}
+
+// The plan of a product whose operands are both in rows: k_one for one row.
+inline Plan plan_rows(size_t esz, long M, long N, long K) {
+  if (M == 1) return Plan{1, 1, 1, ceil_div(N, one_features(N))};
+  return plan_of(esz, M, N, K, false);
 }
 
 template <typename T, class S, bool AT, bool BT, class E>
@@ -820,6 +928,14 @@ hipError_t launch_shape(Prob p, const typename E::Args& ea, const Plan& pl, void
 // part: pl.part_bytes() of workspace
 template <typename T, bool AT, bool BT, class E>
 hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, void* part, hipStream_t st) {
+  if constexpr (!AT && !BT) {
+    if (pl.tile == 1) {
+      if (ea.blocks_of_32()) k_one<T, 32, E><<<(unsigned)ceil_div(p.N, 32), 1024, 0, st>>>(p, ea);
+      else if (one_features(p.N) == 8) k_one<T, 8, E><<<(unsigned)pl.tn, 256, 0, st>>>(p, ea);
+      else k_one<T, 16, E><<<(unsigned)pl.tn, 512, 0, st>>>(p, ea);
+      return hipGetLastError();
+    }
+  }
   if constexpr (sizeof(T) == 2) {
     if (pl.tile == 256) return launch_shape<T, Tile256, AT, BT, E>(p, ea, pl, part, st);
     if (pl.tile == 128) return launch_shape<T, Tile128, AT, BT, E>(p, ea, pl, part, st);

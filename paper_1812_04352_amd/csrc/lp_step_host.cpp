@@ -87,9 +87,9 @@ namespace lp {
 StepLayout step_layout(int dtype, int B, int ni, int no) {
   const size_t e = esize(dtype);
   StepLayout l;
-  l.z = mm::plan_of(e, B, no, ni);
-  l.zx = mm::plan_of(e, B, ni, no);
-  l.zw = mm::plan_of(e, no, ni, B);
+  l.z = mm::plan_rows(e, B, no, ni);
+  l.zx = mm::plan_of(e, B, ni, no, true);
+  l.zw = mm::plan_of(e, no, ni, B, true);
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
     const size_t r = at;
@@ -124,11 +124,11 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
   const int last = nc % l.piece ? nc % l.piece : l.piece, others = (nc - last) / l.piece;
   size_t tiles = 0, split = 0, col = 0;
   for (int n : {l.piece, last}) {
-    const mm::Plan z = mm::plan_of(e, B, n, q);
+    const mm::Plan z = mm::plan_rows(e, B, n, q);
     tiles += (size_t)z.tn * (n == last ? 1 : others);
     split = std::max(split, z.part_bytes());
     if (grad) {
-      split = std::max({split, mm::plan_of(e, B, q, n).part_bytes(), mm::plan_of(e, n, q, B).part_bytes()});
+      split = std::max({split, mm::plan_of(e, B, q, n, true).part_bytes(), mm::plan_of(e, n, q, B, true).part_bytes()});
       col = std::max(col, (size_t)z.tm * n * 4);
     }
     if (l.piece == last) {

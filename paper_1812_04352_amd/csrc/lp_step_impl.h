@@ -95,6 +95,7 @@ struct EpStep {
     uint8_t* ye;
     float h;
     int act;
+    bool blocks_of_32() const { return y8 != nullptr; }  // a workgroup's features are whole checkpoint blocks
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
@@ -104,7 +105,7 @@ struct EpStep {
     with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
-        if (!WHOLE && c.nw + 32 * j >= c.N) continue;
+        if (!WHOLE && c.nw + 32 * j >= c.lim) continue;
         f32x4 bias[4];
         mm::get_bias<WHOLE>(a.b, c, j, bias);
 #pragma unroll
@@ -117,7 +118,7 @@ struct EpStep {
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[q][k] += a.h * sigma<T, decltype(act)::value>(z[k]);
           }
-          mm::put_rows<WHOLE>(a.y, c.N, c.N, c, i, j, buf, v);
+          mm::put_rows<WHOLE>(a.y, c.N, c.lim, c, i, j, buf, v);
           if (a.y8) {
             uint32_t top = 0;
 #pragma unroll
@@ -125,7 +126,7 @@ struct EpStep {
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
                 v[q][k] = (float)(T)v[q][k];
-                if (WHOLE || c.feature(j, q) + k < c.N) top = max(top, abs_bits(v[q][k]));
+                if (WHOLE || c.feature(j, q) + k < c.lim) top = max(top, abs_bits(v[q][k]));
               }
             top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
             const uint32_t byte = ck_byte<T>(top);
@@ -134,7 +135,7 @@ struct EpStep {
             for (int q = 0; q < 4; ++q)
 #pragma unroll
               for (int k = 0; k < 4; ++k) v[q][k] = (float)ck_round(v[q][k], inv);
-            mm::put_rows<WHOLE>(a.y8, c.N, c.N, c, i, j, buf, v);
+            mm::put_rows<WHOLE>(a.y8, c.N, c.lim, c, i, j, buf, v);
             const int m = c.row(i);
             if (m < c.M && c.lane < 32) a.ye[(size_t)m * nb + (c.nw + 32 * j) / CK_BLOCK] = (uint8_t)byte;
           }
@@ -155,6 +156,7 @@ struct EpGrad {
     int ld;
     float* part;  // [tile rows][N]
     int act;
+    bool blocks_of_32() const { return false; }
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
@@ -179,12 +181,12 @@ struct EpGrad {
             const f32x4 z = mm::quad(acc[i][j], q) + bias[q];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const bool in = on && (WHOLE || c.feature(j, q) + k < c.N);
+              const bool in = on && (WHOLE || c.feature(j, q) + k < c.lim);
               g[q][k] = in ? g[q][k] * dsigma<T, decltype(act)::value>(z[k]) : 0.f;
               sums[4 * q + k] += g[q][k];
             }
           }
-          mm::put_rows<WHOLE>(a.g, a.ld, a.ld, c, i, j, buf, g);
+          mm::put_rows<WHOLE>(a.g, a.ld, c.upto(a.ld), c, i, j, buf, g);
         }
         col[j] = mm::fold_columns(sums, c.lane);
       }
@@ -213,62 +215,135 @@ struct EpDx {
         dy.get(c, i, j, buf, v);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] += mm::quad(acc[i][j], q) * a.h;
-        mm::put_rows<WHOLE>(a.dx, c.N, c.N, c, i, j, buf, v);
+        mm::put_rows<WHOLE>(a.dx, c.N, c.lim, c, i, j, buf, v);
       }
   }
 };
 
-// Eight lanes per block of 32 features, four features each; the grid walks the blocks.
-constexpr unsigned CK_GRID = 1u << 20;
+// Checkpoint kernels: four lanes per block of 32 features, eight features each, four blocks a
+// thread in flight; bound by memory. FLAT: rows of whole blocks, which follow one another without
+// a division. (With four features a thread, one block in flight and 64-bit divisions 16384 x 8192
+// bf16 took 127 us to store and 133 us to load.)
+constexpr int CK_U = 4;
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_ck_store(const T* x, int8_t* x8, uint8_t* xe, size_t nblk, int q, int nb) {
-  const int part = threadIdx.x & 7;
-  for (size_t blk = (size_t)blockIdx.x * 32 + (threadIdx.x >> 3); blk < nblk; blk += (size_t)gridDim.x * 32) {
-    const size_t row = blk / nb;
-    const int n = (int)(blk - row * nb) * CK_BLOCK + 4 * part;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (n < q) v = mm::load4(x + row * q, n, q);
-    uint32_t top = max(max(abs_bits(v[0]), abs_bits(v[1])), max(abs_bits(v[2]), abs_bits(v[3])));
+__device__ __forceinline__ void load8(const T* row, int n, int q, f32x4 (&v)[2]) {
+  v[0] = mm::load4(row, n, q);
+  v[1] = mm::load4(row, n + 4, q);
+}
+
+template <typename T, bool FLAT>
+__global__ __launch_bounds__(256) void k_ck_store(const T* x, int8_t* x8, uint8_t* xe, uint32_t nblk, int q, uint32_t nb) {
+  const int part = threadIdx.x & 3;
+  const uint32_t stride = gridDim.x * 64u;
+  for (uint32_t b0 = blockIdx.x * 64u + (threadIdx.x >> 2); b0 < nblk; b0 += CK_U * stride) {
+    f32x4 v[CK_U][2];
+    size_t at[CK_U];
+    int n[CK_U];
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-    const uint32_t byte = ck_byte<T>(top);
-    const float inv = ck_inv(byte);
-    store_ck(x8 + row * q, n, q, v, inv);
-    if (part == 0) xe[blk] = (uint8_t)byte;
+    for (int u = 0; u < CK_U; ++u) {
+      const uint32_t blk = min(b0 + u * stride, nblk - 1), row = FLAT ? 0 : blk / nb;
+      n[u] = FLAT ? 8 * part : (int)(blk - row * nb) * CK_BLOCK + 8 * part;
+      at[u] = FLAT ? (size_t)blk * CK_BLOCK : (size_t)row * q;
+      if constexpr (FLAT) {
+        const auto t = *reinterpret_cast<const typename mm::GVec<T, 8>::type*>(x + at[u] + n[u]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[u][k >> 2][k & 3] = (float)t[k];
+      } else {
+        load8(x + at[u], n[u], q, v[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < CK_U; ++u) {
+      const uint32_t blk = b0 + u * stride;
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top = max(top, abs_bits(v[u][k >> 2][k & 3]));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
+      top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+      const uint32_t byte = ck_byte<T>(top);
+      const float inv = ck_inv(byte);
+      if (blk >= nblk) continue;
+      if constexpr (FLAT) {
+        typename mm::GVec<int8_t, 8>::type w;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = (int8_t)ck_round(v[u][k >> 2][k & 3], inv);
+        *reinterpret_cast<typename mm::GVec<int8_t, 8>::type*>(x8 + at[u] + n[u]) = w;
+      } else {
+        store_ck(x8 + at[u], n[u], q, v[u][0], inv);
+        store_ck(x8 + at[u], n[u] + 4, q, v[u][1], inv);
+      }
+      if (part == 0) xe[blk] = (uint8_t)byte;
+    }
   }
 }
 
-// Rows of ld >= q values, zeros behind the q that count (ld at most the next multiple of 32).
-template <typename T>
-__global__ __launch_bounds__(256) void k_ck_load(const int8_t* x8, const uint8_t* xe, T* x, size_t nblk, int q, int nb,
+// To rows of ld >= q values, zeros behind the q that count (ld at most the next multiple of 32).
+template <typename T, bool FLAT>
+__global__ __launch_bounds__(256) void k_ck_load(const int8_t* x8, const uint8_t* xe, T* x, uint32_t nblk, int q, uint32_t nb,
                                                  int ld) {
-  for (size_t blk = (size_t)blockIdx.x * 32 + (threadIdx.x >> 3); blk < nblk; blk += (size_t)gridDim.x * 32) {
-    const size_t row = blk / nb;
-    const int n = (int)(blk - row * nb) * CK_BLOCK + 4 * (threadIdx.x & 7);
-    // (a block that is not finite is NaN in the row's features only: the rest of ld is zero)
-    f32x4 v = mm::load4(x8 + row * q, n, q) * ck_scale(xe[blk]);
+  const int part = threadIdx.x & 3;
+  const uint32_t stride = gridDim.x * 64u;
+  for (uint32_t b0 = blockIdx.x * 64u + (threadIdx.x >> 2); b0 < nblk; b0 += CK_U * stride) {
+    f32x4 v[CK_U][2];
+    float scale[CK_U];
+    size_t row[CK_U];
+    int n[CK_U];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = n + k < q ? v[k] : 0.f;
-    if (n < ld) mm::store4(x + row * ld, n, ld, v);
+    for (int u = 0; u < CK_U; ++u) {
+      const uint32_t blk = min(b0 + u * stride, nblk - 1);
+      row[u] = FLAT ? 0 : blk / nb;
+      n[u] = FLAT ? 8 * part : (int)(blk - (uint32_t)row[u] * nb) * CK_BLOCK + 8 * part;
+      scale[u] = ck_scale(xe[blk]);
+      if constexpr (FLAT) {
+        row[u] = blk;
+        const auto t = *reinterpret_cast<const typename mm::GVec<int8_t, 8>::type*>(x8 + (size_t)blk * CK_BLOCK + n[u]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[u][k >> 2][k & 3] = (float)t[k];
+      } else {
+        load8(x8 + row[u] * q, n[u], q, v[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < CK_U; ++u) {
+      if (b0 + u * stride >= nblk) continue;
+      if constexpr (FLAT) {
+        typename mm::GVec<T, 8>::type w;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = (T)(v[u][k >> 2][k & 3] * scale[u]);
+        *reinterpret_cast<typename mm::GVec<T, 8>::type*>(x + row[u] * CK_BLOCK + n[u]) = w;
+      } else {
+        // (a block that is not finite is NaN in the row's features only: the rest of ld is zero)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[u][k >> 2][k & 3] = n[u] + k < q ? v[u][k >> 2][k & 3] * scale[u] : 0.f;
+        mm::store4(x + row[u] * ld, n[u], ld, v[u][0]);
+        mm::store4(x + row[u] * ld, n[u] + 4, ld, v[u][1]);
+      }
+    }
   }
 }
 
-inline unsigned ck_grid(size_t nblk) { return (unsigned)std::min<size_t>((nblk + 31) / 32, CK_GRID); }
+// At most 16384 workgroups: CK_U blocks a thread where there are that many, and then again.
+inline unsigned ck_grid(size_t nblk) {
+  const size_t all = (nblk + 63) / 64;
+  return (unsigned)(all <= 1024 ? all : std::min<size_t>((all + CK_U - 1) / CK_U, 16384));
+}
 
 template <typename T>
 hipError_t ck_store_t(const void* x, int8_t* x8, uint8_t* xe, long B, int q, hipStream_t st) {
   const int nb = mm::ceil_div(q, CK_BLOCK);
-  const size_t nblk = (size_t)B * nb;
-  k_ck_store<T><<<ck_grid(nblk), 256, 0, st>>>((const T*)x, x8, xe, nblk, q, nb);
+  const uint32_t nblk = (uint32_t)(B * nb);
+  if (q % CK_BLOCK == 0) k_ck_store<T, true><<<ck_grid(nblk), 256, 0, st>>>((const T*)x, x8, xe, nblk, q, nb);
+  else k_ck_store<T, false><<<ck_grid(nblk), 256, 0, st>>>((const T*)x, x8, xe, nblk, q, nb);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t ck_load_t(const int8_t* x8, const uint8_t* xe, void* x, long B, int q, int ld, hipStream_t st) {
   const int nb = mm::ceil_div(q, CK_BLOCK);
-  const size_t nblk = (size_t)B * nb;
-  k_ck_load<T><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb, ld);
+  const uint32_t nblk = (uint32_t)(B * nb);
+  if (q % CK_BLOCK == 0) k_ck_load<T, true><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb, ld);
+  else k_ck_load<T, false><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb, ld);
   return hipGetLastError();
 }
 
@@ -280,7 +355,8 @@ template <typename T>
 hipError_t step_forward_t(const StepArgs& a, hipStream_t st) {
   const StepLayout l = step_layout(a.dtype, a.B, a.ni, a.no);
   char* w = static_cast<char*>(a.ws);
-  const mm::Operand<T> x(a.x, a.B, a.ni, w + l.x, st), W(a.W, a.no, a.ni, w + l.W, st);
+  const bool one = l.z.tile == 1;
+  const mm::Operand<T> x(a.x, a.B, a.ni, w + l.x, one, st), W(a.W, a.no, a.ni, w + l.W, one, st);
   if (x.e != hipSuccess) return x.e;
   if (W.e != hipSuccess) return W.e;
   typename EpStep<T>::Args e{(const T*)a.b, (const T*)a.r, (T*)a.y, a.y8, a.ye, (float)a.h, a.act};
@@ -296,8 +372,8 @@ hipError_t step_backward_t(const StepArgs& a, hipStream_t st) {
   float* colpart = reinterpret_cast<float*>(w + l.col);
   hipError_t e = hipSuccess;
   if (!a.x && a.B && (e = ck_load_t<T>(a.x8, a.xe, w + l.x, a.B, a.ni, ldx, st)) != hipSuccess) return e;
-  mm::Operand<T> x(a.x ? a.x : w + l.x, a.x ? a.B : 0, a.ni, w + l.x, st);
-  const mm::Operand<T> W(a.W, a.no, a.ni, w + l.W, st);
+  mm::Operand<T> x(a.x ? a.x : w + l.x, a.x ? a.B : 0, a.ni, w + l.x, false, st);
+  const mm::Operand<T> W(a.W, a.no, a.ni, w + l.W, false, st);
   if (x.e != hipSuccess) return x.e;
   if (W.e != hipSuccess) return W.e;
   if (a.B) {  // (an empty batch leaves zero sums: products over no rows)
