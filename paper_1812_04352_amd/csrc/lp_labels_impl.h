@@ -367,14 +367,14 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
     if (a.du && a.B) {
       typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
       const mm::Prob pd{P, Wj.p, ldp, Wj.ld, a.B, a.q, n, count, 1, 0, 0, 0, 0};
-      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n, true), split, st)) != hipSuccess)
+      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n), split, st)) != hipSuccess)
         return e;
     }
     if (a.dW) {
       T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
       const mm::Prob pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
       e = mm::launch_mm<T, true, true, mm::EpScale<T>>(pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale},
-                                                       mm::plan_of(sizeof(T), n, a.q, a.B, true), split, st);
+                                                       mm::plan_of(sizeof(T), n, a.q, a.B), split, st);
       if (e != hipSuccess) return e;
     }
   }

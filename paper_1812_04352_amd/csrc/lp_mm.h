@@ -173,18 +173,22 @@ struct Stage {
   // Requests the next stage; wave: the wave's index in a scalar register. Loads past `left` give
   // zeros: rows past the last (rows), contraction indices past the last (columns); so does an
   // offset of 2^31 (rows: past the contraction's end, which only the last stage can hold).
+  // (The instruction is written out: of the builtin's loads the compiler believes that a transposing
+  // LDS read may depend on every one in flight, and waits for all of them before it.)
   __device__ __forceinline__ void load(unsigned char* lds, int wave) {
-#ifdef __HIP_DEVICE_COMPILE__  // (buffer resources are no type of the host compilation)
-    typedef __attribute__((address_space(3))) void lds_void;
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<unsigned char*>(base), 0, (left >> 31) != 0 ? 0x7fffffff : (int)left, 0x00020000);
+#ifdef __HIP_DEVICE_COMPILE__
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    const i32x4 r = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xffff, (left >> 31) != 0 ? 0x7fffffff : (int)left, 0x00020000};
+    const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + wave * 1024;
     if (!COLS && k + BK > k1) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) off[i] = k + kc >= k1 ? 0x80000000u : off[i];
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(lds + (i * NT + wave * 64) * 16), 16, off[i], 0, 0, 0);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * NT * 16), "v"(off[i]),
+                   "s"(r));
     base += step;
     left -= step;
     k += BK;
@@ -298,11 +302,11 @@ struct Shape {
   static_assert((NS & (NS - 1)) == 0, "a stage's place is its index modulo NS");
 };
 
-// All but N of the wave's loads have landed, and every wave is here.
+// All but N of the wave's loads to LDS have landed, and every wave is here. (The compiler does not
+// count those loads: nothing else waits for them.)
 template <int N>
 __device__ __forceinline__ void wait_and_meet() {
-  if constexpr (N == 0) __syncthreads();
-  else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 template <class S>
@@ -864,6 +868,7 @@ struct Operand {
 // CU, one's epilogue beside the other's products. Small: four stages in flight for short grids.
 typedef Shape<256, 256, 2, 4, 128, 2, 2> Tile256;
 typedef Shape<128, 128, 2, 2, 128, 2, 2> Tile128;
+typedef Shape<128, 128, 2, 2, 128, 4, 2> Tile128d;  // four stages, where a CU holds one workgroup at most
 typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;
 typedef Shape<256, 256, 2, 4, 128, 2, 1> Tile256f;  // float: two steps a stage
 typedef Shape<128, 128, 2, 2, 128, 2, 1> Tile128f;
@@ -871,18 +876,16 @@ typedef Shape<64, 64, 2, 2, 128, 2, 1> Tile64f;
 constexpr int STAGE_BYTES = 128;
 
 // The plan with the least estimated time, from measured times of a stage (us) with one workgroup on
-// a CU and with two (of 256: two in turn; one on every CU takes 1.85); cols: an operand in columns,
-// whose fragments take twice the LDS reads. A split writes and reads its partial sums (3 TB/s both
-// ways) and takes a second launch (3 us). Measured against the other choices, bf16: 1024 x 1024 x
-// 4096 21 us by tiles of 64 (128: 35, 256: 89); 8192 x 1024 x 2048 37 us by 128 (64: 53, 256: 57);
-// 8192 x 4096 x 4096 230 us by 256 (128: 256, 64: over 370). float: 1024 x 1024 x 4096 95 us by 64 (128:
-// 185); 4096 x 2048 x 1024 85 by 128 (64: 110); 8192 x 4096 x 4096 1108 by 256 (128: 1272, 64: 1670).
-inline Plan plan_of(size_t esz, long M, long N, long K, bool cols) {
+// a CU and with two (of 256: two in turn; one on every CU takes 1.8). A split writes and reads its
+// partial sums (3 TB/s both ways) and takes a second launch (3 us). Measured against the other choices,
+// bf16: 1024 x 1024 x 4096 21 us by tiles of 64 (128: 34, 256: 89); 2048 x 2048 x 4096 39 by 128 with four
+// stages (two: 45, 64: 55, 256: 88); 4096 x 2048 x 4096 63 us by 128 with two stages (four: 75); 8192 x 4096 x
+// 4096 230 us by 256 (128: 256, 64: over 370). float: 1024 x 1024 x 4096 90 us by 64 (128: 185); 4096 x 2048 x
+// 2048 160 by 128; 8192 x 4096 x 4096 1108 by 256 (128: 1272, 64: 1670).
+inline Plan plan_of(size_t esz, long M, long N, long K) {
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
-  const double stage[3][3][2] = {{{1.4, 3.6}, {0.65, 1.0}, {0.30, 0.45}},    // 16 bits, rows
-                                 {{1.4, 3.6}, {0.85, 1.1}, {0.59, 0.62}},    // 16 bits, columns
-                                 {{3.95, 8.7}, {1.55, 2.6}, {0.82, 1.0}}};  // float
-  const auto& us = stage[esz == 4 ? 2 : cols];
+  const double stage[2][3][2] = {{{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{3.95, 8.7}, {1.5, 2.5}, {0.72, 1.0}}};
+  const auto& us = stage[esz == 4];
   Plan best{};
   double least = 1e30;
   for (int s = 0; s < 3; ++s) {
@@ -906,7 +909,7 @@ inline Plan plan_of(size_t esz, long M, long N, long K, bool cols) {
 // The plan of a product whose operands are both in rows: k_one for one row.
 inline Plan plan_rows(size_t esz, long M, long N, long K) {
   if (M == 1) return Plan{1, 1, 1, ceil_div(N, one_features(N))};
-  return plan_of(esz, M, N, K, false);
+  return plan_of(esz, M, N, K);
 }
 
 template <typename T, class S, bool AT, bool BT, class E>
@@ -920,7 +923,7 @@ hipError_t launch_shape(Prob p, const typename E::Args& ea, const Plan& pl, void
     k_mm<T, S, AT, BT, E><<<dim3(tiles), S::NT, 0, st>>>(p, ea);
   } else if constexpr (S::BM < 256) {
     k_mm<T, S, AT, BT, EpRaw><<<dim3(tiles, (unsigned)pl.splits), S::NT, 0, st>>>(p, EpRaw::Args{static_cast<f32x4*>(part)});
-    k_finish<S, E><<<dim3(tiles), S::NT, 0, st>>>(p, static_cast<const f32x4*>(part), pl.splits, ea);
+    k_finish<Shape<S::BM, S::BN, S::WGM, S::WGN, 128, 2, 2>, E><<<dim3(tiles), S::NT, 0, st>>>(p, static_cast<const f32x4*>(part), pl.splits, ea);
   }
   return hipGetLastError();
 }
@@ -938,7 +941,10 @@ hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, 
   }
   if constexpr (sizeof(T) == 2) {
     if (pl.tile == 256) return launch_shape<T, Tile256, AT, BT, E>(p, ea, pl, part, st);
-    if (pl.tile == 128) return launch_shape<T, Tile128, AT, BT, E>(p, ea, pl, part, st);
+    if (pl.tile == 128) {
+      if ((long)pl.tm * pl.tn * pl.splits <= 256) return launch_shape<T, Tile128d, AT, BT, E>(p, ea, pl, part, st);
+      return launch_shape<T, Tile128, AT, BT, E>(p, ea, pl, part, st);
+    }
     return launch_shape<T, Tile64, AT, BT, E>(p, ea, pl, part, st);
   } else {
     if (pl.tile == 256) return launch_shape<T, Tile256f, AT, BT, E>(p, ea, pl, part, st);

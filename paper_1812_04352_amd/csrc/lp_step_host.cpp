@@ -88,8 +88,8 @@ StepLayout step_layout(int dtype, int B, int ni, int no) {
   const size_t e = esize(dtype);
   StepLayout l;
   l.z = mm::plan_rows(e, B, no, ni);
-  l.zx = mm::plan_of(e, B, ni, no, true);
-  l.zw = mm::plan_of(e, no, ni, B, true);
+  l.zx = mm::plan_of(e, B, ni, no);
+  l.zw = mm::plan_of(e, no, ni, B);
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
     const size_t r = at;
@@ -128,7 +128,7 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     tiles += (size_t)z.tn * (n == last ? 1 : others);
     split = std::max(split, z.part_bytes());
     if (grad) {
-      split = std::max({split, mm::plan_of(e, B, q, n, true).part_bytes(), mm::plan_of(e, n, q, B, true).part_bytes()});
+      split = std::max({split, mm::plan_of(e, B, q, n).part_bytes(), mm::plan_of(e, n, q, B).part_bytes()});
       col = std::max(col, (size_t)z.tm * n * 4);
     }
     if (l.piece == last) {
