@@ -275,10 +275,11 @@ struct LabelArgs {
 struct LabelLayout {
   size_t part, zl, row;                                           // losses
   size_t u, W;                                                    // copies with rows on 16 bytes
-  size_t from, to, lab, count, scale, lse, P, du, col;            // gradients
+  size_t from, to, lab, count, scale, lse, P, du, col, z;         // gradients
   size_t split;                                                   // partial sums of split products
   size_t total;
   int piece;  // classes taken at a time
+  bool keep;  // the logits are kept for the gradients
 };
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad);
 

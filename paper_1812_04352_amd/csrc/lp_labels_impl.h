@@ -3,10 +3,10 @@
 // a label c_k in 0..nc-1 (n of them):
 //   lse_k = log sum_j exp z_kj,  loss_k = lse_k - z_k[c_k],  J = (1/n) sum loss_k,
 //   P = softmax(z) - onehot,  du = (s/n) P W,  dW = (s/n) P^T u,  dmu = (s/n) sum_k P_k.
-// The logits are never stored. A product over all classes leaves, per tile of classes, each
-// row's maximum and sum of exponentials (8 bytes where the tile had 128 logits); they are
-// joined in order into lse. For the gradients the logits are formed a second time, a piece of
-// the vocabulary after the other; a piece of P is kept in the workspace in the element type (the
+// A product over all classes leaves, per tile of classes, each row's maximum and sum of exponentials
+// (8 bytes where the tile had 128 logits); they are joined in order into lse. For the gradients the
+// logits are formed a second time, a piece of the vocabulary after the other (unless the whole
+// batch's are small enough to be kept: label_layout); a piece of P is kept in the workspace in the element type (the
 // type of the next products' operands), as P times PSCALE: 2^14 for f16, whose range would
 // otherwise lose the small probabilities of a large vocabulary (the least normal value then
 // stands for 3.7e-9), a power of two that the epilogues take back exactly.
@@ -51,11 +51,14 @@ struct EpLse {
     float* zl;              // [rows]: logit of the label
     long rows;              // row stride of part
     int j0;                 // first class of the product
+    float* z;               // logits to keep, rows of ldz values (nullable)
+    int ldz;
     bool blocks_of_32() const { return false; }
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
-    MaxSum* red = reinterpret_cast<MaxSum*>(lds);  // [WGN][rows of the tile]
+    MaxSum* red = reinterpret_cast<MaxSum*>(lds + WGM * WGN * mm::WAVE_LDS / 4);  // [WGN][rows of the tile]
+    unsigned char* buf = mm::wave_lds(lds, c, WGN);
     constexpr int BM = WGM * FM * 32;
     f32x4 mu[FN][4];
 #pragma unroll
@@ -81,6 +84,15 @@ struct EpLse {
           if (WHOLE || c.nw + n < c.lim) top = fmaxf(top, z);
         }
       if (mine) a.zl[m] = zl;
+      if (a.z) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          f32x4 v[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] = mm::quad(acc[i][j], q) + mu[j][q];
+          mm::put_rows<WHOLE>(a.z, a.ldz, c.lim, c, i, j, buf, v);
+        }
+      }
       // a NaN is no maximum; it comes back through the sum (exp of NaN)
       const float ref = top == -INFINITY ? 0.f : top;
       float s = 0.f;
@@ -115,6 +127,8 @@ struct EpProb {
     int ld;
     float* part;            // [tile rows][part_ld], from the piece's first class on (nullable)
     long part_ld;
+    T* dmu;                 // with a single tile row: scale[0] times the sums themselves (nullable)
+    const float* scale;
     int j0;                 // first class of the piece
     bool blocks_of_32() const { return false; }
   };
@@ -158,7 +172,11 @@ struct EpProb {
       }
       if (a.part) col[j] = mm::fold_columns(sums, c.lane);
     }
-    if (a.part) mm::column_sums<FN, WGM, WGN>(col, c, lds, a.part + (size_t)c.mt * a.part_ld);
+    if (a.part)
+      mm::column_sums<FN, WGM, WGN>(col, c, lds, [&](int n, float t) {
+        if (a.dmu) a.dmu[n] = (T)(t * a.scale[0]);
+        else a.part[(size_t)c.mt * a.part_ld + n] = t;
+      });
   }
 };
 
@@ -230,13 +248,46 @@ static __global__ __launch_bounds__(1024) void k_rows(const int64_t* labels, int
   }
 }
 
-// Copies the labelled rows together (rows of ld values, zeros behind the q that count); the other rows' loss and gradient are zero. A wave per row.
+// Copies the labelled rows together (rows of ld values, zeros behind the q that count); the other
+// rows' loss and gradient are zero. A wave per row. Batches of at most ROWS_EACH rows have no k_rows:
+// every workgroup then counts the labelled rows before its own (up to 32 KB of labels from cache).
+constexpr int ROWS_EACH = 4096;
 template <typename T>
-__global__ __launch_bounds__(256) void k_gather(const T* u, const int* to, int B, int q, T* uc, int ld, T* du,
-                                                float* row) {
-  const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+__global__ __launch_bounds__(256) void k_gather(const T* u, const int64_t* labels, int B, int q, int nc, double gs, int* from,
+                                                int* to, int64_t* lab, int* count, float* scale, T* uc, int ld, T* du,
+                                                T* dmu, float* row) {
+  __shared__ int sh[4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, b0 = blockIdx.x * 4, b = b0 + wave;
+  int r = -1;
+  if (B <= ROWS_EACH) {  // (the same for all)
+    int n = 0;
+    for (int i = threadIdx.x; i < b0; i += 256) n += labels[i] >= 0 && labels[i] < nc;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+    if (lane == 0) sh[wave] = n;
+    __syncthreads();
+    int at = sh[0] + sh[1] + sh[2] + sh[3];
+    for (int i = 0; i < 4; ++i) {
+      const int64_t l = b0 + i < B ? labels[b0 + i] : -1;
+      const bool on = l >= 0 && l < nc;
+      if (i == wave && on) {
+        r = at;
+        if (lane == 0) from[at] = b, lab[at] = l;
+      }
+      at += on;
+    }
+    if (b0 + 4 >= B) {
+      if (threadIdx.x == 0) {
+        count[0] = at;
+        scale[0] = (float)(gs / (double)(at > 0 ? at : 1));
+      }
+      if (at == 0 && dmu)  // (with a single column partial the products write dmu, if there are any)
+        for (int i = threadIdx.x; i < nc; i += 256) dmu[i] = (T)0.f;
+    }
+  } else if (b < B) {
+    r = to[b];
+  }
   if (b >= B) return;
-  const int r = to[b];
   if (r < 0) {
     if (lane == 0) row[b] = 0.f;
     if (du)
@@ -246,14 +297,39 @@ __global__ __launch_bounds__(256) void k_gather(const T* u, const int* to, int B
   for (int i = 4 * lane; i < ld; i += 256) mm::store4(uc + (size_t)r * ld, i, ld, mm::load4(u + (size_t)b * q, i, q));
 }
 
+// A piece of P (times PSCALE; zeros from class n to ld) from kept logits z (rows of ld values; of floats P
+// may be z itself), and its column sums over PROB_ROWS rows a workgroup. Four classes a thread.
+constexpr int PROB_ROWS = 32;
+template <typename T>
+__global__ __launch_bounds__(256) void k_prob(const float* z, const float* lse, const int64_t* lab, const int* count, int n,
+                                              int ld, T* P, float* part, T* dmu, const float* scale) {
+  const int c = (blockIdx.y * 256 + threadIdx.x) * 4, m0 = blockIdx.x * PROB_ROWS, m1 = min(m0 + PROB_ROWS, *count);
+  if (c >= ld || m0 >= m1) return;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int m = m0; m < m1; ++m) {
+    f32x4 v = mm::load4<true>(z + (size_t)m * ld, c, ld);
+    const float l = lse[m];
+    const int64_t at = lab[m] - c;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = c + k < n ? exp_of(v[k] - l) - (at == k ? 1.f : 0.f) : 0.f;
+    sum += v;
+    mm::store4<true>(P + (size_t)m * ld, c, ld, v * PSCALE<T>);
+  }
+  if (dmu) mm::store4(dmu, c, n, sum * scale[0]);
+  else if (part) mm::store4(part + (size_t)blockIdx.x * n, c, n, sum);
+}
+
 // Joins the class tiles of a row: lse and the loss. `per` rows (a power of two) by 256 / per threads
 // a workgroup: many threads a row where there are few rows (16 rows of 1024 tiles: 33 us with 16
 // threads a row, 5 with 128).
-// labels as in EpLse; a row without one has loss 0. from (nullable): where row r's loss goes.
+// labels as in EpLse; a row without one has loss 0. from (nullable): where row r's loss goes. J (a single
+// workgroup for all rows): the mean of the labelled rows' losses, summed in fp64 in order.
 static __global__ __launch_bounds__(256) void k_lse(const MaxSum* part, int tiles, long rows, const int64_t* labels, int nc,
                                                     const float* zl, const int* count, int M, const int* from, float* lse,
-                                                    float* loss, int per) {
+                                                    float* loss, int per, float* J) {
   __shared__ MaxSum red[256];
+  __shared__ float rows_loss[256];
   if (count) M = min(M, *count);
   const int r = threadIdx.x & (per - 1), g = threadIdx.x / per, groups = 256 / per, m = blockIdx.x * per + r;
   MaxSum v{-INFINITY, 0.f};
@@ -273,11 +349,25 @@ static __global__ __launch_bounds__(256) void k_lse(const MaxSum* part, int tile
     __syncthreads();
     if (g < half) red[threadIdx.x] = v = join(v, red[threadIdx.x + half * per]);
   }
-  if (g || m >= M) return;
-  const float l = v.m + logf(v.s);
-  if (lse) lse[m] = l;
-  const int64_t lab = labels[m];
-  loss[from ? from[m] : m] = lab >= 0 && lab < nc ? l - zl[m] : 0.f;
+  if (g == 0 && m < M) {
+    const float l = v.m + logf(v.s);
+    if (lse) lse[m] = l;
+    const int64_t lab = labels[m];
+    const bool on = lab >= 0 && lab < nc;
+    const float d = on ? l - zl[m] : 0.f;
+    loss[from ? from[m] : m] = d;
+    rows_loss[r] = d;
+  }
+  if (!J) return;
+  __syncthreads();
+  if (threadIdx.x) return;
+  double sum = 0.0;
+  int n = 0;
+  for (int k = 0; k < per && k < M; ++k) {
+    const int64_t lab = labels[k];
+    if (lab >= 0 && lab < nc) sum += (double)rows_loss[k], ++n;
+  }
+  J[0] = (float)(sum / (n > 0 ? n : 1));
 }
 
 // J = sum of the rows' losses / number of labelled rows, in fp64 and in a fixed order.
@@ -316,63 +406,81 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   float* col = reinterpret_cast<float*>(w + l.col);
   void* split = w + l.split;
   hipError_t e = hipSuccess;
+  float* z = l.keep ? reinterpret_cast<float*>(w + l.z) : nullptr;
+  const int ldp = mm::padded(sizeof(T), l.piece);  // of a whole piece
   // rows of the products: u's own, or with gradients the labelled ones
-  const T* rows = uc;
-  long ldr = ldu;
+  const T* rows = nullptr;
+  long ldr = 0;
   if (grad) {
-    k_rows<<<1, 1024, 0, st>>>(a.labels, a.B, a.nc, a.gscale, from, to, lab, count, scale);
-    if (a.B) k_gather<T><<<(unsigned)mm::ceil_div(a.B, 4), 256, 0, st>>>((const T*)a.u, to, a.B, a.q, uc, ldu, (T*)a.du, row);
-    e = hipGetLastError();
-  } else {
-    const mm::Operand<T> u(a.u, a.B, a.q, uc, a.B == 1, st);
-    rows = u.p;
-    ldr = u.ld;
-    e = u.e;
+    if (a.B > ROWS_EACH) k_rows<<<1, 1024, 0, st>>>(a.labels, a.B, a.nc, a.gscale, from, to, lab, count, scale);
+    if (a.B)
+      k_gather<T><<<(unsigned)mm::ceil_div(a.B, 4), 256, 0, st>>>((const T*)a.u, a.labels, a.B, a.q, a.nc, a.gscale, from, to, lab,
+                                                                  count, scale, uc, ldu, (T*)a.du, (T*)a.dmu, row);
+    else k_rows<<<1, 1024, 0, st>>>(a.labels, 0, a.nc, a.gscale, from, to, lab, count, scale);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (e != hipSuccess) return e;
   const int* cnt = grad ? count : nullptr;
   const int64_t* labels = grad ? lab : a.labels;
   int tiles = 0;  // class tiles so far
   for (int j0 = 0; j0 < a.nc && a.B; j0 += l.piece) {
     const int n = std::min(l.piece, a.nc - j0);
     const mm::Plan pl = mm::plan_rows(sizeof(T), a.B, n, a.q);
-    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, n, a.q, w + l.W, pl.tile == 1, st);
-    if (Wj.e != hipSuccess) return Wj.e;
-    typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)tiles * a.B, zl, a.B, j0};
-    const mm::Prob p{rows, Wj.p, ldr, Wj.ld, a.B, n, a.q, cnt, 1, 0, 0, 0, 0};
+    // (u is copied, if it has to be, with the first piece)
+    const mm::Operands<T> o(grad || j0 ? nullptr : a.u, a.B, uc, W + (size_t)j0 * a.q, n, w + l.W, a.q, pl.tile == 1, st);
+    if (o.e != hipSuccess) return o.e;
+    if (j0 == 0) {
+      rows = grad ? uc : o.p[0];
+      ldr = grad ? ldu : o.ld[0];
+    }
+    typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)tiles * a.B, zl, a.B, j0, z, ldp};
+    const mm::Prob p{rows, o.p[1], ldr, o.ld[1], a.B, n, a.q, cnt, 1, 0, 0, 0, 0};
     if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, pl, split, st)) != hipSuccess) return e;
     tiles += pl.tn;
   }
+  // few rows and tiles: one workgroup joins them all and takes the mean
+  const bool small = a.B <= 64 && (long)a.B * tiles <= 4096;
   if (a.B) {
-    const int per = a.B >= 2048 ? 16 : 2;
-    k_lse<<<(unsigned)mm::ceil_div(a.B, per), 256, 0, st>>>(part, tiles, a.B, labels, a.nc, zl, cnt, a.B,
-                                                            grad ? from : nullptr, grad ? lse : nullptr, row, per);
+    int per = a.B >= 2048 ? 16 : 2;
+    if (small)
+      while (per < a.B) per *= 2;
+    k_lse<<<(unsigned)mm::ceil_div(a.B, per), 256, 0, st>>>(part, tiles, a.B, labels, a.nc, zl, cnt, a.B, grad ? from : nullptr,
+                                                            grad ? lse : nullptr, row, per, small ? a.J : nullptr);
   }
-  k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
+  if (!a.B || !small) k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
   if ((e = hipGetLastError()) != hipSuccess || !grad) return e;
   for (int j0 = 0; j0 < a.nc; j0 += l.piece) {
-    const int n = std::min(l.piece, a.nc - j0), ldp = mm::padded(sizeof(T), n);
-    const mm::Operand<T> Wj(W + (size_t)j0 * a.q, a.B ? n : 0, a.q, w + l.W, false, st);
-    if (Wj.e != hipSuccess) return Wj.e;
-    if (a.B) {
-      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, ldp, a.dmu ? col : nullptr, n, j0};
+    const int n = std::min(l.piece, a.nc - j0);
+    // (the weights' copy of a single piece is still there; of one row's product there was none)
+    const bool again = a.B && (l.piece < a.nc || a.B == 1);
+    const mm::Operands<T> o(nullptr, 0, nullptr, W + (size_t)j0 * a.q, again ? n : 0, w + l.W, a.q, false, st);
+    if (o.e != hipSuccess) return o.e;
+    T* dmu = a.dmu ? (T*)a.dmu + j0 : nullptr;
+    int col_rows = 0, col_step = 1;  // column partials, and the rows of one
+    if (a.B && z) {
+      col_rows = mm::ceil_div(a.B, PROB_ROWS), col_step = PROB_ROWS;
+      const bool own = col_rows == 1;
+      k_prob<T><<<dim3((unsigned)col_rows, (unsigned)mm::ceil_div(ldp, 1024)), 256, 0, st>>>(
+          z, lse, lab, count, n, ldp, P, dmu ? col : nullptr, own ? dmu : nullptr, scale);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else if (a.B) {
       const mm::Plan pl = mm::plan_rows(sizeof(T), a.B, n, a.q);
-      const mm::Prob pp{uc, Wj.p, ldu, Wj.ld, a.B, n, a.q, count, 1, 0, 0, 0, 0};
+      col_rows = pl.tm, col_step = pl.tile;
+      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, mm::padded(sizeof(T), n), dmu ? col : nullptr, n,
+                                  col_rows == 1 ? dmu : nullptr, scale, j0};
+      const mm::Prob pp{uc, o.p[1], ldu, o.ld[1], a.B, n, a.q, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, pl, split, st)) != hipSuccess) return e;
-      if (a.dmu)
-        mm::k_colsum<T><<<(unsigned)mm::ceil_div(n, 64), 256, 0, st>>>(col, pl.tm, pl.tile, count, n, (T*)a.dmu + j0, 1.f, scale);
-    } else if (a.dmu) {
-      mm::k_colsum<T><<<(unsigned)mm::ceil_div(n, 64), 256, 0, st>>>(col, 0, 1, nullptr, n, (T*)a.dmu + j0, 1.f, scale);
     }
+    if (dmu && col_rows != 1)  // (a single partial's kernel has left dmu itself)
+      mm::k_colsum<T><<<(unsigned)mm::ceil_div(n, 64), 256, 0, st>>>(col, col_rows, col_step, a.B ? count : nullptr, n, dmu, 1.f, scale);
     if (a.du && a.B) {
       typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
-      const mm::Prob pd{P, Wj.p, ldp, Wj.ld, a.B, a.q, n, count, 1, 0, 0, 0, 0};
+      const mm::Prob pd{P, o.p[1], mm::padded(sizeof(T), n), o.ld[1], a.B, a.q, n, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n), split, st)) != hipSuccess)
         return e;
     }
     if (a.dW) {
       T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
-      const mm::Prob pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
+      const mm::Prob pw{P, uc, mm::padded(sizeof(T), n), ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
       e = mm::launch_mm<T, true, true, mm::EpScale<T>>(pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale},
                                                        mm::plan_of(sizeof(T), n, a.q, a.B), split, st);
       if (e != hipSuccess) return e;

@@ -282,6 +282,11 @@ struct Place {
   __device__ __forceinline__ int feature(int j, int q) const { return nw + 32 * j + 8 * q + 4 * (lane >> 5); }
 };
 
+// The LDS of an epilogue: a part per wave for a 32 x 32 block of floats in padded rows, and behind
+// them 8 bytes per row of the tile and wave column.
+constexpr int WAVE_LDS = 32 * (32 * 4 + 16);
+constexpr int epilogue_lds(int waves, int bm, int wgn) { return waves * WAVE_LDS + bm * wgn * 8; }
+
 // Workgroups go to the eight XCDs in turn, each with its own L2: an XCD takes a run of
 // tiles, ordered in groups of GROUP tile rows by all tile columns, so that neighbours in
 // time share their operands.
@@ -343,6 +348,7 @@ __global__ __launch_bounds__(S::NT) void k_mm(Prob p, typename E::Args ea) {
   typedef Stage<T, BN, KB, NT, BT> SB;
   constexpr int LOADS = SA::PER + SB::PER;
   __shared__ __attribute__((aligned(16))) unsigned char lds[NS][(BM + BN) * KB];
+  static_assert(epilogue_lds(WGM * WGN, BM, WGN) <= NS * (BM + BN) * KB, "the epilogue's LDS");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int K;
   const Place c = place<S>(p, wave, K);
@@ -522,8 +528,7 @@ struct BlockIO {
   }
 };
 
-// The LDS of an epilogue: a part per wave, as large as the largest type needs.
-constexpr int WAVE_LDS = BlockIO<float>::BYTES;
+static_assert(WAVE_LDS == BlockIO<float>::BYTES, "a wave's part of the LDS");
 __device__ __forceinline__ unsigned char* wave_lds(float* lds, const Place& c, int wgn) {
   return reinterpret_cast<unsigned char*>(lds) + (c.wm * wgn + c.wn) * WAVE_LDS;
 }
@@ -605,9 +610,9 @@ __device__ __forceinline__ float fold_columns(const f32x16& v, int lane) {
   return w[0] + __shfl_xor(w[0], 1, 64);
 }
 
-// The waves' folded sums of each block column, added in order: out[n], n = n0 ..
-template <int FN, int WGM, int WGN>
-__device__ __forceinline__ void column_sums(const float (&s)[FN], const Place& c, float* lds, float* out) {
+// The waves' folded sums of each block column, added in order: out(n, sum), n = n0 ..
+template <int FN, int WGM, int WGN, typename F>
+__device__ __forceinline__ void column_sums(const float (&s)[FN], const Place& c, float* lds, F out) {
   constexpr int BNW = 32 * FN;
   const int r = (c.lane >> 1) & 15;
   c.meet<WGM * WGN>();  // the waves' parts of the LDS are free
@@ -621,7 +626,7 @@ __device__ __forceinline__ void column_sums(const float (&s)[FN], const Place& c
     float t = 0.f;
 #pragma unroll
     for (int w = 0; w < WGM; ++w) t += lds[w * (WGN * BNW) + n];
-    if (c.n0 + n < c.lim) out[c.n0 + n] = t;
+    if (c.n0 + n < c.lim) out(c.n0 + n, t);
   }
 }
 
@@ -675,7 +680,7 @@ struct EpScale {
 template <class S, class E>
 __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int splits, typename E::Args ea) {
   constexpr int WGM = S::WGM, WGN = S::WGN, FM = S::BM / WGM / 32, FN = S::BN / WGN / 32, Q = 4 * FM * FN;
-  __shared__ __attribute__((aligned(16))) float lds[WGM * WGN * WAVE_LDS / 4];  // as much as an epilogue uses
+  __shared__ __attribute__((aligned(16))) float lds[epilogue_lds(WGM * WGN, S::BM, WGN) / 4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int K;
   const Place c = place<S>(p, wave, K);
@@ -720,7 +725,7 @@ template <typename T, int NF, class E>
 __global__ __launch_bounds__(32 * NF) void k_one(Prob p, typename E::Args ea) {
   constexpr int V = 16 / (int)sizeof(T), RUN = 64 * V, R = 2, U = 4;
   typedef typename GVec<T, V>::type GChunk;
-  __shared__ __attribute__((aligned(16))) float lds[WAVE_LDS / 4];
+  __shared__ __attribute__((aligned(16))) float lds[epilogue_lds(1, 32, 1) / 4];
   __shared__ float sums[32];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (p.count && *p.count == 0) return;
@@ -815,24 +820,28 @@ __global__ __launch_bounds__(256) void k_colsum(const float* part, int tiles, in
   out[i] = (T)((float)s * (scale ? f * scale[0] : f));
 }
 
-// Rows of `cols` values to rows of ld values, zeros behind them (ld a multiple of a chunk): a
-// copy whose rows start on 16 bytes.
+// Rows of `cols` values to rows of ld values, zeros behind them (ld a multiple of a chunk): copies of
+// two arrays whose rows then start on 16 bytes. 1 << shift threads a row.
 template <typename T>
-__global__ __launch_bounds__(256) void k_repack(const T* in, T* out, size_t rows, int cols, int ld) {
+__global__ __launch_bounds__(256) void k_repack(const T* in0, T* out0, long rows0, const T* in1, T* out1, long rows1, int cols,
+                                                int ld, int shift) {
   constexpr int V = 16 / sizeof(T);
-  const int per = ld / V;
-  for (size_t id = (size_t)blockIdx.x * 256 + threadIdx.x; id < rows * per; id += (size_t)gridDim.x * 256) {
-    const size_t r = id / per;
-    const int c = (int)(id - r * per) * V;
-    const T* p = in + r * cols + c;
-    typename GVec<T, V>::type v;
-    if (c + V <= cols) {
-      v = *reinterpret_cast<const typename GVec<T, V>::type*>(p);
-    } else {
+  const int per = ld / V, tpr = 1 << shift, t = threadIdx.x & (tpr - 1);
+  const long step = (long)gridDim.x * (256 >> shift);
+  for (long r = (long)blockIdx.x * (256 >> shift) + (threadIdx.x >> shift); r < rows0 + rows1; r += step) {
+    const T* in = r < rows0 ? in0 + r * cols : in1 + (r - rows0) * cols;
+    T* out = r < rows0 ? out0 + r * ld : out1 + (r - rows0) * ld;
+    for (int i = t; i < per; i += tpr) {
+      const int c = i * V;
+      typename GVec<T, V>::type v;
+      if (c + V <= cols) {
+        v = *reinterpret_cast<const typename GVec<T, V>::type*>(in + c);
+      } else {
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = c + k < cols ? p[k] : (T)0.f;
+        for (int k = 0; k < V; ++k) v[k] = c + k < cols ? in[c + k] : (T)0.f;
+      }
+      *reinterpret_cast<typename GVec<T, V>::type*>(out + c) = v;
     }
-    *reinterpret_cast<typename GVec<T, V>::type*>(out + r * ld + c) = v;
   }
 }
 
@@ -843,23 +852,38 @@ inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 // The leading dimension of a row of n values that starts on 16 bytes.
 inline int padded(size_t esz, int n) { return ceil_div(n, 16 / (int)esz) * (16 / (int)esz); }
 
-// An operand as the products need it: the caller's array where its rows start on 16 bytes,
-// else a copy in the workspace.
+// Two operands of rows of `cols` values as the products need them: the caller's arrays where their
+// rows start on 16 bytes, else copies in the workspace (one launch for both).
 template <typename T>
-struct Operand {
-  const T* p;
-  long ld;
-  hipError_t e;
+struct Operands {
+  const T* p[2];
+  long ld[2];
+  hipError_t e = hipSuccess;
   // as_is: any alignment will do
-  Operand(const void* in, size_t rows, int cols, void* copy, bool as_is, hipStream_t st)
-      : p(static_cast<const T*>(in)), ld(cols), e(hipSuccess) {
-    if (as_is || (cols * sizeof(T) % 16 == 0 && (uintptr_t)in % 16 == 0)) return;
-    ld = padded(sizeof(T), cols);
-    p = static_cast<const T*>(copy);
-    const size_t n = rows * (ld * sizeof(T) / 16);
-    if (n == 0) return;
-    k_repack<T><<<(unsigned)std::min<size_t>((n + 255) / 256, 1u << 20), 256, 0, st>>>(
-        static_cast<const T*>(in), static_cast<T*>(copy), rows, cols, (int)ld);
+  Operands(const void* in0, size_t rows0, void* copy0, const void* in1, size_t rows1, void* copy1, int cols, bool as_is,
+           hipStream_t st) {
+    const void* in[2] = {in0, in1};
+    void* copy[2] = {copy0, copy1};
+    size_t rows[2] = {rows0, rows1};
+    const int lp = padded(sizeof(T), cols);
+    for (int i = 0; i < 2; ++i) {
+      p[i] = static_cast<const T*>(in[i]);
+      ld[i] = cols;
+      if (as_is || !in[i] || (cols == lp && (uintptr_t)in[i] % 16 == 0)) {
+        rows[i] = 0;
+      } else {
+        p[i] = static_cast<const T*>(copy[i]);
+        ld[i] = lp;
+      }
+    }
+    const size_t all = rows[0] + rows[1];
+    if (all == 0) return;
+    int shift = 0;
+    while (shift < 8 && (1 << shift) < lp * (int)sizeof(T) / 16) ++shift;
+    const size_t blocks = (all + (256 >> shift) - 1) / (256 >> shift);
+    k_repack<T><<<(unsigned)std::min<size_t>(blocks, 1u << 20), 256, 0, st>>>(
+        static_cast<const T*>(in0), static_cast<T*>(copy0), (long)rows[0], static_cast<const T*>(in1), static_cast<T*>(copy1),
+        (long)rows[1], cols, lp, shift);
     e = hipGetLastError();
   }
 };

@@ -108,6 +108,7 @@ StepLayout step_layout(int dtype, int B, int ni, int no) {
 // A piece of the vocabulary holds at most PIECE_BYTES of probabilities and of (copied) weights,
 // in whole tiles of classes (at least one).
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;
+constexpr int KEEP_Q = 512;
 
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
   const size_t e = esize(dtype), ldq = mm::padded(e, q);
@@ -129,7 +130,7 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     split = std::max(split, z.part_bytes());
     if (grad) {
       split = std::max({split, mm::plan_of(e, B, q, n).part_bytes(), mm::plan_of(e, n, q, B).part_bytes()});
-      col = std::max(col, (size_t)z.tm * n * 4);
+      col = std::max(col, (size_t)std::max(z.tm, mm::ceil_div(B, 32)) * n * 4);  // (of products, or of 32 rows each)
     }
     if (l.piece == last) {
       tiles = (size_t)z.tn * (others + 1);
@@ -149,7 +150,12 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     l.count = take(4);
     l.scale = take(4);
     l.lse = take((size_t)B * 4);
-    l.P = take((size_t)B * mm::padded(e, l.piece) * e);
+    // All logits in fp32, where they are no more than a piece may take: forming P from them instead of
+    // from a second product of 2 q operations a logit (777 x 1000 x 50021 f16: see KEEP_Q)
+    const size_t logits = (size_t)B * mm::padded(e, l.piece) * 4;
+    l.keep = l.piece == nc && logits <= PIECE_BYTES && (q >= KEEP_Q || B <= 64);
+    if (l.keep) l.z = take(logits);
+    l.P = l.keep && e == 4 ? l.z : take((size_t)B * mm::padded(e, l.piece) * e);
     l.du = take(l.piece < nc ? (size_t)B * q * 4 : 0);
     l.col = take(col);
   }

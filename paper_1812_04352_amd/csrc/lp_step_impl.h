@@ -155,6 +155,8 @@ struct EpGrad {
     T* g;
     int ld;
     float* part;  // [tile rows][N]
+    T* db;        // with a single tile row: h times the sums themselves
+    float h;
     int act;
     bool blocks_of_32() const { return false; }
   };
@@ -191,7 +193,10 @@ struct EpGrad {
         col[j] = mm::fold_columns(sums, c.lane);
       }
     });
-    mm::column_sums<FN, WGM, WGN>(col, c, lds, a.part + (size_t)c.mt * c.N);
+    mm::column_sums<FN, WGM, WGN>(col, c, lds, [&](int n, float t) {
+      if (a.db) a.db[n] = (T)(a.h * t);
+      else a.part[(size_t)c.mt * c.N + n] = t;
+    });
   }
 };
 
@@ -355,12 +360,11 @@ template <typename T>
 hipError_t step_forward_t(const StepArgs& a, hipStream_t st) {
   const StepLayout l = step_layout(a.dtype, a.B, a.ni, a.no);
   char* w = static_cast<char*>(a.ws);
-  const bool one = l.z.tile == 1;
-  const mm::Operand<T> x(a.x, a.B, a.ni, w + l.x, one, st), W(a.W, a.no, a.ni, w + l.W, one, st);
-  if (x.e != hipSuccess) return x.e;
-  if (W.e != hipSuccess) return W.e;
+  const mm::Operands<T> o(a.x, a.B, w + l.x, a.W, a.no, w + l.W, a.ni, l.z.tile == 1, st);
+  if (o.e != hipSuccess) return o.e;
   typename EpStep<T>::Args e{(const T*)a.b, (const T*)a.r, (T*)a.y, a.y8, a.ye, (float)a.h, a.act};
-  return mm::launch_mm<T, false, false, EpStep<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), e, l.z, w + l.part, st);
+  return mm::launch_mm<T, false, false, EpStep<T>>(prob(o.p[0], o.ld[0], o.p[1], o.ld[1], a.B, a.no, a.ni), e, l.z,
+                                                  w + l.part, st);
 }
 
 template <typename T>
@@ -368,31 +372,32 @@ hipError_t step_backward_t(const StepArgs& a, hipStream_t st) {
   const StepLayout l = step_layout(a.dtype, a.B, a.ni, a.no);
   char* w = static_cast<char*>(a.ws);
   T* g = reinterpret_cast<T*>(w + l.g);
-  const int ldg = mm::padded(sizeof(T), a.no), ldx = mm::padded(sizeof(T), a.ni);
+  const int ldg = mm::padded(sizeof(T), a.no), ldck = mm::padded(sizeof(T), a.ni);
   float* colpart = reinterpret_cast<float*>(w + l.col);
   hipError_t e = hipSuccess;
-  if (!a.x && a.B && (e = ck_load_t<T>(a.x8, a.xe, w + l.x, a.B, a.ni, ldx, st)) != hipSuccess) return e;
-  mm::Operand<T> x(a.x ? a.x : w + l.x, a.x ? a.B : 0, a.ni, w + l.x, false, st);
-  const mm::Operand<T> W(a.W, a.no, a.ni, w + l.W, false, st);
-  if (x.e != hipSuccess) return x.e;
-  if (W.e != hipSuccess) return W.e;
+  if (!a.x && a.B && (e = ck_load_t<T>(a.x8, a.xe, w + l.x, a.B, a.ni, ldck, st)) != hipSuccess) return e;
+  const mm::Operands<T> o(a.B ? a.x : nullptr, a.B, w + l.x, a.W, a.no, w + l.W, a.ni, false, st);
+  if (o.e != hipSuccess) return o.e;
+  const T* x = a.x ? o.p[0] : reinterpret_cast<const T*>(w + l.x);
+  const long ldx = a.x ? o.ld[0] : ldck;
+  const float h = (float)a.h;
+  const bool own_db = a.B && a.db && l.z.tm == 1;  // a single tile row leaves db itself
   if (a.B) {  // (an empty batch leaves zero sums: products over no rows)
-    typename EpGrad<T>::Args eg{(const T*)a.b, (const T*)a.dy, g, ldg, colpart, a.act};
-    e = mm::launch_mm<T, false, false, EpGrad<T>>(prob(x.p, x.ld, W.p, W.ld, a.B, a.no, a.ni), eg, l.z, w + l.part, st);
+    typename EpGrad<T>::Args eg{(const T*)a.b, (const T*)a.dy, g, ldg, colpart, own_db ? (T*)a.db : nullptr, h, a.act};
+    e = mm::launch_mm<T, false, false, EpGrad<T>>(prob(x, ldx, o.p[1], o.ld[1], a.B, a.no, a.ni), eg, l.z, w + l.part, st);
     if (e != hipSuccess) return e;
   }
-  const float h = (float)a.h;
   if (a.dx && a.B) {
     typename EpDx<T>::Args ed{a.residual ? (const T*)a.dy : nullptr, (T*)a.dx, h};
-    e = mm::launch_mm<T, false, true, EpDx<T>>(prob(g, ldg, W.p, W.ld, a.B, a.ni, a.no), ed, l.zx, w + l.part, st);
+    e = mm::launch_mm<T, false, true, EpDx<T>>(prob(g, ldg, o.p[1], o.ld[1], a.B, a.ni, a.no), ed, l.zx, w + l.part, st);
     if (e != hipSuccess) return e;
   }
   if (a.dW) {
-    e = mm::launch_mm<T, true, true, mm::EpScale<T>>(prob(g, ldg, x.p, x.ld, a.no, a.ni, a.B),
+    e = mm::launch_mm<T, true, true, mm::EpScale<T>>(prob(g, ldg, x, ldx, a.no, a.ni, a.B),
                                                      typename mm::EpScale<T>::Args{(T*)a.dW, h, nullptr}, l.zw, w + l.part, st);
     if (e != hipSuccess) return e;
   }
-  if (a.db) {
+  if (a.db && !own_db) {
     mm::k_colsum<T><<<(unsigned)mm::ceil_div(a.no, 64), 256, 0, st>>>(colpart, a.B ? l.z.tm : 0, l.z.tile, nullptr, a.no,
                                                                     (T*)a.db, h, nullptr);
     e = hipGetLastError();
