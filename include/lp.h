@@ -407,9 +407,11 @@ typedef struct {
 } lp_label_head;
 
 /* Workspace bytes of lp_loss_labels, with grad != 0 when any gradient is asked
- * for; 0 for an invalid head. It holds 8 bytes per row and tile of 64 to 256
- * classes, and with gradients the probabilities of one piece of the vocabulary at
- * a time (256 MiB or 256 classes). */
+ * for; 0 for an invalid head. It holds 8 bytes per row and tile of 8 to 256
+ * classes, a copy of the weights of one piece of the vocabulary (256 MiB or 256
+ * classes; used where rows of W do not start on 16 bytes), and with gradients
+ * the probabilities of one piece (256 MiB or 256 classes) and, where all logits
+ * are no more than 256 MiB in fp32, those. */
 size_t lp_loss_labels_workspace_bytes(const lp_label_head* head, int32_t grad);
 
 /* Softmax cross-entropy of integer labels: z_k = W u_k + mu, u [B][q], W [nc][q],

@@ -279,7 +279,8 @@ struct LabelLayout {
   size_t split;                                                   // partial sums of split products
   size_t total;
   int piece;  // classes taken at a time
-  bool keep;  // the logits are kept for the gradients
+  int copied;  // and where the weights have to be copied
+  bool keep;  // the logits of a single piece are kept for the gradients
 };
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad);
 

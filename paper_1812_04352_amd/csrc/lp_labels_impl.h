@@ -406,8 +406,10 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   float* col = reinterpret_cast<float*>(w + l.col);
   void* split = w + l.split;
   hipError_t e = hipSuccess;
-  float* z = l.keep ? reinterpret_cast<float*>(w + l.z) : nullptr;
-  const int ldp = mm::padded(sizeof(T), l.piece);  // of a whole piece
+  const bool as_is = a.q % (16 / (int)sizeof(T)) == 0 && (uintptr_t)W % 16 == 0;  // the weights
+  const int piece = as_is ? l.piece : l.copied;
+  float* z = l.keep && piece == a.nc ? reinterpret_cast<float*>(w + l.z) : nullptr;
+  const int ldp = mm::padded(sizeof(T), piece);  // of a whole piece
   // rows of the products: u's own, or with gradients the labelled ones
   const T* rows = nullptr;
   long ldr = 0;
@@ -422,8 +424,8 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   const int* cnt = grad ? count : nullptr;
   const int64_t* labels = grad ? lab : a.labels;
   int tiles = 0;  // class tiles so far
-  for (int j0 = 0; j0 < a.nc && a.B; j0 += l.piece) {
-    const int n = std::min(l.piece, a.nc - j0);
+  for (int j0 = 0; j0 < a.nc && a.B; j0 += piece) {
+    const int n = std::min(piece, a.nc - j0);
     const mm::Plan pl = mm::plan_rows(sizeof(T), a.B, n, a.q);
     // (u is copied, if it has to be, with the first piece)
     const mm::Operands<T> o(grad || j0 ? nullptr : a.u, a.B, uc, W + (size_t)j0 * a.q, n, w + l.W, a.q, pl.tile == 1, st);
@@ -448,10 +450,10 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   }
   if (!a.B || !small) k_mean_loss<<<1, 1024, 0, st>>>(row, a.labels, a.B, a.nc, a.J);
   if ((e = hipGetLastError()) != hipSuccess || !grad) return e;
-  for (int j0 = 0; j0 < a.nc; j0 += l.piece) {
-    const int n = std::min(l.piece, a.nc - j0);
+  for (int j0 = 0; j0 < a.nc; j0 += piece) {
+    const int n = std::min(piece, a.nc - j0);
     // (the weights' copy of a single piece is still there; of one row's product there was none)
-    const bool again = a.B && (l.piece < a.nc || a.B == 1);
+    const bool again = a.B && (piece < a.nc || a.B == 1);
     const mm::Operands<T> o(nullptr, 0, nullptr, W + (size_t)j0 * a.q, again ? n : 0, w + l.W, a.q, false, st);
     if (o.e != hipSuccess) return o.e;
     T* dmu = a.dmu ? (T*)a.dmu + j0 : nullptr;

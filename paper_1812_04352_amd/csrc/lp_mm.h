@@ -304,6 +304,8 @@ __device__ __forceinline__ void tile_of(int id, int tm, int tn, int& mt, int& nt
 template <int BM_, int BN_, int WGM_, int WGN_, int KB_, int NS_, int GK_>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, KB = KB_, NS = NS_, GK = GK_, NT = 64 * WGM_ * WGN_;
+  // waves a SIMD has to hold: two workgroups of four waves where their LDS fits twice
+  static constexpr int WAVES = NT == 512 || 2 * NS_ * (BM_ + BN_) * KB_ <= 160 * 1024 ? 2 : 1;
   static_assert((NS & (NS - 1)) == 0, "a stage's place is its index modulo NS");
 };
 
@@ -339,7 +341,7 @@ __device__ __forceinline__ Place place(const Prob& p, int wave, int& K) {
 }
 
 template <typename T, class S, bool AT, bool BT, class E>
-__global__ __launch_bounds__(S::NT) void k_mm(Prob p, typename E::Args ea) {
+__global__ __launch_bounds__(S::NT, S::WAVES) void k_mm(Prob p, typename E::Args ea) {
   constexpr int BM = S::BM, BN = S::BN, WGM = S::WGM, WGN = S::WGN, KB = S::KB, NS = S::NS, NT = S::NT;
   constexpr int FM = BM / WGM / 32, FN = BN / WGN / 32, GK = S::GK;
   constexpr int NG = KB / (16 * (int)sizeof(T)) / GK;
@@ -538,23 +540,25 @@ __device__ __forceinline__ unsigned char* wave_lds(float* lds, const Place& c, i
 template <bool WHOLE, typename T, int FM, int FN>
 struct Rows {
   typedef BlockIO<T> IO;
+  static constexpr bool AHEAD = sizeof(T) == 2;
   const T* a;
   long ld;
   typename IO::Block next;
   __device__ __forceinline__ Rows(const T* a_, long ld_, const Place& c) : a(a_), ld(ld_) {
-    if constexpr (WHOLE) {
+    if constexpr (WHOLE && AHEAD) {
       if (a) next = IO::fetch(a, ld, c, 0, 0);
     }
   }
-  // the quads of block (i, j) (zeros without an array); requests the next block's
+  // the quads of block (i, j) (zeros without an array); requests the next block's (of floats there
+  // are too many registers in use for that)
   __device__ __forceinline__ void get(const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
     if (!a) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = 0.f;
     } else if constexpr (WHOLE) {
-      const typename IO::Block b = next;
-      if (i + 1 < FM) next = IO::fetch(a, ld, c, i + 1, j);
-      else if (j + 1 < FN) next = IO::fetch(a, ld, c, 0, j + 1);
+      const typename IO::Block b = AHEAD ? next : IO::fetch(a, ld, c, i, j);
+      if (AHEAD && i + 1 < FM) next = IO::fetch(a, ld, c, i + 1, j);
+      else if (AHEAD && j + 1 < FN) next = IO::fetch(a, ld, c, 0, j + 1);
       IO::quads(b, buf, c, v);
     } else {
       const T* row = a + (size_t)min(c.row(i), c.M - 1) * ld;
@@ -915,12 +919,14 @@ inline Plan plan_of(size_t esz, long M, long N, long K) {
   for (int s = 0; s < 3; ++s) {
     const int tile = 256 >> s;
     const long tm = ceil_div(M, tile), tn = ceil_div(N, tile);
-    const double two = us[s][1], one = tile == 256 && tm * tn > 128 ? two / 2 : us[s][0];
+    // (one tile row reads its weights once, from memory: 0.42 a stage with one workgroup on a CU)
+    const double two = us[s][1],
+                 one = tile == 256 && tm * tn > 128 ? two / 2 : tile == 64 && tm == 1 && esz == 2 ? 0.42 : us[s][0];
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (splits > 1 && (steps < 4 * splits || tile == 256)) break;  // (a split large tile would be two middle ones)
       const long n = ceil_div(tm * tn * splits, 256);
       double t = ceil_div(steps, splits) * ((n / 2) * two + (n % 2) * one);
-      if (splits > 1) t += 3.0 + 2.0 * splits * tm * tn * tile * tile * 4 / 3e6;
+      if (splits > 1) t += 3.0 + 2.0 * splits * M * tn * tile * 4 / 3e6;
       if (t < least) {
         least = t;
         best = Plan{tile, splits, (int)tm, (int)tn};

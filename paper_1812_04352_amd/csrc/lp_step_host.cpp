@@ -105,9 +105,13 @@ StepLayout step_layout(int dtype, int B, int ni, int no) {
   return l;
 }
 
-// A piece of the vocabulary holds at most PIECE_BYTES of probabilities and of (copied) weights,
-// in whole tiles of classes (at least one).
+// A piece of the vocabulary holds at most PIECE_BYTES of probabilities, and of weights where those are
+// copied (rows that do not start on 16 bytes), in whole tiles of classes (at least one).
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;
+
+// The logits are kept in fp32 where they are no more than a piece may take, and forming them twice
+// would cost more: 2 q operations a logit against 8 bytes written and read (measured at 777 rows of
+// 1000 features, 50021 classes f16: 120 us against 35).
 constexpr int KEEP_Q = 512;
 
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
@@ -119,29 +123,34 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     at += up(bytes);
     return r;
   };
-  const size_t fit = PIECE_BYTES / (std::max<size_t>(grad ? B : 0, ldq) * e) / 256 * 256;
-  l.piece = (int)std::min<size_t>(nc, std::max<size_t>(fit, 256));
-  // every piece but the last is alike
-  const int last = nc % l.piece ? nc % l.piece : l.piece, others = (nc - last) / l.piece;
+  const auto classes = [&](size_t row_bytes) {
+    const size_t fit = row_bytes ? PIECE_BYTES / row_bytes / 256 * 256 : nc;
+    return (int)std::min<size_t>(nc, std::max<size_t>(fit, 256));
+  };
+  l.piece = classes(grad ? B * e : 0);
+  l.copied = std::min(l.piece, classes(ldq * e));
   size_t tiles = 0, split = 0, col = 0;
-  for (int n : {l.piece, last}) {
-    const mm::Plan z = mm::plan_rows(e, B, n, q);
-    tiles += (size_t)z.tn * (n == last ? 1 : others);
-    split = std::max(split, z.part_bytes());
-    if (grad) {
-      split = std::max({split, mm::plan_of(e, B, q, n).part_bytes(), mm::plan_of(e, n, q, B).part_bytes()});
-      col = std::max(col, (size_t)std::max(z.tm, mm::ceil_div(B, 32)) * n * 4);  // (of products, or of 32 rows each)
+  for (int piece : {l.piece, l.copied}) {
+    // every piece but the last is alike
+    const int last = nc % piece ? nc % piece : piece, others = (nc - last) / piece;
+    size_t t = 0;
+    for (int i = 0; i < 2; ++i) {
+      const int n = i ? last : piece;
+      const mm::Plan z = mm::plan_rows(e, B, n, q);
+      t += (size_t)z.tn * (i ? 1 : others);
+      split = std::max(split, z.part_bytes());
+      if (grad) {
+        split = std::max({split, mm::plan_of(e, B, q, n).part_bytes(), mm::plan_of(e, n, q, B).part_bytes()});
+        col = std::max(col, (size_t)std::max(z.tm, mm::ceil_div(B, 32)) * n * 4);  // (of products, or of 32 rows each)
+      }
     }
-    if (l.piece == last) {
-      tiles = (size_t)z.tn * (others + 1);
-      break;
-    }
+    tiles = std::max(tiles, t);
   }
   l.part = take(tiles * B * 8);
   l.zl = take((size_t)B * 4);
   l.row = take((size_t)B * 4);
   l.u = take((size_t)B * ldq * e);
-  l.W = take((size_t)l.piece * ldq * e);
+  l.W = take((size_t)l.copied * ldq * e);
   l.split = take(split);
   if (grad) {
     l.from = take((size_t)B * 4);
@@ -150,13 +159,11 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     l.count = take(4);
     l.scale = take(4);
     l.lse = take((size_t)B * 4);
-    // All logits in fp32, where they are no more than a piece may take: forming P from them instead of
-    // from a second product of 2 q operations a logit (777 x 1000 x 50021 f16: see KEEP_Q)
     const size_t logits = (size_t)B * mm::padded(e, l.piece) * 4;
     l.keep = l.piece == nc && logits <= PIECE_BYTES && (q >= KEEP_Q || B <= 64);
     if (l.keep) l.z = take(logits);
     l.P = l.keep && e == 4 ? l.z : take((size_t)B * mm::padded(e, l.piece) * e);
-    l.du = take(l.piece < nc ? (size_t)B * q * 4 : 0);
+    l.du = take(l.copied < nc ? (size_t)B * q * 4 : 0);
     l.col = take(col);
   }
   l.total = std::max<size_t>(at, 256);
