@@ -900,7 +900,7 @@ typedef Shape<128, 128, 2, 2, 128, 4, 2> Tile128d;  // four stages, where a CU h
 typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;
 typedef Shape<256, 256, 2, 4, 128, 2, 1> Tile256f;  // float: two steps a stage
 typedef Shape<128, 128, 2, 2, 128, 2, 1> Tile128f;
-typedef Shape<64, 64, 2, 2, 128, 2, 1> Tile64f;
+typedef Shape<64, 64, 2, 2, 128, 4, 1> Tile64f;
 constexpr int STAGE_BYTES = 128;
 
 // The plan with the least estimated time, from measured times of a stage (us) with one workgroup on
