@@ -278,9 +278,9 @@ struct LabelLayout {
   size_t from, to, lab, count, scale, lse, P, du, col, z;         // gradients
   size_t split;                                                   // partial sums of split products
   size_t total;
-  int piece;  // classes taken at a time
+  int piece;   // classes taken at a time
   int copied;  // and where the weights have to be copied
-  bool keep;  // the logits of a single piece are kept for the gradients
+  bool keep;   // the logits are kept for the gradients
 };
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad);
 

@@ -4,12 +4,12 @@
 //   lse_k = log sum_j exp z_kj,  loss_k = lse_k - z_k[c_k],  J = (1/n) sum loss_k,
 //   P = softmax(z) - onehot,  du = (s/n) P W,  dW = (s/n) P^T u,  dmu = (s/n) sum_k P_k.
 // A product over all classes leaves, per tile of classes, each row's maximum and sum of exponentials
-// (8 bytes where the tile had 128 logits); they are joined in order into lse. For the gradients the
-// logits are formed a second time, a piece of the vocabulary after the other (unless the whole
-// batch's are small enough to be kept: label_layout); a piece of P is kept in the workspace in the element type (the
-// type of the next products' operands), as P times PSCALE: 2^14 for f16, whose range would
-// otherwise lose the small probabilities of a large vocabulary (the least normal value then
-// stands for 3.7e-9), a power of two that the epilogues take back exactly.
+// (8 bytes where the tile had 128 logits); they are joined in order into lse. For the gradients a
+// piece of the vocabulary is taken after the other: its logits, kept by the first product or, of
+// batches too large for that (label_layout), formed a second time, become a piece of P in the
+// workspace in the element type (the type of the next products' operands), as P times PSCALE: 2^14
+// for f16, whose range would otherwise lose the small probabilities of a large vocabulary (the least
+// normal value then stands for 3.7e-9), a power of two that the epilogues take back exactly.
 // Rows without a label take no part in the gradients, whatever they hold: the labelled rows are
 // first copied together, so a product runs over n rows.
 #pragma once
@@ -297,24 +297,25 @@ __global__ __launch_bounds__(256) void k_gather(const T* u, const int64_t* label
   for (int i = 4 * lane; i < ld; i += 256) mm::store4(uc + (size_t)r * ld, i, ld, mm::load4(u + (size_t)b * q, i, q));
 }
 
-// A piece of P (times PSCALE; zeros from class n to ld) from kept logits z (rows of ld values; of floats P
-// may be z itself), and its column sums over PROB_ROWS rows a workgroup. Four classes a thread.
+// A piece of P (times PSCALE; rows of ldp values, zeros from class n to `to`, a multiple of four) from
+// its kept logits z (rows of ldz values; of floats P may be z itself), and its column sums over
+// PROB_ROWS rows a workgroup. Four classes a thread.
 constexpr int PROB_ROWS = 32;
 template <typename T>
-__global__ __launch_bounds__(256) void k_prob(const float* z, const float* lse, const int64_t* lab, const int* count, int n,
-                                              int ld, T* P, float* part, T* dmu, const float* scale) {
+__global__ __launch_bounds__(256) void k_prob(const float* z, int ldz, const float* lse, const int64_t* lab, const int* count,
+                                              int j0, int n, int to, T* P, int ldp, float* part, T* dmu, const float* scale) {
   const int c = (blockIdx.y * 256 + threadIdx.x) * 4, m0 = blockIdx.x * PROB_ROWS, m1 = min(m0 + PROB_ROWS, *count);
-  if (c >= ld || m0 >= m1) return;
+  if (c >= to || m0 >= m1) return;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int m = m0; m < m1; ++m) {
-    f32x4 v = mm::load4<true>(z + (size_t)m * ld, c, ld);
+    f32x4 v = mm::load4<true>(z + (size_t)m * ldz, c, to);
     const float l = lse[m];
-    const int64_t at = lab[m] - c;
+    const int64_t at = lab[m] - j0 - c;
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = c + k < n ? exp_of(v[k] - l) - (at == k ? 1.f : 0.f) : 0.f;
     sum += v;
-    mm::store4<true>(P + (size_t)m * ld, c, ld, v * PSCALE<T>);
+    mm::store4<true>(P + (size_t)m * ldp, c, to, v * PSCALE<T>);
   }
   if (dmu) mm::store4(dmu, c, n, sum * scale[0]);
   else if (part) mm::store4(part + (size_t)blockIdx.x * n, c, n, sum);
@@ -408,8 +409,8 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
   hipError_t e = hipSuccess;
   const bool as_is = a.q % (16 / (int)sizeof(T)) == 0 && (uintptr_t)W % 16 == 0;  // the weights
   const int piece = as_is ? l.piece : l.copied;
-  float* z = l.keep && piece == a.nc ? reinterpret_cast<float*>(w + l.z) : nullptr;
-  const int ldp = mm::padded(sizeof(T), piece);  // of a whole piece
+  float* z = l.keep ? reinterpret_cast<float*>(w + l.z) : nullptr;
+  const int ldz = mm::padded(sizeof(T), a.nc);
   // rows of the products: u's own, or with gradients the labelled ones
   const T* rows = nullptr;
   long ldr = 0;
@@ -434,7 +435,7 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
       rows = grad ? uc : o.p[0];
       ldr = grad ? ldu : o.ld[0];
     }
-    typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)tiles * a.B, zl, a.B, j0, z, ldp};
+    typename EpLse<T>::Args ea{mu ? mu + j0 : nullptr, labels, part + (size_t)tiles * a.B, zl, a.B, j0, z ? z + j0 : nullptr, ldz};
     const mm::Prob p{rows, o.p[1], ldr, o.ld[1], a.B, n, a.q, cnt, 1, 0, 0, 0, 0};
     if ((e = mm::launch_mm<T, false, false, EpLse<T>>(p, ea, pl, split, st)) != hipSuccess) return e;
     tiles += pl.tn;
@@ -458,16 +459,18 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
     if (o.e != hipSuccess) return o.e;
     T* dmu = a.dmu ? (T*)a.dmu + j0 : nullptr;
     int col_rows = 0, col_step = 1;  // column partials, and the rows of one
+    const int wide = mm::padded(sizeof(T), n), ldp = z && sizeof(T) == 4 ? ldz : wide;
+    if (z && sizeof(T) == 4) P = reinterpret_cast<T*>(z + j0);  // (in place)
     if (a.B && z) {
       col_rows = mm::ceil_div(a.B, PROB_ROWS), col_step = PROB_ROWS;
       const bool own = col_rows == 1;
-      k_prob<T><<<dim3((unsigned)col_rows, (unsigned)mm::ceil_div(ldp, 1024)), 256, 0, st>>>(
-          z, lse, lab, count, n, ldp, P, dmu ? col : nullptr, own ? dmu : nullptr, scale);
+      k_prob<T><<<dim3((unsigned)col_rows, (unsigned)mm::ceil_div(wide, 1024)), 256, 0, st>>>(
+          z + j0, ldz, lse, lab, count, j0, n, wide, P, ldp, dmu ? col : nullptr, own ? dmu : nullptr, scale);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     } else if (a.B) {
       const mm::Plan pl = mm::plan_rows(sizeof(T), a.B, n, a.q);
       col_rows = pl.tm, col_step = pl.tile;
-      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, mm::padded(sizeof(T), n), dmu ? col : nullptr, n,
+      typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, ldp, dmu ? col : nullptr, n,
                                   col_rows == 1 ? dmu : nullptr, scale, j0};
       const mm::Prob pp{uc, o.p[1], ldu, o.ld[1], a.B, n, a.q, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, pl, split, st)) != hipSuccess) return e;
@@ -476,13 +479,13 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
       mm::k_colsum<T><<<(unsigned)mm::ceil_div(n, 64), 256, 0, st>>>(col, col_rows, col_step, a.B ? count : nullptr, n, dmu, 1.f, scale);
     if (a.du && a.B) {
       typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
-      const mm::Prob pd{P, o.p[1], mm::padded(sizeof(T), n), o.ld[1], a.B, a.q, n, count, 1, 0, 0, 0, 0};
+      const mm::Prob pd{P, o.p[1], ldp, o.ld[1], a.B, a.q, n, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n), split, st)) != hipSuccess)
         return e;
     }
     if (a.dW) {
       T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
-      const mm::Prob pw{P, uc, mm::padded(sizeof(T), n), ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
+      const mm::Prob pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
       e = mm::launch_mm<T, true, true, mm::EpScale<T>>(pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale},
                                                        mm::plan_of(sizeof(T), n, a.q, a.B), split, st);
       if (e != hipSuccess) return e;

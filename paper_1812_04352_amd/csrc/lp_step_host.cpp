@@ -109,10 +109,11 @@ StepLayout step_layout(int dtype, int B, int ni, int no) {
 // copied (rows that do not start on 16 bytes), in whole tiles of classes (at least one).
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;
 
-// The logits are kept in fp32 where they are no more than a piece may take, and forming them twice
-// would cost more: 2 q operations a logit against 8 bytes written and read (measured at 777 rows of
-// 1000 features, 50021 classes f16: 120 us against 35).
-constexpr int KEEP_Q = 512;
+// The logits are kept in fp32 for the gradients where they are no more than KEEP_BYTES, a 70th of the
+// card's memory: writing and reading them took less than forming them twice at every size tried (520
+// rows, 50021 classes, f16: 143 us against 170 with 128 features, 395 against 458 with 1000; f32 285
+// against 344 and 1132 against 1469; 16 rows of 1024 features, 100000 classes: 186 against 225).
+constexpr size_t KEEP_BYTES = (size_t)4 << 30;
 
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
   const size_t e = esize(dtype), ldq = mm::padded(e, q);
@@ -159,8 +160,9 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     l.count = take(4);
     l.scale = take(4);
     l.lse = take((size_t)B * 4);
-    const size_t logits = (size_t)B * mm::padded(e, l.piece) * 4;
-    l.keep = l.piece == nc && logits <= PIECE_BYTES && (q >= KEEP_Q || B <= 64);
+    const size_t logits = (size_t)B * mm::padded(e, nc) * 4;
+    // (of floats the kept logits become P in place: a tile's rows, up to 256, lie within 2 GiB of each other)
+    l.keep = logits <= KEEP_BYTES && (size_t)std::min(B, 256) * mm::padded(e, nc) * 4 < (size_t)1 << 31;
     if (l.keep) l.z = take(logits);
     l.P = l.keep && e == 4 ? l.z : take((size_t)B * mm::padded(e, l.piece) * e);
     l.du = take(l.copied < nc ? (size_t)B * q * 4 : 0);
