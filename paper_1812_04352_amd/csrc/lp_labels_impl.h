@@ -44,6 +44,7 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
 // Per row: maximum and sum of exponentials over the tile's classes, and the label's logit.
 template <typename T>
 struct EpLse {
+  static constexpr bool ONE = true;
   struct Args {
     const T* mu;            // nullable, of the product's first class
     const int64_t* labels;  // of D's rows
@@ -119,6 +120,7 @@ struct EpLse {
 // sums over the tile's rows (fp32, before rounding).
 template <typename T>
 struct EpProb {
+  static constexpr bool ONE = false;
   struct Args {
     const T* mu;            // nullable, of the piece
     const int64_t* labels;  // of D's rows
@@ -130,7 +132,6 @@ struct EpProb {
     T* dmu;                 // with a single tile row: scale[0] times the sums themselves (nullable)
     const float* scale;
     int j0;                 // first class of the piece
-    bool blocks_of_32() const { return false; }
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
@@ -184,6 +185,7 @@ struct EpProb {
 // rounded and written to the row that the labelled row came from.
 template <typename T>
 struct EpDu {
+  static constexpr bool ONE = false;
   struct Args {
     float* acc32;      // [rows][N]: sum over the pieces
     T* du;
@@ -468,7 +470,7 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
           z + j0, ldz, lse, lab, count, j0, n, wide, P, ldp, dmu ? col : nullptr, own ? dmu : nullptr, scale);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     } else if (a.B) {
-      const mm::Plan pl = mm::plan_rows(sizeof(T), a.B, n, a.q);
+      const mm::Plan pl = mm::plan_of(sizeof(T), a.B, n, a.q);  // (one row's logits are always kept)
       col_rows = pl.tm, col_step = pl.tile;
       typename EpProb<T>::Args ep{mu ? mu + j0 : nullptr, lab, lse, P, ldp, dmu ? col : nullptr, n,
                                   col_rows == 1 ? dmu : nullptr, scale, j0};

@@ -637,6 +637,7 @@ __device__ __forceinline__ void column_sums(const float (&s)[FN], const Place& c
 // The partial sums of a split contraction as the lanes hold them; k_finish adds them in the order
 // of the splits and runs the product's epilogue.
 struct EpRaw {
+  static constexpr bool ONE = false;
   struct Args {
     f32x4* part;  // [splits][tiles][quads of a lane][threads]
   };
@@ -658,11 +659,11 @@ struct EpRaw {
 // out = f * scale[0] * D (scale: device value, nullable)
 template <typename T>
 struct EpScale {
+  static constexpr bool ONE = false;
   struct Args {
     T* out;  // [M][N]
     float f;
     const float* scale;
-    bool blocks_of_32() const { return false; }
   };
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
@@ -912,7 +913,7 @@ constexpr int STAGE_BYTES = 128;
 // 2048 160 by 128; 8192 x 4096 x 4096 1108 by 256 (128: 1272, 64: 1670).
 inline Plan plan_of(size_t esz, long M, long N, long K) {
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
-  const double stage[2][3][2] = {{{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{3.95, 8.7}, {1.5, 2.5}, {0.72, 1.0}}};
+  const double stage[2][3][2] = {{{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{4.1, 8.7}, {1.8, 2.7}, {0.75, 1.15}}};
   const auto& us = stage[esz == 4];
   Plan best{};
   double least = 1e30;
@@ -958,10 +959,10 @@ hipError_t launch_shape(Prob p, const typename E::Args& ea, const Plan& pl, void
   return hipGetLastError();
 }
 
-// part: pl.part_bytes() of workspace
+// part: pl.part_bytes() of workspace. Epilogues of products that one row may have (ONE) come in one-row kernels too.
 template <typename T, bool AT, bool BT, class E>
 hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, void* part, hipStream_t st) {
-  if constexpr (!AT && !BT) {
+  if constexpr (!AT && !BT && E::ONE) {
     if (pl.tile == 1) {
       if (ea.blocks_of_32()) k_one<T, 32, E><<<(unsigned)ceil_div(p.N, 32), 1024, 0, st>>>(p, ea);
       else if (one_features(p.N) == 8) k_one<T, 8, E><<<(unsigned)pl.tn, 256, 0, st>>>(p, ea);

@@ -87,6 +87,7 @@ __device__ __forceinline__ void with_act(int act, F f) {
 // checkpoint block, held by lanes l and l ^ 32; the checkpoint is that of y as stored.
 template <typename T>
 struct EpStep {
+  static constexpr bool ONE = true;
   struct Args {
     const T* b;
     const T* r;  // nullable
@@ -149,6 +150,7 @@ struct EpStep {
 // columns over the tile's rows (fp32, before rounding)
 template <typename T>
 struct EpGrad {
+  static constexpr bool ONE = true;
   struct Args {
     const T* b;
     const T* dy;
@@ -203,6 +205,7 @@ struct EpGrad {
 // dx = h D (+ dy)
 template <typename T>
 struct EpDx {
+  static constexpr bool ONE = false;
   struct Args {
     const T* dy;  // nullable
     T* dx;

@@ -258,3 +258,74 @@ def test_gradients_against_differences():
     terms = [a.double().cpu() * d for a, d in zip(got[2:], dirs)]
     ana, mag = sum(float(t.sum()) for t in terms), sum(float(t.abs().sum()) for t in terms)
     assert abs(num - ana) <= 1e-6 * mag + 1e-8
+
+
+def on_gpu(dtype, u, W, mu, lab):
+    """J, row, du, dW, dmu in 64 bits on the GPU, a slice of the rows at a time."""
+    B, q = u.shape
+    on = lab >= 0
+    n = max(1, int(on.sum()))
+    row, du = torch.zeros(B, dtype=torch.float64, device="cuda"), torch.zeros((B, q), dtype=torch.float64, device="cuda")
+    dW = torch.zeros(W.shape, dtype=torch.float64, device="cuda")
+    dmu = torch.zeros(W.shape[0], dtype=torch.float64, device="cuda")
+    Wd = W.double()
+    per = max(1, 2 ** 28 // W.shape[0])
+    for k in range(0, B, per):
+        at = torch.nonzero(on[k:k + per]).flatten() + k
+        if not len(at):
+            continue
+        z = u[at].double() @ Wd.t() + (0 if mu is None else mu.double())
+        lse = torch.logsumexp(z, 1)
+        i = torch.arange(len(at), device="cuda")
+        row[at] = lse - z[i, lab[at]]
+        P = torch.exp(z - lse[:, None])
+        P[i, lab[at]] -= 1
+        du[at] = P @ Wd / n
+        dW += P.t() @ u[at].double() / n
+        dmu += P.sum(0) / n
+        del z, P
+    return row.sum().reshape(1) / n, row, du, dW, dmu
+
+
+# norms, as in the test of several pieces: half a step of P and of the result, and fp32 sums; and half
+# of the type's smallest step for each value (a mean over 7500 rows of probabilities near 1 / 131000
+# leaves dW of f16 near 3e-6, below its normal range of 6.1e-5: each value may be off by 2^-25 = 3e-8,
+# together 2^-25 sqrt(numel), which is 4e-4 of that norm)
+NORMS = {"bf16": 2 ** -8, "f16": 2 ** -11, "f32": 2 ** -18}
+
+
+def near(dtype, got, refs):
+    for name, a, r in zip(("J", "row", "du", "dW", "dmu"), got, refs):
+        d, n = float((a.double().reshape(-1) - r.reshape(-1)).norm()), float(r.norm())
+        lim = 2 ** -18 * n if name in ("J", "row") else NORMS[dtype] * n + T.tiny(dtype) * math.sqrt(r.numel())
+        assert d <= lim, (name, d, n)
+
+
+@pytest.mark.parametrize("dtype,B,nc", [("f16", 8300, 131000), ("f32", 8300, 131000), ("bf16", 140, 3900001),
+                                        ("f32", 140, 3900001)])
+def test_logits_formed_a_second_time(dtype, B, nc):
+    """Batches whose logits are too many to be kept (over 4 GiB in fp32), or too far apart."""
+    u, W, mu, lab = (t.cuda() for t in inputs(12, dtype, B, 8, nc, ignored=0.1))
+    hd = L.label_head(dtype, B, 8, nc)
+    # (without them: the probabilities of a piece, and for each row and tile 8 bytes)
+    assert L.lp_loss_labels_workspace_bytes(hd, True) < B * nc * 4
+    near(dtype, run(dtype, u, W, mu, lab, gscale=1.0), on_gpu(dtype, u, W, mu, lab))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B", [1, 3, 70])
+def test_weights_copied_in_pieces(dtype, B):
+    """Rows of W that do not start on 16 bytes, and more of them than are copied at a time."""
+    q, nc = 4097, 40000
+    u, W, mu, lab = (t.cuda() for t in inputs(14, dtype, B, q, nc))
+    assert nc * q * u.element_size() > 256 << 20
+    near(dtype, run(dtype, u, W, mu, lab), on_gpu(dtype, u, W, mu, lab))
+    near(dtype, run(dtype, u, W, mu, lab, want=(False,) * 3)[:2], on_gpu(dtype, u, W, mu, lab)[:2])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_many_rows(dtype):
+    """More rows than a workgroup lists by itself, of one piece."""
+    B, q, nc = 5003, 24, 300
+    u, W, mu, lab = inputs(15, dtype, B, q, nc, ignored=0.3)
+    compare(run(dtype, *[T.gpu(t) for t in (u, W, mu, lab)]), T.loss(u, W, mu, lab, 1.0, dtype))

@@ -316,3 +316,39 @@ def test_gradients_against_differences():
         # smoothed ReLU's kinks in its slope
         mag = float((dx * dirs[0]).abs().sum() + (dW * dirs[1]).abs().sum() + (db * dirs[2]).abs().sum())
         assert abs(num - ana) <= 1e-6 * mag + 1e-4 * abs(num), (act, num, ana)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("B,ni,no", [(4090, 605, 4090), (4090, 4090, 104), (104, 4090, 4090), (4096, 512, 4096)])
+def test_large_tiles(dtype, B, ni, no):
+    """Results of enough values for the largest tiles, ragged and whole ones, in each of the three
+    products (on the GPU in 64 bits)."""
+    x, W, b, r, dy = (t.cuda() for t in inputs(37, dtype, B, ni, no, "other"))
+    s = T.Step(dtype, "tanh", B, ni, no, 0.5)
+    y = s.forward(x, W, b, r)
+    T.check(y, *T.forward(x, W, b, r, "tanh", 0.5, dtype), "y")
+    got = s.backward(x, W, b, dy, ni == no)
+    for name, a, (v, e) in zip(("dx", "dW", "db"), got, T.backward(x, W, b, dy, "tanh", 0.5, ni == no, dtype)):
+        T.check(a, v, e, name)
+
+
+@pytest.mark.parametrize("B", [1, 70, 300])
+def test_floats_beyond_the_largest_bf16_value(B):
+    """Operands between the largest bf16 value and the largest float take part exactly, and sums that
+    overflow are infinite with their sign, both without touching the other results."""
+    ni, no = 96, 72
+    x, W, b, _, dy = inputs(41, "f32", B, ni, no, "none")
+    W[:, 5] *= 2.0 ** -100
+    x[0, 5] = 3.4e38
+    x[B // 2, 5] = -torch.finfo(torch.float32).max
+    s = T.Step("f32", "identity", B, ni, no, 1.0)
+    y = s.forward(T.gpu(x), T.gpu(W), T.gpu(b), None)
+    T.check(y, *T.forward(x, W, b, None, "identity", 1.0, "f32"), "y")
+    x[B - 1, 7] = 3e38
+    W[3, 7], W[4, 7] = 100.0, -100.0
+    y = s.forward(T.gpu(x), T.gpu(W), T.gpu(b), None).cpu()
+    assert y[B - 1, 3] == math.inf and y[B - 1, 4] == -math.inf
+    ref, bound = T.forward(x, W, b, None, "identity", 1.0, "f32")
+    fits = ref.abs() < torch.finfo(torch.float32).max / 2  # (sums near the largest float may overflow on the way)
+    assert int((~fits).sum()) < no
+    T.check(y[fits], ref[fits], bound[fits], "the others")
