@@ -340,8 +340,8 @@ int32_t lp_accuracy(const lp_problem* prob, int32_t nc, const void* uN, const vo
 
 /* ---- layer steps of any width, 8-bit checkpoints, heads over large vocabularies ----
  * The layer of Section 2.2 for wide networks in 16-bit or fp32 types, one step per
- * call, the network head for integer labels over a vocabulary whose logits are
- * never stored, and activations kept in 8 bits for the way back. Arrays of
+ * call, the network head for integer labels over a vocabulary of any size, a
+ * piece of it at a time, and activations kept in 8 bits for the way back. Arrays of
  * floating-point values have the call's dtype (LP_F32, LP_BF16 or LP_F16; LP_F64
  * returns LP_EUNSUPPORTED) unless stated; every sum is held in fp32 or more and
  * rounded to the dtype once. Products run on the matrix cores. No call waits for
@@ -362,7 +362,9 @@ typedef struct {
   double h;              /* factor of the activation, finite */
 } lp_step;
 
-/* Workspace bytes of lp_step_forward and lp_step_backward; 0 for an invalid step. */
+/* Workspace bytes of lp_step_forward and lp_step_backward; 0 for an invalid step. It
+ * holds g, copies of x and W (used where their rows do not start on 16 bytes, and
+ * for an x read back from its checkpoint) and the partial sums of split products. */
 size_t lp_step_workspace_bytes(const lp_step* step);
 
 /* The step. b, r nullable. r may be x (the residual layer of Section 2.2, ni = no),
@@ -410,8 +412,8 @@ typedef struct {
  * for; 0 for an invalid head. It holds 8 bytes per row and tile of 8 to 256
  * classes, a copy of the weights of one piece of the vocabulary (256 MiB or 256
  * classes; used where rows of W do not start on 16 bytes), and with gradients
- * the probabilities of one piece (256 MiB or 256 classes) and, where all logits
- * are no more than 256 MiB in fp32, those. */
+ * the probabilities of one piece (256 MiB or 256 classes) and, where they take no
+ * more than 4 GiB in fp32, all logits (else the gradients form them again). */
 size_t lp_loss_labels_workspace_bytes(const lp_label_head* head, int32_t grad);
 
 /* Softmax cross-entropy of integer labels: z_k = W u_k + mu, u [B][q], W [nc][q],

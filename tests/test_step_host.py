@@ -140,3 +140,43 @@ def test_binding_refuses_tensors():
         L.lp_checkpoint_store(torch.zeros(4, dtype=torch.int32), None, None)
     with pytest.raises(KeyError):
         L.step("f8", "tanh", 1, 1, 1)
+
+
+def test_binding_refuses_tensors_of_another_device(monkeypatch):
+    """Every tensor of a call is on the current device, whose stream the call uses."""
+    class Elsewhere:
+        dtype, is_cuda, device = torch.bfloat16, True, "cuda:1"
+
+        def get_device(self):
+            return 1
+
+        def is_contiguous(self):
+            return True
+
+        def numel(self):
+            return 128
+
+        def element_size(self):
+            return 2
+
+        def data_ptr(self):
+            return 0
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    t = Elsewhere()
+    with pytest.raises(ValueError, match="current device is cuda:0"):
+        L._dev(t, 128, "x", torch.bfloat16, 0)
+    with pytest.raises(ValueError, match="workspace is on cuda:1"):
+        L._dev_ws(t, 0)
+    with pytest.raises(ValueError, match="cuda:1"):
+        L.lp_step_forward(st(), t, t, None, None, t, t)
+
+
+def test_loss_workspace_with_and_without_the_logits():
+    """Logits of up to 4 GiB in fp32 are kept for the gradients; losses alone keep none."""
+    kept, again, alone = (L.lp_loss_labels_workspace_bytes(L.label_head("bf16", B, 64, 2 ** 17), g)
+                          for B, g in ((8192, True), (8193, True), (8192, False)))
+    assert 2 ** 32 < kept < 2 ** 32 + 2 ** 31
+    assert again < 2 ** 31 and alone < 2 ** 29
+    # (too far apart for 32-bit offsets within a tile of rows)
+    assert L.lp_loss_labels_workspace_bytes(L.label_head("f32", 256, 8, 2 ** 21), True) < 2 ** 30 + 2 ** 28
