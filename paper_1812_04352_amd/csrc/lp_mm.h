@@ -898,8 +898,8 @@ struct Operands {
 typedef Shape<256, 256, 2, 4, 128, 2, 2> Tile256;
 typedef Shape<128, 128, 2, 2, 128, 2, 2> Tile128;
 typedef Shape<128, 128, 2, 2, 128, 4, 2> Tile128d;  // four stages, where a CU holds one workgroup at most
-typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;
-typedef Shape<256, 256, 2, 4, 128, 2, 1> Tile256f;  // float: two steps a stage
+typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;  // (eight stages are no faster: 12.7 to 13.9 us on 24 x 8192 x 2048)
+typedef Shape<256, 256, 2, 4, 128, 2, 1> Tile256f;  // float: two steps a stage; bound by the split's vector instructions
 typedef Shape<128, 128, 2, 2, 128, 2, 1> Tile128f;
 typedef Shape<64, 64, 2, 2, 128, 4, 1> Tile64f;
 constexpr int STAGE_BYTES = 128;
@@ -909,8 +909,9 @@ constexpr int STAGE_BYTES = 128;
 // partial sums (3 TB/s both ways) and takes a second launch (3 us). Measured against the other choices,
 // bf16: 1024 x 1024 x 4096 21 us by tiles of 64 (128: 34, 256: 89); 2048 x 2048 x 4096 39 by 128 with four
 // stages (two: 45, 64: 55, 256: 88); 4096 x 2048 x 4096 63 us by 128 with two stages (four: 75); 8192 x 4096 x
-// 4096 230 us by 256 (128: 256, 64: over 370). float: 1024 x 1024 x 4096 90 us by 64 (128: 185); 4096 x 2048 x
-// 2048 160 by 128; 8192 x 4096 x 4096 1108 by 256 (128: 1272, 64: 1670).
+// 4096 230 us by 256 (128: 256, 64: over 370). float: 4096 x 1024 x 1024 60 us by 128 (64: 74, 256: 134);
+// 1024 x 1024 x 4096 (columns) 68 by 128 in four splits (64 in two: 77, 256: 501); 4096 x 4096 x 4096 545 by 256
+// (128: 600 to 694, 64: 1008).
 inline Plan plan_of(size_t esz, long M, long N, long K) {
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
   const double stage[2][3][2] = {{{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{4.1, 8.7}, {1.8, 2.7}, {0.75, 1.15}}};

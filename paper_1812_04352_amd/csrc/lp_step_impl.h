@@ -6,6 +6,10 @@
 //                                          of g, so that a small step does not push it out of the
 //                                          range of f16)
 //              dx = h g W (+ dy),  dW = h g^T x,  db = h sum g (from g before its rounding)
+// Bound by the products (2 B ni no operations each): 8192 x 4096 -> 4096 bf16 forward with its
+// checkpoint 275 us (1.0 PFLOP/s), back 286 + 250 + 223 us, of which the epilogue of g takes some 50:
+// the largest tiles fill a CU, so nothing runs beside an epilogue. Small batches are bound by reading W
+// (one row of 4096 x 4096: 6.5 us, 5.2 TB/s) and by launches.
 #pragma once
 
 #include <type_traits>
