@@ -412,8 +412,9 @@ typedef struct {
  * for; 0 for an invalid head. It holds 8 bytes per row and tile of 8 to 256
  * classes, a copy of the weights of one piece of the vocabulary (256 MiB or 256
  * classes; used where rows of W do not start on 16 bytes), and with gradients
- * the probabilities of one piece (256 MiB or 256 classes) and, where they take no
- * more than 4 GiB in fp32, all logits (else the gradients form them again). */
+ * the probabilities of one piece (256 MiB or 256 classes) and, where that is
+ * faster and they take no more than 4 GiB in fp32, all logits (else the gradients
+ * form them again). */
 size_t lp_loss_labels_workspace_bytes(const lp_label_head* head, int32_t grad);
 
 /* Softmax cross-entropy of integer labels: z_k = W u_k + mu, u [B][q], W [nc][q],

@@ -854,8 +854,12 @@ __global__ __launch_bounds__(256) void k_repack(const T* in0, T* out0, long rows
 
 inline int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
-// The leading dimension of a row of n values that starts on 16 bytes.
-inline int padded(size_t esz, int n) { return ceil_div(n, 16 / (int)esz) * (16 / (int)esz); }
+// The leading dimension of the workspace's rows of n values: they start on 16 bytes, long ones on 128, a
+// cache line and a stage's row (9990 x 3136 x 6849 bf16: 405 us with rows of 6912 values, 533 with 6856).
+inline int padded(size_t esz, int n) {
+  const int unit = (n * (long)esz > 1024 ? 128 : 16) / (int)esz;
+  return ceil_div(n, unit) * unit;
+}
 
 // Two operands of rows of `cols` values as the products need them: the caller's arrays where their
 // rows start on 16 bytes, else copies in the workspace (one launch for both).
@@ -874,7 +878,7 @@ struct Operands {
     for (int i = 0; i < 2; ++i) {
       p[i] = static_cast<const T*>(in[i]);
       ld[i] = cols;
-      if (as_is || !in[i] || (cols == lp && (uintptr_t)in[i] % 16 == 0)) {
+      if (as_is || !in[i] || (cols % (16 / (int)sizeof(T)) == 0 && (uintptr_t)in[i] % 16 == 0)) {
         rows[i] = 0;
       } else {
         p[i] = static_cast<const T*>(copy[i]);

@@ -109,11 +109,17 @@ StepLayout step_layout(int dtype, int B, int ni, int no) {
 // copied (rows that do not start on 16 bytes), in whole tiles of classes (at least one).
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;
 
-// The logits are kept in fp32 for the gradients where they are no more than KEEP_BYTES, a 70th of the
-// card's memory: writing and reading them took less than forming them twice at every size tried (520
-// rows, 50021 classes, f16: 143 us against 170 with 128 features, 395 against 458 with 1000; f32 285
-// against 344 and 1132 against 1469; 16 rows of 1024 features, 100000 classes: 186 against 225).
-constexpr size_t KEEP_BYTES = (size_t)4 << 30;
+// The logits are kept in fp32 for the gradients where that takes less time than forming them twice:
+// few enough to stay in the last cache (KEEP_CACHED: 520 rows, 50021 classes, 128 features f16 143 us
+// against 170; 1024 rows, 32000 classes bf16 142 against 141; 2048 rows 270 against 230), or enough
+// features (4096 rows, 65536 classes: bf16 1167 us against 1057 with 256, 1462 against 1480 with 512, 2137
+// against 2351 with 1024; f32 1581 against 1533 with 64, 2047 against 2146 with 128, 4947 against 5980 with
+// 512), and no more than KEEP_BYTES, a 70th of the card's memory.
+constexpr size_t KEEP_BYTES = (size_t)4 << 30, KEEP_CACHED = (size_t)128 << 20;
+
+bool keep_logits(size_t e, size_t bytes, int q) {
+  return bytes <= KEEP_CACHED || (bytes <= KEEP_BYTES && q >= (e == 2 ? 512 : 128));
+}
 
 LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
   const size_t e = esize(dtype), ldq = mm::padded(e, q);
@@ -162,7 +168,7 @@ LabelLayout label_layout(int dtype, int B, int q, int nc, bool grad) {
     l.lse = take((size_t)B * 4);
     const size_t logits = (size_t)B * mm::padded(e, nc) * 4;
     // (of floats the kept logits become P in place: a tile's rows, up to 256, lie within 2 GiB of each other)
-    l.keep = logits <= KEEP_BYTES && (size_t)std::min(B, 256) * mm::padded(e, nc) * 4 < (size_t)1 << 31;
+    l.keep = keep_logits(e, logits, q) && (size_t)std::min(B, 256) * mm::padded(e, nc) * 4 < (size_t)1 << 31;
     if (l.keep) l.z = take(logits);
     l.P = l.keep && e == 4 ? l.z : take((size_t)B * mm::padded(e, l.piece) * e);
     l.du = take(l.copied < nc ? (size_t)B * q * 4 : 0);

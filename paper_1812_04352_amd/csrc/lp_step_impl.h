@@ -290,7 +290,7 @@ __global__ __launch_bounds__(256) void k_ck_store(const T* x, int8_t* x8, uint8_
   }
 }
 
-// To rows of ld >= q values, zeros behind the q that count (ld at most the next multiple of 32).
+// To rows of ld >= q values, zeros behind the q that count (to the end of their last block).
 template <typename T, bool FLAT>
 __global__ __launch_bounds__(256) void k_ck_load(const int8_t* x8, const uint8_t* xe, T* x, uint32_t nblk, int q, uint32_t nb,
                                                  int ld) {
@@ -354,7 +354,7 @@ template <typename T>
 hipError_t ck_load_t(const int8_t* x8, const uint8_t* xe, void* x, long B, int q, int ld, hipStream_t st) {
   const int nb = mm::ceil_div(q, CK_BLOCK);
   const uint32_t nblk = (uint32_t)(B * nb);
-  if (q % CK_BLOCK == 0) k_ck_load<T, true><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb, ld);
+  if (q % CK_BLOCK == 0 && ld == q) k_ck_load<T, true><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb, ld);
   else k_ck_load<T, false><<<ck_grid(nblk), 256, 0, st>>>(x8, xe, (T*)x, nblk, q, nb, ld);
   return hipGetLastError();
 }

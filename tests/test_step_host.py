@@ -173,10 +173,12 @@ def test_binding_refuses_tensors_of_another_device(monkeypatch):
 
 
 def test_loss_workspace_with_and_without_the_logits():
-    """Logits of up to 4 GiB in fp32 are kept for the gradients; losses alone keep none."""
-    kept, again, alone = (L.lp_loss_labels_workspace_bytes(L.label_head("bf16", B, 64, 2 ** 17), g)
+    """Logits of up to 4 GiB in fp32 are kept for the gradients where there are many features;
+    losses alone keep none."""
+    kept, again, alone = (L.lp_loss_labels_workspace_bytes(L.label_head("bf16", B, 512, 2 ** 17), g)
                           for B, g in ((8192, True), (8193, True), (8192, False)))
     assert 2 ** 32 < kept < 2 ** 32 + 2 ** 31
     assert again < 2 ** 31 and alone < 2 ** 29
+    assert L.lp_loss_labels_workspace_bytes(L.label_head("bf16", 8192, 511, 2 ** 17), True) < 2 ** 31
     # (too far apart for 32-bit offsets within a tile of rows)
-    assert L.lp_loss_labels_workspace_bytes(L.label_head("f32", 256, 8, 2 ** 21), True) < 2 ** 30 + 2 ** 28
+    assert L.lp_loss_labels_workspace_bytes(L.label_head("f32", 256, 128, 2 ** 21), True) < 2 ** 30 + 2 ** 29
