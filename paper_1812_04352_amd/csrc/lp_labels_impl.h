@@ -481,21 +481,22 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
       const mm::Prob pp{uc, o.p[1], ldu, o.ld[1], a.B, n, a.q, count, 1, 0, 0, 0, 0};
       if ((e = mm::launch_mm<T, false, false, EpProb<T>>(pp, ep, pl, split, st)) != hipSuccess) return e;
     }
-    if (dmu && col_rows != 1)  // (a single partial's kernel has left dmu itself)
-      mm::k_colsum<T><<<(unsigned)mm::ceil_div(n, 64), 256, 0, st>>>(col, col_rows, col_step, a.B ? count : nullptr, n, dmu, 1.f, scale);
-    if (a.du && a.B) {
-      typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
-      const mm::Prob pd{P, o.p[1], ldp, o.ld[1], a.B, a.q, n, count, 1, 0, 0, 0, 0};
-      if ((e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, mm::plan_of(sizeof(T), a.B, a.q, n), split, st)) != hipSuccess)
-        return e;
+    // (a single column partial's kernel has left dmu itself)
+    const mm::ColSum<T> cs{col, col_rows, col_step, a.B ? count : nullptr, n, col_rows != 1 ? dmu : nullptr, 1.f, scale};
+    typedef mm::EpScale<T> EpDW;
+    const typename EpDu<T>::Args ed{acc32, (T*)a.du, from, scale, 1.f / PSCALE<T>, j0 == 0, j0 + n == a.nc};
+    const typename EpDW::Args ew{a.dW ? (T*)a.dW + (size_t)j0 * a.q : nullptr, 1.f / PSCALE<T>, scale};
+    const mm::Prob pd{P, o.p[1], ldp, o.ld[1], a.B, a.q, n, count, 1, 0, 0, 0, 0}, pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
+    const mm::Plan zd = mm::plan_of(sizeof(T), a.B, a.q, n), zw = mm::plan_of(sizeof(T), n, a.q, a.B);
+    const bool du = a.du && a.B;
+    if (du && a.dW) {
+      e = mm::launch_both<T, EpDu<T>, EpDW>(pd, ed, zd, pw, ew, zw, cs, split, st);
+    } else {
+      if (du) e = mm::launch_mm<T, false, true, EpDu<T>>(pd, ed, zd, split, st);
+      if (a.dW && e == hipSuccess) e = mm::launch_mm<T, true, true, EpDW>(pw, ew, zw, split, st);
+      if (cs.out && e == hipSuccess) e = mm::launch_colsum(cs, st);
     }
-    if (a.dW) {
-      T* dW = static_cast<T*>(a.dW) + (size_t)j0 * a.q;
-      const mm::Prob pw{P, uc, ldp, ldu, n, a.q, a.B, count, 0, 1, 0, 0, 0};
-      e = mm::launch_mm<T, true, true, mm::EpScale<T>>(pw, typename mm::EpScale<T>::Args{dW, 1.f / PSCALE<T>, scale},
-                                                       mm::plan_of(sizeof(T), n, a.q, a.B), split, st);
-      if (e != hipSuccess) return e;
-    }
+    if (e != hipSuccess) return e;
   }
   return hipGetLastError();
 }

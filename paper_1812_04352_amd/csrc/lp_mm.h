@@ -316,8 +316,9 @@ __device__ __forceinline__ void wait_and_meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// id: the workgroup's index among the product's
 template <class S>
-__device__ __forceinline__ Place place(const Prob& p, int wave, int& K) {
+__device__ __forceinline__ Place place(const Prob& p, int id, int wave, int& K) {
   Place c;
   K = p.K;
   c.M = p.M;
@@ -327,7 +328,7 @@ __device__ __forceinline__ Place place(const Prob& p, int wave, int& K) {
     if (p.count_m) c.M = min(c.M, n);
     if (p.count_k) K = min(K, n);
   }
-  tile_of(blockIdx.x, p.tm, p.tn, c.mt, c.nt);
+  tile_of(id, p.tm, p.tn, c.mt, c.nt);
   c.m0 = c.mt * S::BM;
   c.n0 = c.nt * S::BN;
   c.lim = min(c.N, c.n0 + S::BN);
@@ -340,8 +341,14 @@ __device__ __forceinline__ Place place(const Prob& p, int wave, int& K) {
   return c;
 }
 
+// LDS of a workgroup: the stages
+template <class S>
+struct Stages {
+  __attribute__((aligned(16))) unsigned char at[S::NS][(S::BM + S::BN) * S::KB];
+};
+
 template <typename T, class S, bool AT, bool BT, class E>
-__global__ __launch_bounds__(S::NT, S::WAVES) void k_mm(Prob p, typename E::Args ea) {
+__device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& ea, int id, Stages<S>& stages) {
   constexpr int BM = S::BM, BN = S::BN, WGM = S::WGM, WGN = S::WGN, KB = S::KB, NS = S::NS, NT = S::NT;
   constexpr int FM = BM / WGM / 32, FN = BN / WGN / 32, GK = S::GK;
   constexpr int NG = KB / (16 * (int)sizeof(T)) / GK;
@@ -349,11 +356,11 @@ __global__ __launch_bounds__(S::NT, S::WAVES) void k_mm(Prob p, typename E::Args
   typedef Stage<T, BM, KB, NT, AT> SA;
   typedef Stage<T, BN, KB, NT, BT> SB;
   constexpr int LOADS = SA::PER + SB::PER;
-  __shared__ __attribute__((aligned(16))) unsigned char lds[NS][(BM + BN) * KB];
+  auto& lds = stages.at;
   static_assert(epilogue_lds(WGM * WGN, BM, WGN) <= NS * (BM + BN) * KB, "the epilogue's LDS");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int K;
-  const Place c = place<S>(p, wave, K);
+  const Place c = place<S>(p, id, wave, K);
   if (c.m0 >= c.M) return;
   const int k0 = blockIdx.y * p.kper, k1 = min(K, k0 + p.kper);
   const int steps = k1 > k0 ? (k1 - k0 + SA::BK - 1) / SA::BK : 0;
@@ -455,6 +462,12 @@ __global__ __launch_bounds__(S::NT, S::WAVES) void k_mm(Prob p, typename E::Args
   // whole quads of features everywhere: straight-line code, no test per quad
   if (c.n0 + BN <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, el);
   else E::template run<false, FM, FN, WGM, WGN>(ea, c, acc, el);
+}
+
+template <typename T, class S, bool AT, bool BT, class E>
+__global__ __launch_bounds__(S::NT, S::WAVES) void k_mm(Prob p, typename E::Args ea) {
+  __shared__ Stages<S> stages;
+  mm_tile<T, S, AT, BT, E>(p, ea, blockIdx.x, stages);
 }
 
 // The four values of quad q of a block
@@ -688,7 +701,7 @@ __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int
   __shared__ __attribute__((aligned(16))) float lds[epilogue_lds(WGM * WGN, S::BM, WGN) / 4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int K;
-  const Place c = place<S>(p, wave, K);
+  const Place c = place<S>(p, blockIdx.x, wave, K);
   if (c.m0 >= c.M) return;
   f32x16 acc[FM][FN];
 #pragma unroll
@@ -800,11 +813,22 @@ __global__ __launch_bounds__(32 * NF) void k_one(Prob p, typename E::Args ea) {
 // runs of tile rows a workgroup). With `count` given, only the tile rows that hold rows below it
 // were written.
 template <typename T>
-__global__ __launch_bounds__(256) void k_colsum(const float* part, int tiles, int bm, const int* count, int n, T* out,
-                                                float f, const float* scale) {
-  __shared__ double sh[4][64];
-  const int i = blockIdx.x * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
-  if (count) tiles = min(tiles, (*count + bm - 1) / bm);
+struct ColSum {
+  const float* part;
+  int tiles, bm;
+  const int* count;  // nullable
+  int n;
+  T* out;
+  float f;
+  const float* scale;  // nullable
+  unsigned blocks() const { return (unsigned)((n + 63) / 64); }
+};
+
+template <typename T>
+__device__ __forceinline__ void col_sum(const ColSum<T>& a, int id, double (*sh)[64]) {
+  const int i = id * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6, n = a.n;
+  const float* part = a.part;
+  const int tiles = a.count ? min(a.tiles, (*a.count + a.bm - 1) / a.bm) : a.tiles;
   const int per = (tiles + 3) / 4, t1 = min(tiles, (g + 1) * per);
   double s = 0.0;
   if (i < n) {
@@ -822,7 +846,24 @@ __global__ __launch_bounds__(256) void k_colsum(const float* part, int tiles, in
   __syncthreads();
   if (g || i >= n) return;
   s = ((sh[0][threadIdx.x] + sh[1][threadIdx.x]) + sh[2][threadIdx.x]) + sh[3][threadIdx.x];
-  out[i] = (T)((float)s * (scale ? f * scale[0] : f));
+  a.out[i] = (T)((float)s * (a.scale ? a.f * a.scale[0] : a.f));
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_colsum(ColSum<T> a) {
+  __shared__ double sh[4][64];
+  col_sum(a, blockIdx.x, sh);
+}
+
+// The products that follow a gradient's first one, and its column sums, none of which needs another's
+// result, as one launch: A B in (rows, columns), then A^T B in (columns, columns), then the sums.
+template <typename T, class S, class E1, class E2>
+__global__ __launch_bounds__(S::NT, S::WAVES) void k_both(Prob p1, typename E1::Args e1, Prob p2, typename E2::Args e2, ColSum<T> cs) {
+  __shared__ Stages<S> stages;
+  const int n1 = p1.tm * p1.tn, n2 = p2.tm * p2.tn, id = blockIdx.x;
+  if (id < n1) mm_tile<T, S, false, true, E1>(p1, e1, id, stages);
+  else if (id < n1 + n2) mm_tile<T, S, true, true, E2>(p2, e2, id - n1, stages);
+  else col_sum(cs, id - n1 - n2, reinterpret_cast<double(*)[64]>(&stages));
 }
 
 // Rows of `cols` values to rows of ld values, zeros behind them (ld a multiple of a chunk): copies of
@@ -948,6 +989,12 @@ inline Plan plan_rows(size_t esz, long M, long N, long K) {
   return plan_of(esz, M, N, K);
 }
 
+template <typename T>
+hipError_t launch_colsum(const ColSum<T>& cs, hipStream_t st) {
+  k_colsum<T><<<cs.blocks(), 256, 0, st>>>(cs);
+  return hipGetLastError();
+}
+
 template <typename T, class S, bool AT, bool BT, class E>
 hipError_t launch_shape(Prob p, const typename E::Args& ea, const Plan& pl, void* part, hipStream_t st) {
   constexpr int BK = S::KB / (int)sizeof(T);
@@ -987,6 +1034,29 @@ hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, 
     if (pl.tile == 128) return launch_shape<T, Tile128f, AT, BT, E>(p, ea, pl, part, st);
     return launch_shape<T, Tile64f, AT, BT, E>(p, ea, pl, part, st);
   }
+}
+
+// Two products and a gradient's column sums (cs.out nullable): one launch where both take the small
+// tiles unsplit, when each fills a part of the card only and takes little more than its launch; else one each.
+template <typename T, class E1, class E2>
+hipError_t launch_both(Prob p1, const typename E1::Args& e1, const Plan& pl1, Prob p2, const typename E2::Args& e2,
+                       const Plan& pl2, const ColSum<T>& cs, void* part, hipStream_t st) {
+  const auto one = [](Prob& p, const Plan& pl) {
+    if (pl.tile != 64 || pl.splits != 1) return false;
+    p.tm = pl.tm, p.tn = pl.tn;
+    p.kper = std::max(1, ceil_div(p.K * (long)sizeof(T), STAGE_BYTES)) * (STAGE_BYTES / (int)sizeof(T));
+    return true;
+  };
+  if (one(p1, pl1) && one(p2, pl2)) {
+    typedef std::conditional_t<sizeof(T) == 2, Tile64, Tile64f> S;
+    const unsigned grid = (unsigned)(p1.tm * p1.tn + p2.tm * p2.tn) + (cs.out ? cs.blocks() : 0);
+    k_both<T, S, E1, E2><<<grid, S::NT, 0, st>>>(p1, e1, p2, e2, cs);
+    return hipGetLastError();
+  }
+  hipError_t e = launch_mm<T, false, true, E1>(p1, e1, pl1, part, st);
+  if (e == hipSuccess) e = launch_mm<T, true, true, E2>(p2, e2, pl2, part, st);
+  if (e == hipSuccess && cs.out) e = launch_colsum(cs, st);
+  return e;
 }
 
 }  // namespace mm

@@ -394,21 +394,16 @@ hipError_t step_backward_t(const StepArgs& a, hipStream_t st) {
     e = mm::launch_mm<T, false, false, EpGrad<T>>(prob(x, ldx, o.p[1], o.ld[1], a.B, a.no, a.ni), eg, l.z, w + l.part, st);
     if (e != hipSuccess) return e;
   }
-  if (a.dx && a.B) {
-    typename EpDx<T>::Args ed{a.residual ? (const T*)a.dy : nullptr, (T*)a.dx, h};
-    e = mm::launch_mm<T, false, true, EpDx<T>>(prob(g, ldg, o.p[1], o.ld[1], a.B, a.ni, a.no), ed, l.zx, w + l.part, st);
-    if (e != hipSuccess) return e;
-  }
-  if (a.dW) {
-    e = mm::launch_mm<T, true, true, mm::EpScale<T>>(prob(g, ldg, x, ldx, a.no, a.ni, a.B),
-                                                     typename mm::EpScale<T>::Args{(T*)a.dW, h, nullptr}, l.zw, w + l.part, st);
-    if (e != hipSuccess) return e;
-  }
-  if (a.db && !own_db) {
-    mm::k_colsum<T><<<(unsigned)mm::ceil_div(a.no, 64), 256, 0, st>>>(colpart, a.B ? l.z.tm : 0, l.z.tile, nullptr, a.no,
-                                                                    (T*)a.db, h, nullptr);
-    e = hipGetLastError();
-  }
+  typedef mm::EpScale<T> EpDW;
+  const typename EpDx<T>::Args ed{a.residual ? (const T*)a.dy : nullptr, (T*)a.dx, h};
+  const typename EpDW::Args ew{(T*)a.dW, h, nullptr};
+  const mm::Prob px = prob(g, ldg, o.p[1], o.ld[1], a.B, a.ni, a.no), pw = prob(g, ldg, x, ldx, a.no, a.ni, a.B);
+  const bool dx = a.dx && a.B;
+  const mm::ColSum<T> cs{colpart, a.B ? l.z.tm : 0, l.z.tile, nullptr, a.no, own_db ? nullptr : (T*)a.db, h, nullptr};
+  if (dx && a.dW) return mm::launch_both<T, EpDx<T>, EpDW>(px, ed, l.zx, pw, ew, l.zw, cs, w + l.part, st);
+  if (dx) e = mm::launch_mm<T, false, true, EpDx<T>>(px, ed, l.zx, w + l.part, st);
+  if (a.dW && e == hipSuccess) e = mm::launch_mm<T, true, true, EpDW>(pw, ew, l.zw, w + l.part, st);
+  if (cs.out && e == hipSuccess) e = mm::launch_colsum(cs, st);
   return e;
 }
 
