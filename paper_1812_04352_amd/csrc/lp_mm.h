@@ -1037,7 +1037,8 @@ hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, 
 }
 
 // Two products and a gradient's column sums (cs.out nullable): one launch where both take the small
-// tiles unsplit, when each fills a part of the card only and takes little more than its launch; else one each.
+// tiles unsplit, when each fills a part of the card only and takes little more than its launch (320 x 60 -> 384 bf16
+// 20.8 us against 27.1, 209 x 649 -> 649 28.5 against 32.2); else one each.
 template <typename T, class E1, class E2>
 hipError_t launch_both(Prob p1, const typename E1::Args& e1, const Plan& pl1, Prob p2, const typename E2::Args& e2,
                        const Plan& pl2, const ColSum<T>& cs, void* part, hipStream_t st) {

@@ -329,3 +329,14 @@ def test_many_rows(dtype):
     B, q, nc = 5003, 24, 300
     u, W, mu, lab = inputs(15, dtype, B, q, nc, ignored=0.3)
     compare(run(dtype, *[T.gpu(t) for t in (u, W, mu, lab)]), T.loss(u, W, mu, lab, 1.0, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_kept_logits_of_several_pieces(dtype):
+    """Logits kept for the gradients, whose probabilities are taken a piece at a time (fp32: in place)."""
+    B, q, nc = 2100, 520, 70001
+    u, W, mu, lab = (t.cuda() for t in inputs(16, dtype, B, q, nc, ignored=0.2))
+    hd = L.label_head(dtype, B, q, nc)
+    assert B * nc * u.element_size() > 256 << 20
+    assert L.lp_loss_labels_workspace_bytes(hd, True) > B * nc * 4
+    near(dtype, run(dtype, u, W, mu, lab), on_gpu(dtype, u, W, mu, lab))
