@@ -550,10 +550,9 @@ __device__ __forceinline__ unsigned char* wave_lds(float* lds, const Place& c, i
 
 // An array of rows of ld values, those below c.lim of which count (WHOLE: all of the tile's), as a lane's quads,
 // block by block in the order i = 0.. within j = 0..
-template <bool WHOLE, typename T, int FM, int FN>
+template <bool WHOLE, typename T, int FM, int FN, bool AHEAD = sizeof(T) == 2>
 struct Rows {
   typedef BlockIO<T> IO;
-  static constexpr bool AHEAD = sizeof(T) == 2;
   const T* a;
   long ld;
   typename IO::Block next;
@@ -562,8 +561,8 @@ struct Rows {
       if (a) next = IO::fetch(a, ld, c, 0, 0);
     }
   }
-  // the quads of block (i, j) (zeros without an array); requests the next block's (of floats there
-  // are too many registers in use for that)
+  // the quads of block (i, j) (zeros without an array); requests the next block's (AHEAD: of floats
+  // there are too many registers in use for that)
   __device__ __forceinline__ void get(const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
     if (!a) {
 #pragma unroll

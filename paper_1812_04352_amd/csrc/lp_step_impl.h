@@ -7,7 +7,7 @@
 //                                          range of f16)
 //              dx = h g W (+ dy),  dW = h g^T x,  db = h sum g (from g before its rounding)
 // Bound by the products (2 B ni no operations each): 8192 x 4096 -> 4096 bf16 forward with its
-// checkpoint 275 us (1.0 PFLOP/s), back 286 + 250 + 223 us, of which the epilogue of g takes some 50:
+// checkpoint 275 us (1.0 PFLOP/s), back 270 + 250 + 223 us, of which the epilogue of g takes some 40:
 // the largest tiles fill a CU, so nothing runs beside an epilogue. Small batches are bound by reading W
 // (one row of 4096 x 4096: 6.5 us, 5.2 TB/s) and by launches.
 #pragma once
@@ -170,7 +170,9 @@ struct EpGrad {
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     float col[FN];
     unsigned char* buf = mm::wave_lds(lds, c, WGN);
-    mm::Rows<WHOLE, T, FM, FN> dy(a.dy, c.N, c);
+    // (the largest tiles have no registers left for dy ahead: with it 90 spilled, 774 us against 751 for
+    // the whole way back of 8192 x 4096 -> 4096 bf16)
+    mm::Rows<WHOLE, T, FM, FN, sizeof(T) == 2 && (FM * FN < 8)> dy(a.dy, c.N, c);
     with_act(a.act, [&](auto act) {
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
