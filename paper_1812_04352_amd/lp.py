@@ -457,14 +457,20 @@ WIDE_DTYPE = {"f32": LP_F32, "f64": LP_F64, "bf16": LP_BF16, "f16": LP_F16}
 CHECKPOINT_BLOCK = 32  # features of a row that share a scale
 
 
+def _count(n: int) -> int:
+    """A count for a 32-bit argument, which ctypes would cut to its low bits: one beyond them becomes
+    the largest (or least) value, which the library refuses."""
+    return min(max(n, -2 ** 31), 2 ** 31 - 1)
+
+
 def step(dtype: str, act: str, B: int, ni: int, no: int, h: float = 1.0) -> LpStep:
     """One layer step y = r + h sigma(x W^T + b), x [B][ni], W [no][ni]; dtype "f32", "bf16" or "f16"."""
-    return LpStep(LP_ABI_VERSION, WIDE_DTYPE[dtype], ACT[act], B, ni, no, h)
+    return LpStep(LP_ABI_VERSION, WIDE_DTYPE[dtype], ACT[act], _count(B), _count(ni), _count(no), h)
 
 
 def label_head(dtype: str, B: int, q: int, nc: int) -> LpLabelHead:
     """Softmax head over nc classes for B rows of q features; dtype "f32", "bf16" or "f16"."""
-    return LpLabelHead(LP_ABI_VERSION, WIDE_DTYPE[dtype], B, q, nc)
+    return LpLabelHead(LP_ABI_VERSION, WIDE_DTYPE[dtype], _count(B), _count(q), _count(nc))
 
 
 _torch_dtypes: dict = {}  # library dtype -> torch dtype, and back
@@ -583,7 +589,7 @@ def _ck_args(x, x8, xe):
     import torch
     q = x.shape[-1]
     B = x.numel() // q if q else 0
-    return (kind, B, q, _dev(x, B * q, "x", x.dtype, dev), _dev(x8, B * q, "x8", torch.int8, dev),
+    return (kind, _count(B), _count(q), _dev(x, B * q, "x", x.dtype, dev), _dev(x8, B * q, "x8", torch.int8, dev),
             _dev(xe, B * _blocks(q), "xe", torch.uint8, dev), _stream_of(dev))
 
 
