@@ -479,9 +479,9 @@ _torch_dtypes: dict = {}  # library dtype -> torch dtype, and back
 def _kinds() -> dict:
     if not _torch_dtypes:
         import torch
-        for k, t in ((LP_F32, torch.float32), (LP_F64, torch.float64), (LP_BF16, torch.bfloat16),
-                     (LP_F16, torch.float16)):
-            _torch_dtypes[k], _torch_dtypes[t] = t, k
+        pairs = ((LP_F32, torch.float32), (LP_F64, torch.float64), (LP_BF16, torch.bfloat16), (LP_F16, torch.float16))
+        # (at once: another thread's call finds none of them or all)
+        _torch_dtypes.update([(k, t) for k, t in pairs] + [(t, k) for k, t in pairs])
     return _torch_dtypes
 
 

@@ -55,3 +55,19 @@ def test_checkpoints_of_more_rows_than_32_bits_count(monkeypatch):
             with pytest.raises(L.LpError) as e:
                 call()
             assert e.value.status == L.LP_EUNSUPPORTED
+
+
+def test_first_calls_of_two_threads(monkeypatch):
+    """While one thread's first call fills the table of dtypes, another's finds it empty or whole."""
+    seen = []
+
+    class Watched(dict):
+        def __setitem__(self, k, v):
+            super().__setitem__(k, v)
+            if not seen:
+                seen.append(None)
+                seen.append(L._wide_dtype(L.LP_BF16))  # what a call between two entries gets
+
+    monkeypatch.setattr(L, "_torch_dtypes", Watched())
+    assert L._wide_dtype(L.LP_BF16) == torch.bfloat16
+    assert seen in ([], [None, torch.bfloat16])
