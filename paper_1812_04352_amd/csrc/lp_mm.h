@@ -174,7 +174,12 @@ struct Stage {
   // zeros: rows past the last (rows), contraction indices past the last (columns); so does an
   // offset of 2^31 (rows: past the contraction's end, which only the last stage can hold).
   // (The instruction is written out: of the builtin's loads the compiler believes that a transposing
-  // LDS read may depend on every one in flight, and waits for all of them before it.)
+  // LDS read may depend on every one in flight, and waits for all of them before it. The program's LDS
+  // accesses stay on their side of it. The compiler does not see its hazards: s_nop 0 is the wait state
+  // between m0 and a load, and the five between a vector instruction that writes a scalar of the
+  // descriptor, such as a spilled one's return, and a load are there since the descriptor is formed by
+  // scalar instructions: tests/test_wide_code.py reads the generated code for it. Waiting for them here
+  // costs the large products 1 %.)
   __device__ __forceinline__ void load(unsigned char* lds, int wave) {
 #ifdef __HIP_DEVICE_COMPILE__
     typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -185,10 +190,14 @@ struct Stage {
 #pragma unroll
       for (int i = 0; i < PER; ++i) off[i] = k + kc >= k1 ? 0x80000000u : off[i];
     }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is reserved: a note that it may be needed around the statement, where nothing holds it)
 #pragma unroll
     for (int i = 0; i < PER; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * NT * 16), "v"(off[i]),
-                   "s"(r));
+                   "s"(r)
+                   : "m0", "memory");
+#pragma clang diagnostic pop
     base += step;
     left -= step;
     k += BK;
@@ -259,6 +268,14 @@ struct Prob {
   int kper;          // contraction per split (grid y), a multiple of a stage's
 };
 
+// A wave's LDS writes before its other lanes' reads and the other way round: the wave's accesses are
+// made in order, so the compiler alone has to be kept from exchanging them.
+__device__ __forceinline__ void wave_in_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // What an epilogue knows of its place: row m of D is mw + 32 i + lane % 32 of block row i,
 // feature n = nw + 32 j + 8 q + 4 (lane / 32) of quad q of block column j.
 struct Place {
@@ -275,7 +292,7 @@ struct Place {
   // the workgroup's waves meet (a single wave's LDS accesses are in order by themselves)
   template <int WAVES>
   __device__ __forceinline__ void meet() const {
-    if constexpr (WAVES == 1) __builtin_amdgcn_wave_barrier();
+    if constexpr (WAVES == 1) wave_in_order();
     else __syncthreads();
   }
   __device__ __forceinline__ int row(int i) const { return mw + 32 * i + (lane & 31); }
@@ -509,7 +526,7 @@ struct BlockIO {
       const int id = c.lane + 64 * t;
       *reinterpret_cast<LPiece*>(buf + id / CPR * PITCH + id % CPR * 16) = b.p[t];
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_in_order();
     const unsigned char* r = buf + (c.lane & 31) * PITCH + (c.lane >> 5) * 4 * sizeof(T);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -517,7 +534,7 @@ struct BlockIO {
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[q][k] = (float)x[k];
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_in_order();
   }
 
   // row(m): the index of row m in the array
@@ -532,14 +549,14 @@ struct BlockIO {
       for (int k = 0; k < 4; ++k) x[k] = (T)v[q][k];
       *reinterpret_cast<Quad*>(w + 8 * q * sizeof(T)) = x;
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_in_order();
 #pragma unroll
     for (int t = 0; t < ITER; ++t) {
       const int id = c.lane + 64 * t, m = c.mw + 32 * i + id / CPR;
       const Piece x = *reinterpret_cast<const LPiece*>(buf + id / CPR * PITCH + id % CPR * 16);
       if (m < c.M) *reinterpret_cast<Piece*>(a + (size_t)row(m) * ld + c.nw + 32 * j + id % CPR * V) = x;
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_in_order();
   }
 };
 
