@@ -465,8 +465,9 @@ hipError_t loss_labels_t(const LabelArgs& a, hipStream_t st) {
     if (o.e != hipSuccess) return o.e;
     T* dmu = a.dmu ? (T*)a.dmu + j0 : nullptr;
     int col_rows = 0, col_step = 1;  // column partials, and the rows of one
-    const int wide = mm::padded(sizeof(T), n), ldp = z && sizeof(T) == 4 ? ldz : wide;
-    if (z && sizeof(T) == 4) P = reinterpret_cast<T*>(z + j0);  // (in place)
+    const bool place = z && sizeof(T) == 4;  // P takes its logits' place: the last piece ends with their rows
+    const int wide = place && j0 + n == a.nc ? ldz - j0 : mm::padded(sizeof(T), n), ldp = place ? ldz : wide;
+    if (place) P = reinterpret_cast<T*>(z + j0);
     if (a.B && z) {
       col_rows = mm::ceil_div(a.B, PROB_ROWS), col_step = PROB_ROWS;
       const bool own = col_rows == 1;

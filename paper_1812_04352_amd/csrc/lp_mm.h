@@ -160,7 +160,9 @@ struct Stage {
     } else {
       kc = 0;
       base = static_cast<const unsigned char*>(p) + ((long)k0 * ld + r0) * (long)sizeof(T);
-      left = ((long)(k1 - k0) * ld - r0) * (long)sizeof(T);
+      // (to the last chunk of row k1 - 1 that counts: behind it may lie what no kernel has written, which
+      // must not decide whether a float tile is formed again)
+      left = ((long)(k1 - k0 - 1) * ld + (rows + V - 1) / V * V - r0) * (long)sizeof(T);
       step = BK * ld * (long)sizeof(T);
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
