@@ -72,6 +72,25 @@ __device__ __forceinline__ Split8 split8(f32x8 x) {
   return s;
 }
 
+// sign * x, split: sign is 1 or -1, the same for all of the wave. (The first part's words change their
+// sign bits, the rest is formed by one multiply-add as without a sign by one subtraction.)
+__device__ __forceinline__ Split8 split8(f32x8 x, float sign) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const uint32_t flip = __builtin_bit_cast(uint32_t, sign) & 0x80000000u;
+  Split8 s;
+  const u32x4 w = __builtin_bit_cast(u32x4, __builtin_convertvector(x, bf16x8)) ^ (flip | flip >> 16);
+  s.p[0] = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = fmaf(x[2 * i], sign, -__builtin_bit_cast(float, w[i] << 16));
+    x[2 * i + 1] = fmaf(x[2 * i + 1], sign, -__builtin_bit_cast(float, w[i] & 0xffff0000u));
+  }
+  s.p[1] = __builtin_convertvector(x, bf16x8);
+  x = split_rest(x, s.p[1]);
+  s.p[2] = __builtin_convertvector(x, bf16x8);
+  return s;
+}
+
 __device__ __forceinline__ Split8 split8(split_f32x4 a, split_f32x4 b) {
   return split8(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }

@@ -70,3 +70,65 @@ def test_any_workspace_gives_the_same_bits(dtype):
             L.lp_loss_labels(hd, u, W, mu, lab, J, ws, row=row, du=out[0], dW=out[1], dmu=out[2])
             results.append([J, row] + out)
         assert all(torch.equal(a, c) for a, c in zip(*results)), (B, q, nc)
+
+
+# fp32 products are split bf16 ones, whose instruction's sums round towards minus infinity. Summed with
+# one sign, sums of K positive products have a mean relative error (measured, 96000 results each) of
+# -1.3e-8, -6.1e-9 and -2.1e-8 for K = 220, 1024 and 8192. The middle half is summed with the other sign,
+# which cancels the error of a sum that grows evenly but for the steps of its last place (a binade's
+# step is constant: for an end anywhere in its binade that leaves at most a quarter) and the unevenness
+# of the quarters (7 stages at K = 220: a seventh). Limit: a third of the drift, and three standard
+# deviations of the mean of N results that are off by 2^-22 at most, each on its own: 3 2^-22 / sqrt(N).
+DRIFT = {220: 1.3e-8, 1024: 6.1e-9, 8192: 2.1e-8}
+
+
+def sides(K, positive):
+    g = torch.Generator("cuda").manual_seed(K + positive)
+    a, b = (torch.randn(n, K, generator=g, device="cuda") for n in (300, 320))
+    return (a.abs(), b.abs()) if positive else (a, b)
+
+
+@pytest.mark.parametrize("form", ["z", "dx", "dW"])
+@pytest.mark.parametrize("positive", [True, False])
+@pytest.mark.parametrize("K", [220, 1024, 8192])
+def test_fp32_products_do_not_drift(K, positive, form):
+    """The mean error of each of a step's three products, as a part of the sum of its terms' magnitudes
+    (cancelling sums stay smaller than that on the way, and so does their drift)."""
+    a, b = sides(K, positive)
+    M, N = len(a), len(b)
+    out = torch.empty(M, N, device="cuda")
+    if form == "z":
+        st = L.step("f32", "identity", M, K, N)
+        L.lp_step_forward(st, a, b, None, None, out, L.alloc_step_workspace(st))
+    elif form == "dx":  # h g W with g = dy = a, W = b^T
+        st = L.step("f32", "identity", M, N, K)
+        L.lp_step_backward(st, torch.zeros(M, N, device="cuda"), b.t().contiguous(), None, a, out, None, None,
+                           L.alloc_step_workspace(st))
+    else:  # h g^T x with g = dy = a^T, x = b^T
+        st = L.step("f32", "identity", K, N, M)
+        L.lp_step_backward(st, b.t().contiguous(), torch.zeros(M, N, device="cuda"), None, a.t().contiguous(), None, out,
+                           None, L.alloc_step_workspace(st))
+    ref = a.double() @ b.double().t().contiguous()
+    mag = a.abs().double() @ b.abs().double().t().contiguous()
+    mean = float(((out.double() - ref) / mag).mean())
+    assert abs(mean) <= DRIFT[K] / 3 + 3 * 2 ** -22 / math.sqrt(M * N), mean
+
+
+def test_fp32_layers_have_no_common_bias():
+    """Residual steps of the identity in a row: the mean relative error of their increments (the rounding
+    of the state is unbiased, about 1e-6 of an increment: 5e-10 in the mean of three million)."""
+    q, B, N = 220, 200, 64
+    g = torch.Generator("cuda").manual_seed(3)
+    st = L.step("f32", "identity", B, q, q)
+    ws = L.alloc_step_workspace(st)
+    u = torch.randn(B, q, generator=g, device="cuda").abs() + 0.5
+    mean = []
+    for _ in range(N):
+        W = torch.randn(q, q, generator=g, device="cuda").abs()
+        W *= 0.1 / W.sum(1).mean()
+        y = torch.empty_like(u)
+        L.lp_step_forward(st, u, W, None, u, y, ws)
+        z = u.double() @ W.double().t().contiguous()
+        mean.append(((y.double() - u.double()) / z - 1).mean())
+        u = y
+    assert abs(float(torch.stack(mean).mean())) <= DRIFT[220] / 3 + 5e-10
