@@ -907,13 +907,17 @@ __global__ __launch_bounds__(256) void k_colsum(ColSum<T> a) {
 }
 
 // The products that follow a gradient's first one, and its column sums, none of which needs another's
-// result, as one launch: A B in (rows, columns), then A^T B in (columns, columns), then the sums.
+// result, as one launch: A B in (rows, columns), A^T B in (columns, columns), the longer contraction's
+// tiles first, so that they are not what the launch ends with (931 x 4269 -> 186 f32 79 us against 88), then
+// the sums.
 template <typename T, class S, class E1, class E2>
 __global__ __launch_bounds__(S::NT, S::WAVES) void k_both(Prob p1, typename E1::Args e1, Prob p2, typename E2::Args e2, ColSum<T> cs) {
   __shared__ Stages<S> stages;
   const int n1 = p1.tm * p1.tn, n2 = p2.tm * p2.tn, id = blockIdx.x;
-  if (id < n1) mm_tile<T, S, false, true, E1>(p1, e1, id, stages);
-  else if (id < n1 + n2) mm_tile<T, S, true, true, E2>(p2, e2, id - n1, stages);
+  const bool swap = p2.K > p1.K;
+  const int b1 = swap ? n2 : 0, b2 = swap ? 0 : n1;  // where each product's workgroups begin
+  if (id >= b1 && id < b1 + n1) mm_tile<T, S, false, true, E1>(p1, e1, id - b1, stages);
+  else if (id < n1 + n2) mm_tile<T, S, true, true, E2>(p2, e2, id - b2, stages);
   else col_sum(cs, id - n1 - n2, reinterpret_cast<double(*)[64]>(&stages));
 }
 
@@ -1088,15 +1092,20 @@ hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, 
 }
 
 // Two products and a gradient's column sums (cs.out nullable): one launch where both take the small
-// tiles unsplit, when each fills a part of the card only and takes little more than its launch (320 x 60 -> 384 bf16
-// 20.8 us against 27.1, 209 x 649 -> 649 28.5 against 32.2); else one each.
+// tiles unsplit and contract over at most BOTH_STAGES stages, else one each. 98 shapes of 2 to 2000
+// workgroups, one launch against three, times of the whole way back: 11.7 us against 18.2 (93 x 32 -> 62 bf16) to
+// 0.95 times (564 x 6751 -> 567 f32); 9 % less with 61 and 48 stages (3010 x 499 -> 3868 bf16), 3 % with 51 and
+// 50 of floats (1598 x 2483 -> 1614). Beyond, launches do not count: with 109 stages each 1 % less, with 102 and
+// 179 (11419 x 266 -> 6519 bf16) 2 % more, since the launch ends unevenly.
+constexpr int BOTH_STAGES = 64;
 template <typename T, class E1, class E2>
 hipError_t launch_both(Prob p1, const typename E1::Args& e1, const Plan& pl1, Prob p2, const typename E2::Args& e2,
                        const Plan& pl2, const ColSum<T>& cs, void* part, hipStream_t st) {
   const auto one = [](Prob& p, const Plan& pl) {
-    if (pl.tile != 64 || pl.splits != 1) return false;
+    const int stages = std::max(1, ceil_div(p.K * (long)sizeof(T), STAGE_BYTES));
+    if (pl.tile != 64 || pl.splits != 1 || stages > BOTH_STAGES) return false;
     p.tm = pl.tm, p.tn = pl.tn;
-    p.kper = std::max(1, ceil_div(p.K * (long)sizeof(T), STAGE_BYTES)) * (STAGE_BYTES / (int)sizeof(T));
+    p.kper = stages * (STAGE_BYTES / (int)sizeof(T));
     return true;
   };
   if (one(p1, pl1) && one(p2, pl2)) {
