@@ -344,7 +344,9 @@ int32_t lp_accuracy(const lp_problem* prob, int32_t nc, const void* uN, const vo
  * piece of it at a time, and activations kept in 8 bits for the way back. Arrays of
  * floating-point values have the call's dtype (LP_F32, LP_BF16 or LP_F16; LP_F64
  * returns LP_EUNSUPPORTED) unless stated; every sum is held in fp32 or more and
- * rounded to the dtype once. Products run on the matrix cores. No call waits for
+ * rounded to the dtype once. Products run on the matrix cores; those of fp32 values
+ * take each value as the sum of three bf16 ones, exactly from 2^-110 in magnitude on and
+ * to within 2^-134 below (x W^T and u W^T of a single row exactly). No call waits for
  * the stream or reads anything back, so all can be captured into a graph; two
  * calls or graphs that may overlap in time need workspaces of their own. Arrays
  * must not overlap except where stated. Results are bitwise reproducible. Limits

@@ -132,3 +132,28 @@ def test_fp32_layers_have_no_common_bias():
         mean.append(((y.double() - u.double()) / z - 1).mean())
         u = y
     assert abs(float(torch.stack(mean).mean())) <= DRIFT[220] / 3 + 5e-10
+
+
+@pytest.mark.parametrize("k", [108, 114, 122, 130])
+@pytest.mark.parametrize("B", [1, 70])
+def test_small_fp32_operands(k, B):
+    """A value is taken as three bf16 ones, the last of which is a multiple of 2^-133 (half of it off):
+    2^-134 of every other operand's value on top of the usual bound, nothing for a row alone."""
+    ni, no = 64, 72
+    g = torch.Generator().manual_seed(k)
+    x = (torch.randn((B, ni), generator=g, dtype=torch.float64) * 2.0 ** -k).float()
+    W = (torch.randn((no, ni), generator=g, dtype=torch.float64) * 2.0 ** 60).float()
+    dy = (torch.randn((B, no), generator=g, dtype=torch.float64) * 2.0 ** -k).float()
+    s = T.Step("f32", "identity", B, ni, no, 1.0)
+    y = s.forward(T.gpu(x), T.gpu(W), None, None)
+    ref, bound = T.preact(x, W, None)
+    part = 2.0 ** -134
+    off = 0 if B == 1 else part * (W.double().abs().sum(1)[None] + x.double().abs().sum(1)[:, None])
+    T.check(y, ref, (bound + off) * (1 + 2 ** -20) + T.half_step("f32") * ref.abs() + T.tiny("f32"), "y")
+    dx, dW, _ = s.backward(T.gpu(x), T.gpu(W), None, T.gpu(dy), False)
+    d, w, v = dy.double(), W.double(), x.double()
+    for name, got, r, mag, n, o in (
+            ("dx", dx, d @ w, d.abs() @ w.abs(), no, w.abs().sum(0)[None] + d.abs().sum(1)[:, None]),
+            ("dW", dW, d.t() @ v, d.abs().t() @ v.abs(), B, v.abs().sum(0)[None] + d.abs().sum(0)[:, None])):
+        T.check(got, r, ((n + 2) * T.E32 * mag + part * o) * (1 + 2 ** -20) + T.half_step("f32") * r.abs() + T.tiny("f32"),
+                name)
