@@ -134,6 +134,45 @@ def test_fp32_layers_have_no_common_bias():
     assert abs(float(torch.stack(mean).mean())) <= DRIFT[220] / 3 + 5e-10
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("ni,no", [(40, 16385), (33, 20001)])
+def test_one_row_to_many_outputs(dtype, ni, no):
+    """More outputs than the narrower one-row kernel serves, with and without a checkpoint, and back."""
+    g = torch.Generator().manual_seed(no)
+    x, W, b, dy = T.draw(g, (1, ni), dtype), T.draw(g, (no, ni), dtype, 1 / math.sqrt(ni)), T.draw(g, (no,), dtype, 0.3), \
+        T.draw(g, (1, no), dtype, 0.1)
+    r = T.draw(g, (1, no), dtype)
+    s = T.Step(dtype, "tanh", 1, ni, no, 0.5)
+    dev = [T.gpu(t) for t in (x, W, b)]
+    y, y8, ye = s.forward(*dev, T.gpu(r), ck=True)
+    T.check(y, *T.forward(x, W, b, r, "tanh", 0.5, dtype), "y")
+    e8, ee = T.pack(y.cpu())
+    assert torch.equal(y8.cpu(), e8) and torch.equal(ye.cpu(), ee)
+    T.check(s.forward(*dev, T.gpu(r)), *T.forward(x, W, b, r, "tanh", 0.5, dtype), "y without a checkpoint")
+    got = s.backward(*dev, T.gpu(dy), False)
+    for name, a, (v, e) in zip(("dx", "dW", "db"), got, T.backward(x, W, b, dy, "tanh", 0.5, False, dtype)):
+        T.check(a, v, e, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_one_row_of_many_classes(dtype):
+    q, nc = 64, 20001
+    g = torch.Generator().manual_seed(4)
+    u, W, mu = T.draw(g, (1, q), dtype), T.draw(g, (nc, q), dtype, 2 / math.sqrt(q)), T.draw(g, (nc,), dtype, 0.5)
+    lab = torch.tensor([nc - 1])
+    hd = L.label_head(dtype, 1, q, nc)
+    ws = L.alloc_loss_labels_workspace(hd)
+    out, flat = zip(*[T.out(s, T.DT[dtype]) for s in ((1, q), (nc, q), (nc,))])
+    J, row = torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    L.lp_loss_labels(hd, T.gpu(u), T.gpu(W), T.gpu(mu), lab.cuda(), J, ws, row=row, du=out[0], dW=out[1], dmu=out[2])
+    torch.cuda.synchronize()
+    assert all(T.guarded(f, o.numel()) for o, f in zip(out, flat))
+    (rJ, eJ), *rest = T.loss(u, W, mu, lab, 1.0, dtype)
+    T.check(J, rJ.reshape(1), eJ.reshape(1), "J")
+    for name, a, (r, e) in zip(("row", "du", "dW", "dmu"), (row,) + out, rest):
+        T.check(a, r, e, name)
+
+
 @pytest.mark.parametrize("k", [108, 114, 122, 130])
 @pytest.mark.parametrize("B", [1, 70])
 def test_small_fp32_operands(k, B):
