@@ -19,8 +19,8 @@ OBJ = os.path.join(HERE, "_build")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_step_host.cpp", "lp_host.cpp", "lp_common.hip", "lp_loss.hip", "lp_dense_f32.hip", "lp_dense_narrow.hip",
-           "lp_dense_mfma.hip", "lp_dense_resid.hip", "lp_dense_serial.hip",
+SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_step_host.cpp", "lp_host.cpp", "lp_common.hip",
+           "lp_loss.hip", "lp_dense_f32.hip", "lp_dense_narrow.hip", "lp_dense_mfma.hip", "lp_dense_resid.hip", "lp_dense_serial.hip",
            "lp_dense_wide.hip", "lp_conv.hip", "lp_noalloc.hip"]
 
 FLAGS = [
@@ -46,7 +46,8 @@ def _compile(src: str) -> str:
 SAN_FLAGS = ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer",
              "-Xarch_host", "-shared-libasan"]
-SAN_SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_step_host.cpp", "lp_host.cpp", "lp_noalloc.hip"]  # the translation units with host logic beyond launches
+# the translation units with host logic beyond launches
+SAN_SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_step_host.cpp", "lp_host.cpp", "lp_noalloc.hip"]
 SAN_OUT = os.path.join(OBJ, "liblp_san.so")
 
 
@@ -57,26 +58,27 @@ def sanitizer_runtime() -> str:
     return r.stdout.strip()
 
 
+def _sanitized_object(src: str) -> str:
+    if src not in SAN_SOURCES:
+        obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
+        return obj if os.path.exists(obj) else _compile(src)
+    obj = os.path.join(OBJ, "san", os.path.splitext(src)[0] + ".o")
+    flags = [f for f in FLAGS if f != "-O3"] + SAN_FLAGS
+    cmd = [HIPCC, *flags, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"hipcc failed on {src} (sanitized):\n{r.stdout}\n{r.stderr}")
+    return obj
+
+
 def build_sanitized(verbose: bool = True) -> str:
     """Build _build/liblp_san.so: the library with its host logic (argument
     checks, workspace layout, MGRIT schedule) compiled with AddressSanitizer and
     UndefinedBehaviorSanitizer; the kernel translation units are the ordinary
     objects (built first if missing)."""
     os.makedirs(os.path.join(OBJ, "san"), exist_ok=True)
-    objs = []
-    for src in SOURCES:
-        if src in SAN_SOURCES:
-            obj = os.path.join(OBJ, "san", os.path.splitext(src)[0] + ".o")
-            flags = [f for f in FLAGS if f != "-O3"] + SAN_FLAGS
-            cmd = [HIPCC, *flags, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
-            r = subprocess.run(cmd, capture_output=True, text=True)
-            if r.returncode != 0:
-                raise RuntimeError(f"hipcc failed on {src} (sanitized):\n{r.stdout}\n{r.stderr}")
-        else:
-            obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
-            if not os.path.exists(obj):
-                obj = _compile(src)
-        objs.append(obj)
+    with cf.ThreadPoolExecutor(max(1, min(6, os.cpu_count() or 1))) as ex:
+        objs = list(ex.map(_sanitized_object, SOURCES))
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-Xarch_host", "-fsanitize=address",
            "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-shared-libasan", *objs, "-o", SAN_OUT]
     r = subprocess.run(cmd, capture_output=True, text=True)
