@@ -171,7 +171,8 @@ struct EpGrad {
     float col[FN];
     unsigned char* buf = mm::wave_lds(lds, c, WGN);
     // (the largest tiles have no registers left for dy ahead: with it 90 spilled, 774 us against 751 for
-    // the whole way back of 8192 x 4096 -> 4096 bf16)
+    // the whole way back of 8192 x 4096 -> 4096 bf16. Floats, never read ahead, spill 74 there all the same, 144
+    // bytes a lane once a tile: order of the loads and the width of the column sums do not change that)
     mm::Rows<WHOLE, T, FM, FN, sizeof(T) == 2 && (FM * FN < 8)> dy(a.dy, c.N, c);
     with_act(a.act, [&](auto act) {
 #pragma unroll

@@ -72,17 +72,17 @@ def test_exchanges_over_a_waves_lds_are_ordered(ir):
 
 @pytest.fixture(scope="module")
 def code(tmp_path_factory):
-    """Assembly of the operators' kernels, by element type."""
+    """Assembly of the operators' kernels and the compiler's remarks on their resources, by element type."""
     if not os.path.exists(B.HIPCC):
         pytest.skip("no compiler")
     d = tmp_path_factory.mktemp("asm")
 
     def compiled(t):
-        r = subprocess.run([B.HIPCC, *B.FLAGS, "--offload-device-only", "-S", "-x", "hip",
-                            os.path.join(B.CSRC, f"lp_step_{t}.hip"), "-o", str(d / f"{t}.s")], capture_output=True, text=True,
+        r = subprocess.run([B.HIPCC, *B.FLAGS, "-Rpass-analysis=kernel-resource-usage", "--offload-device-only", "-S", "-x",
+                            "hip", os.path.join(B.CSRC, f"lp_step_{t}.hip"), "-o", str(d / f"{t}.s")], capture_output=True, text=True,
                            timeout=600)
         assert r.returncode == 0, r.stderr[-2000:]
-        return (d / f"{t}.s").read_text()
+        return (d / f"{t}.s").read_text(), r.stderr
 
     types = ("bf16", "f16", "f32")
     with cf.ThreadPoolExecutor(3) as ex:
@@ -168,5 +168,16 @@ def test_the_check_for_hazards_sees_them():
 def test_descriptors_of_loads_to_lds_are_settled(code, t):
     """A vector memory instruction takes a scalar that a vector instruction wrote five wait states later
     at the earliest, and the compiler does not look into instructions that are written out."""
-    loads, bad = hazards(code[t])
+    loads, bad = hazards(code[t][0])
     assert loads >= 500 and not bad, (loads, bad[:3])
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+def test_kernels_hardly_spill(code, t):
+    """Registers kept in memory, as the compiler reports them: only the gradient's epilogue on the largest
+    tiles has any (16-bit types 12 bytes a lane, floats 144), a step without one would show more."""
+    use = re.findall(r"Function Name: (\S+).*?ScratchSize \[bytes/lane\]: (\d+)", code[t][1], re.S)
+    assert len(use) >= 60
+    spilled = {n: int(s) for n, s in use if int(s)}
+    assert len(spilled) <= 1 and all(re.search(r"k_mm.*ShapeILi256.*EpGrad", n) for n in spilled), spilled
+    assert sum(spilled.values()) <= (160 if t == "f32" else 16), spilled
