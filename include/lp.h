@@ -437,6 +437,7 @@ int32_t lp_loss_labels(const lp_label_head* head, const void* u, const void* W, 
                        void* stream);
 
 /* ---- tracing (a profiling aid, not part of the method) ----
+ * (The kernels of layer steps, checkpoints and label heads are of no kind here.)
  * When enabled for a kernel kind, every launch of that kind records a pair of
  * HIP events on the launch's stream; lp_trace_read sums their elapsed times.
  * Kinds: the three sweeps of a non-coarsest MGRIT level, the coarsest-level

@@ -46,8 +46,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 using lp::f32x8;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // N consecutive values in global memory, with their element's alignment
 template <typename T, int N> struct GVec { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
@@ -1006,12 +1004,13 @@ constexpr int STAGE_BYTES = 128;
 
 // The plan with the least estimated time, from measured times of a stage (us) with one workgroup on
 // a CU and with two (of 256: two in turn; one on every CU takes 1.8). A split writes and reads its
-// partial sums (3 TB/s both ways) and takes a second launch (3 us). Measured against the other choices,
+// partial sums (3 TB/s both ways) and takes a second launch (3 us). The epilogue is not in it: short
+// contractions and heavy epilogues (gradients, losses) take up to twice the estimate. Measured against the other choices,
 // bf16: 1024 x 1024 x 4096 21 us by tiles of 64 (128: 34, 256: 89); 2048 x 2048 x 4096 39 by 128 with four
 // stages (two: 45, 64: 55, 256: 88); 4096 x 2048 x 4096 63 us by 128 with two stages (four: 75); 8192 x 4096 x
 // 4096 230 us by 256 (128: 256, 64: over 370). float: 4096 x 1024 x 1024 60 us by 128 (64: 74, 256: 134);
-// 1024 x 1024 x 4096 (columns) 68 by 128 in four splits (64 in two: 77, 256: 501); 4096 x 4096 x 4096 545 by 256
-// (128: 600 to 694, 64: 1008).
+// 1024 x 1024 x 4096 (columns) 70 by 128 in eight splits, which the estimate takes, 68 in four (64 in two: 77,
+// 256: 501); 4096 x 4096 x 4096 545 by 256 (128: 600 to 694, 64: 1008).
 inline Plan plan_of(size_t esz, long M, long N, long K) {
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
   const double stage[2][3][2] = {{{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{4.1, 8.7}, {1.8, 2.7}, {0.75, 1.15}}};
