@@ -196,3 +196,58 @@ def test_small_fp32_operands(k, B):
             ("dW", dW, d.t() @ v, d.abs().t() @ v.abs(), B, v.abs().sum(0)[None] + d.abs().sum(0)[:, None])):
         T.check(got, r, ((n + 2) * T.E32 * mag + part * o) * (1 + 2 ** -20) + T.half_step("f32") * r.abs() + T.tiny("f32"),
                 name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,ni,no", [(2 ** 24, 3, 2), (3, 2 ** 20, 5), (2, 5, 2 ** 20), (1, 2 ** 20, 33)])
+def test_steps_at_the_limits(dtype, B, ni, no):
+    """The most rows, the widest input and output (64 bits on the GPU)."""
+    g = torch.Generator("cuda").manual_seed(B)
+    dt = T.DT[dtype]
+    x, W, b, dy = (torch.randn(s, generator=g, device="cuda").mul_(f).to(dt)
+                   for s, f in (((B, ni), 1.0), ((no, ni), ni ** -0.5), ((no,), 0.3), ((B, no), 0.1)))
+    s = T.Step(dtype, "tanh", B, ni, no, 0.5)
+    y, y8, ye = s.forward(x, W, b, None, ck=True)
+    T.check(y, *T.forward(x, W, b, None, "tanh", 0.5, dtype), "y")
+    back = torch.empty_like(y)
+    L.lp_checkpoint_load(y8, ye, back)
+    q8, qe, other = torch.empty_like(y8), torch.empty_like(ye), torch.empty_like(y)
+    L.lp_checkpoint_store(y, q8, qe)
+    L.lp_checkpoint_load(q8, qe, other)
+    assert torch.equal(q8, y8) and torch.equal(qe, ye) and torch.equal(other, back)
+    got = s.backward(x, W, b, dy, False)
+    for name, a, (v, e) in zip(("dx", "dW", "db"), got, T.backward(x, W, b, dy, "tanh", 0.5, False, dtype)):
+        T.check(a, v, e, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,q,nc", [(2 ** 24, 3, 2), (3, 2 ** 20, 40), (3, 4, 2 ** 24), (1, 5, 2 ** 24)])
+def test_heads_at_the_limits(dtype, B, q, nc):
+    """The most rows, features and classes, in norms: half a step of P and of the result, and fp32 sums
+    (a probability below 2^-126 may be zero: nc 2^-126 is nothing here)."""
+    g = torch.Generator("cuda").manual_seed(nc)
+    dt = T.DT[dtype]
+    u, W, mu = (torch.randn(s, generator=g, device="cuda").mul_(f).to(dt)
+                for s, f in (((B, q), 1.0), ((nc, q), q ** -0.5), ((nc,), 0.5)))
+    lab = torch.randint(0, nc, (B,), generator=g, device="cuda")
+    if B > 2:
+        lab[1] = -1
+    hd = L.label_head(dtype, B, q, nc)
+    ws = L.alloc_loss_labels_workspace(hd)
+    J, row = torch.empty(1, device="cuda"), torch.empty(B, device="cuda")
+    out = [torch.empty(s, dtype=dt, device="cuda") for s in ((B, q), (nc, q), (nc,))]
+    L.lp_loss_labels(hd, u, W, mu, lab, J, ws, row=row, du=out[0], dW=out[1], dmu=out[2])
+    on = lab >= 0
+    n = int(on.sum())
+    z = u.double() @ W.double().t() + mu.double()
+    lse = torch.logsumexp(z, 1)
+    rows = torch.arange(B, device="cuda")
+    ref = torch.where(on, lse - z[rows, lab.clamp(min=0)], 0)
+    P = z.sub_(lse[:, None]).exp_()
+    P[rows, lab.clamp(min=0)] -= 1
+    P[~on] = 0
+    refs = [(ref.sum() / n).reshape(1), ref, P @ W.double() / n, P.t() @ u.double() / n, P.sum(0) / n]
+    half = 2 ** -8 if dtype == "bf16" else 2 ** -18
+    for name, a, r in zip(("J", "row", "du", "dW", "dmu"), [J, row] + out, refs):
+        d = float((a.double() - r).norm() / r.norm())
+        assert d <= (2 ** -18 if name in ("J", "row") else half), (name, d)
