@@ -10,10 +10,10 @@
 // workspace in the element type (the type of the next products' operands), as P times PSCALE: 2^14
 // for f16, whose range would otherwise lose the small probabilities of a large vocabulary (the least
 // normal value then stands for 3.7e-9), a power of two that the epilogues take back exactly.
-// Bound by the products: 8192 rows of 2048 features, 65536 classes bf16 6.4 ms, of which the three
-// products 525, 442 and 433 us a piece of 16384 classes (1.05, 1.24 and 1.27 PFLOP/s; the first also
-// writes the logits) and P 155 us (reading and writing, 5.2 TB/s). Losses alone of 16 rows of 4096
-// features, 131072 classes: 178 us, reading the weights at 6 TB/s.
+// Bound by the products: 8192 rows of 2048 features, 65536 classes bf16 6.5 ms, of which the three
+// products 533, 449 and 433 us a piece of 16384 classes (1.01, 1.20 and 1.24 PFLOP/s for the 98 % of the
+// rows that have a label; the first also writes the logits) and P 162 us (reading and writing, 4.9 TB/s).
+// Losses alone of 16 rows of 4096 features, 131072 classes: 179 us, reading the weights at 6 TB/s.
 // Rows without a label take no part in the gradients, whatever they hold: the labelled rows are
 // first copied together, so a product runs over n rows.
 #pragma once

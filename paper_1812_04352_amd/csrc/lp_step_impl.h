@@ -7,9 +7,9 @@
 //                                          range of f16)
 //              dx = h g W (+ dy),  dW = h g^T x,  db = h sum g (from g before its rounding)
 // Bound by the products (2 B ni no operations each): 8192 x 4096 -> 4096 bf16 forward with its
-// checkpoint 275 us (1.0 PFLOP/s), back 270 + 250 + 223 us, of which the epilogue of g takes some 40:
+// checkpoint 257 us (1.07 PFLOP/s), back 263 + 241 + 214 us, of which the epilogue of g takes some 40:
 // the largest tiles fill a CU, so nothing runs beside an epilogue. Small batches are bound by reading W
-// (one row of 4096 x 4096: 6.5 us, 5.2 TB/s) and by launches.
+// (one row of 4096 x 4096: 6.8 us, 4.9 TB/s) and by launches.
 #pragma once
 
 #include <type_traits>
