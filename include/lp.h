@@ -436,8 +436,44 @@ int32_t lp_loss_labels(const lp_label_head* head, const void* u, const void* W, 
                        double gscale, float* J, float* row, void* du, void* dW, void* dmu, void* ws, size_t ws_bytes,
                        void* stream);
 
+/* ---- gated layers ----
+ * Types, limits, streams, workspaces and reproducibility as for the layer steps above. */
+
+/* Gates of gated layers besides lp_step's activations: silu(z) = z / (1 + exp(-z)), and gelu(z) = z times
+ * the standard normal distribution function of z. */
+enum { LP_SILU = 4, LP_GELU = 5 };
+
+/* One gated layer y = sigma(x Wg^T) (x Wu^T), the product taken value by value: x [B][ni],
+ * Wg (gate) and Wu (up) [no][ni], y [B][no]. With lp_step_forward (LP_IDENTITY, r = x's residual
+ * stream) as the projection back it is the gated feed-forward block. */
+typedef struct {
+  int32_t abi_version;   /* must equal LP_ABI_VERSION */
+  int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16 */
+  int32_t act;           /* LP_TANH | LP_RELU | LP_SMOOTHRELU | LP_IDENTITY | LP_SILU | LP_GELU */
+  int32_t B;             /* rows, >= 0 (0: nothing to do; weight gradients are zero) */
+  int32_t ni, no;        /* input and output width, >= 1 */
+} lp_gated;
+
+/* Workspace bytes of lp_gated_forward, with grad != 0 of both calls; 0 for an invalid layer. It
+ * holds copies of x and the weights (used where their rows do not start on 16 bytes), the partial sums of
+ * split products and, with grad, both pre-activations' gradients. */
+size_t lp_gated_workspace_bytes(const lp_gated* layer, int32_t grad);
+
+/* The layer: both products, the activation and their product in one kernel (two with a split
+ * contraction). */
+int32_t lp_gated_forward(const lp_gated* layer, const void* x, const void* Wg, const void* Wu, void* y, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* Gradients of the layer for dy [B][no], from its inputs (zg = x Wg^T and zu = x Wu^T are formed again):
+ *   dzg = dy zu sigma'(zg),  dzu = dy sigma(zg)   (rounded to the dtype for the next products)
+ *   dx  = dzg Wg + dzu Wu   [B][ni]   (one sum, rounded once)
+ *   dWg = dzg^T x,  dWu = dzu^T x   [no][ni]
+ * dx, dWg, dWu nullable: not wanted. Outputs must not alias inputs. */
+int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, const void* Wu, const void* dy, void* dx,
+                          void* dWg, void* dWu, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- tracing (a profiling aid, not part of the method) ----
- * (The kernels of layer steps, checkpoints and label heads are of no kind here.)
+ * (The kernels of layer steps, checkpoints, label heads and gated layers are of no kind here.)
  * When enabled for a kernel kind, every launch of that kind records a pair of
  * HIP events on the launch's stream; lp_trace_read sums their elapsed times.
  * Kinds: the three sweeps of a non-coarsest MGRIT level, the coarsest-level

@@ -1,0 +1,148 @@
+// Host side of the gated layers (include/lp.h): argument checks, workspace layouts, dispatch by
+// element type.
+#include <math.h>
+
+#include <algorithm>
+
+#include "../../include/lp.h"
+#include "lp_internal.h"
+#include "lp_mm.h"
+
+namespace {
+
+using lp::check_ws;
+using lp::fail;
+using lp::hip_fail;
+
+constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+// Limits as for the layer steps (lp_step_host.cpp): 32-bit index arithmetic inside a tile stays far from its own.
+constexpr int kMaxRows = 1 << 24, kMaxWidth = 1 << 20;
+constexpr double kMaxValues = 34359738368.0;  // 2^35
+
+size_t esize(int32_t d) { return d == LP_F32 ? 4 : 2; }
+
+int check_type(int32_t abi, int32_t dtype) {
+  if (abi != LP_ABI_VERSION) return fail(LP_EINVAL, "abi_version %d != %d", abi, LP_ABI_VERSION);
+  if (dtype == LP_F64) return fail(LP_EUNSUPPORTED, "no kernel for dtype LP_F64 (LP_F32, LP_BF16, LP_F16)");
+  if (dtype != LP_F32 && dtype != LP_BF16 && dtype != LP_F16) return fail(LP_EINVAL, "bad dtype %d", dtype);
+  return LP_OK;
+}
+
+int check_rows(int32_t B) {
+  if (B < 0) return fail(LP_EINVAL, "B = %d < 0", B);
+  if (B > kMaxRows) return fail(LP_EUNSUPPORTED, "B = %d > %d", B, kMaxRows);
+  return LP_OK;
+}
+
+int check_gated(const lp_gated* g) {
+  if (!g) return fail(LP_EINVAL, "layer is NULL");
+  int rc = check_type(g->abi_version, g->dtype);
+  if (rc) return rc;
+  if (g->act < LP_TANH || g->act > LP_GELU) return fail(LP_EINVAL, "bad activation %d", g->act);
+  if ((rc = check_rows(g->B))) return rc;
+  if (g->ni < 1 || g->no < 1) return fail(LP_EINVAL, "bad widths ni = %d, no = %d", g->ni, g->no);
+  if (g->ni > kMaxWidth || g->no > kMaxWidth)
+    return fail(LP_EUNSUPPORTED, "widths ni = %d, no = %d > %d", g->ni, g->no, kMaxWidth);
+  if (std::max({(double)g->B * g->no, (double)g->B * g->ni, (double)g->no * g->ni}) > kMaxValues)
+    return fail(LP_EUNSUPPORTED, "more than 2^35 values in an array");
+  return LP_OK;
+}
+
+// whether two of n arrays (nullable) are the same
+bool any_same(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (auto o = outs.begin(); o != outs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* i : ins)
+      if (*o == i) return true;
+    for (auto p = outs.begin(); p != o; ++p)
+      if (*o == *p) return true;
+  }
+  return false;
+}
+
+// Offsets of a workspace's parts
+struct Parts {
+  size_t at = 0;
+  size_t take(size_t bytes) {
+    const size_t r = at;
+    at += up(bytes);
+    return r;
+  }
+  size_t total() const { return std::max<size_t>(at, 256); }
+};
+
+}  // namespace
+
+namespace lp {
+
+GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad) {
+  const size_t e = esize(dtype), row = mm::padded(e, ni) * e;
+  const int two = 2 * mm::ceil_div(no, mm::PAIR_BLOCK) * mm::PAIR_BLOCK;
+  GatedLayout l{};
+  // (a pair's tile holds half a tile's features of each: the tiles of a product of 2 no features)
+  l.z = mm::plan_of(e, B, 2L * no, ni);
+  if (B == 1 && !grad) l.z = mm::Plan{1, 1, 1, mm::ceil_div(no, mm::one_features(2L * no) / 2)};
+  size_t part = l.z.part_bytes();
+  Parts p;
+  if (grad) {
+    l.zx = mm::plan_of(e, B, ni, two);
+    l.zw = mm::plan_of(e, two, ni, B);
+    part = std::max({part, l.zx.part_bytes(), l.zw.part_bytes()});
+    // (and the layer itself, whose plan differs for one row only and then has no sums to join)
+    l.dz = p.take((size_t)B * two * e);
+  }
+  l.x = p.take(B * row);
+  l.Wg = p.take(no * row);
+  l.Wu = p.take(no * row);
+  l.part = p.take(part);
+  l.total = p.total();
+  return l;
+}
+
+}  // namespace lp
+
+#define LP_BY_TYPE(dtype, call, ...)                     \
+  ((dtype) == LP_F32    ? lp::call##_f32(__VA_ARGS__)    \
+   : (dtype) == LP_BF16 ? lp::call##_bf16(__VA_ARGS__)   \
+                        : lp::call##_f16(__VA_ARGS__))
+
+extern "C" {
+
+size_t lp_gated_workspace_bytes(const lp_gated* g, int32_t grad) {
+  if (check_gated(g) != LP_OK) return 0;
+  lp::clear_error();
+  return lp::gated_layout(g->dtype, g->B, g->ni, g->no, grad != 0).total;
+}
+
+int32_t lp_gated_forward(const lp_gated* g, const void* x, const void* Wg, const void* Wu, void* y, void* ws,
+                         size_t ws_bytes, void* stream) {
+  int rc = check_gated(g);
+  if (rc) return rc;
+  if (!Wg || !Wu || (g->B && (!x || !y))) return fail(LP_EINVAL, "NULL array argument");
+  if (g->B && any_same({y}, {x, Wg, Wu})) return fail(LP_EINVAL, "y aliases an input");
+  if ((rc = check_ws(ws, ws_bytes, lp::gated_layout(g->dtype, g->B, g->ni, g->no, false).total))) return rc;
+  if (g->B == 0) return LP_OK;
+  lp::GatedArgs a{};
+  a.dtype = g->dtype, a.act = g->act, a.B = g->B, a.ni = g->ni, a.no = g->no;
+  a.x = x, a.Wg = Wg, a.Wu = Wu, a.y = y, a.ws = ws;
+  const hipError_t e = LP_BY_TYPE(g->dtype, gated_forward, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? LP_OK : hip_fail(e, "gated forward");
+}
+
+int32_t lp_gated_backward(const lp_gated* g, const void* x, const void* Wg, const void* Wu, const void* dy, void* dx,
+                          void* dWg, void* dWu, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_gated(g);
+  if (rc) return rc;
+  if (!Wg || !Wu || (g->B && (!x || !dy))) return fail(LP_EINVAL, "NULL array argument");
+  if (any_same({dx, dWg, dWu}, {x, Wg, Wu, dy})) return fail(LP_EINVAL, "an output aliases an input or another output");
+  if ((rc = check_ws(ws, ws_bytes, lp::gated_layout(g->dtype, g->B, g->ni, g->no, true).total))) return rc;
+  if (!dx && !dWg && !dWu) return LP_OK;
+  lp::GatedArgs a{};
+  a.dtype = g->dtype, a.act = g->act, a.B = g->B, a.ni = g->ni, a.no = g->no;
+  a.x = x, a.Wg = Wg, a.Wu = Wu, a.dy = dy, a.dx = dx, a.dWg = dWg, a.dWu = dWu, a.ws = ws;
+  const hipError_t e = LP_BY_TYPE(g->dtype, gated_backward, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? LP_OK : hip_fail(e, "gated backward");
+}
+
+}  // extern "C"

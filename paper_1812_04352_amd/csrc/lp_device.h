@@ -8,7 +8,8 @@
 
 namespace lp {
 
-enum Act { ACT_TANH = 0, ACT_RELU = 1, ACT_SMOOTHRELU = 2, ACT_IDENTITY = 3 };
+enum Act { ACT_TANH = 0, ACT_RELU = 1, ACT_SMOOTHRELU = 2, ACT_IDENTITY = 3,
+           ACT_SILU = 4, ACT_GELU = 5 };  // (the last two in gated layers only)
 
 // tanh: the device library's accurate tanh. sigma'(z) = 1 - tanh(z)^2.
 __device__ __forceinline__ float dev_tanh(float z) { return tanhf(z); }

@@ -295,6 +295,30 @@ LP_STEP_LAUNCHERS(f16)
 LP_STEP_LAUNCHERS(f32)
 #undef LP_STEP_LAUNCHERS
 
+// ---- layer norm, gated layers, orthogonalised updates ----
+struct GatedArgs {
+  int dtype, act;
+  int B, ni, no;
+  const void *x, *Wg, *Wu;  // [B][ni], [no][ni] each
+  void* y;                  // forward: [B][no]
+  const void* dy;           // backward: [B][no]
+  void *dx, *dWg, *dWu;     // nullable
+  void* ws;
+};
+struct GatedLayout {
+  size_t dz, x, Wg, Wu, part, total;
+  mm::Plan z, zx, zw;  // the pair x Wg^T, x Wu^T, and dz W, dz^T x
+};
+GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad);
+
+#define LP_GATED_LAUNCHERS(T)                                      \
+  hipError_t gated_forward_##T(const GatedArgs& a, hipStream_t st); \
+  hipError_t gated_backward_##T(const GatedArgs& a, hipStream_t st);
+LP_GATED_LAUNCHERS(bf16)
+LP_GATED_LAUNCHERS(f16)
+LP_GATED_LAUNCHERS(f32)
+#undef LP_GATED_LAUNCHERS
+
 // Error reporting shared by the host translation units (lp_host.cpp): sets the thread's
 // last error and returns the code.
 int fail(int code, const char* fmt, ...);

@@ -187,29 +187,99 @@ struct Stage {
   // scalar instructions: tests/test_wide_code.py reads the generated code for it. Waiting for them here
   // costs the large products 1 %.)
   __device__ __forceinline__ void load(unsigned char* lds, int wave) {
+    last_stage();
+    request<0, PER>(base, left, lds, wave);
+    advance();
+  }
+  __device__ __forceinline__ void last_stage() {  // (it ends with the contraction)
+    if (!COLS && k + BK > k1) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) off[i] = k + kc >= k1 ? 0x80000000u : off[i];
+    }
+  }
+  __device__ __forceinline__ void advance() {
+    base += step;
+    left -= step;
+    k += BK;
+  }
+  // the thread's chunks I0 .. I1 - 1
+  template <int I0, int I1>
+  __device__ __forceinline__ void request(const unsigned char* base, long left, unsigned char* lds, int wave) {
 #ifdef __HIP_DEVICE_COMPILE__
     typedef int i32x4 __attribute__((ext_vector_type(4)));
     const uint64_t at = reinterpret_cast<uint64_t>(base);
     const i32x4 r = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xffff, (left >> 31) != 0 ? 0x7fffffff : (int)left, 0x00020000};
     const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds + wave * 1024;
-    if (!COLS && k + BK > k1) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) off[i] = k + kc >= k1 ? 0x80000000u : off[i];
-    }
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"  // (m0 is reserved: a note that it may be needed around the statement, where nothing holds it)
 #pragma unroll
-    for (int i = 0; i < PER; ++i)
+    for (int i = I0; i < I1; ++i)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * NT * 16), "v"(off[i]),
                    "s"(r)
                    : "m0", "memory");
 #pragma clang diagnostic pop
-    base += step;
-    left -= step;
-    k += BK;
 #endif
   }
+};
 
+// The weights' tile of a pair of arrays of rows of the same shape: RR rows of the first, then the same
+// rows of the second.
+template <typename T, int R, int KB, int NT>
+struct PairRows : Stage<T, R / 2, KB, NT, false> {
+  typedef Stage<T, R / 2, KB, NT, false> S;
+  static constexpr int PER = 2 * S::PER;
+  long hop;  // from the first array to the second
+  __device__ __forceinline__ void start(const void* p, const void* p2, long ld, int r0, int rows, int k0, int k1) {
+    S::start(p, ld, r0, rows, k0, k1);
+    hop = static_cast<const unsigned char*>(p2) - static_cast<const unsigned char*>(p);
+  }
+  __device__ __forceinline__ void load(unsigned char* lds, int wave) {
+    this->last_stage();
+    this->template request<0, S::PER>(this->base, this->left, lds, wave);
+    this->template request<0, S::PER>(this->base + hop, this->left, lds + R / 2 * KB, wave);
+    this->advance();
+  }
+};
+
+// The tile of a pair of arrays of `rows` columns whose contraction indices alternate: PAIR_BLOCK rows of the
+// first, the same rows of the second, and so on, zeros behind the kw rows that each has. A stage of
+// 16-bit values holds a block of each, one of floats a block of either in turn. (k0: a multiple of a stage.)
+constexpr int PAIR_BLOCK = 32;
+template <typename T, int R, int KB, int NT>
+struct PairCols : Stage<T, R, KB, NT, true> {
+  typedef Stage<T, R, KB, NT, true> S;
+  static constexpr bool BOTH = S::BK == 2 * PAIR_BLOCK;
+  static_assert(BOTH || S::BK == PAIR_BLOCK, "whole blocks");
+  static_assert(!BOTH || (S::PER % 2 == 0 && S::PER / 2 * NT / S::CH == PAIR_BLOCK), "a load's chunks lie in one block");
+  long hop, lhop;  // BOTH: from the first array to the second; else what the next stage adds to base and takes off left
+  __device__ __forceinline__ void start(const void* p, const void* p2, long ld, int r0, int rows, int kw, int k0) {
+    const int k = k0 / (2 * PAIR_BLOCK) * PAIR_BLOCK;  // the row of both arrays that k0 lies in
+    S::start(p, ld, r0, rows, k, kw);
+    hop = static_cast<const unsigned char*>(p2) - static_cast<const unsigned char*>(p);
+    this->step = PAIR_BLOCK * ld * (long)sizeof(T);
+    if constexpr (BOTH) {
+      const uint32_t back = (uint32_t)(PAIR_BLOCK * ld * (long)sizeof(T));
+#pragma unroll
+      for (int i = S::PER / 2; i < S::PER; ++i) this->off[i] -= back;
+    } else {
+      lhop = 0;
+      if (k0 / PAIR_BLOCK % 2) turn();
+    }
+  }
+  __device__ __forceinline__ void turn() {  // the other array's rows are next
+    this->base += hop, this->left -= lhop;
+    hop = this->step - hop, lhop = this->step - lhop;
+  }
+  __device__ __forceinline__ void load(unsigned char* lds, int wave) {
+    if constexpr (BOTH) {
+      this->template request<0, S::PER / 2>(this->base, this->left, lds, wave);
+      this->template request<S::PER / 2, S::PER>(this->base + hop, this->left, lds, wave);
+      this->base += this->step, this->left -= this->step;
+    } else {
+      this->template request<0, S::PER>(this->base, this->left, lds, wave);
+      turn();
+    }
+  }
 };
 
 // Reads a wave's fragments of one operand: NF blocks of 32 rows of D from row r0 of the tile on.
@@ -272,6 +342,8 @@ struct Prob {
   int count_m, count_k;
   int tm, tn;        // tiles of D
   int kper;          // contraction per split (grid y), a multiple of a stage's
+  const void* B2 = nullptr;  // pairs of arrays: the second one
+  int kw = 0;                // PAIR_COLS: rows of each
 };
 
 // A wave's LDS writes before its other lanes' reads and the other way round: the wave's accesses are
@@ -322,15 +394,40 @@ __device__ __forceinline__ void tile_of(int id, int tm, int tn, int& mt, int& nt
   nt = in / rows;
 }
 
+// Tiles of a symmetric D on and below its diagonal, tm (tm + 1) / 2 of them: a run of tile rows an XCD.
+__device__ __forceinline__ void tile_below(int id, int tm, int& mt, int& nt) {
+  const int total = tm * (tm + 1) / 2, q = total / 8, r = total % 8, x = id % 8;
+  const int at = x * q + min(x, r) + id / 8;
+  mt = (int)((sqrtf(8.f * (float)at + 1.f) - 1.f) * 0.5f);  // (off by one at most: settled below)
+  while ((mt + 1) * (mt + 2) / 2 <= at) ++mt;
+  while (mt * (mt + 1) / 2 > at) --mt;
+  nt = at - mt * (mt + 1) / 2;
+}
+
+// What B is: one array; a pair of arrays in rows, D1 and D2 formed side by side, half a tile's features
+// of each (an epilogue finds those of D1 in block column 0, those of D2 in block column 1); a pair of arrays in
+// columns whose contraction indices alternate by PAIR_BLOCK.
+enum { PAIR_NONE = 0, PAIR_ROWS = 1, PAIR_COLS = 2 };
+
 // Tile shapes: BM x BN values of D by WGM x WGN waves; NS stages of KB bytes in LDS; fragments
 // are read GK steps at a time, a group ahead of their products.
 template <int BM_, int BN_, int WGM_, int WGN_, int KB_, int NS_, int GK_>
 struct Shape {
+  static constexpr int PAIR = PAIR_NONE, BNO = BN_;  // BNO: features of D a tile
+  static constexpr bool SYM = false;
   static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, KB = KB_, NS = NS_, GK = GK_, NT = 64 * WGM_ * WGN_;
   // waves a SIMD has to hold: two workgroups of four waves where their LDS fits twice
   static constexpr int WAVES = NT == 512 || 2 * NS_ * (BM_ + BN_) * KB_ <= 160 * 1024 ? 2 : 1;
   static_assert((NS & (NS - 1)) == 0, "a stage's place is its index modulo NS");
 };
+
+// The same tiles for a pair of arrays
+template <class S, int PAIR_>
+struct PairShape : S {
+  static constexpr int PAIR = PAIR_, BNO = PAIR_ == PAIR_ROWS ? S::BN / 2 : S::BN;
+  static_assert(PAIR_ != PAIR_ROWS || S::BN / S::WGN == 64, "one block column of each");
+};
+template <class S, int PAIR> using Paired = std::conditional_t<PAIR == PAIR_NONE, S, PairShape<S, PAIR>>;
 
 // All but N of the wave's loads to LDS have landed, and every wave is here. (The compiler does not
 // count those loads: nothing else waits for them.)
@@ -351,15 +448,16 @@ __device__ __forceinline__ Place place(const Prob& p, int id, int wave, int& K) 
     if (p.count_m) c.M = min(c.M, n);
     if (p.count_k) K = min(K, n);
   }
-  tile_of(id, p.tm, p.tn, c.mt, c.nt);
+  if constexpr (S::SYM) tile_below(id, p.tm, c.mt, c.nt);
+  else tile_of(id, p.tm, p.tn, c.mt, c.nt);
   c.m0 = c.mt * S::BM;
-  c.n0 = c.nt * S::BN;
-  c.lim = min(c.N, c.n0 + S::BN);
+  c.n0 = c.nt * S::BNO;
+  c.lim = min(c.N, c.n0 + S::BNO);
   c.lane = threadIdx.x & 63;
   c.wm = wave / S::WGN;
   c.wn = wave % S::WGN;
   c.mw = c.m0 + c.wm * (S::BM / S::WGM);
-  c.nw = c.n0 + c.wn * (S::BN / S::WGN);
+  c.nw = c.n0 + c.wn * (S::BNO / S::WGN);
   c.split = blockIdx.y;
   return c;
 }
@@ -377,7 +475,11 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
   constexpr int NG = KB / (16 * (int)sizeof(T)) / GK;
   static_assert(NG % 2 == 0, "the fragment sets alternate within a stage");
   typedef Stage<T, BM, KB, NT, AT> SA;
-  typedef Stage<T, BN, KB, NT, BT> SB;
+  constexpr int PAIR = S::PAIR;
+  static_assert(PAIR == PAIR_NONE || BT == (PAIR == PAIR_COLS), "how the pair lies");
+  typedef std::conditional_t<PAIR == PAIR_ROWS, PairRows<T, BN, KB, NT>,
+                             std::conditional_t<PAIR == PAIR_COLS, PairCols<T, BN, KB, NT>, Stage<T, BN, KB, NT, BT>>>
+      SB;
   constexpr int LOADS = SA::PER + SB::PER;
   auto& lds = stages.at;
   static_assert(epilogue_lds(WGM * WGN, BM, WGN) <= NS * (BM + BN) * KB, "the epilogue's LDS");
@@ -388,7 +490,8 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
   const int k0 = blockIdx.y * p.kper, k1 = min(K, k0 + p.kper);
   const int steps = k1 > k0 ? (k1 - k0 + SA::BK - 1) / SA::BK : 0;
   const Reader<T, SA, KB, FM, AT> ra(c.wm * (BM / WGM), c.lane);
-  const Reader<T, SB, KB, FN, BT> rb(c.wn * (BN / WGN), c.lane);
+  // (of a pair in rows: the blocks of both halves, which lie BN / 2 rows apart)
+  const Reader<T, Stage<T, BN, KB, NT, BT>, KB, PAIR == PAIR_ROWS ? 1 : FN, BT> rb(c.wn * (S::BNO / WGN), c.lane);
   f32x16 acc[FM][FN];
   // The contraction. A group's fragments are read during the products of the group before; the
   // last group of a stage reads the next stage's first fragments, behind the stage's one barrier:
@@ -398,7 +501,9 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
     SA sa;
     SB sb;
     sa.start(p.A, p.lda, c.m0, c.M, k0, k1);
-    sb.start(p.B, p.ldb, c.n0, c.N, k0, k1);
+    if constexpr (PAIR == PAIR_ROWS) sb.start(p.B, p.B2, p.ldb, c.n0, c.N, k0, k1);
+    else if constexpr (PAIR == PAIR_COLS) sb.start(p.B, p.B2, p.ldb, c.n0, c.N, p.kw, k0);
+    else sb.start(p.B, p.ldb, c.n0, c.N, k0, k1);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -411,7 +516,8 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
 #pragma unroll
         for (int i = 0; i < FM; ++i) fa[to][k][i] = ra(la, i, g * GK + k);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) fb[to][k][j] = rb(la + BM * KB, j, g * GK + k);
+        for (int j = 0; j < FN; ++j)
+          fb[to][k][j] = PAIR == PAIR_ROWS ? rb(la + (BM + j * (BN / 2)) * KB, 0, g * GK + k) : rb(la + BM * KB, j, g * GK + k);
       }
     };
     const auto request = [&](int s) {
@@ -510,7 +616,7 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
   __syncthreads();  // the epilogue may use the stages' LDS
   float* el = reinterpret_cast<float*>(&lds[0][0]);
   // whole quads of features everywhere: straight-line code, no test per quad
-  if (c.n0 + BN <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, el);
+  if (c.n0 + S::BNO <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, el);
   else E::template run<false, FM, FN, WGM, WGN>(ea, c, acc, el);
 }
 
@@ -773,7 +879,7 @@ __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int
         }
     }
   }
-  if (c.n0 + S::BN <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, lds);
+  if (c.n0 + S::BNO <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, lds);
   else E::template run<false, FM, FN, WGM, WGN>(ea, c, acc, lds);
 }
 
@@ -788,19 +894,23 @@ __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int
 // two to four rows on the vector ALU 21, where split tiles still take 12.)
 inline int one_features(long N) { return N <= 16384 ? 8 : 16; }
 
-template <typename T, int NF, class E>
+// PAIR: of a pair of weight arrays in rows, NF rows of the two together a workgroup, a wave those of one feature.
+template <typename T, int NF, class E, bool PAIR = false>
 __global__ __launch_bounds__(32 * NF) void k_one(Prob p, typename E::Args ea) {
-  constexpr int V = 16 / (int)sizeof(T), RUN = 64 * V, R = 2, U = 4;
+  constexpr int V = 16 / (int)sizeof(T), RUN = 64 * V, R = 2, U = 4, FN = PAIR ? 2 : 1, NFO = NF / FN;
   typedef typename GVec<T, V>::type GChunk;
   __shared__ __attribute__((aligned(16))) float lds[epilogue_lds(1, 32, 1) / 4];
-  __shared__ float sums[32];
+  __shared__ float sums[32 * FN];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (p.count && *p.count == 0) return;
-  const int n0 = blockIdx.x * NF;
+  const int n0 = blockIdx.x * NFO;
   const T* a = static_cast<const T*>(p.A);
   const T* b[R];
 #pragma unroll
-  for (int j = 0; j < R; ++j) b[j] = static_cast<const T*>(p.B) + (long)min(n0 + wave * R + j, p.N - 1) * p.ldb;
+  for (int j = 0; j < R; ++j) {
+    if constexpr (PAIR) b[j] = static_cast<const T*>(j ? p.B2 : p.B) + (long)min(n0 + wave, p.N - 1) * p.ldb;
+    else b[j] = static_cast<const T*>(p.B) + (long)min(n0 + wave * R + j, p.N - 1) * p.ldb;
+  }
   float acc[R] = {};
   const auto add = [&](const GChunk (&w)[R], const GChunk& x) {
 #pragma unroll
@@ -837,25 +947,27 @@ __global__ __launch_bounds__(32 * NF) void k_one(Prob p, typename E::Args ea) {
     }
     add(w, x);
   }
-  if (threadIdx.x < 32) sums[threadIdx.x] = 0.f;
+  if (threadIdx.x < 32 * FN) sums[threadIdx.x] = 0.f;
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < R; ++j) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) acc[j] += __shfl_xor(acc[j], o, 64);
-    if (lane == 0) sums[wave * R + j] = acc[j];
+    if (lane == 0) sums[PAIR ? 32 * j + wave : wave * R + j] = acc[j];
   }
   __syncthreads();
   if (wave) return;
   // lane l's quad q: row m = l % 32 (of which there is one), features 8 q + 4 (l / 32) ..
-  f32x16 d[1][1];
+  f32x16 d[1][FN];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) d[0][0][r] = sums[8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)];
+  for (int j = 0; j < FN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) d[0][j][r] = sums[32 * j + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)];
   Place c;
-  c.M = 1, c.N = p.N, c.lim = min(p.N, n0 + NF), c.m0 = 0, c.n0 = n0, c.mw = 0, c.nw = n0, c.wm = 0, c.wn = 0;
+  c.M = 1, c.N = p.N, c.lim = min(p.N, n0 + NFO), c.m0 = 0, c.n0 = n0, c.mw = 0, c.nw = n0, c.wm = 0, c.wn = 0;
   c.mt = 0, c.nt = blockIdx.x, c.split = 0, c.lane = lane;
-  if (n0 + 32 <= c.lim) E::template run<true, 1, 1, 1, 1>(ea, c, d, lds);
-  else E::template run<false, 1, 1, 1, 1>(ea, c, d, lds);
+  if (n0 + 32 <= c.lim) E::template run<true, 1, FN, 1, 1>(ea, c, d, lds);
+  else E::template run<false, 1, FN, 1, 1>(ea, c, d, lds);
 }
 
 // out[n] = f * scale[0] * sum over tile rows of part[t][n], in fp64 and in order (64 columns by 4
@@ -955,6 +1067,16 @@ inline int padded(size_t esz, int n) {
   return ceil_div(n, unit) * unit;
 }
 
+template <typename T>
+hipError_t launch_repack(const T* in0, T* out0, size_t rows0, const T* in1, T* out1, size_t rows1, int cols, int ld, hipStream_t st) {
+  int shift = 0;
+  while (shift < 8 && (1 << shift) < ld * (int)sizeof(T) / 16) ++shift;
+  const size_t blocks = (rows0 + rows1 + (256 >> shift) - 1) / (256 >> shift);
+  k_repack<T><<<(unsigned)std::min<size_t>(blocks, 1u << 20), 256, 0, st>>>(in0, out0, (long)rows0, in1, out1, (long)rows1, cols, ld,
+                                                                          shift);
+  return hipGetLastError();
+}
+
 // Two operands of rows of `cols` values as the products need them: the caller's arrays where their
 // rows start on 16 bytes, else copies in the workspace (one launch for both).
 template <typename T>
@@ -979,15 +1101,9 @@ struct Operands {
         ld[i] = lp;
       }
     }
-    const size_t all = rows[0] + rows[1];
-    if (all == 0) return;
-    int shift = 0;
-    while (shift < 8 && (1 << shift) < lp * (int)sizeof(T) / 16) ++shift;
-    const size_t blocks = (all + (256 >> shift) - 1) / (256 >> shift);
-    k_repack<T><<<(unsigned)std::min<size_t>(blocks, 1u << 20), 256, 0, st>>>(
-        static_cast<const T*>(in0), static_cast<T*>(copy0), (long)rows[0], static_cast<const T*>(in1), static_cast<T*>(copy1),
-        (long)rows[1], cols, lp, shift);
-    e = hipGetLastError();
+    if (rows[0] + rows[1])
+      e = launch_repack<T>(static_cast<const T*>(in0), static_cast<T*>(copy0), rows[0], static_cast<const T*>(in1),
+                           static_cast<T*>(copy1), rows[1], cols, lp, st);
   }
 };
 
@@ -1000,6 +1116,9 @@ typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;  // (eight stages are no faster: 
 typedef Shape<256, 256, 2, 4, 128, 2, 1> Tile256f;  // float: two steps a stage; bound by the split's vector instructions
 typedef Shape<128, 128, 2, 2, 128, 2, 1> Tile128f;
 typedef Shape<64, 64, 2, 2, 128, 4, 1> Tile64f;
+// of a pair of arrays in rows: 32 features of each, a wave holds both products of its rows
+typedef Shape<64, 64, 2, 1, 128, 4, 2> Tile64p;
+typedef Shape<64, 64, 2, 1, 128, 4, 1> Tile64pf;
 constexpr int STAGE_BYTES = 128;
 
 // The plan with the least estimated time, from measured times of a stage (us) with one workgroup on
@@ -1060,33 +1179,38 @@ hipError_t launch_shape(Prob p, const typename E::Args& ea, const Plan& pl, void
     k_mm<T, S, AT, BT, E><<<dim3(tiles), S::NT, 0, st>>>(p, ea);
   } else if constexpr (S::BM < 256) {
     k_mm<T, S, AT, BT, EpRaw><<<dim3(tiles, (unsigned)pl.splits), S::NT, 0, st>>>(p, EpRaw::Args{static_cast<f32x4*>(part)});
-    k_finish<Shape<S::BM, S::BN, S::WGM, S::WGN, 128, 2, 2>, E><<<dim3(tiles), S::NT, 0, st>>>(p, static_cast<const f32x4*>(part), pl.splits, ea);
+    k_finish<Paired<Shape<S::BM, S::BN, S::WGM, S::WGN, 128, 2, 2>, S::PAIR>, E><<<dim3(tiles), S::NT, 0, st>>>(p, static_cast<const f32x4*>(part), pl.splits, ea);
   }
   return hipGetLastError();
 }
 
 // part: pl.part_bytes() of workspace. Epilogues of products that one row may have (ONE) come in one-row kernels too.
-template <typename T, bool AT, bool BT, class E>
+template <typename T, bool AT, bool BT, class E, int PAIR = PAIR_NONE>
 hipError_t launch_mm(const Prob& p, const typename E::Args& ea, const Plan& pl, void* part, hipStream_t st) {
   if constexpr (!AT && !BT && E::ONE) {
     if (pl.tile == 1) {
-      if (ea.blocks_of_32()) k_one<T, 32, E><<<(unsigned)ceil_div(p.N, 32), 1024, 0, st>>>(p, ea);
-      else if (one_features(p.N) == 8) k_one<T, 8, E><<<(unsigned)pl.tn, 256, 0, st>>>(p, ea);
-      else k_one<T, 16, E><<<(unsigned)pl.tn, 512, 0, st>>>(p, ea);
+      if constexpr (PAIR == PAIR_ROWS) {
+        if (one_features(2L * p.N) == 8) k_one<T, 8, E, true><<<(unsigned)pl.tn, 256, 0, st>>>(p, ea);
+        else k_one<T, 16, E, true><<<(unsigned)pl.tn, 512, 0, st>>>(p, ea);
+      } else {
+        if (ea.blocks_of_32()) k_one<T, 32, E><<<(unsigned)ceil_div(p.N, 32), 1024, 0, st>>>(p, ea);
+        else if (one_features(p.N) == 8) k_one<T, 8, E><<<(unsigned)pl.tn, 256, 0, st>>>(p, ea);
+        else k_one<T, 16, E><<<(unsigned)pl.tn, 512, 0, st>>>(p, ea);
+      }
       return hipGetLastError();
     }
   }
   if constexpr (sizeof(T) == 2) {
-    if (pl.tile == 256) return launch_shape<T, Tile256, AT, BT, E>(p, ea, pl, part, st);
+    if (pl.tile == 256) return launch_shape<T, Paired<Tile256, PAIR>, AT, BT, E>(p, ea, pl, part, st);
     if (pl.tile == 128) {
-      if ((long)pl.tm * pl.tn * pl.splits <= 256) return launch_shape<T, Tile128d, AT, BT, E>(p, ea, pl, part, st);
-      return launch_shape<T, Tile128, AT, BT, E>(p, ea, pl, part, st);
+      if ((long)pl.tm * pl.tn * pl.splits <= 256) return launch_shape<T, Paired<Tile128d, PAIR>, AT, BT, E>(p, ea, pl, part, st);
+      return launch_shape<T, Paired<Tile128, PAIR>, AT, BT, E>(p, ea, pl, part, st);
     }
-    return launch_shape<T, Tile64, AT, BT, E>(p, ea, pl, part, st);
+    return launch_shape<T, Paired<std::conditional_t<PAIR == PAIR_ROWS, Tile64p, Tile64>, PAIR>, AT, BT, E>(p, ea, pl, part, st);
   } else {
-    if (pl.tile == 256) return launch_shape<T, Tile256f, AT, BT, E>(p, ea, pl, part, st);
-    if (pl.tile == 128) return launch_shape<T, Tile128f, AT, BT, E>(p, ea, pl, part, st);
-    return launch_shape<T, Tile64f, AT, BT, E>(p, ea, pl, part, st);
+    if (pl.tile == 256) return launch_shape<T, Paired<Tile256f, PAIR>, AT, BT, E>(p, ea, pl, part, st);
+    if (pl.tile == 128) return launch_shape<T, Paired<Tile128f, PAIR>, AT, BT, E>(p, ea, pl, part, st);
+    return launch_shape<T, Paired<std::conditional_t<PAIR == PAIR_ROWS, Tile64pf, Tile64f>, PAIR>, AT, BT, E>(p, ea, pl, part, st);
   }
 }
 

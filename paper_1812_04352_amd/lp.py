@@ -23,6 +23,7 @@ LP_F32, LP_F64 = 0, 1
 LP_BF16, LP_F16 = 2, 3  # layer steps, checkpoints and label heads only
 LP_DENSE, LP_CONV3X3 = 0, 1
 LP_TANH, LP_RELU, LP_SMOOTHRELU, LP_IDENTITY = 0, 1, 2, 3
+LP_SILU, LP_GELU = 4, 5  # gated layers only
 LP_RELAX_F, LP_RELAX_FCF, LP_RELAX_FCFCF = 0, 1, 2
 LP_CYCLE_V, LP_CYCLE_F = 0, 1
 LP_STATE, LP_ADJOINT = 0, 1
@@ -30,6 +31,7 @@ LP_OPEN_IDENTITY, LP_OPEN_DENSE_ACT, LP_OPEN_CONV_ACT = 0, 1, 2
 LP_STORE_ALL, LP_STORE_CPOINTS = 0, 1
 
 ACT = {"tanh": LP_TANH, "relu": LP_RELU, "smoothrelu": LP_SMOOTHRELU, "identity": LP_IDENTITY}
+GATE = {**ACT, "silu": LP_SILU, "gelu": LP_GELU}
 LAYER = {"dense": LP_DENSE, "conv3x3": LP_CONV3X3}
 RELAX = {"F": LP_RELAX_F, "FCF": LP_RELAX_FCF, "FCFCF": LP_RELAX_FCFCF}
 CYCLE = {"V": LP_CYCLE_V, "F": LP_CYCLE_F}
@@ -44,6 +46,7 @@ EXPORTS = (
     "lp_trace_enable", "lp_trace_read",
     "lp_step_workspace_bytes", "lp_step_forward", "lp_step_backward", "lp_checkpoint_store", "lp_checkpoint_load",
     "lp_loss_labels_workspace_bytes", "lp_loss_labels",
+    "lp_gated_workspace_bytes", "lp_gated_forward", "lp_gated_backward",
 )
 
 
@@ -75,6 +78,11 @@ class LpLabelHead(ctypes.Structure):
                 ("q", ctypes.c_int32), ("nc", ctypes.c_int32)]
 
 
+class LpGated(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
+                ("B", ctypes.c_int32), ("ni", ctypes.c_int32), ("no", ctypes.c_int32)]
+
+
 class LpError(RuntimeError):
     def __init__(self, status: int, call: str, detail: str):
         super().__init__(f"{call}: status {status} ({detail})")
@@ -87,6 +95,7 @@ _P = ctypes.POINTER(LpProblem)
 _M = ctypes.POINTER(LpMgrit)
 _S = ctypes.POINTER(LpStep)
 _H = ctypes.POINTER(LpLabelHead)
+_G = ctypes.POINTER(LpGated)
 _v = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _sz = ctypes.c_size_t
@@ -124,6 +133,9 @@ _SIGS = {
     "lp_checkpoint_load": ([_i32, _i32, _i32, _v, _v, _v, _v], _i32),
     "lp_loss_labels_workspace_bytes": ([_H, _i32], _sz),
     "lp_loss_labels": ([_H, _v, _v, _v, _v, ctypes.c_double, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
+    "lp_gated_workspace_bytes": ([_G, _i32], _sz),
+    "lp_gated_forward": ([_G, _v, _v, _v, _v, _v, _sz, _v], _i32),
+    "lp_gated_backward": ([_G, _v, _v, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
 }
 
 
@@ -640,3 +652,51 @@ def lp_loss_labels(hd: LpLabelHead, u, W, mu, labels, J, ws, row=None, du=None, 
         _dev(dmu, nc, "dmu", dt, dev, True), wp, wn, _stream_of(dev))
     if rc:
         _check(rc, "lp_loss_labels")
+
+
+# ---------------------------------------------------------------- gated layers
+
+def gated(dtype: str, act: str, B: int, ni: int, no: int) -> LpGated:
+    """One gated layer y = sigma(x Wg^T) (x Wu^T), x [B][ni], Wg and Wu [no][ni]; dtype "f32", "bf16" or
+    "f16", act one of GATE."""
+    return LpGated(LP_ABI_VERSION, WIDE_DTYPE[dtype], GATE[act], _count(B), _count(ni), _count(no))
+
+
+def lp_gated_workspace_bytes(gd: LpGated, grad: bool) -> int:
+    n = load().lp_gated_workspace_bytes(ctypes.byref(gd), int(bool(grad)))
+    if n == 0:
+        raise LpError(LP_EINVAL, "lp_gated_workspace_bytes", load().lp_last_error().decode())
+    return int(n)
+
+
+def alloc_gated_workspace(gd: LpGated, grad: bool = True, device="cuda"):
+    """grad: whether gradients will be asked for (the layer alone needs far less)."""
+    import torch
+    return torch.empty(lp_gated_workspace_bytes(gd, grad), dtype=torch.uint8, device=device)
+
+
+def lp_gated_forward(gd: LpGated, x, Wg, Wu, y, ws) -> None:
+    """y = sigma(x Wg^T) (x Wu^T)."""
+    dt = _wide_dtype(gd.dtype)
+    dev = _here(Wg, "Wg")
+    B, ni, no = gd.B, gd.ni, gd.no
+    wp, wn = _dev_ws(ws, dev)
+    rc = (_lib or load()).lp_gated_forward(
+        ctypes.byref(gd), _dev(x, B * ni, "x", dt, dev), _dev(Wg, no * ni, "Wg", dt, dev), _dev(Wu, no * ni, "Wu", dt, dev),
+        _dev(y, B * no, "y", dt, dev), wp, wn, _stream_of(dev))
+    if rc:
+        _check(rc, "lp_gated_forward")
+
+
+def lp_gated_backward(gd: LpGated, x, Wg, Wu, dy, dx, dWg, dWu, ws) -> None:
+    """Gradients of lp_gated_forward for dy. dx, dWg, dWu may be None (not wanted)."""
+    dt = _wide_dtype(gd.dtype)
+    dev = _here(Wg, "Wg")
+    B, ni, no = gd.B, gd.ni, gd.no
+    wp, wn = _dev_ws(ws, dev)
+    rc = (_lib or load()).lp_gated_backward(
+        ctypes.byref(gd), _dev(x, B * ni, "x", dt, dev), _dev(Wg, no * ni, "Wg", dt, dev), _dev(Wu, no * ni, "Wu", dt, dev),
+        _dev(dy, B * no, "dy", dt, dev), _dev(dx, B * ni, "dx", dt, dev, True), _dev(dWg, no * ni, "dWg", dt, dev, True),
+        _dev(dWu, no * ni, "dWu", dt, dev, True), wp, wn, _stream_of(dev))
+    if rc:
+        _check(rc, "lp_gated_backward")

@@ -1,0 +1,102 @@
+"""Plain 64-bit forms of the layer norm, the gated layers and the orthogonalised update, with
+element-by-element error bounds, for the GPU tests.
+
+The bounds follow from the arithmetic alone, as in wide_testutil: half a step of the element type for each
+rounding to it, a whole step of fp32 per addition of a sum, EF = 2^-20 for the activation formulas."""
+from __future__ import annotations
+
+import math
+
+import torch
+
+import wide_testutil as T
+from paper_1812_04352_amd import lp as L
+
+E32, EF = T.E32, T.EF
+ACTS = ("tanh", "relu", "smoothrelu", "identity", "silu", "gelu")
+# the largest second derivative of each activation (that of relu jumps, see slope_error)
+BEND = {"tanh": 0.77, "smoothrelu": 5.0, "identity": 0.0, "silu": 0.5, "gelu": 0.8}
+
+
+def gate(z, act):
+    """The activation and its slope."""
+    if act == "silu":
+        t = torch.sigmoid(z)
+        return z * t, t + z * t * torch.sigmoid(-z)
+    if act == "gelu":
+        cdf = 0.5 * torch.erfc(-z * math.sqrt(0.5))
+        return z * cdf, cdf + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    return T.sigma(z, act), T.dsigma(z, act)
+
+
+def gate_error(z, ez, act):
+    """What the activation and its slope may be off for a z that is off by ez: slopes of 1.2 at most; the
+    formulas' relative error grows with |z|, the exponent's size (by 1 / 8 of EF)."""
+    s, ds = gate(z, act)
+    grow = EF * (1 + z.abs() / 8)
+    slope = (z.abs() <= ez).double() if act == "relu" else BEND[act] * ez
+    return 1.2 * ez + grow * (s.abs() + (1.0 if act in ("tanh", "smoothrelu") else 0.0)), slope + grow * (1 + ds.abs())
+
+
+def gated_forward(x, Wg, Wu, act, dtype):
+    zg, eg = T.preact(x, Wg, None)
+    zu, eu = T.preact(x, Wu, None)
+    s, _ = gate(zg, act)
+    es, _ = gate_error(zg, eg, act)
+    y = s * zu
+    err = s.abs() * eu + (zu.abs() + eu) * es + 2 * E32 * y.abs()
+    return y, err + T.half_step(dtype) * (y.abs() + err) + T.tiny(dtype)
+
+
+def gated_backward(x, Wg, Wu, dy, act, dtype):
+    """(dx, dWg, dWu), each with its bound."""
+    zg, eg = T.preact(x, Wg, None)
+    zu, eu = T.preact(x, Wu, None)
+    x, Wg, Wu, dy = x.double(), Wg.double(), Wu.double(), dy.double()
+    s, ds = gate(zg, act)
+    es, eds = gate_error(zg, eg, act)
+    u, tiny = T.half_step(dtype), T.tiny(dtype)
+    dzu, dzg = dy * s, dy * zu * ds
+    eu32 = dy.abs() * es + 2 * E32 * dzu.abs()
+    eg32 = dy.abs() * (zu.abs() * eds + (ds.abs() + eds) * eu) + 4 * E32 * dzg.abs()
+    ezu = eu32 + u * (dzu.abs() + eu32) + tiny
+    ezg = eg32 + u * (dzg.abs() + eg32) + tiny
+    B, no = dy.shape
+    dx = dzg @ Wg + dzu @ Wu
+    ex = ezg @ Wg.abs() + ezu @ Wu.abs() + (2 * no + 66) * E32 * ((dzg.abs() + ezg) @ Wg.abs() + (dzu.abs() + ezu) @ Wu.abs())
+    out = [(dx, ex)]
+    for d, e in ((dzg, ezg), (dzu, ezu)):
+        out.append((d.t() @ x, e.t() @ x.abs() + (B + 2) * E32 * ((d.abs() + e).t() @ x.abs())))
+    return [(v, e + u * (v.abs() + e) + tiny) for v, e in out]
+
+
+def scribble(ws):
+    """A workspace that holds NaN in every type."""
+    ws.fill_(255)
+    return ws
+
+
+class Gated:
+    """One layer's calls, outputs guarded, from a workspace full of NaN."""
+
+    def __init__(self, dtype, act, B, ni, no):
+        self.dtype, self.gd = dtype, L.gated(dtype, act, B, ni, no)
+        self.B, self.ni, self.no = B, ni, no
+
+    def forward(self, x, Wg, Wu):
+        ws = scribble(L.alloc_gated_workspace(self.gd, grad=False))
+        y, yf = T.out((self.B, self.no), T.DT[self.dtype])
+        L.lp_gated_forward(self.gd, x, Wg, Wu, y, ws)
+        torch.cuda.synchronize()
+        assert T.guarded(yf, y.numel())
+        return y
+
+    def backward(self, x, Wg, Wu, dy, want=(True, True, True)):
+        ws = scribble(L.alloc_gated_workspace(self.gd, grad=True))
+        shapes = ((self.B, self.ni), (self.no, self.ni), (self.no, self.ni))
+        bufs = [T.out(s, T.DT[self.dtype]) if w else (None, None) for s, w in zip(shapes, want)]
+        L.lp_gated_backward(self.gd, x, Wg, Wu, dy, *[v for v, _ in bufs], ws)
+        torch.cuda.synchronize()
+        for v, f in bufs:
+            assert v is None or T.guarded(f, v.numel())
+        return [v for v, _ in bufs]

@@ -1,0 +1,94 @@
+"""Refusals of the gated layers on the host (no GPU): every bad call returns its documented status before
+any device work, the binding refuses bad tensors, and workspaces hold what they have to."""
+import ctypes
+import random
+
+import pytest
+import torch
+
+from paper_1812_04352_amd import lp as L
+
+FAKE = [ctypes.c_void_p(0x1000 * (i + 1)) for i in range(16)]  # never dereferenced
+BIG = 1 << 50
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+
+
+def gated(dtype="bf16", act="silu", B=8, ni=16, no=24):
+    return L.gated(dtype, act, B, ni, no)
+
+
+def forward(gd, x=FAKE[0], Wg=FAKE[1], Wu=FAKE[2], y=FAKE[3], ws=FAKE[4], n=BIG):
+    return L.load().lp_gated_forward(ctypes.byref(gd) if gd else None, x, Wg, Wu, y, ws, n, None)
+
+
+def backward(gd, x=FAKE[0], Wg=FAKE[1], Wu=FAKE[2], dy=FAKE[3], dx=FAKE[4], dWg=FAKE[5], dWu=FAKE[6], ws=FAKE[7], n=BIG):
+    return L.load().lp_gated_backward(ctypes.byref(gd) if gd else None, x, Wg, Wu, dy, dx, dWg, dWu, ws, n, None)
+
+
+def bad_workspaces(need):
+    return (dict(ws=None), dict(ws=ctypes.c_void_p(0x1010)), dict(n=need - 1))
+
+
+def test_gated_descriptor():
+    assert forward(None) == L.LP_EINVAL and backward(None) == L.LP_EINVAL
+    for call in (forward, backward):
+        for kw in (dict(B=-1), dict(ni=0), dict(no=-3)):
+            assert call(gated(**kw)) == L.LP_EINVAL, kw
+        for kw in (dict(dtype="f64"), dict(B=(1 << 24) + 1), dict(ni=(1 << 20) + 1), dict(no=(1 << 20) + 1),
+                   dict(B=1 << 24, ni=1 << 12), dict(ni=1 << 18, no=(1 << 17) + 1)):
+            assert call(gated(**kw)) == L.LP_EUNSUPPORTED, kw
+        for field, value in (("act", 6), ("act", -1), ("dtype", 9), ("abi_version", 3)):
+            g = gated()
+            setattr(g, field, value)
+            assert call(g) == L.LP_EINVAL
+            assert L.load().lp_gated_workspace_bytes(ctypes.byref(g), 1) == 0
+    with pytest.raises(L.LpError):
+        L.lp_gated_workspace_bytes(gated(ni=0), False)
+    for n in (2 ** 31, 2 ** 32 + 8, 2 ** 63):
+        for kw in (dict(B=n), dict(ni=n), dict(no=n)):
+            with pytest.raises(L.LpError):
+                L.lp_gated_workspace_bytes(gated(**kw), True)
+
+
+def test_gated_arguments():
+    g = gated()
+    for kw in (dict(x=None), dict(Wg=None), dict(Wu=None), dict(y=None), dict(y=FAKE[0]), dict(y=FAKE[1]), dict(y=FAKE[2])):
+        assert forward(g, **kw) == L.LP_EINVAL, kw
+    for kw in (dict(x=None), dict(Wg=None), dict(Wu=None), dict(dy=None), dict(dx=FAKE[3]), dict(dx=FAKE[0]), dict(dWg=FAKE[1]),
+               dict(dWu=FAKE[2]), dict(dWu=FAKE[5]), dict(dx=FAKE[6])):
+        assert backward(g, **kw) == L.LP_EINVAL, kw
+    for kw in bad_workspaces(L.lp_gated_workspace_bytes(g, False)):
+        assert forward(g, **kw) == L.LP_EWORKSPACE, kw
+    for kw in bad_workspaces(L.lp_gated_workspace_bytes(g, True)):
+        assert backward(g, **kw) == L.LP_EWORKSPACE, kw
+    # the step has no such gates
+    assert L.load().lp_step_workspace_bytes(ctypes.byref(L.LpStep(L.LP_ABI_VERSION, L.LP_BF16, L.LP_SILU, 8, 16, 16, 1.0))) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gated_workspaces(dtype):
+    """Over the whole range: what a workspace holds at least and at most."""
+    rng, seen, e = random.Random(3), 0, SIZE[dtype]
+    for _ in range(400):
+        B, ni, no = (rng.choice((1, t, t - 1, int(2 ** rng.uniform(0, t.bit_length() - 1)))) for t in (2 ** 24, 2 ** 20, 2 ** 20))
+        g = gated(dtype, B=B, ni=ni, no=no)
+        if max(B * no, B * ni, no * ni) > 2 ** 35:
+            with pytest.raises(L.LpError):
+                L.lp_gated_workspace_bytes(g, True)
+            continue
+        alone, grad = (L.lp_gated_workspace_bytes(g, k) for k in (False, True))
+        copies = (B + 2 * no) * ni * e
+        seen += 1
+        assert copies <= alone <= copies + 128 * (B + 2 * no) + 2 ** 31 and alone <= grad, (B, ni, no)
+        assert copies + 2 * B * no * e <= grad <= copies + 2 * B * (no + 32) * e + 128 * (B + 2 * no) + 2 ** 31, (B, ni, no)
+    assert seen > 100
+
+
+def test_binding_refuses_tensors():
+    t = torch.zeros(8, 24, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):  # not on a GPU
+        L.lp_gated_forward(gated(), t, t, t, t, torch.zeros(256, dtype=torch.uint8))
+    with pytest.raises(ValueError):
+        L.lp_gated_backward(gated(), t, t, t, t, None, None, None, None)
+    with pytest.raises(KeyError):
+        L.gated("bf16", "swish", 1, 1, 1)
