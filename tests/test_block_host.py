@@ -79,8 +79,8 @@ def test_gated_workspaces(dtype):
         alone, grad = (L.lp_gated_workspace_bytes(g, k) for k in (False, True))
         copies = (B + 2 * no) * ni * e
         seen += 1
-        # (a split has at most 32 parts, and only where its tiles do not fill the card: 256 of at most 128 x 128)
-        parts = 32 * 4 * 128 * 128 * 256 * 8
+        # (a contraction has at most 32 splits, each with its sums of whole tiles of 128 in fp32)
+        parts = 32 * 4 * max((B + 128) * (2 * no + 128), (B + 128) * (ni + 128), (2 * no + 192) * (ni + 128))
         assert copies <= alone <= copies + 128 * (B + 2 * no) + parts and alone <= grad, (B, ni, no)
         assert copies + 2 * B * no * e <= grad <= copies + 2 * B * (no + 32) * e + 128 * (B + 2 * no) + parts, (B, ni, no)
     assert seen > 100
