@@ -436,8 +436,33 @@ int32_t lp_loss_labels(const lp_label_head* head, const void* u, const void* W, 
                        double gscale, float* J, float* row, void* du, void* dW, void* dmu, void* ws, size_t ws_bytes,
                        void* stream);
 
-/* ---- gated layers ----
+/* ---- layer norm, gated layers ----
  * Types, limits, streams, workspaces and reproducibility as for the layer steps above. */
+
+/* Layer norm over the q features of every row: with the row's mean m and r = 1 / sqrt(v + eps), v the mean
+ * of (x - m)^2,   y = gamma (x - m) r + beta;   x, y [B][q], gamma, beta [q]. */
+typedef struct {
+  int32_t abi_version;   /* must equal LP_ABI_VERSION */
+  int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16 */
+  int32_t B;             /* rows, >= 0 (0: nothing to do; weight gradients are zero) */
+  int32_t q;             /* features of a row, >= 1 */
+  double eps;            /* >= 0, finite in fp32 (0: a row of equal values gives NaN) */
+} lp_norm;
+
+/* gamma (1 without it) and beta (0) nullable. y may be x. Statistics are fp32: the sum of (x - m)^2 has to
+ * stay in its range. An infinity or a NaN makes its own row NaN. */
+int32_t lp_norm_forward(const lp_norm* norm, const void* x, const void* gamma, const void* beta, void* y, void* stream);
+
+/* Workspace bytes of lp_norm_backward (partial sums of the weights' gradients); 0 for an invalid norm. */
+size_t lp_norm_workspace_bytes(const lp_norm* norm);
+
+/* Gradients of the norm for dy [B][q], from its input x (the statistics are formed again): with
+ * xh = (x - m) r and g = gamma dy,
+ *   dx     = r (g - mean(g) - xh mean(g xh)) (+ dr, the gradient that reaches x by a residual; nullable)   [B][q]
+ *   dgamma = sum_k dy_k xh_k,  dbeta = sum_k dy_k   [q]
+ * dx, dgamma, dbeta nullable: not wanted. dx may be dr; outputs must not alias other inputs. */
+int32_t lp_norm_backward(const lp_norm* norm, const void* x, const void* gamma, const void* dy, const void* dr, void* dx,
+                         void* dgamma, void* dbeta, void* ws, size_t ws_bytes, void* stream);
 
 /* Gates of gated layers besides lp_step's activations: silu(z) = z / (1 + exp(-z)), and gelu(z) = z times
  * the standard normal distribution function of z. */
@@ -473,7 +498,7 @@ int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, 
                           void* dWg, void* dWu, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- tracing (a profiling aid, not part of the method) ----
- * (The kernels of layer steps, checkpoints, label heads and gated layers are of no kind here.)
+ * (The kernels of layer steps, checkpoints, label heads, norms and gated layers are of no kind here.)
  * When enabled for a kernel kind, every launch of that kind records a pair of
  * HIP events on the launch's stream; lp_trace_read sums their elapsed times.
  * Kinds: the three sweeps of a non-coarsest MGRIT level, the coarsest-level

@@ -1,4 +1,4 @@
-// Host side of the gated layers (include/lp.h): argument checks, workspace layouts, dispatch by
+// Host side of the layer norm and the gated layers (include/lp.h): argument checks, workspace layouts, dispatch by
 // element type.
 #include <math.h>
 
@@ -46,6 +46,17 @@ int check_gated(const lp_gated* g) {
     return fail(LP_EUNSUPPORTED, "widths ni = %d, no = %d > %d", g->ni, g->no, kMaxWidth);
   if (std::max({(double)g->B * g->no, (double)g->B * g->ni, (double)g->no * g->ni}) > kMaxValues)
     return fail(LP_EUNSUPPORTED, "more than 2^35 values in an array");
+  return LP_OK;
+}
+
+int check_norm(const lp_norm* n) {
+  if (!n) return fail(LP_EINVAL, "norm is NULL");
+  int rc = check_type(n->abi_version, n->dtype);
+  if (rc || (rc = check_rows(n->B))) return rc;
+  if (n->q < 1) return fail(LP_EINVAL, "q = %d < 1", n->q);
+  if (n->q > kMaxWidth) return fail(LP_EUNSUPPORTED, "q = %d > %d", n->q, kMaxWidth);
+  if ((double)n->B * n->q > kMaxValues) return fail(LP_EUNSUPPORTED, "more than 2^35 values in an array");
+  if (!(n->eps >= 0) || !isfinite((float)n->eps)) return fail(LP_EINVAL, "eps must be >= 0 and finite in fp32");
   return LP_OK;
 }
 
@@ -108,6 +119,41 @@ GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad) {
                         : lp::call##_f16(__VA_ARGS__))
 
 extern "C" {
+
+size_t lp_norm_workspace_bytes(const lp_norm* n) {
+  if (check_norm(n) != LP_OK) return 0;
+  lp::clear_error();
+  return lp::norm_layout(n->dtype, n->B, n->q).total;
+}
+
+int32_t lp_norm_forward(const lp_norm* n, const void* x, const void* gamma, const void* beta, void* y, void* stream) {
+  int rc = check_norm(n);
+  if (rc) return rc;
+  if (n->B && (!x || !y)) return fail(LP_EINVAL, "NULL array argument");
+  if (n->B && any_same({y}, {gamma, beta})) return fail(LP_EINVAL, "y aliases a weight");
+  if (n->B == 0) return LP_OK;
+  lp::NormArgs a{};
+  a.dtype = n->dtype, a.B = n->B, a.q = n->q, a.eps = n->eps;
+  a.x = x, a.gamma = gamma, a.beta = beta, a.y = y;
+  const hipError_t e = LP_BY_TYPE(n->dtype, norm_forward, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? LP_OK : hip_fail(e, "norm forward");
+}
+
+int32_t lp_norm_backward(const lp_norm* n, const void* x, const void* gamma, const void* dy, const void* dr, void* dx,
+                         void* dgamma, void* dbeta, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_norm(n);
+  if (rc) return rc;
+  if (n->B && (!x || !dy)) return fail(LP_EINVAL, "NULL array argument");
+  if (any_same({dx, dgamma, dbeta}, {x, gamma, dy}) || any_same({dgamma, dbeta}, {dr}))
+    return fail(LP_EINVAL, "an output aliases an input or another output");
+  if ((rc = check_ws(ws, ws_bytes, lp::norm_layout(n->dtype, n->B, n->q).total))) return rc;
+  if (!dx && !dgamma && !dbeta) return LP_OK;
+  lp::NormArgs a{};
+  a.dtype = n->dtype, a.B = n->B, a.q = n->q, a.eps = n->eps;
+  a.x = x, a.gamma = gamma, a.dy = dy, a.dr = dr, a.dx = dx, a.dgamma = dgamma, a.dbeta = dbeta, a.ws = ws;
+  const hipError_t e = LP_BY_TYPE(n->dtype, norm_backward, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? LP_OK : hip_fail(e, "norm backward");
+}
 
 size_t lp_gated_workspace_bytes(const lp_gated* g, int32_t grad) {
   if (check_gated(g) != LP_OK) return 0;

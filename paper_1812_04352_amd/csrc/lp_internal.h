@@ -296,6 +296,29 @@ LP_STEP_LAUNCHERS(f32)
 #undef LP_STEP_LAUNCHERS
 
 // ---- layer norm, gated layers, orthogonalised updates ----
+struct NormArgs {
+  int dtype, B, q;
+  double eps;
+  const void *x, *gamma, *beta;  // [B][q], [q], [q]; the weights nullable
+  void* y;                       // forward: [B][q]
+  const void *dy, *dr;           // backward: [B][q]; dr nullable
+  void *dx, *dgamma, *dbeta;     // nullable
+  void* ws;
+};
+struct NormLayout {  // of a backward call (lp_norm.hip)
+  size_t stats, part, total;
+  int groups, rows;  // workgroups with a row of partial sums each, and the rows of x that they take
+};
+NormLayout norm_layout(int dtype, int B, int q);
+
+#define LP_NORM_LAUNCHERS(T)                                     \
+  hipError_t norm_forward_##T(const NormArgs& a, hipStream_t st); \
+  hipError_t norm_backward_##T(const NormArgs& a, hipStream_t st);
+LP_NORM_LAUNCHERS(bf16)
+LP_NORM_LAUNCHERS(f16)
+LP_NORM_LAUNCHERS(f32)
+#undef LP_NORM_LAUNCHERS
+
 struct GatedArgs {
   int dtype, act;
   int B, ni, no;

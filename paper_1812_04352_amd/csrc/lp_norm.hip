@@ -1,0 +1,468 @@
+// Layer norm over the features of every row, y = gamma (x - mean) / sqrt(var + eps) + beta, and its gradients.
+//   forward:   one read of x, one write of y: a group of TPR threads holds a row in registers (C pieces of
+//              16 bytes a thread), so the mean and then the mean square of x - mean, which does not cancel
+//              as the mean square of x minus that of the mean would, cost no second read
+//   backward:  with g = gamma dy, xh = (x - mean) r, r = 1 / sqrt(var + eps), over a row's q features
+//                dx = r (g - mean g - xh mean(g xh)) (+ dr),  dgamma = sum_rows dy xh,  dbeta = sum_rows dy
+//              one read of x, dy (and dr), one write of dx: the statistics are formed again from the row at
+//              hand, in two rounds of exchanges (the sums of x and g, then of (x - mean)^2 and g (x - mean)).
+//              A thread keeps the same features of all its rows, so it sums their dgamma and dbeta in
+//              registers; a workgroup adds its groups' in order and writes one row of partial sums, which a
+//              second kernel adds in fp64 (a single workgroup writes the gradients themselves).
+// Bound by memory. Rows that no group can hold are read again for every pass.
+#include <algorithm>
+
+#include "lp_internal.h"
+#include "lp_mm.h"
+
+namespace lp {
+namespace norm {
+
+using mm::GVec;
+
+constexpr int NT_F = 256;   // threads of a forward workgroup (more where a row takes more)
+constexpr int NT_B = 1024;  // and of a backward one: few rows of partial sums
+
+// A thread's pieces of a row: features (c TPR + t) V .. of the group's thread t
+template <typename T, int TPR, int C>
+struct Piece {
+  static constexpr int V = 16 / (int)sizeof(T);
+  typedef typename GVec<T, V>::type Vec;
+  Vec v[C];
+  static __device__ __forceinline__ int first(int t, int c) { return (c * TPR + t) * V; }
+  // zeros behind the row's end
+  __device__ __forceinline__ void load(const T* row, int t, int q) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int n = first(t, c);
+      if (n + V <= q) {
+        v[c] = *reinterpret_cast<const Vec*>(row + n);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[c][k] = n + k < q ? row[n + k] : (T)0.f;
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(T* row, int t, int q, int c, const float (&f)[V]) {
+    const int n = first(t, c);
+    if (n + V <= q) {
+      Vec x;
+#pragma unroll
+      for (int k = 0; k < V; ++k) x[k] = (T)f[k];
+      *reinterpret_cast<Vec*>(row + n) = x;
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (n + k < q) row[n + k] = (T)f[k];
+    }
+  }
+};
+
+// Sums of two values over a group of TPR threads, the same in all of them. Groups wider than a wave
+// exchange through the LDS: `at` alternates between its two halves, so that one barrier a sum is enough
+// (a wave that writes a half again has passed the barrier behind which all have read it).
+template <int TPR, int NT>
+struct GroupSum {
+  static constexpr int W = TPR / 64;  // waves of a group
+  float2 (*lds)[NT / 64];
+  int at = 0;
+  __device__ __forceinline__ float2 operator()(float2 s) {
+#pragma unroll
+    for (int o = (TPR < 64 ? TPR : 64) / 2; o > 0; o >>= 1) {
+      s.x += __shfl_xor(s.x, o, 64);
+      s.y += __shfl_xor(s.y, o, 64);
+    }
+    if constexpr (TPR > 64) {
+      const int wave = threadIdx.x >> 6;
+      if ((threadIdx.x & 63) == 0) lds[at][wave] = s;
+      __syncthreads();
+      const float2* g = lds[at] + wave / W * W;
+      s = g[0];
+#pragma unroll
+      for (int w = 1; w < W; ++w) s.x += g[w].x, s.y += g[w].y;
+      at ^= 1;
+    }
+    return s;
+  }
+};
+
+template <typename T, int TPR, int C, int NT>
+__global__ __launch_bounds__(NT) void k_forward(const T* x, const T* gamma, const T* beta, T* y, int B, int q, float eps) {
+  typedef Piece<T, TPR, C> P;
+  constexpr int V = P::V, G = NT / TPR;
+  __shared__ float2 lds[2][NT / 64];
+  GroupSum<TPR, NT> sum{lds};
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  P ga, be;
+  if (gamma) ga.load(gamma, t, q);
+  if (beta) be.load(beta, t, q);
+  const float n = (float)q;
+  for (long r0 = (long)blockIdx.x * G; r0 < B; r0 += (long)gridDim.x * G) {  // (the same rounds for every thread)
+    const long r = r0 + g;
+    P p;
+    p.load(x + min(r, (long)B - 1) * q, t, q);
+    float2 s = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < V; ++k) s.x += (float)p.v[c][k];
+    const float mean = sum(s).x / n;
+    s = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float d = P::first(t, c) + k < q ? (float)p.v[c][k] - mean : 0.f;
+        s.x = fmaf(d, d, s.x);
+      }
+    const float rstd = 1.f / sqrtf(sum(s).x / n + eps);
+    if (r >= B) continue;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float f[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        f[k] = ((float)p.v[c][k] - mean) * rstd;
+        if (gamma) f[k] *= (float)ga.v[c][k];
+        if (beta) f[k] += (float)be.v[c][k];
+      }
+      P::store(y + r * q, t, q, c, f);
+    }
+  }
+}
+
+struct BackArgs {
+  const void *x, *gamma, *dy, *dr;  // gamma, dr nullable
+  void *dx, *dgamma, *dbeta;        // nullable
+  float* part;                      // [workgroups][2][q] partial sums of dgamma and dbeta
+  int B, q;
+  int rows;                         // of a workgroup
+  float eps;
+};
+
+// A workgroup's sums of one array, of its groups in order: to the array itself or to a row of partial sums
+template <typename T, int TPR, int C>
+__device__ __forceinline__ void add_groups(const float (&acc)[C][16 / sizeof(T)], float* lds, int q, T* out, float* part) {
+  typedef Piece<T, TPR, C> P;
+  constexpr int V = P::V, G = NT_B / TPR, ROW = TPR * C * V;
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  if constexpr (G == 1) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int n = P::first(t, c) + k;
+        if (n < q) {
+          if (part) part[n] = acc[c][k];
+          else out[n] = (T)acc[c][k];
+        }
+      }
+    }
+  } else {
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < V; k += 4)
+        *reinterpret_cast<float4*>(lds + g * ROW + P::first(t, c) + k) = make_float4(acc[c][k], acc[c][k + 1], acc[c][k + 2], acc[c][k + 3]);
+    __syncthreads();
+    for (int n = threadIdx.x; n < q; n += NT_B) {
+      float s = lds[n];
+#pragma unroll
+      for (int i = 1; i < G; ++i) s += lds[i * ROW + n];
+      if (part) part[n] = s;
+      else out[n] = (T)s;
+    }
+  }
+}
+
+template <typename T, int TPR, int C>
+__global__ __launch_bounds__(NT_B) void k_backward(BackArgs a) {
+  typedef Piece<T, TPR, C> P;
+  constexpr int V = P::V, G = NT_B / TPR;
+  __shared__ float2 lds[2][NT_B / 64];
+  __shared__ __attribute__((aligned(16))) float sums[G == 1 ? 4 : NT_B * C * V];
+  GroupSum<TPR, NT_B> sum{lds};
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, q = a.q;
+  const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = static_cast<const T*>(a.dr);
+  T* dx = static_cast<T*>(a.dx);
+  P ga;
+  if (a.gamma) ga.load(static_cast<const T*>(a.gamma), t, q);
+  const float n = (float)q;
+  float dg[C][V] = {}, db[C][V] = {};
+  const long r1 = min((long)a.B, (long)(blockIdx.x + 1) * a.rows);
+  for (long r0 = (long)blockIdx.x * a.rows; r0 < r1; r0 += G) {  // (the same rounds for every thread)
+    const long r = r0 + g;
+    const bool on = r < r1;
+    P px, pd, pr;
+    px.load(x + min(r, r1 - 1) * q, t, q);
+    pd.load(dy + min(r, r1 - 1) * q, t, q);
+    if (dr && dx) pr.load(dr + min(r, r1 - 1) * q, t, q);
+    float2 s = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        s.x += (float)px.v[c][k];
+        s.y = a.gamma ? fmaf((float)pd.v[c][k], (float)ga.v[c][k], s.y) : s.y + (float)pd.v[c][k];
+      }
+    s = sum(s);
+    const float mean = s.x / n, m1 = s.y / n;
+    s = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float d = P::first(t, c) + k < q ? (float)px.v[c][k] - mean : 0.f;
+        const float gk = a.gamma ? (float)pd.v[c][k] * (float)ga.v[c][k] : (float)pd.v[c][k];
+        s.x = fmaf(d, d, s.x);
+        s.y = fmaf(gk, d, s.y);
+      }
+    s = sum(s);
+    const float rstd = 1.f / sqrtf(s.x / n + a.eps), m2 = s.y / n * rstd;
+    if (!on) continue;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float f[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float d = (float)pd.v[c][k], xh = ((float)px.v[c][k] - mean) * rstd;
+        const float gk = a.gamma ? d * (float)ga.v[c][k] : d;
+        f[k] = rstd * (gk - m1 - xh * m2);
+        if (dr && dx) f[k] += (float)pr.v[c][k];
+        dg[c][k] = fmaf(d, xh, dg[c][k]);
+        db[c][k] += d;
+      }
+      if (dx) P::store(dx + r * q, t, q, c, f);
+    }
+  }
+  float* part = a.part ? a.part + (size_t)blockIdx.x * 2 * q : nullptr;
+  if (a.dgamma) add_groups<T, TPR, C>(dg, sums, q, static_cast<T*>(a.dgamma), part);
+  if (a.dbeta) add_groups<T, TPR, C>(db, sums, q, static_cast<T*>(a.dbeta), part ? part + q : nullptr);
+}
+
+// dgamma and dbeta from the partial sums, in fp64 and in order: 64 features by 16 runs of rows a workgroup
+template <typename T>
+__global__ __launch_bounds__(1024) void k_sum(const float* part, int rows, int q, T* dgamma, T* dbeta) {
+  __shared__ double sh[16][64];
+  const int half = (q + 63) / 64, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const bool second = (int)blockIdx.x >= half;
+  const int n = ((int)blockIdx.x - (second ? half : 0)) * 64 + lane;
+  T* out = second ? dbeta : dgamma;
+  const int per = (rows + 15) / 16, i1 = min(rows, (w + 1) * per);
+  double s = 0.0;
+  if (n < q && out) {
+    const float* p = part + (second ? q : 0) + n;
+    int i = w * per;
+    for (; i + 8 <= i1; i += 8) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = p[(size_t)(i + k) * 2 * q];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += (double)v[k];
+    }
+    for (; i < i1; ++i) s += (double)p[(size_t)i * 2 * q];
+  }
+  sh[w][lane] = s;
+  __syncthreads();
+  if (w || n >= q || !out) return;
+  for (int k = 1; k < 16; ++k) s += sh[k][lane];
+  out[n] = (T)(float)s;
+}
+
+// ---- rows that no group holds: every pass reads them again
+
+// mean and 1 / sqrt(var + eps) of a row, and with dy given the means of g and g xh, over a workgroup of 1024
+template <typename T>
+__device__ __forceinline__ void long_stats(const T* x, const T* dy, const T* gamma, int q, float eps, GroupSum<1024, 1024>& sum,
+                                           float& mean, float& rstd, float& m1, float& m2) {
+  const float n = (float)q;
+  float2 s = {0.f, 0.f};
+  for (int i = threadIdx.x; i < q; i += 1024) {
+    s.x += (float)x[i];
+    if (dy) s.y += (gamma ? (float)gamma[i] : 1.f) * (float)dy[i];
+  }
+  s = sum(s);
+  mean = s.x / n, m1 = s.y / n;
+  s = {0.f, 0.f};
+  for (int i = threadIdx.x; i < q; i += 1024) {
+    const float d = (float)x[i] - mean;
+    s.x = fmaf(d, d, s.x);
+    if (dy) s.y = fmaf((gamma ? (float)gamma[i] : 1.f) * (float)dy[i], d, s.y);
+  }
+  s = sum(s);
+  rstd = 1.f / sqrtf(s.x / n + eps), m2 = s.y / n * rstd;
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void k_forward_long(const T* x, const T* gamma, const T* beta, T* y, int B, int q, float eps) {
+  __shared__ float2 lds[2][16];
+  GroupSum<1024, 1024> sum{lds};
+  for (long r = blockIdx.x; r < B; r += gridDim.x) {
+    float mean, rstd, m1, m2;
+    long_stats<T>(x + r * q, nullptr, nullptr, q, eps, sum, mean, rstd, m1, m2);
+    for (int i = threadIdx.x; i < q; i += 1024) {
+      float f = ((float)x[r * q + i] - mean) * rstd;
+      if (gamma) f *= (float)gamma[i];
+      if (beta) f += (float)beta[i];
+      y[r * q + i] = (T)f;
+    }
+  }
+}
+
+// dx, and the statistics of every row (mean, rstd) for the weights' gradients
+template <typename T>
+__global__ __launch_bounds__(1024) void k_backward_long(BackArgs a, float2* stats) {
+  __shared__ float2 lds[2][16];
+  GroupSum<1024, 1024> sum{lds};
+  const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = static_cast<const T*>(a.dr);
+  const T* gamma = static_cast<const T*>(a.gamma);
+  T* dx = static_cast<T*>(a.dx);
+  const int q = a.q;
+  for (long r = blockIdx.x; r < a.B; r += gridDim.x) {
+    float mean, rstd, m1, m2;
+    long_stats<T>(x + r * q, dy + r * q, gamma, q, a.eps, sum, mean, rstd, m1, m2);
+    if (threadIdx.x == 0) stats[r] = {mean, rstd};
+    if (!dx) continue;
+    for (int i = threadIdx.x; i < q; i += 1024) {
+      const float xh = ((float)x[r * q + i] - mean) * rstd;
+      float f = rstd * ((gamma ? (float)gamma[i] : 1.f) * (float)dy[r * q + i] - m1 - xh * m2);
+      if (dr) f += (float)dr[r * q + i];
+      dx[r * q + i] = (T)f;
+    }
+  }
+}
+
+// partial sums of dgamma and dbeta: a thread's feature over a run of rows (grid y)
+template <typename T>
+__global__ __launch_bounds__(256) void k_weights_long(BackArgs a, const float2* stats) {
+  const int i = blockIdx.x * 256 + threadIdx.x, q = a.q;
+  if (i >= q) return;
+  const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy);
+  float dg = 0.f, db = 0.f;
+  const long r1 = min((long)a.B, (long)(blockIdx.y + 1) * a.rows);
+  for (long r = (long)blockIdx.y * a.rows; r < r1; ++r) {
+    const float2 s = stats[r];
+    const float d = (float)dy[r * q + i];
+    dg = fmaf(d, ((float)x[r * q + i] - s.x) * s.y, dg);
+    db += d;
+  }
+  float* part = a.part + (size_t)blockIdx.y * 2 * q;
+  part[i] = dg;
+  part[q + i] = db;
+}
+
+// ---------------------------------------------------------------- launches
+
+// The group that holds a row of q values: threads and pieces a thread (tpr = 0: none does).
+struct Group {
+  int tpr, c;
+};
+
+inline Group forward_group(size_t esz, int B, int q) {
+  const int v = 16 / (int)esz, pieces = mm::ceil_div(q, v);
+  for (int tpr : {4, 8, 16, 32, 64})
+    if (pieces <= tpr) return {tpr, 1};
+  if (B >= 1024) {  // enough rows for a wave each
+    for (int c : {2, 4, 8})
+      if (pieces <= 64 * c) return {64, c};
+  }
+  for (int c : {1, 2, 4, 8})
+    if (pieces <= 256 * c) return {256, c};
+  return pieces <= 1024 * 8 ? Group{1024, 8} : Group{0, 0};
+}
+
+inline Group backward_group(size_t esz, int q) {
+  const int v = 16 / (int)esz, pieces = mm::ceil_div(q, v);
+  for (int tpr : {4, 8, 16, 32, 64})
+    if (pieces <= tpr) return {tpr, 1};
+  if (pieces <= 128) return {64, 2};
+  for (int c : {1, 2})
+    if (pieces <= 256 * c) return {256, c};
+  for (int c : {1, 2})
+    if (pieces <= 1024 * c) return {1024, c};
+  return {0, 0};
+}
+
+// Rows of a backward workgroup
+inline int backward_rows(int groups, int B) {
+  const int most = 256;  // workgroups: one a CU, each with all the waves it can hold
+  const int rows = std::max(mm::ceil_div(B, most), 4 * groups);
+  return mm::ceil_div(std::min(rows, 2048 * groups), groups) * groups;  // (at most 2048 rows in a sum of fp32)
+}
+
+template <typename T, int TPR, int C>
+hipError_t forward_g(const NormArgs& a, hipStream_t st) {
+  constexpr int NT = TPR > NT_F ? TPR : NT_F, G = NT / TPR;
+  const unsigned grid = (unsigned)std::min<long>(mm::ceil_div(a.B, G), 4096);
+  k_forward<T, TPR, C, NT><<<grid, NT, 0, st>>>((const T*)a.x, (const T*)a.gamma, (const T*)a.beta, (T*)a.y, a.B, a.q, (float)a.eps);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t forward_t(const NormArgs& a, hipStream_t st) {
+  const Group g = forward_group(sizeof(T), a.B, a.q);
+#define LP_CASE(TPR, C) \
+  if (g.tpr == TPR && g.c == C) return forward_g<T, TPR, C>(a, st);
+  LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(64, 2) LP_CASE(64, 4) LP_CASE(64, 8)
+  LP_CASE(256, 1) LP_CASE(256, 2) LP_CASE(256, 4) LP_CASE(256, 8) LP_CASE(1024, 8)
+#undef LP_CASE
+  k_forward_long<T><<<(unsigned)std::min(a.B, 2048), 1024, 0, st>>>((const T*)a.x, (const T*)a.gamma, (const T*)a.beta, (T*)a.y, a.B,
+                                                                  a.q, (float)a.eps);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward_t(const NormArgs& a, hipStream_t st) {
+  const NormLayout l = norm_layout(a.dtype, a.B, a.q);
+  char* w = static_cast<char*>(a.ws);
+  const bool weights = a.dgamma || a.dbeta;
+  BackArgs b{a.x, a.gamma, a.dy, a.dr, a.dx, a.dgamma, a.dbeta, l.groups > 1 ? reinterpret_cast<float*>(w + l.part) : nullptr,
+             a.B, a.q, l.rows, (float)a.eps};
+  const Group g = backward_group(sizeof(T), a.q);
+  if (g.tpr) {
+#define LP_CASE(TPR, C) \
+  if (g.tpr == TPR && g.c == C) k_backward<T, TPR, C><<<(unsigned)l.groups, NT_B, 0, st>>>(b);
+    LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(64, 2) LP_CASE(256, 1) LP_CASE(256, 2)
+    LP_CASE(1024, 1) LP_CASE(1024, 2)
+#undef LP_CASE
+  } else {
+    float2* stats = reinterpret_cast<float2*>(w + l.stats);
+    b.part = reinterpret_cast<float*>(w + l.part);
+    if (a.B) k_backward_long<T><<<(unsigned)std::min(a.B, 2048), 1024, 0, st>>>(b, stats);
+    if (weights) k_weights_long<T><<<dim3((unsigned)mm::ceil_div(a.q, 256), (unsigned)l.groups), 256, 0, st>>>(b, stats);
+  }
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && weights && b.part) {
+    k_sum<T><<<2 * (unsigned)mm::ceil_div(a.q, 64), 1024, 0, st>>>(b.part, l.groups, a.q, (T*)a.dgamma, (T*)a.dbeta);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace norm
+
+NormLayout norm_layout(int dtype, int B, int q) {
+  const norm::Group g = norm::backward_group(dtype == 0 ? 4 : 2, q);
+  NormLayout l{};
+  if (g.tpr) {
+    l.rows = norm::backward_rows(norm::NT_B / g.tpr, B);
+  } else {
+    l.rows = std::min(2048, std::max(16, mm::ceil_div(B, 1024)));
+    l.stats = ((size_t)B * 8 + 255) / 256 * 256;
+  }
+  l.groups = std::max(1, mm::ceil_div(B, l.rows));
+  l.part = l.stats;  // (the rows' statistics come first)
+  l.stats = 0;
+  l.total = std::max<size_t>(l.part + (l.groups > 1 || !g.tpr ? (size_t)l.groups * 2 * q * 4 : 0), 256);
+  return l;
+}
+
+hipError_t norm_forward_f32(const NormArgs& a, hipStream_t st) { return norm::forward_t<float>(a, st); }
+hipError_t norm_forward_bf16(const NormArgs& a, hipStream_t st) { return norm::forward_t<__bf16>(a, st); }
+hipError_t norm_forward_f16(const NormArgs& a, hipStream_t st) { return norm::forward_t<_Float16>(a, st); }
+hipError_t norm_backward_f32(const NormArgs& a, hipStream_t st) { return norm::backward_t<float>(a, st); }
+hipError_t norm_backward_bf16(const NormArgs& a, hipStream_t st) { return norm::backward_t<__bf16>(a, st); }
+hipError_t norm_backward_f16(const NormArgs& a, hipStream_t st) { return norm::backward_t<_Float16>(a, st); }
+
+}  // namespace lp

@@ -46,6 +46,7 @@ EXPORTS = (
     "lp_trace_enable", "lp_trace_read",
     "lp_step_workspace_bytes", "lp_step_forward", "lp_step_backward", "lp_checkpoint_store", "lp_checkpoint_load",
     "lp_loss_labels_workspace_bytes", "lp_loss_labels",
+    "lp_norm_workspace_bytes", "lp_norm_forward", "lp_norm_backward",
     "lp_gated_workspace_bytes", "lp_gated_forward", "lp_gated_backward",
 )
 
@@ -78,6 +79,11 @@ class LpLabelHead(ctypes.Structure):
                 ("q", ctypes.c_int32), ("nc", ctypes.c_int32)]
 
 
+class LpNorm(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_int32), ("dtype", ctypes.c_int32), ("B", ctypes.c_int32),
+                ("q", ctypes.c_int32), ("eps", ctypes.c_double)]
+
+
 class LpGated(ctypes.Structure):
     _fields_ = [("abi_version", ctypes.c_int32), ("dtype", ctypes.c_int32), ("act", ctypes.c_int32),
                 ("B", ctypes.c_int32), ("ni", ctypes.c_int32), ("no", ctypes.c_int32)]
@@ -95,6 +101,7 @@ _P = ctypes.POINTER(LpProblem)
 _M = ctypes.POINTER(LpMgrit)
 _S = ctypes.POINTER(LpStep)
 _H = ctypes.POINTER(LpLabelHead)
+_N = ctypes.POINTER(LpNorm)
 _G = ctypes.POINTER(LpGated)
 _v = ctypes.c_void_p
 _i32 = ctypes.c_int32
@@ -133,6 +140,9 @@ _SIGS = {
     "lp_checkpoint_load": ([_i32, _i32, _i32, _v, _v, _v, _v], _i32),
     "lp_loss_labels_workspace_bytes": ([_H, _i32], _sz),
     "lp_loss_labels": ([_H, _v, _v, _v, _v, ctypes.c_double, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
+    "lp_norm_workspace_bytes": ([_N], _sz),
+    "lp_norm_forward": ([_N, _v, _v, _v, _v, _v], _i32),
+    "lp_norm_backward": ([_N, _v, _v, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
     "lp_gated_workspace_bytes": ([_G, _i32], _sz),
     "lp_gated_forward": ([_G, _v, _v, _v, _v, _v, _sz, _v], _i32),
     "lp_gated_backward": ([_G, _v, _v, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
@@ -654,7 +664,53 @@ def lp_loss_labels(hd: LpLabelHead, u, W, mu, labels, J, ws, row=None, du=None, 
         _check(rc, "lp_loss_labels")
 
 
-# ---------------------------------------------------------------- gated layers
+# ---------------------------------------------------------------- layer norm, gated layers
+
+def norm(dtype: str, B: int, q: int, eps: float = 1e-5) -> LpNorm:
+    """Layer norm of B rows over their q features; dtype "f32", "bf16" or "f16"."""
+    return LpNorm(LP_ABI_VERSION, WIDE_DTYPE[dtype], _count(B), _count(q), eps)
+
+
+def lp_norm_workspace_bytes(nd: LpNorm) -> int:
+    n = load().lp_norm_workspace_bytes(ctypes.byref(nd))
+    if n == 0:
+        raise LpError(LP_EINVAL, "lp_norm_workspace_bytes", load().lp_last_error().decode())
+    return int(n)
+
+
+def alloc_norm_workspace(nd: LpNorm, device="cuda"):
+    """Workspace of lp_norm_backward."""
+    import torch
+    return torch.empty(lp_norm_workspace_bytes(nd), dtype=torch.uint8, device=device)
+
+
+def lp_norm_forward(nd: LpNorm, x, gamma, beta, y) -> None:
+    """y = gamma (x - mean) / sqrt(var + eps) + beta over the features of every row. gamma and beta may be
+    None (1 and 0); y may be x."""
+    dt = _wide_dtype(nd.dtype)
+    dev = _here(x, "x")
+    B, q = nd.B, nd.q
+    rc = (_lib or load()).lp_norm_forward(
+        ctypes.byref(nd), _dev(x, B * q, "x", dt, dev), _dev(gamma, q, "gamma", dt, dev, True),
+        _dev(beta, q, "beta", dt, dev, True), _dev(y, B * q, "y", dt, dev), _stream_of(dev))
+    if rc:
+        _check(rc, "lp_norm_forward")
+
+
+def lp_norm_backward(nd: LpNorm, x, gamma, dy, dr, dx, dgamma, dbeta, ws) -> None:
+    """Gradients of lp_norm_forward for dy; dr (or None): the gradient that reaches x by a residual, added to
+    dx. dx, dgamma, dbeta may be None (not wanted); dx may be dr."""
+    dt = _wide_dtype(nd.dtype)
+    dev = _here(x, "x")
+    B, q = nd.B, nd.q
+    wp, wn = _dev_ws(ws, dev)
+    rc = (_lib or load()).lp_norm_backward(
+        ctypes.byref(nd), _dev(x, B * q, "x", dt, dev), _dev(gamma, q, "gamma", dt, dev, True),
+        _dev(dy, B * q, "dy", dt, dev), _dev(dr, B * q, "dr", dt, dev, True), _dev(dx, B * q, "dx", dt, dev, True),
+        _dev(dgamma, q, "dgamma", dt, dev, True), _dev(dbeta, q, "dbeta", dt, dev, True), wp, wn, _stream_of(dev))
+    if rc:
+        _check(rc, "lp_norm_backward")
+
 
 def gated(dtype: str, act: str, B: int, ni: int, no: int) -> LpGated:
     """One gated layer y = sigma(x Wg^T) (x Wu^T), x [B][ni], Wg and Wu [no][ni]; dtype "f32", "bf16" or

@@ -70,6 +70,54 @@ def gated_backward(x, Wg, Wu, dy, act, dtype):
     return [(v, e + u * (v.abs() + e) + tiny) for v, e in out]
 
 
+def norm_stats(x, eps):
+    """xh, 1 / sqrt(var + eps) and their bounds. A thread adds at most 64 values of a row that its group holds (a
+    1024th of a longer one), and 16 exchanges follow."""
+    x = x.double()
+    q = x.shape[1]
+    n = 84 + q / 1024
+    mean = x.mean(1, keepdim=True)
+    d = x - mean
+    ed = n * E32 * x.abs().mean(1, keepdim=True) + E32 * d.abs()
+    var = (d * d).mean(1, keepdim=True)
+    ev = (2 * d.abs() * ed + ed * ed).mean(1, keepdim=True) + n * E32 * var
+    rstd = (var + eps) ** -0.5
+    er = rstd * (0.5 * ev / (var + eps) + 4 * E32)
+    xh = d * rstd
+    return xh, (ed * (rstd + er) + d.abs() * er + E32 * xh.abs()), rstd, er, n
+
+
+def norm_forward(x, gamma, beta, eps, dtype):
+    xh, exh, *_ = norm_stats(x, eps)
+    ga = 1.0 if gamma is None else gamma.double()
+    y = xh * ga + (0.0 if beta is None else beta.double())
+    err = exh * (ga if gamma is None else ga.abs()) + 2 * E32 * ((xh * ga).abs() + y.abs())
+    return y, err + T.half_step(dtype) * (y.abs() + err) + T.tiny(dtype)
+
+
+def norm_backward(x, gamma, dy, dr, eps, dtype):
+    """(dx, dgamma, dbeta), each with its bound."""
+    xh, exh, rstd, er, n = norm_stats(x, eps)
+    dy = dy.double()
+    g = dy if gamma is None else dy * gamma.double()
+    B = x.shape[0]
+    m1, m2 = g.mean(1, keepdim=True), (g * xh).mean(1, keepdim=True)
+    e1 = n * E32 * g.abs().mean(1, keepdim=True)
+    e2 = (g.abs() * exh).mean(1, keepdim=True) + (n + 3) * E32 * (g * xh).abs().mean(1, keepdim=True)
+    inner = g - m1 - xh * m2
+    ei = e1 + exh * m2.abs() + (xh.abs() + exh) * e2 + 3 * E32 * (g.abs() + m1.abs() + (xh * m2).abs())
+    dx = rstd * inner
+    ex = (rstd + er) * ei + er * inner.abs() + E32 * dx.abs()
+    if dr is not None:
+        dx = dx + dr.double()
+        ex = ex + E32 * (dx.abs() + dr.double().abs())
+    dgamma, dbeta = (dy * xh).sum(0), dy.sum(0)
+    eg = (dy.abs() * exh).sum(0) + (B + 4) * E32 * (dy * xh).abs().sum(0)
+    eb = (B + 4) * E32 * dy.abs().sum(0)
+    u = T.half_step(dtype)
+    return [(v, e + u * (v.abs() + e) + T.tiny(dtype)) for v, e in ((dx, ex), (dgamma, eg), (dbeta, eb))]
+
+
 def scribble(ws):
     """A workspace that holds NaN in every type."""
     ws.fill_(255)
@@ -96,6 +144,31 @@ class Gated:
         shapes = ((self.B, self.ni), (self.no, self.ni), (self.no, self.ni))
         bufs = [T.out(s, T.DT[self.dtype]) if w else (None, None) for s, w in zip(shapes, want)]
         L.lp_gated_backward(self.gd, x, Wg, Wu, dy, *[v for v, _ in bufs], ws)
+        torch.cuda.synchronize()
+        for v, f in bufs:
+            assert v is None or T.guarded(f, v.numel())
+        return [v for v, _ in bufs]
+
+
+class Norm:
+    """One norm's calls, outputs guarded, from a workspace full of NaN."""
+
+    def __init__(self, dtype, B, q, eps=1e-5):
+        self.dtype, self.nd = dtype, L.norm(dtype, B, q, eps)
+        self.B, self.q = B, q
+
+    def forward(self, x, gamma, beta):
+        y, yf = T.out((self.B, self.q), T.DT[self.dtype])
+        L.lp_norm_forward(self.nd, x, gamma, beta, y)
+        torch.cuda.synchronize()
+        assert T.guarded(yf, y.numel())
+        return y
+
+    def backward(self, x, gamma, dy, dr, want=(True, True, True)):
+        ws = scribble(L.alloc_norm_workspace(self.nd))
+        shapes = ((self.B, self.q), (self.q,), (self.q,))
+        bufs = [T.out(s, T.DT[self.dtype]) if w else (None, None) for s, w in zip(shapes, want)]
+        L.lp_norm_backward(self.nd, x, gamma, dy, dr, *[v for v, _ in bufs], ws)
         torch.cuda.synchronize()
         for v, f in bufs:
             assert v is None or T.guarded(f, v.numel())

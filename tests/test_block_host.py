@@ -1,4 +1,4 @@
-"""Refusals of the gated layers on the host (no GPU): every bad call returns its documented status before
+"""Refusals of the layer norm and the gated layers on the host (no GPU): every bad call returns its documented status before
 any device work, the binding refuses bad tensors, and workspaces hold what they have to."""
 import ctypes
 import random
@@ -86,11 +86,64 @@ def test_gated_workspaces(dtype):
     assert seen > 100
 
 
+def norm_forward(nd, x=FAKE[0], gamma=FAKE[1], beta=FAKE[2], y=FAKE[3]):
+    return L.load().lp_norm_forward(ctypes.byref(nd) if nd else None, x, gamma, beta, y, None)
+
+
+def norm_backward(nd, x=FAKE[0], gamma=FAKE[1], dy=FAKE[2], dr=FAKE[3], dx=FAKE[4], dgamma=FAKE[5], dbeta=FAKE[6], ws=FAKE[7],
+                  n=BIG):
+    return L.load().lp_norm_backward(ctypes.byref(nd) if nd else None, x, gamma, dy, dr, dx, dgamma, dbeta, ws, n, None)
+
+
+def test_norm_descriptor():
+    assert norm_forward(None) == L.LP_EINVAL and norm_backward(None) == L.LP_EINVAL
+    for call in (norm_forward, norm_backward):
+        for d in (("bf16", -1, 8), ("bf16", 8, 0), ("f32", 8, 8, -1e-9), ("f32", 8, 8, float("nan")), ("f32", 8, 8, 1e39)):
+            assert call(L.norm(*d)) == L.LP_EINVAL, d
+        for d in (("f64", 8, 8), ("bf16", (1 << 24) + 1, 8), ("bf16", 8, (1 << 20) + 1), ("bf16", 1 << 24, 1 << 12)):
+            assert call(L.norm(*d)) == L.LP_EUNSUPPORTED, d
+        bad = L.norm("bf16", 8, 8)
+        bad.abi_version = 3
+        assert call(bad) == L.LP_EINVAL
+    for n in (2 ** 31, 2 ** 32 + 8):
+        with pytest.raises(L.LpError):
+            L.lp_norm_workspace_bytes(L.norm("bf16", n, 8))
+        with pytest.raises(L.LpError):
+            L.lp_norm_workspace_bytes(L.norm("bf16", 8, n))
+
+
+def test_norm_arguments():
+    nd = L.norm("bf16", 1000, 16)
+    for kw in (dict(x=None), dict(y=None), dict(y=FAKE[1]), dict(y=FAKE[2])):
+        assert norm_forward(nd, **kw) == L.LP_EINVAL, kw
+    for kw in (dict(x=None), dict(dy=None), dict(dx=FAKE[0]), dict(dx=FAKE[1]), dict(dx=FAKE[2]), dict(dgamma=FAKE[3]),
+               dict(dbeta=FAKE[2]), dict(dgamma=FAKE[4]), dict(dbeta=FAKE[5])):
+        assert norm_backward(nd, **kw) == L.LP_EINVAL, kw
+    for kw in bad_workspaces(L.lp_norm_workspace_bytes(nd)):
+        assert norm_backward(nd, **kw) == L.LP_EWORKSPACE, kw
+    assert norm_forward(L.norm("bf16", 0, 16), None, None, None, None) == L.LP_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_norm_workspaces(dtype):
+    """Partial sums of few rows, however many rows there are."""
+    rng, seen = random.Random(4), 0
+    for _ in range(400):
+        B, q = (rng.choice((1, t, t - 1, int(2 ** rng.uniform(0, t.bit_length() - 1)))) for t in (2 ** 24, 2 ** 20))
+        if B * q > 2 ** 35:
+            continue
+        seen += 1
+        assert 256 <= L.lp_norm_workspace_bytes(L.norm(dtype, B, q)) <= 8 * B + 8 * q * max(1100, B // 2048 + 1) + 512, (B, q)
+    assert seen > 100
+
+
 def test_binding_refuses_tensors():
     t = torch.zeros(8, 24, dtype=torch.bfloat16)
     with pytest.raises(ValueError):  # not on a GPU
         L.lp_gated_forward(gated(), t, t, t, t, torch.zeros(256, dtype=torch.uint8))
     with pytest.raises(ValueError):
         L.lp_gated_backward(gated(), t, t, t, t, None, None, None, None)
+    with pytest.raises(ValueError):
+        L.lp_norm_forward(L.norm("bf16", 8, 24), t, None, None, t)
     with pytest.raises(KeyError):
         L.gated("bf16", "swish", 1, 1, 1)
