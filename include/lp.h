@@ -497,8 +497,45 @@ int32_t lp_gated_forward(const lp_gated* layer, const void* x, const void* Wg, c
 int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, const void* Wu, const void* dy, void* dx,
                           void* dWg, void* dWu, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- orthogonalised updates ----
+ * Types, streams, workspaces and reproducibility as for the layer steps above. */
+
+/* Update of N weight matrices [no][ni] by their orthogonalised momentum (compare lp_sgd_update):
+ *   m' = mu m + g,   v = m' (nesterov: g + mu m'),   X = v / (|v| + eps), |v| the root of the sum of squares,
+ *   `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T,
+ *   W  = alpha X + beta r,
+ * each matrix by itself. The iteration maps each singular value s of X to a s + b s^3 + c s^5 and keeps the
+ * singular vectors: with a, b, c = 3.4445, -4.7750, 2.0315 five steps bring those above 0.003 to between 0.7 and
+ * 1.2, with 15/8, -10/8, 3/8 those near one converge to one.
+ * fp32: every product is one of fp32 values. 16-bit types: X, A and b A + c A^2 are rounded to f16, X times a
+ * power of two, so a, b, c have to keep singular values below about 10. A rounding error grows like a small
+ * singular value does, by about a factor a a step: with the first coefficients and five steps X is off by
+ * 1e-3 to 3e-3 of its norm on noise, more where a few directions exceed the others a hundredfold (4e-2). */
+typedef struct {
+  int32_t abi_version;   /* must equal LP_ABI_VERSION */
+  int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16: g, r and W; m is fp32 */
+  int32_t N;             /* matrices, >= 0, <= 2^24 */
+  int32_t no, ni;        /* rows and columns, >= 1; <= 2^20, the smaller of them <= 2^15 */
+  int32_t steps;         /* 1..64 */
+  int32_t nesterov;      /* 0 | 1 (1 needs a momentum) */
+  double a, b, c;        /* finite in fp32 */
+  double eps;            /* >= 0, finite (0: a matrix of zeros gives NaN) */
+  double mu;             /* finite in fp32 */
+} lp_orth;
+
+/* Workspace bytes of lp_orth_update; 0 for an invalid update. It holds X twice, A and b A + c A^2 of as many
+ * matrices as 128 MiB hold (at least one), and the partial sums of split products. */
+size_t lp_orth_workspace_bytes(const lp_orth* orth);
+
+/* The update. g, r, W [N][no][ni]; m, mo [N][no][ni] fp32: m' goes to mo, which may be m. Without mo (m NULL
+ * too) there is no momentum, v = g; without m, m' = g. r nullable (W = alpha X), r may be W. No other array
+ * may overlap another. alpha and beta finite in fp32. */
+int32_t lp_orth_update(const lp_orth* orth, const void* g, const float* m, float* mo, double alpha, double beta,
+                       const void* r, void* W, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- tracing (a profiling aid, not part of the method) ----
- * (The kernels of layer steps, checkpoints, label heads, norms and gated layers are of no kind here.)
+ * (The kernels of layer steps, checkpoints, label heads, norms, gated layers and orthogonalised
+ * updates are of no kind here.)
  * When enabled for a kernel kind, every launch of that kind records a pair of
  * HIP events on the launch's stream; lp_trace_read sums their elapsed times.
  * Kinds: the three sweeps of a non-coarsest MGRIT level, the coarsest-level

@@ -20,7 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_gated_bf16.hip", "lp_gated_f16.hip", "lp_gated_f32.hip",
-           "lp_norm.hip", "lp_step_host.cpp", "lp_block_host.cpp", "lp_host.cpp", "lp_common.hip",
+           "lp_orth_f16.hip", "lp_orth_f32.hip", "lp_norm.hip", "lp_step_host.cpp", "lp_block_host.cpp", "lp_host.cpp", "lp_common.hip",
            "lp_loss.hip", "lp_dense_f32.hip", "lp_dense_narrow.hip", "lp_dense_mfma.hip", "lp_dense_resid.hip", "lp_dense_serial.hip",
            "lp_dense_wide.hip", "lp_conv.hip", "lp_noalloc.hip"]
 
@@ -49,7 +49,8 @@ SAN_FLAGS = ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-
              "-Xarch_host", "-shared-libasan"]
 # the translation units with host logic beyond launches
 SAN_SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_gated_bf16.hip", "lp_gated_f16.hip", "lp_gated_f32.hip",
-               "lp_norm.hip", "lp_step_host.cpp", "lp_block_host.cpp", "lp_host.cpp", "lp_noalloc.hip"]
+               "lp_orth_f16.hip", "lp_orth_f32.hip", "lp_norm.hip", "lp_step_host.cpp", "lp_block_host.cpp", "lp_host.cpp",
+               "lp_noalloc.hip"]
 SAN_OUT = os.path.join(OBJ, "liblp_san.so")
 
 

@@ -1,4 +1,4 @@
-// Host side of the layer norm and the gated layers (include/lp.h): argument checks, workspace layouts, dispatch by
+// Host side of the layer norm, the gated layers and the orthogonalised updates (include/lp.h): argument checks, workspace layouts, dispatch by
 // element type.
 #include <math.h>
 
@@ -17,7 +17,7 @@ using lp::hip_fail;
 constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
 // Limits as for the layer steps (lp_step_host.cpp): 32-bit index arithmetic inside a tile stays far from its own.
-constexpr int kMaxRows = 1 << 24, kMaxWidth = 1 << 20;
+constexpr int kMaxRows = 1 << 24, kMaxWidth = 1 << 20, kMaxShort = 1 << 15, kMaxSteps = 64;
 constexpr double kMaxValues = 34359738368.0;  // 2^35
 
 size_t esize(int32_t d) { return d == LP_F32 ? 4 : 2; }
@@ -57,6 +57,23 @@ int check_norm(const lp_norm* n) {
   if (n->q > kMaxWidth) return fail(LP_EUNSUPPORTED, "q = %d > %d", n->q, kMaxWidth);
   if ((double)n->B * n->q > kMaxValues) return fail(LP_EUNSUPPORTED, "more than 2^35 values in an array");
   if (!(n->eps >= 0) || !isfinite((float)n->eps)) return fail(LP_EINVAL, "eps must be >= 0 and finite in fp32");
+  return LP_OK;
+}
+
+int check_orth(const lp_orth* o) {
+  if (!o) return fail(LP_EINVAL, "update is NULL");
+  const int rc = check_type(o->abi_version, o->dtype);
+  if (rc) return rc;
+  if (o->N < 0) return fail(LP_EINVAL, "N = %d < 0", o->N);
+  if (o->no < 1 || o->ni < 1) return fail(LP_EINVAL, "bad sizes no = %d, ni = %d", o->no, o->ni);
+  if (o->steps < 1 || o->steps > kMaxSteps) return fail(LP_EINVAL, "steps = %d, not in 1..%d", o->steps, kMaxSteps);
+  if (o->nesterov != 0 && o->nesterov != 1) return fail(LP_EINVAL, "nesterov must be 0 or 1");
+  for (double v : {o->a, o->b, o->c, o->mu})
+    if (!isfinite(v) || !isfinite((float)v)) return fail(LP_EINVAL, "a, b, c and mu must be finite in fp32");
+  if (!(o->eps >= 0) || !isfinite(o->eps)) return fail(LP_EINVAL, "eps must be >= 0 and finite");
+  if (o->N > kMaxRows || o->no > kMaxWidth || o->ni > kMaxWidth || std::min(o->no, o->ni) > kMaxShort)
+    return fail(LP_EUNSUPPORTED, "N = %d > %d, no = %d or ni = %d > %d, or both > %d", o->N, kMaxRows, o->no, o->ni, kMaxWidth, kMaxShort);
+  if ((double)o->N * o->no * o->ni > kMaxValues) return fail(LP_EUNSUPPORTED, "more than 2^35 values in an array");
   return LP_OK;
 }
 
@@ -107,6 +124,35 @@ GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad) {
   l.Wg = p.take(no * row);
   l.Wu = p.take(no * row);
   l.part = p.take(part);
+  l.total = p.total();
+  return l;
+}
+
+// Matrices are taken a chunk at a time, whose X, A and P stay in the last cache (256 MB) and of which there are enough to
+// fill the card with tiles.
+constexpr size_t ORTH_CHUNK = (size_t)128 << 20;
+
+OrthLayout orth_layout(int dtype, int N, int no, int ni) {
+  const size_t e = esize(dtype);  // (of the products: f16 for both 16-bit types)
+  const int n = std::min(no, ni), k = std::max(no, ni);
+  OrthLayout l{};
+  l.ld = mm::padded(e, ni);
+  l.lda = mm::padded(e, n);
+  const size_t x = (size_t)no * l.ld * e, a = (size_t)n * l.lda * e;
+  l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a)), 1), 16384));
+  l.parts = (int)std::min<size_t>(((size_t)no * ni + 4095) / 4096, 128);
+  l.gram = mm::plan_of(e, n, n, k, l.chunk, true);
+  l.poly = mm::plan_of(e, n, n, n, l.chunk, true);
+  l.next = mm::plan_of(e, no, ni, n, l.chunk);
+  const auto part = [&](const mm::Plan& p, bool sym) {
+    return p.splits > 1 ? (size_t)l.chunk * p.splits * tiles_of(p, sym) * p.tile * p.tile * 4 : 0;
+  };
+  Parts p;
+  l.norms = p.take((size_t)l.chunk * l.parts * 8);
+  for (size_t& at : l.X) at = p.take(l.chunk * x);
+  l.A = p.take(l.chunk * a);
+  l.P = p.take(l.chunk * a);
+  l.part = p.take(std::max({part(l.gram, true), part(l.poly, true), part(l.next, false)}));
   l.total = p.total();
   return l;
 }
@@ -189,6 +235,30 @@ int32_t lp_gated_backward(const lp_gated* g, const void* x, const void* Wg, cons
   a.x = x, a.Wg = Wg, a.Wu = Wu, a.dy = dy, a.dx = dx, a.dWg = dWg, a.dWu = dWu, a.ws = ws;
   const hipError_t e = LP_BY_TYPE(g->dtype, gated_backward, a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? LP_OK : hip_fail(e, "gated backward");
+}
+
+size_t lp_orth_workspace_bytes(const lp_orth* o) {
+  if (check_orth(o) != LP_OK) return 0;
+  lp::clear_error();
+  return lp::orth_layout(o->dtype, o->N, o->no, o->ni).total;
+}
+
+int32_t lp_orth_update(const lp_orth* o, const void* g, const float* m, float* mo, double alpha, double beta, const void* r,
+                       void* W, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_orth(o);
+  if (rc) return rc;
+  if (!isfinite(alpha) || !isfinite((float)alpha) || !isfinite(beta) || !isfinite((float)beta))
+    return fail(LP_EINVAL, "alpha and beta must be finite in fp32");
+  if (o->N && (!g || !W)) return fail(LP_EINVAL, "NULL array argument");
+  if (m && !mo) return fail(LP_EINVAL, "m is given without mo");
+  if (o->nesterov && !mo) return fail(LP_EINVAL, "nesterov without a momentum");
+  if (any_same({W, mo}, {g}) || any_same({W}, {m}) || any_same({mo}, {r}))
+    return fail(LP_EINVAL, "an output aliases an input or another output");
+  if ((rc = check_ws(ws, ws_bytes, lp::orth_layout(o->dtype, o->N, o->no, o->ni).total))) return rc;
+  if (o->N == 0) return LP_OK;
+  lp::OrthArgs a{o->dtype, o->N, o->no, o->ni, o->steps, o->nesterov, o->a, o->b, o->c, o->eps, o->mu, alpha, beta, g, m, mo, r, W, ws};
+  const hipError_t e = LP_BY_TYPE(o->dtype, orth_update, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? LP_OK : hip_fail(e, "orthogonalised update");
 }
 
 }  // extern "C"

@@ -319,6 +319,29 @@ LP_NORM_LAUNCHERS(f16)
 LP_NORM_LAUNCHERS(f32)
 #undef LP_NORM_LAUNCHERS
 
+struct OrthArgs {
+  int dtype, N, no, ni, steps, nesterov;
+  double a, b, c, eps, mu, alpha, beta;
+  const void* g;   // [N][no][ni]
+  const float* m;  // [N][no][ni], nullable
+  float* mo;       // [N][no][ni], nullable
+  const void* r;   // [N][no][ni], nullable
+  void* W;         // [N][no][ni]
+  void* ws;
+};
+struct OrthLayout {
+  size_t norms, X[2], A, P, part, total;
+  int ld, lda;            // rows of X and of A, P
+  int chunk, parts;       // matrices taken at a time; partial sums of a matrix's squares
+  mm::Plan gram, poly, next;  // the products A, A^2 and P X
+};
+OrthLayout orth_layout(int dtype, int N, int no, int ni);
+// tiles of a plan (of a symmetric result: on and below the diagonal)
+inline long tiles_of(const mm::Plan& p, bool sym) { return sym ? (long)p.tm * (p.tm + 1) / 2 : (long)p.tm * p.tn; }
+hipError_t orth_update_bf16(const OrthArgs& a, hipStream_t st);
+hipError_t orth_update_f16(const OrthArgs& a, hipStream_t st);
+hipError_t orth_update_f32(const OrthArgs& a, hipStream_t st);
+
 struct GatedArgs {
   int dtype, act;
   int B, ni, no;

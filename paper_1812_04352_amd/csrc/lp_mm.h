@@ -851,7 +851,7 @@ struct EpScale {
 
 // Adds the partial sums of a split contraction in order and runs the epilogue.
 template <class S, class E>
-__global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int splits, typename E::Args ea) {
+__device__ __forceinline__ void finish_tile(const Prob& p, const f32x4* part, int splits, const typename E::Args& ea) {
   constexpr int WGM = S::WGM, WGN = S::WGN, FM = S::BM / WGM / 32, FN = S::BN / WGN / 32, Q = 4 * FM * FN;
   __shared__ __attribute__((aligned(16))) float lds[epilogue_lds(WGM * WGN, S::BM, WGN) / 4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -881,6 +881,11 @@ __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int
   }
   if (c.n0 + S::BNO <= c.N) E::template run<true, FM, FN, WGM, WGN>(ea, c, acc, lds);
   else E::template run<false, FM, FN, WGM, WGN>(ea, c, acc, lds);
+}
+
+template <class S, class E>
+__global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int splits, typename E::Args ea) {
+  finish_tile<S, E>(p, part, splits, ea);
 }
 
 // A product of one row of A (both operands in rows): bound by reading B once. A workgroup takes NF
@@ -1130,7 +1135,8 @@ constexpr int STAGE_BYTES = 128;
 // 4096 230 us by 256 (128: 256, 64: over 370). float: 4096 x 1024 x 1024 60 us by 128 (64: 74, 256: 134);
 // 1024 x 1024 x 4096 (columns) 70 by 128 in eight splits, which the estimate takes, 68 in four (64 in two: 77,
 // 256: 501); 4096 x 4096 x 4096 545 by 256 (128: 600 to 694, 64: 1008).
-inline Plan plan_of(size_t esz, long M, long N, long K) {
+// batch: products of this size in one launch; sym: only the tiles on and below the diagonal.
+inline Plan plan_of(size_t esz, long M, long N, long K, long batch = 1, bool sym = false) {
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
   const double stage[2][3][2] = {{{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{4.1, 8.7}, {1.8, 2.7}, {0.75, 1.15}}};
   const auto& us = stage[esz == 4];
@@ -1138,15 +1144,15 @@ inline Plan plan_of(size_t esz, long M, long N, long K) {
   double least = 1e30;
   for (int s = 0; s < 3; ++s) {
     const int tile = 256 >> s;
-    const long tm = ceil_div(M, tile), tn = ceil_div(N, tile);
+    const long tm = ceil_div(M, tile), tn = ceil_div(N, tile), tiles = batch * (sym ? tm * (tm + 1) / 2 : tm * tn);
     // (one tile row reads its weights once, from memory: 0.42 a stage with one workgroup on a CU)
     const double two = us[s][1],
-                 one = tile == 256 && tm * tn > 128 ? two / 2 : tile == 64 && tm == 1 && esz == 2 ? 0.42 : us[s][0];
+                 one = tile == 256 && tiles > 128 ? two / 2 : tile == 64 && tm == 1 && esz == 2 ? 0.42 : us[s][0];
     for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (splits > 1 && (steps < 4 * splits || tile == 256)) break;  // (a split large tile would be two middle ones)
-      const long n = ceil_div(tm * tn * splits, 256);
+      const long n = ceil_div(tiles * splits, 256);
       double t = ceil_div(steps, splits) * ((n / 2) * two + (n % 2) * one);
-      if (splits > 1) t += 3.0 + 2.0 * splits * M * tn * tile * 4 / 3e6;
+      if (splits > 1) t += 3.0 + 2.0 * splits * M * tn * tile * 4 * (sym ? 0.5 : 1.0) * batch / 3e6;
       if (t < least) {
         least = t;
         best = Plan{tile, splits, (int)tm, (int)tn};

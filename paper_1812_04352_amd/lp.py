@@ -48,6 +48,7 @@ EXPORTS = (
     "lp_loss_labels_workspace_bytes", "lp_loss_labels",
     "lp_norm_workspace_bytes", "lp_norm_forward", "lp_norm_backward",
     "lp_gated_workspace_bytes", "lp_gated_forward", "lp_gated_backward",
+    "lp_orth_workspace_bytes", "lp_orth_update",
 )
 
 
@@ -89,6 +90,12 @@ class LpGated(ctypes.Structure):
                 ("B", ctypes.c_int32), ("ni", ctypes.c_int32), ("no", ctypes.c_int32)]
 
 
+class LpOrth(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_int32), ("dtype", ctypes.c_int32), ("N", ctypes.c_int32), ("no", ctypes.c_int32),
+                ("ni", ctypes.c_int32), ("steps", ctypes.c_int32), ("nesterov", ctypes.c_int32), ("a", ctypes.c_double),
+                ("b", ctypes.c_double), ("c", ctypes.c_double), ("eps", ctypes.c_double), ("mu", ctypes.c_double)]
+
+
 class LpError(RuntimeError):
     def __init__(self, status: int, call: str, detail: str):
         super().__init__(f"{call}: status {status} ({detail})")
@@ -103,6 +110,7 @@ _S = ctypes.POINTER(LpStep)
 _H = ctypes.POINTER(LpLabelHead)
 _N = ctypes.POINTER(LpNorm)
 _G = ctypes.POINTER(LpGated)
+_O = ctypes.POINTER(LpOrth)
 _v = ctypes.c_void_p
 _i32 = ctypes.c_int32
 _sz = ctypes.c_size_t
@@ -145,6 +153,8 @@ _SIGS = {
     "lp_norm_backward": ([_N, _v, _v, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
     "lp_gated_workspace_bytes": ([_G, _i32], _sz),
     "lp_gated_forward": ([_G, _v, _v, _v, _v, _v, _sz, _v], _i32),
+    "lp_orth_workspace_bytes": ([_O], _sz),
+    "lp_orth_update": ([_O, _v, _v, _v, ctypes.c_double, ctypes.c_double, _v, _v, _v, _sz, _v], _i32),
     "lp_gated_backward": ([_G, _v, _v, _v, _v, _v, _v, _v, _v, _sz, _v], _i32),
 }
 
@@ -756,3 +766,44 @@ def lp_gated_backward(gd: LpGated, x, Wg, Wu, dy, dx, dWg, dWu, ws) -> None:
         _dev(dWu, no * ni, "dWu", dt, dev, True), wp, wn, _stream_of(dev))
     if rc:
         _check(rc, "lp_gated_backward")
+
+
+# ---------------------------------------------------------------- orthogonalised updates
+
+QUINTIC = (3.4445, -4.7750, 2.0315)  # singular values in (0.003, 1] to 0.7 .. 1.2 in five steps
+
+
+def orth(dtype: str, N: int, no: int, ni: int, steps: int = 5, coeffs: Sequence[float] = QUINTIC, eps: float = 1e-7,
+         mu: float = 0.0, nesterov: bool = False) -> LpOrth:
+    """Orthogonalised update of N matrices [no][ni]; dtype "f32", "bf16" or "f16". mu, nesterov: of the momentum."""
+    a, b, c = coeffs
+    return LpOrth(LP_ABI_VERSION, WIDE_DTYPE[dtype], _count(N), _count(no), _count(ni), _count(steps), int(bool(nesterov)),
+                  a, b, c, eps, mu)
+
+
+def lp_orth_workspace_bytes(od: LpOrth) -> int:
+    n = load().lp_orth_workspace_bytes(ctypes.byref(od))
+    if n == 0:
+        raise LpError(LP_EINVAL, "lp_orth_workspace_bytes", load().lp_last_error().decode())
+    return int(n)
+
+
+def alloc_orth_workspace(od: LpOrth, device="cuda"):
+    import torch
+    return torch.empty(lp_orth_workspace_bytes(od), dtype=torch.uint8, device=device)
+
+
+def lp_orth_update(od: LpOrth, g, m, mo, r, W, ws, alpha: float, beta: float = 1.0) -> None:
+    """W = alpha O + beta r, O the orthogonalised momentum: mo (float32) <- mu m + g, m its value before (None: mo
+    <- g); without mo no momentum. r may be None (W = alpha O) or W itself; mo may be m."""
+    import torch
+    dt = _wide_dtype(od.dtype)
+    dev = _here(g, "g")
+    n = od.N * od.no * od.ni
+    wp, wn = _dev_ws(ws, dev)
+    rc = (_lib or load()).lp_orth_update(
+        ctypes.byref(od), _dev(g, n, "g", dt, dev), _dev(m, n, "m", torch.float32, dev, True),
+        _dev(mo, n, "mo", torch.float32, dev, True), alpha, beta, _dev(r, n, "r", dt, dev, True), _dev(W, n, "W", dt, dev),
+        wp, wn, _stream_of(dev))
+    if rc:
+        _check(rc, "lp_orth_update")

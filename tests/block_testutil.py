@@ -173,3 +173,80 @@ class Norm:
         for v, f in bufs:
             assert v is None or T.guarded(f, v.numel())
         return [v for v, _ in bufs]
+
+
+def momentum(g, m, mu, nesterov, dtype):
+    """m' and v, with the error of m' (two fp32 roundings)."""
+    g = g.double()
+    if m is None and mu is None:
+        return None, g
+    mo = g if m is None else mu * m.double() + g
+    return mo, (g + mu * mo if nesterov else mo)
+
+
+def iterate(v, steps, coeffs, eps, keep=None):
+    """The iteration on a batch of matrices; keep: a rounding made where the kernels make one."""
+    a, b, c = coeffs
+    keep = keep or (lambda t: t)
+    X = keep(v / (torch.linalg.vector_norm(v, dim=(1, 2), keepdim=True) + eps))
+    tall = v.shape[1] > v.shape[2]
+    X = X.transpose(1, 2).contiguous() if tall else X
+    for s in range(steps):
+        A = keep(torch.matmul(X, X.transpose(1, 2).contiguous()))
+        P = keep(b * A + c * torch.matmul(A, A))
+        X = a * X + torch.matmul(P, X)
+        if s + 1 < steps:
+            X = keep(X)
+    return X.transpose(1, 2) if tall else X
+
+
+def rounding(dtype, shape, seed=0):
+    """What the products' operands are rounded to: f16 of values times about the root of the long side (only X has
+    values that small), fp32, with the products' own error, by 2^-21."""
+    if dtype == "f32":
+        g = torch.Generator(device="cpu").manual_seed(seed)
+        return lambda t: t * (1 + (2 * torch.rand(t.shape, generator=g, dtype=torch.float64).to(t.device) - 1) * 2.0 ** -21)
+    up = 2.0 ** round(0.5 * math.log2(max(shape[1:])))
+
+    def keep(t):
+        f = 1.0 if t.shape[1] == t.shape[2] and shape[1] != shape[2] else up
+        return (t * f).half().double() / f
+    return keep
+
+
+def orth_check(W, v, r, steps, coeffs, eps, alpha, beta, dtype, what):
+    """W against 64 bits: no further off than three times what the same roundings cost in 64-bit products
+    (roundings that fall otherwise cost another amount of that size), in the norm of every matrix and in
+    the largest element, besides those of W itself."""
+    O = iterate(v, steps, coeffs, eps)
+    E = iterate(v, steps, coeffs, eps, rounding(dtype, v.shape))
+    ref = alpha * O + (0.0 if r is None else beta * r.to(v.device).double())
+    err, em = (W.to(v.device).double() - ref).abs(), abs(alpha) * (E - O).abs()
+    own = T.half_step(dtype) * ref.abs() + 3 * E32 * (ref.abs() + abs(alpha) * O.abs()) + T.tiny(dtype)
+    norm = lambda t: torch.linalg.vector_norm(t, dim=(1, 2))
+    size = v.shape[1] * v.shape[2]
+    # (few values: one rounding decides; those of a matrix of a few values are allowed their largest step)
+    slack = 4.0 if size >= 64 else 12.0
+    step = 2.0 ** -21 if dtype == "f32" else 2.0 ** -11
+    grow = sum(max(abs(coeffs[0]), 4.0) ** k for k in range(steps + 1))
+    few = abs(alpha) * step * grow * norm(O) / math.sqrt(size) if size < 64 else 0.0
+    over = norm(err) > slack * norm(em) + norm(own) + few
+    assert not over.any(), (what, norm(err)[over], norm(em)[over], norm(own)[over])
+    worst = (err - own).flatten(1).amax(1)
+    assert (worst <= slack * em.flatten(1).amax(1) + few).all(), (what, worst, em.flatten(1).amax(1))
+
+
+class Orth:
+    """One update's calls, outputs guarded, from a workspace full of NaN."""
+
+    def __init__(self, dtype, N, no, ni, **kw):
+        self.dtype, self.od = dtype, L.orth(dtype, N, no, ni, **kw)
+        self.shape = (N, no, ni)
+
+    def __call__(self, g, m, mo, r, alpha, beta=1.0):
+        ws = scribble(L.alloc_orth_workspace(self.od))
+        W, wf = T.out(self.shape, T.DT[self.dtype])
+        L.lp_orth_update(self.od, g, m, mo, r, W, ws, alpha=alpha, beta=beta)
+        torch.cuda.synchronize()
+        assert T.guarded(wf, W.numel())
+        return W

@@ -1,4 +1,4 @@
-"""Refusals of the layer norm and the gated layers on the host (no GPU): every bad call returns its documented status before
+"""Refusals of the layer norm, the gated layers and the orthogonalised updates on the host (no GPU): every bad call returns its documented status before
 any device work, the binding refuses bad tensors, and workspaces hold what they have to."""
 import ctypes
 import random
@@ -135,6 +135,64 @@ def test_norm_workspaces(dtype):
         seen += 1
         assert 256 <= L.lp_norm_workspace_bytes(L.norm(dtype, B, q)) <= 8 * B + 8 * q * max(1100, B // 2048 + 1) + 512, (B, q)
     assert seen > 100
+
+
+def orth(od, g=FAKE[0], m=FAKE[1], mo=FAKE[2], alpha=1.0, beta=1.0, r=FAKE[3], W=FAKE[4], ws=FAKE[5], n=BIG):
+    return L.load().lp_orth_update(ctypes.byref(od) if od else None, g, m, mo, alpha, beta, r, W, ws, n, None)
+
+
+def test_orth_descriptor():
+    assert orth(None) == L.LP_EINVAL
+    nan, inf = float("nan"), float("inf")
+    for d, kw in ((("bf16", -1, 4, 4), {}), (("bf16", 2, 0, 4), {}), (("bf16", 2, 4, -1), {}), (("bf16", 2, 4, 4), dict(steps=0)),
+                  (("bf16", 2, 4, 4), dict(steps=65)), (("f32", 2, 4, 4), dict(coeffs=(nan, 1, 1))),
+                  (("f32", 2, 4, 4), dict(coeffs=(1, 1e39, 1))), (("f32", 2, 4, 4), dict(eps=-1.0)), (("f32", 2, 4, 4), dict(eps=inf)),
+                  (("f32", 2, 4, 4), dict(mu=inf))):
+        assert orth(L.orth(*d, **kw)) == L.LP_EINVAL, (d, kw)
+        with pytest.raises(L.LpError):
+            L.lp_orth_workspace_bytes(L.orth(*d, **kw))
+    for d in (("f64", 2, 4, 4), ("bf16", (1 << 24) + 1, 4, 4), ("bf16", 1, (1 << 20) + 1, 4), ("bf16", 1, 4, (1 << 20) + 1),
+              ("bf16", 1, (1 << 15) + 1, (1 << 15) + 1), ("bf16", 1 << 24, 64, 64)):
+        assert orth(L.orth(*d)) == L.LP_EUNSUPPORTED, d
+    for field, value in (("abi_version", 3), ("dtype", 9), ("nesterov", 2)):
+        o = L.orth("bf16", 2, 4, 4)
+        setattr(o, field, value)
+        assert orth(o) == L.LP_EINVAL, field
+    for n in (2 ** 31, 2 ** 32 + 8):
+        for d in ((n, 4, 4), (1, n, 4), (1, 4, n)):
+            with pytest.raises(L.LpError):
+                L.lp_orth_workspace_bytes(L.orth("bf16", *d))
+
+
+def test_orth_arguments():
+    o = L.orth("bf16", 3, 16, 24, nesterov=True)
+    for kw in (dict(g=None), dict(W=None), dict(mo=None), dict(m=None, mo=None), dict(W=FAKE[0]), dict(W=FAKE[1]), dict(W=FAKE[2]),
+               dict(mo=FAKE[0]), dict(r=FAKE[2]), dict(alpha=float("nan")), dict(beta=1e39)):
+        assert orth(o, **kw) == L.LP_EINVAL, kw
+    for kw in bad_workspaces(L.lp_orth_workspace_bytes(o)):
+        assert orth(o, **kw) == L.LP_EWORKSPACE, kw
+    assert orth(L.orth("bf16", 0, 16, 24), g=None, m=None, mo=None, r=None, W=None) == L.LP_OK
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_orth_workspaces(dtype):
+    """What one matrix takes at least; a batch takes no more than some or that of one."""
+    rng, seen, e = random.Random(5), 0, SIZE[dtype]
+    for _ in range(400):
+        N, a, b = (rng.choice((1, t, t - 1, int(2 ** rng.uniform(0, t.bit_length() - 1)))) for t in (2 ** 24, 2 ** 15, 2 ** 20))
+        if N * a * b > 2 ** 35:
+            continue
+        no, ni = (a, b) if rng.random() < 0.5 else (b, a)
+        n = min(no, ni)
+        seen += 1
+        one, all_ = (L.lp_orth_workspace_bytes(L.orth(dtype, k, no, ni)) for k in (1, N))
+        held = 2 * (no * ni + n * n) * e
+        assert held <= one, (no, ni)
+        # (X, A and their like in rows of up to 128 bytes more; at most 32 sums of whole tiles of 128 for each product)
+        rows = held + 2 * 128 * (no + n) + 8 * 128
+        parts = 128 * max((n + 128) ** 2, (no + 128) * (ni + 128))
+        assert all_ <= max(rows, 2 ** 27 + 16384 * 1024 + rows) + min(N, max(1, 2 ** 27 // held)) * parts + 4096, (N, no, ni, all_)
+    assert seen > 60
 
 
 def test_binding_refuses_tensors():
