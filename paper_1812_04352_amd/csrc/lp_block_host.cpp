@@ -136,11 +136,15 @@ OrthLayout orth_layout(int dtype, int N, int no, int ni) {
   const size_t e = esize(dtype);  // (of the products: f16 for both 16-bit types)
   const int n = std::min(no, ni), k = std::max(no, ni);
   OrthLayout l{};
+  if (orth_small(no, ni)) {
+    l.total = 256;
+    return l;
+  }
   l.ld = mm::padded(e, ni);
   l.lda = mm::padded(e, n);
   const size_t x = (size_t)no * l.ld * e, a = (size_t)n * l.lda * e;
   l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a)), 1), 16384));
-  l.parts = (int)std::min<size_t>(((size_t)no * ni + 4095) / 4096, 128);
+  l.parts = (int)std::min<size_t>(((size_t)no * ni + 4095) / 4096, 2048);
   l.gram = mm::plan_of(e, n, n, k, l.chunk, true);
   l.poly = mm::plan_of(e, n, n, n, l.chunk, true);
   l.next = mm::plan_of(e, no, ni, n, l.chunk);

@@ -336,6 +336,8 @@ struct OrthLayout {
   mm::Plan gram, poly, next;  // the products A, A^2 and P X
 };
 OrthLayout orth_layout(int dtype, int N, int no, int ni);
+// a workgroup holds such a matrix (lp_orth_impl.h)
+inline bool orth_small(int no, int ni) { return (no < ni ? no : ni) <= 64 && (no < ni ? ni : no) <= 256; }
 // tiles of a plan (of a symmetric result: on and below the diagonal)
 inline long tiles_of(const mm::Plan& p, bool sym) { return sym ? (long)p.tm * (p.tm + 1) / 2 : (long)p.tm * p.tn; }
 hipError_t orth_update_bf16(const OrthArgs& a, hipStream_t st);

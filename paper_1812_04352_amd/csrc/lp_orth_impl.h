@@ -89,7 +89,6 @@ struct Momentum {
 };
 
 constexpr int VV = 4;           // values a thread takes at a time
-constexpr int MOST_PARTS = 128;  // partial sums of a matrix's squares
 
 // m', and partial sums of v's squares in fp64 (grid y: the matrix)
 template <typename TI>
@@ -117,8 +116,8 @@ __global__ __launch_bounds__(256) void k_scale(Momentum<TI, VV> u, int no, int n
   __shared__ double sh;
   if (threadIdx.x < 64) {
     const double* p = part + (size_t)blockIdx.y * parts;
-    double s = (int)threadIdx.x < parts ? p[threadIdx.x] : 0.0;
-    if ((int)threadIdx.x + 64 < parts) s += p[threadIdx.x + 64];
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 64) s += p[i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if (threadIdx.x == 0) sh = up / (sqrt(s) + eps);
@@ -144,6 +143,193 @@ __global__ __launch_bounds__(256) void k_scale(Momentum<TI, VV> u, int no, int n
     }
     *reinterpret_cast<typename GVec<T, VV>::type*>(X + r * ld + c) = x;
   }
+}
+
+// ---------------------------------------------------------------- small matrices
+
+// A matrix whose short side is at most SMALL_N and its long one at most SMALL_K takes one workgroup and one launch: X stays
+// in registers in fp32 (as the accumulators of its product, the short side on rows: a tall matrix is
+// turned as it is read and written), and the LDS holds what the products read, X and then A and P in its place,
+// as the sum of two f16 values each (2^-22 relative): three instructions a product of two such values.
+//   wave (wi, wj): rows 32 wi .., of A and P columns 32 wj .., of X the blocks wj, wj + 2, .. of 32 columns.
+// 2048 of 64 x 64 f32 LP_SMALL_US us.
+constexpr int SMALL_N = 64, SMALL_K = 256;
+constexpr float A_UP = 256.f;  // A and P are kept times this: their small values stay normal f16 numbers
+
+struct Half2 {
+  mm::h16x8 h, l;
+};
+
+// KB: columns of X in blocks of 64
+template <int KB>
+struct SmallLds {
+  static constexpr int XP = (64 * KB + 8) * 2, AP = (64 + 8) * 2;  // bytes a row
+  __attribute__((aligned(16))) unsigned char x[2][64 * XP];
+  __attribute__((aligned(16))) unsigned char a[2][64 * AP];
+  double sum[4];
+};
+
+// a 32 x 32 block of values to both parts: rows m0 + lane % 32, columns n0 ..
+template <int PITCH, int SIZE>
+__device__ __forceinline__ void put_parts(unsigned char (&at)[2][SIZE], int m0, int n0, int lane, const f32x16& v, float up) {
+  typedef _Float16 h16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    h16x4 h, l;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float f = v[4 * q + k] * up;
+      h[k] = (_Float16)f;
+      l[k] = (_Float16)(f - (float)h[k]);
+    }
+    const int o = (m0 + (lane & 31)) * PITCH + (n0 + 8 * q + 4 * (lane >> 5)) * 2;
+    *reinterpret_cast<h16x4*>(at[0] + o) = h;
+    *reinterpret_cast<h16x4*>(at[1] + o) = l;
+  }
+}
+
+// eight contraction values from 16 kk + 8 (lane / 32) on of row r0 + lane % 32
+template <int PITCH, int SIZE>
+__device__ __forceinline__ Half2 get_rows(const unsigned char (&at)[2][SIZE], int r0, int kk, int lane) {
+  const int o = (r0 + (lane & 31)) * PITCH + (16 * kk + 8 * (lane >> 5)) * 2;
+  return {*reinterpret_cast<const mm::h16x8*>(at[0] + o), *reinterpret_cast<const mm::h16x8*>(at[1] + o)};
+}
+// and where the contraction runs over the rows: of column c0 + lane % 32 (transposing LDS reads, as in lp_mm.h)
+template <int PITCH, int SIZE>
+__device__ __forceinline__ Half2 get_columns(const unsigned char (&at)[2][SIZE], int c0, int kk, int lane) {
+  Half2 r;
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef __attribute__((address_space(3))) mm::s16x4 lds4;
+  const int o = (16 * kk + 8 * (lane >> 5) + ((lane >> 2) & 3)) * PITCH + (c0 + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)) * 2;
+  mm::s16x4 v[2][2];
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) v[p][j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at[p] + o + 4 * j * PITCH));
+  r.h = __builtin_bit_cast(mm::h16x8, __builtin_shufflevector(v[0][0], v[0][1], 0, 1, 2, 3, 4, 5, 6, 7));
+  r.l = __builtin_bit_cast(mm::h16x8, __builtin_shufflevector(v[1][0], v[1][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#endif
+  return r;
+}
+__device__ __forceinline__ f32x16 mma2(const Half2& n, const Half2& m, f32x16 c) {
+  c = mm::mma(n.l, m.h, c);
+  c = mm::mma(n.h, m.l, c);
+  return mm::mma(n.h, m.h, c);
+}
+
+struct SmallArgs {
+  int no, ni, steps;
+  float a, b, c, alpha, beta;
+  double eps, up;  // X is kept times up
+};
+
+template <typename TI, int KB, bool TALL>
+__global__ __launch_bounds__(256) void k_small(Momentum<TI, TALL ? 1 : 4> u, const TI* r, TI* W, SmallArgs a) {
+  typedef SmallLds<KB> Lds;
+  __shared__ Lds lds;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 1, wj = wave & 1;
+  const int n = TALL ? a.ni : a.no, k = TALL ? a.no : a.ni, m = 32 * wi + (lane & 31);
+  const size_t base = (size_t)blockIdx.x * a.no * a.ni;
+  // f(t, e, at, w): w values at index `at`, the elements e .. of block t
+  const auto each = [&](auto f) {
+#pragma unroll
+    for (int t = 0; t < KB; ++t)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = 32 * (wj + 2 * t) + 8 * q + 4 * (lane >> 5);
+        if constexpr (TALL) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m < n && c + e < k) f(t, 4 * q + e, base + (size_t)(c + e) * a.ni + m, 1);
+        } else {
+          if (m < n && c < k) f(t, 4 * q, base + (size_t)m * a.ni + c, min(4, k - c));
+        }
+      }
+  };
+  constexpr int V = TALL ? 1 : 4;
+  f32x16 x[KB];
+#pragma unroll
+  for (int t = 0; t < KB; ++t) x[t] = 0.f;
+  double s = 0.0;
+  each([&](int t, int e, size_t at, int w) {
+    float v[V];
+    u.update(at, w, v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (i < w) x[t][e + i] = v[i];
+      if (i < w) s += (double)v[i] * (double)v[i];
+    }
+  });
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (lane == 0) lds.sum[wave] = s;
+  __syncthreads();
+  const double scale = a.up / (sqrt(((lds.sum[0] + lds.sum[1]) + lds.sum[2]) + lds.sum[3]) + a.eps);
+#pragma unroll
+  for (int t = 0; t < KB; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[t][e] = (float)((double)x[t][e] * scale);
+  const float down = (float)(1.0 / (a.up * a.up));
+  for (int step = 0; step < a.steps; ++step) {
+#pragma unroll
+    for (int t = 0; t < KB; ++t) put_parts<Lds::XP>(lds.x, 32 * wi, 32 * (wj + 2 * t), lane, x[t], 1.f);
+    __syncthreads();
+    f32x16 A = 0.f, P = 0.f;
+#pragma unroll 4
+    for (int kk = 0; kk < 4 * KB; ++kk)
+      A = mma2(get_rows<Lds::XP>(lds.x, 32 * wj, kk, lane), get_rows<Lds::XP>(lds.x, 32 * wi, kk, lane), A);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) A[e] *= down;
+    put_parts<Lds::AP>(lds.a, 32 * wi, 32 * wj, lane, A, A_UP);
+    __syncthreads();
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+      P = mma2(get_rows<Lds::AP>(lds.a, 32 * wj, kk, lane), get_rows<Lds::AP>(lds.a, 32 * wi, kk, lane), P);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) P[e] = a.b * A[e] + (a.c / (A_UP * A_UP)) * P[e];
+    __syncthreads();  // every wave has read A
+    put_parts<Lds::AP>(lds.a, 32 * wi, 32 * wj, lane, P, A_UP);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < KB; ++t) {
+      f32x16 D = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        D = mma2(get_columns<Lds::XP>(lds.x, 32 * (wj + 2 * t), kk, lane), get_rows<Lds::AP>(lds.a, 32 * wi, kk, lane), D);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][e] = a.a * x[t][e] + D[e] * (1.f / A_UP);
+    }
+    __syncthreads();  // and X and P
+  }
+  const float alpha = (float)(a.alpha / a.up);
+  each([&](int t, int e, size_t at, int w) {
+    float f[V];
+    if (r) u.get(r + at, w, f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = alpha * (i < w ? x[t][e + i] : 0.f) + (r ? a.beta * f[i] : 0.f);
+    if (w == V) {
+      typename GVec<TI, V>::type y;
+#pragma unroll
+      for (int i = 0; i < V; ++i) y[i] = (TI)f[i];
+      *reinterpret_cast<typename GVec<TI, V>::type*>(W + at) = y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < w) W[at + i] = (TI)f[i];
+    }
+  });
+}
+
+template <typename TI, int KB>
+hipError_t small_t(const OrthArgs& a, hipStream_t st) {
+  const double up = ldexp(1.0, (int)lround(0.5 * log2((double)a.no * a.ni)));
+  const SmallArgs s{a.no, a.ni, a.steps, (float)a.a, (float)a.b, (float)a.c, (float)a.alpha, (float)a.beta, a.eps, up};
+  const TI *g = (const TI*)a.g, *r = (const TI*)a.r;
+  if (a.no > a.ni)
+    k_small<TI, KB, true><<<(unsigned)a.N, 256, 0, st>>>({g, a.m, a.mo, (float)a.mu, a.nesterov}, r, (TI*)a.W, s);
+  else
+    k_small<TI, KB, false><<<(unsigned)a.N, 256, 0, st>>>({g, a.m, a.mo, (float)a.mu, a.nesterov}, r, (TI*)a.W, s);
+  return hipGetLastError();
 }
 
 // ---------------------------------------------------------------- products
@@ -356,6 +542,10 @@ inline mm::Prob prob(const void* A, long lda, const void* B, long ldb, int M, in
 // TI: gradient and weights, T: the products
 template <typename TI, typename T>
 hipError_t update_t(const OrthArgs& a, hipStream_t st) {
+  if (orth_small(a.no, a.ni)) {
+    const int k = std::max(a.no, a.ni);
+    return k <= 64 ? small_t<TI, 1>(a, st) : k <= 128 ? small_t<TI, 2>(a, st) : small_t<TI, 4>(a, st);
+  }
   const OrthLayout l = orth_layout(a.dtype, a.N, a.no, a.ni);
   char* w = static_cast<char*>(a.ws);
   double* norms = reinterpret_cast<double*>(w + l.norms);
@@ -370,7 +560,7 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
     const int batch = std::min(l.chunk, a.N - z0);
     const size_t from = z0 * size;
     const Momentum<TI, VV> u{(const TI*)a.g + from, a.m ? a.m + from : nullptr, a.mo ? a.mo + from : nullptr, (float)a.mu, a.nesterov};
-    const unsigned gx = (unsigned)std::min<size_t>((size * VV + 4095) / 4096, 256);
+    const unsigned gx = (unsigned)std::min<size_t>((sx + 4095) / 4096, 2048);
     k_momentum<TI><<<dim3((unsigned)l.parts, (unsigned)batch), 256, 0, st>>>(u, size, norms);
     k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>(u, a.no, a.ni, ld, norms, l.parts, a.eps, ldexp(1.0, shift), X[0]);
     hipError_t e = hipGetLastError();

@@ -187,6 +187,9 @@ def test_orth_workspaces(dtype):
         seen += 1
         one, all_ = (L.lp_orth_workspace_bytes(L.orth(dtype, k, no, ni)) for k in (1, N))
         held = 2 * (no * ni + n * n) * e
+        if n <= 64 and max(no, ni) <= 256:  # held by a workgroup
+            assert one == all_ == 256
+            continue
         assert held <= one, (no, ni)
         # (X, A and their like in rows of up to 128 bytes more; at most 32 sums of whole tiles of 128 for each product)
         rows = held + 2 * 128 * (no + n) + 8 * 128

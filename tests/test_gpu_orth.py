@@ -16,7 +16,7 @@ Q = L.QUINTIC
 # single values, rows and columns; wide, square and tall; odd sizes; below, at and above tiles; long sides that are split
 SHAPES = [(1, 1, 1), (3, 1, 5), (2, 7, 1), (4, 8, 8), (7, 21, 36), (5, 36, 21), (3, 64, 64), (2, 65, 63), (5, 33, 130), (2, 220, 220),
           (1, 300, 1000), (1, 1000, 70), (2, 129, 257), (1, 64, 4096), (1, 4096, 40), (1, 8, 5000), (1, 520, 520), (1, 1100, 1100),
-          (40, 100, 90)]
+          (40, 100, 90), (9, 64, 256), (3, 256, 33), (5, 17, 129), (2, 65, 256), (3, 257, 20), (300, 3, 2)]
 
 
 def gradients(seed, dtype, N, no, ni):
@@ -82,7 +82,7 @@ def test_large(dtype, shape):
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_batches_of_several_chunks(dtype):
     """More matrices than the workspace holds at once; each is treated by itself."""
-    N, no, ni = (9000, 20, 60) if dtype == "f32" else (17000, 20, 60)
+    N, no, ni = (2200, 70, 66) if dtype == "f32" else (4300, 70, 66)
     g = gradients(6, dtype, 64, no, ni)
     s = K.Orth(dtype, N, no, ni, steps=3)
     one = K.Orth(dtype, 64, no, ni, steps=3)
