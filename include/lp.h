@@ -507,10 +507,12 @@ int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, 
  * each matrix by itself. The iteration maps each singular value s of X to a s + b s^3 + c s^5 and keeps the
  * singular vectors: with a, b, c = 3.4445, -4.7750, 2.0315 five steps bring those above 0.003 to between 0.7 and
  * 1.2, with 15/8, -10/8, 3/8 those near one converge to one.
- * fp32: every product is one of fp32 values. 16-bit types: X, A and b A + c A^2 are rounded to f16, X times a
- * power of two, so a, b, c have to keep singular values below about 10. A rounding error grows like a small
- * singular value does, by about a factor a a step: with the first coefficients and five steps X is off by
- * 1e-3 to 3e-3 of its norm on noise, more where a few directions exceed the others a hundredfold (4e-2). */
+ * fp32: the products' operands X, A and b A + c A^2 are kept as sums of two f16 values each (2^-22 relative).
+ * 16-bit types: they are rounded to f16, or of matrices of at most 64 x 256 kept as such sums too. Powers of two keep
+ * them in range, for which a, b, c have to keep singular values below about 3. A rounding error grows like a
+ * small singular value does, by about a factor a a step: with the first coefficients and five steps X is off
+ * by 1e-3 to 3e-3 of its norm on noise (fp32: 3e-6), more where a few directions exceed the others a
+ * hundredfold (4e-2; 1e-4). */
 typedef struct {
   int32_t abi_version;   /* must equal LP_ABI_VERSION */
   int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16: g, r and W; m is fp32 */

@@ -140,14 +140,15 @@ OrthLayout orth_layout(int dtype, int N, int no, int ni) {
     l.total = 256;
     return l;
   }
-  l.ld = mm::padded(e, ni);
-  l.lda = mm::padded(e, n);
+  const bool duo = dtype == LP_F32;
+  l.ld = (mm::padded(e, ni) + 7) / 8 * 8;
+  l.lda = (mm::padded(e, n) + 7) / 8 * 8;
   const size_t x = (size_t)no * l.ld * e, a = (size_t)n * l.lda * e;
   l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a)), 1), 16384));
   l.parts = (int)std::min<size_t>(((size_t)no * ni + 4095) / 4096, 2048);
-  l.gram = mm::plan_of(e, n, n, k, l.chunk, true);
-  l.poly = mm::plan_of(e, n, n, n, l.chunk, true);
-  l.next = mm::plan_of(e, no, ni, n, l.chunk);
+  l.gram = mm::plan_of(e, n, n, k, l.chunk, true, duo);
+  l.poly = mm::plan_of(e, n, n, n, l.chunk, true, duo);
+  l.next = mm::plan_of(e, no, ni, n, l.chunk, false, duo);
   const auto part = [&](const mm::Plan& p, bool sym) {
     return p.splits > 1 ? (size_t)l.chunk * p.splits * tiles_of(p, sym) * p.tile * p.tile * 4 : 0;
   };

@@ -50,6 +50,15 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // N consecutive values in global memory, with their element's alignment
 template <typename T, int N> struct GVec { typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
 
+// A value as the sum of two f16 ones, hi + lo (2^-22 relative, 2^-25 absolute): rows of such values hold eight hi and the
+// same eight lo in turn, 4 bytes a value; rows have a multiple of eight of them. Workspace arrays only.
+struct Duo {
+  uint32_t bits;
+};
+struct DuoFrag {
+  h16x8 hi, lo;
+};
+
 // What a lane reads of one operand for a step of 16 contraction values (eight of them), and what
 // the matrix instructions take: floats are split into three bf16 parts (lp_split.h), six products
 // of which make one of floats: 2.4 times the float instructions' rate, with a smaller error.
@@ -57,10 +66,12 @@ template <typename T> struct Frag;
 template <> struct Frag<bf16> { typedef b16x8 type; typedef b16x8 ready; };
 template <> struct Frag<f16> { typedef h16x8 type; typedef h16x8 ready; };
 template <> struct Frag<float> { typedef f32x8 type; typedef Split8 ready; };
+template <> struct Frag<Duo> { typedef DuoFrag type; typedef DuoFrag ready; };
 
 __device__ __forceinline__ b16x8 prepare(b16x8 x) { return x; }
 __device__ __forceinline__ h16x8 prepare(h16x8 x) { return x; }
 __device__ __forceinline__ Split8 prepare(f32x8 x) { return split8(x); }
+__device__ __forceinline__ DuoFrag prepare(const DuoFrag& x) { return x; }
 // of sign * x (sign = 1 or -1, the same for the wave; 16-bit types have none)
 template <typename F>
 __device__ __forceinline__ auto prepare(F x, float sign) {
@@ -73,6 +84,11 @@ __device__ __forceinline__ f32x16 mma(b16x8 a, b16x8 b, f32x16 c) {
 }
 __device__ __forceinline__ f32x16 mma(h16x8 a, h16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(const DuoFrag& a, const DuoFrag& b, f32x16 c) {  // (lo lo is below 2^-22)
+  c = mma(a.lo, b.hi, c);
+  c = mma(a.hi, b.lo, c);
+  return mma(a.hi, b.hi, c);
 }
 __device__ __forceinline__ f32x16 mma(const Split8& a, const Split8& b, f32x16 c) {
   constexpr int ia[6] = {0, 2, 1, 0, 1, 0}, ib[6] = {2, 0, 1, 1, 0, 0};
@@ -130,12 +146,14 @@ struct Stage {
   static constexpr int RC = KB / 16;                 // rows: chunks per row
   static constexpr int PER = R * RC / NT;            // chunks per thread
   static constexpr int CH = R / V;                   // columns: chunks per row of the stage
-  static constexpr int SWZ = (sizeof(T) == 2 ? 12 : 8) & (CH - 1);
+  static constexpr bool TURNS = !std::is_same<T, float>::value;  // columns: read by transposing loads
+  static constexpr int SWZ = (TURNS ? 12 : 8) & (CH - 1);
+  static constexpr int UNIT = std::is_same<T, Duo>::value ? 8 : V;  // values that lie together
   static_assert(R * RC % NT == 0, "whole chunks per thread");
   static_assert(KB == 64 || KB == 128, "the rows' exchange");
 
   static __device__ __forceinline__ int swz(int k) {  // columns: chunk exchange of row k
-    return (sizeof(T) == 2 ? k << 2 : k) & SWZ;
+    return (TURNS ? k << 2 : k) & SWZ;
   }
   static __device__ __forceinline__ int rswz(int r) {  // rows: chunk exchange of row r
     return KB == 128 ? r & 7 : (r >> 1) & 3;
@@ -155,7 +173,7 @@ struct Stage {
     k1 = k1_;
     if constexpr (!COLS) {
       const int c = (t % RC) ^ rswz(t / RC);
-      kc = c * V;
+      kc = c * V / UNIT * UNIT;
       base = static_cast<const unsigned char*>(p) + ((long)r0 * ld + k0) * (long)sizeof(T);
       left = ((long)(rows - r0) * ld - k0) * (long)sizeof(T);
       step = KB;
@@ -166,7 +184,7 @@ struct Stage {
       base = static_cast<const unsigned char*>(p) + ((long)k0 * ld + r0) * (long)sizeof(T);
       // (to the last chunk of row k1 - 1 that counts: behind it may lie what no kernel has written, which
       // must not decide whether a float tile is formed again)
-      left = ((long)(k1 - k0 - 1) * ld + (rows + V - 1) / V * V - r0) * (long)sizeof(T);
+      left = ((long)(k1 - k0 - 1) * ld + (rows + UNIT - 1) / UNIT * UNIT - r0) * (long)sizeof(T);
       step = BK * ld * (long)sizeof(T);
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -297,6 +315,9 @@ struct Reader {
       if constexpr (!COLS) {  // 16 bits: step x; float: chunk x % 2 of step x / 2
         const int r = r0 + (lane & 31), c = sizeof(T) == 2 ? 2 * x + (lane >> 5) : 4 * (x / 2) + 2 * (lane >> 5) + x % 2;
         at[x] = (r * S::RC + (c ^ S::rswz(r))) * 16;
+      } else if constexpr (std::is_same<T, Duo>::value) {
+        const int col = r0 + 32 * x + 16 * ((lane >> 4) & 1) + 4 * (lane & 3), k = 8 * (lane >> 5) + ((lane >> 2) & 3);
+        at[x] = (k * S::CH + ((col / 8 * 2) ^ S::swz(k))) * 16 + (col % 8) * 2;
       } else if constexpr (sizeof(T) == 2) {
         const int col = r0 + 32 * x + 16 * ((lane >> 4) & 1) + 4 * (lane & 3), k = 8 * (lane >> 5) + ((lane >> 2) & 3);
         at[x] = (k * S::CH + ((col / S::V) ^ S::swz(k))) * 16 + (col % S::V) * 2;
@@ -312,11 +333,24 @@ struct Reader {
     if constexpr (!COLS) {
       if constexpr (sizeof(T) == 2) {
         return *reinterpret_cast<const F*>(lds + at[kk] + i * 32 * KB);
+      } else if constexpr (std::is_same<T, Duo>::value) {
+        return F{*reinterpret_cast<const h16x8*>(lds + at[2 * kk] + i * 32 * KB),
+                 *reinterpret_cast<const h16x8*>(lds + at[2 * kk + 1] + i * 32 * KB)};
       } else {
         const f32x4 lo = *reinterpret_cast<const f32x4*>(lds + at[2 * kk] + i * 32 * KB);
         const f32x4 hi = *reinterpret_cast<const f32x4*>(lds + at[2 * kk + 1] + i * 32 * KB);
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
+    } else if constexpr (std::is_same<T, Duo>::value) {
+      typedef __attribute__((address_space(3))) s16x4 lds4;
+      s16x4 h[2][2];
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          h[p][j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + at[i] + 16 * p + (16 * kk + 4 * j) * S::CH * 16));
+      return F{__builtin_bit_cast(h16x8, __builtin_shufflevector(h[0][0], h[0][1], 0, 1, 2, 3, 4, 5, 6, 7)),
+               __builtin_bit_cast(h16x8, __builtin_shufflevector(h[1][0], h[1][1], 0, 1, 2, 3, 4, 5, 6, 7))};
     } else if constexpr (sizeof(T) == 2) {
       typedef __attribute__((address_space(3))) s16x4 lds4;
       s16x4 h[2];
@@ -568,7 +602,7 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
     // with it (a sum of 220 is off by 1.8e-7 either way; one of a single stage, 32 products, keeps its
     // -2.3e-9). It takes 1 to 2 % of the time of large products, 5 % of 1000 x 220 -> 220. (Of 16-bit types
     // the results' own rounding is 2^-9 and more.)
-    constexpr bool SIGNS = sizeof(T) == 4 && !decltype(as_float)::value;
+    constexpr bool SIGNS = std::is_same<T, float>::value && !decltype(as_float)::value;
     const int minus = steps / 4, plus = minus + (steps + 1) / 2;  // (a single stage keeps its sign)
     const auto turn = [&](int s) {
       if (SIGNS && steps > 1 && (s == minus || s == plus)) {
@@ -600,7 +634,7 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
     }
   };
   contract(std::false_type{});
-  if constexpr (sizeof(T) == 4) {
+  if constexpr (std::is_same<T, float>::value) {
     // An operand that is infinite or beyond the largest bf16 value makes split products NaN: a tile
     // with a result that is not finite is formed again by the float instructions, which give
     // infinities and overflow as fp32 has them.
@@ -699,7 +733,60 @@ struct BlockIO {
   }
 };
 
-static_assert(WAVE_LDS == BlockIO<float>::BYTES, "a wave's part of the LDS");
+// Of values in two parts: an array's rows are whole pieces, ld of them; what lies behind them is not touched.
+template <>
+struct BlockIO<Duo> {
+  static constexpr int W = 128, PITCH = W + 16, CPR = W / 16, V = 4;
+  static constexpr int ITER = 32 * CPR / 64, BYTES = 32 * PITCH;
+  typedef f32x4 Piece;
+  typedef _Float16 Quad __attribute__((ext_vector_type(4)));
+
+  static __device__ __forceinline__ void put(unsigned char* at, f32x4 v) {
+    Quad h, l;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      h[k] = (_Float16)v[k];
+      l[k] = (_Float16)(v[k] - (float)h[k]);
+    }
+    *reinterpret_cast<Quad*>(at) = h;
+    *reinterpret_cast<Quad*>(at + 16) = l;
+  }
+  static __device__ __forceinline__ void quads(const Duo* a, long ld, const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
+#pragma unroll
+    for (int t = 0; t < ITER; ++t) {
+      const int id = c.lane + 64 * t, m = min(c.mw + 32 * i + id / CPR, c.M - 1), n = c.nw + 32 * j + id % CPR * V;
+      *reinterpret_cast<Piece*>(buf + id / CPR * PITCH + id % CPR * 16) =
+          n < ld ? *reinterpret_cast<const Piece*>(a + (size_t)m * ld + n) : Piece{0.f, 0.f, 0.f, 0.f};
+    }
+    wave_in_order();
+    const unsigned char* r = buf + (c.lane & 31) * PITCH + (c.lane >> 5) * 8;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const Quad h = *reinterpret_cast<const Quad*>(r + 32 * q), l = *reinterpret_cast<const Quad*>(r + 32 * q + 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[q][k] = (float)h[k] + (float)l[k];
+    }
+    wave_in_order();
+  }
+  // rows m0 .. m0 + 31 below M, columns n0 .. from the wave's LDS
+  static __device__ __forceinline__ void flush(Duo* a, long ld, int m0, int M, int n0, int lane, const unsigned char* buf) {
+    wave_in_order();
+#pragma unroll
+    for (int t = 0; t < ITER; ++t) {
+      const int id = lane + 64 * t, m = m0 + id / CPR, n = n0 + id % CPR * V;
+      const Piece x = *reinterpret_cast<const Piece*>(buf + id / CPR * PITCH + id % CPR * 16);
+      if (m < M && n < ld) *reinterpret_cast<Piece*>(a + (size_t)m * ld + n) = x;
+    }
+    wave_in_order();
+  }
+  static __device__ __forceinline__ void store(Duo* a, long ld, const Place& c, int i, int j, unsigned char* buf, const f32x4 (&v)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put(buf + (c.lane & 31) * PITCH + 32 * q + (c.lane >> 5) * 8, v[q]);
+    flush(a, ld, c.mw + 32 * i, c.M, c.nw + 32 * j, c.lane, buf);
+  }
+};
+
+static_assert(WAVE_LDS == BlockIO<float>::BYTES && WAVE_LDS == BlockIO<Duo>::BYTES, "a wave's part of the LDS");
 __device__ __forceinline__ unsigned char* wave_lds(float* lds, const Place& c, int wgn) {
   return reinterpret_cast<unsigned char*>(lds) + (c.wm * wgn + c.wn) * WAVE_LDS;
 }
@@ -736,6 +823,21 @@ struct Rows {
   }
 };
 
+template <bool WHOLE, int FM, int FN, bool AHEAD>
+struct Rows<WHOLE, Duo, FM, FN, AHEAD> {
+  const Duo* a;
+  long ld;
+  __device__ __forceinline__ Rows(const Duo* a_, long ld_, const Place&) : a(a_), ld(ld_) {}
+  __device__ __forceinline__ void get(const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
+    if (a) {
+      BlockIO<Duo>::quads(a, ld, c, i, j, buf, v);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = 0.f;
+    }
+  }
+};
+
 // The quads of block (i, j) to an array of rows of ld values, n of which are written.
 template <bool WHOLE, typename T, typename F>
 __device__ __forceinline__ void put_rows(T* a, long ld, int n, const Place& c, int i, int j, unsigned char* buf,
@@ -752,6 +854,12 @@ template <bool WHOLE, typename T>
 __device__ __forceinline__ void put_rows(T* a, long ld, int n, const Place& c, int i, int j, unsigned char* buf,
                                          const f32x4 (&v)[4]) {
   put_rows<WHOLE>(a, ld, n, c, i, j, buf, v, [](int m) { return m; });
+}
+
+// (values in two parts: whole rows)
+template <bool WHOLE>
+__device__ __forceinline__ void put_rows(Duo* a, long ld, int, const Place& c, int i, int j, unsigned char* buf, const f32x4 (&v)[4]) {
+  BlockIO<Duo>::store(a, ld, c, i, j, buf, v);
 }
 
 // Four features of a row vector (a bias) for each quad of block column j; zeros without one.
@@ -1135,11 +1243,13 @@ constexpr int STAGE_BYTES = 128;
 // 4096 230 us by 256 (128: 256, 64: over 370). float: 4096 x 1024 x 1024 60 us by 128 (64: 74, 256: 134);
 // 1024 x 1024 x 4096 (columns) 70 by 128 in eight splits, which the estimate takes, 68 in four (64 in two: 77,
 // 256: 501); 4096 x 4096 x 4096 545 by 256 (128: 600 to 694, 64: 1008).
-// batch: products of this size in one launch; sym: only the tiles on and below the diagonal.
-inline Plan plan_of(size_t esz, long M, long N, long K, long batch = 1, bool sym = false) {
+// batch: products of this size in one launch; sym: only the tiles on and below the diagonal; duo: values in two
+// parts (half again the products of 16-bit values a stage).
+inline Plan plan_of(size_t esz, long M, long N, long K, long batch = 1, bool sym = false, bool duo = false) {
   const int steps = ceil_div(K * (long)esz, STAGE_BYTES);
-  const double stage[2][3][2] = {{{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{4.1, 8.7}, {1.8, 2.7}, {0.75, 1.15}}};
-  const auto& us = stage[esz == 4];
+  const double stage[3][3][2] = {
+      {{1.4, 3.6}, {0.60, 1.0}, {0.30, 0.45}}, {{4.1, 8.7}, {1.8, 2.7}, {0.75, 1.15}}, {{2.1, 5.4}, {0.9, 1.5}, {0.40, 0.65}}};
+  const auto& us = stage[duo ? 2 : esz == 4];
   Plan best{};
   double least = 1e30;
   for (int s = 0; s < 3; ++s) {

@@ -4,6 +4,9 @@
 // one, then `steps` times, with A the short side's A = X X^T (X^T X of a tall matrix),
 //   X <- a X + (b A + c A^2) X   (tall: a X + X (b A + c A^2)),
 // which maps every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.
+// fp32 gradients: X, A and P are kept as sums of two f16 values (mm::Duo), a product of which is three of f16: half of
+// what splitting floats into three bf16 parts costs, and no split in the products' loop. O is off by 3e-6 of its norm on
+// noise (fp32 products: 2e-6). aX is added to the product in fp32.
 //   A and P = b A + c A^2 are symmetric: only tiles on and below the diagonal are formed, and stored on both sides of
 //   it. a X is added in fp32 in the last product's epilogue, that of the last step updates W.
 // 16-bit gradients: X, A and P are kept in f16 whatever the gradient's type is. No singular value exceeds 1.3 or
@@ -29,6 +32,9 @@ using mm::f32x16;
 using mm::f32x4;
 using mm::GVec;
 using mm::Place;
+
+constexpr float A_UP = 256.f;     // A and P are kept times this, X times 2^shift: small values stay normal f16 numbers
+constexpr int MOST_SHIFT = 13;  // (X's values are at most 1.3 2^13)
 
 // ---------------------------------------------------------------- v, its norm, and X
 
@@ -109,9 +115,22 @@ __global__ __launch_bounds__(256) void k_momentum(Momentum<TI, VV> u, size_t siz
   if (threadIdx.x == 0) part[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = ((sh[0] + sh[1]) + sh[2]) + sh[3];
 }
 
+template <typename T>
+__device__ __forceinline__ void put_values(T* row, int c, const float (&v)[8]) {
+  if constexpr (std::is_same<T, mm::Duo>::value) {
+    mm::BlockIO<mm::Duo>::put(reinterpret_cast<unsigned char*>(row + c), f32x4{v[0], v[1], v[2], v[3]});
+    mm::BlockIO<mm::Duo>::put(reinterpret_cast<unsigned char*>(row + c) + 8, f32x4{v[4], v[5], v[6], v[7]});
+  } else {
+    typename GVec<T, 8>::type x;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = (T)v[k];
+    *reinterpret_cast<typename GVec<T, 8>::type*>(row + c) = x;
+  }
+}
+
 // X = v 2^shift / (|v| + eps) in rows of ld values, zeros behind the ni that count (grid y: the matrix)
 template <typename TI, typename T>
-__global__ __launch_bounds__(256) void k_scale(Momentum<TI, VV> u, int no, int ni, int ld, const double* part, int parts, double eps,
+__global__ __launch_bounds__(256) void k_scale(Momentum<TI, 8> u, int no, int ni, int ld, const double* part, int parts, double eps,
                                                double up, T* X) {
   __shared__ double sh;
   if (threadIdx.x < 64) {
@@ -125,23 +144,19 @@ __global__ __launch_bounds__(256) void k_scale(Momentum<TI, VV> u, int no, int n
   __syncthreads();
   const double scale = sh;
   const size_t base = (size_t)blockIdx.y * no * ni;
-  const uint32_t per = (uint32_t)(ld / VV);
+  const uint32_t per = (uint32_t)(ld / 8);
   const size_t all = (size_t)no * per;
   X += (size_t)blockIdx.y * no * ld;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
     const size_t r = i / per;
-    const int c = (int)(i - r * per) * VV, n = min(VV, ni - c);
-    typename GVec<T, VV>::type x;
-    if (n <= 0) {
-#pragma unroll
-      for (int k = 0; k < VV; ++k) x[k] = (T)0.f;
-    } else {
-      float v[VV];
+    const int c = (int)(i - r * per) * 8, n = min(8, ni - c);
+    float v[8] = {};
+    if (n > 0) {
       u.again(base + r * ni + c, n, v);
 #pragma unroll
-      for (int k = 0; k < VV; ++k) x[k] = k < n ? (T)(float)((double)v[k] * scale) : (T)0.f;
+      for (int k = 0; k < 8; ++k) v[k] = k < n ? (float)((double)v[k] * scale) : 0.f;
     }
-    *reinterpret_cast<typename GVec<T, VV>::type*>(X + r * ld + c) = x;
+    put_values(X + r * ld, c, v);
   }
 }
 
@@ -154,7 +169,6 @@ __global__ __launch_bounds__(256) void k_scale(Momentum<TI, VV> u, int no, int n
 //   wave (wi, wj): rows 32 wi .., of A and P columns 32 wj .., of X the blocks wj, wj + 2, .. of 32 columns.
 // 2048 of 64 x 64 f32 LP_SMALL_US us.
 constexpr int SMALL_N = 64, SMALL_K = 256;
-constexpr float A_UP = 256.f;  // A and P are kept times this: their small values stay normal f16 numbers
 
 struct Half2 {
   mm::h16x8 h, l;
@@ -354,6 +368,21 @@ __device__ __forceinline__ void put_mirror(T* a, long ld, const Place& c, int i,
   mm::wave_in_order();
 }
 
+__device__ __forceinline__ void put_mirror(mm::Duo* a, long ld, const Place& c, int i, int j, unsigned char* buf, const f32x4 (&v)[4]) {
+  typedef mm::BlockIO<mm::Duo> IO;
+  const int m = c.lane & 31;
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      unsigned char* at = buf + (8 * q + 4 * (c.lane >> 5) + k) * IO::PITCH + m / 8 * 32 + m % 8 * 2;
+      const _Float16 h = (_Float16)v[q][k];
+      *reinterpret_cast<_Float16*>(at) = h;
+      *reinterpret_cast<_Float16*>(at + 16) = (_Float16)(v[q][k] - (float)h);
+    }
+  IO::flush(a, ld, c.nw + 32 * j, c.N, c.mw + 32 * i, c.lane, buf);
+}
+
 // f D + b A of a symmetric D, rows of ld values (A nullable)
 template <typename T>
 struct EpSym {
@@ -390,7 +419,7 @@ struct EpSym {
   }
 };
 
-// a X + D
+// a X + d D
 template <typename T>
 struct EpNext {
   struct Args {
@@ -398,7 +427,7 @@ struct EpNext {
     T* out;
     int ld;
     size_t stride;
-    float a;
+    float a, d;
   };
   static __device__ __forceinline__ Args at(Args a, int z) {
     a.X += z * a.stride;
@@ -419,13 +448,13 @@ struct EpNext {
         for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            v[q][k] = WHOLE || c.feature(j, q) + k < c.lim ? a.a * v[q][k] + acc[i][j][4 * q + k] : 0.f;
+            v[q][k] = WHOLE || c.feature(j, q) + k < c.lim ? a.a * v[q][k] + a.d * acc[i][j][4 * q + k] : 0.f;
         mm::put_rows<WHOLE>(a.out, a.ld, c.upto(a.ld), c, i, j, buf, v);
       }
   }
 };
 
-// W = alpha (a X + D) + beta r, rows of N values (r nullable)
+// W = alpha (a X + d D) + beta r, rows of N values (r nullable)
 template <typename T, typename TO>
 struct EpUpdate {
   struct Args {
@@ -435,7 +464,7 @@ struct EpUpdate {
     const TO* r;
     TO* W;
     size_t wstride;  // of r and W
-    float a, alpha, beta;
+    float a, d, alpha, beta;
   };
   static __device__ __forceinline__ Args at(Args a, int z) {
     a.X += z * a.stride;
@@ -456,7 +485,7 @@ struct EpUpdate {
         X.get(c, i, j, buf, v);
         r.get(c, i, j, buf, w);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = (v[q] * a.a + mm::quad(acc[i][j], q)) * a.alpha + w[q] * a.beta;
+        for (int q = 0; q < 4; ++q) v[q] = (v[q] * a.a + mm::quad(acc[i][j], q) * a.d) * a.alpha + w[q] * a.beta;
         mm::put_rows<WHOLE>(a.W, c.N, c.lim, c, i, j, buf, v);
       }
   }
@@ -554,15 +583,16 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
   const bool tall = a.no > a.ni;
   const int n = std::min(a.no, a.ni), k = std::max(a.no, a.ni), ld = l.ld, lda = l.lda;
   const size_t size = (size_t)a.no * a.ni, sx = (size_t)a.no * ld, sA = (size_t)n * lda;
-  const int shift = sizeof(T) == 2 ? (int)lround(0.5 * log2((double)k)) : 0;
+  const int shift = std::min((int)lround(0.5 * log2((double)n * k)), MOST_SHIFT);
   const float down = ldexpf(1.f, -shift);
   for (int z0 = 0; z0 < a.N; z0 += l.chunk) {
     const int batch = std::min(l.chunk, a.N - z0);
     const size_t from = z0 * size;
-    const Momentum<TI, VV> u{(const TI*)a.g + from, a.m ? a.m + from : nullptr, a.mo ? a.mo + from : nullptr, (float)a.mu, a.nesterov};
+    const TI* g = (const TI*)a.g + from;
+    float* mo = a.mo ? a.mo + from : nullptr;
     const unsigned gx = (unsigned)std::min<size_t>((sx + 4095) / 4096, 2048);
-    k_momentum<TI><<<dim3((unsigned)l.parts, (unsigned)batch), 256, 0, st>>>(u, size, norms);
-    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>(u, a.no, a.ni, ld, norms, l.parts, a.eps, ldexp(1.0, shift), X[0]);
+    k_momentum<TI><<<dim3((unsigned)l.parts, (unsigned)batch), 256, 0, st>>>({g, a.m ? a.m + from : nullptr, mo, (float)a.mu, a.nesterov}, size, norms);
+    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>({g, nullptr, mo, (float)a.mu, a.nesterov}, a.no, a.ni, ld, norms, l.parts, a.eps, ldexp(1.0, shift), X[0]);
     hipError_t e = hipGetLastError();
     for (int s = 0; s < a.steps && e == hipSuccess; ++s) {
       const T* x = X[s & 1];
@@ -570,7 +600,7 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
         return Product{p, sa * sizeof(T), sb * sizeof(T), pl, batch, reinterpret_cast<mm::f32x4*>(w + l.part), st};
       };
       // A, the scale of X taken out; P = b A + c A^2
-      const typename EpSym<T>::Args ea{nullptr, A, lda, sA, down * down, 0.f}, ep{A, P, lda, sA, (float)a.c, (float)a.b};
+      const typename EpSym<T>::Args ea{nullptr, A, lda, sA, down * down * A_UP, 0.f}, ep{A, P, lda, sA, (float)a.c / A_UP, (float)a.b};
       const Product gram = product(prob(x, ld, x, ld, n, n, k), sx, sx, l.gram);
       e = tall ? launch_product<T, true, true, true, EpSym<T>>(gram, ea) : launch_product<T, false, false, true, EpSym<T>>(gram, ea);
       if (e != hipSuccess) break;
@@ -579,11 +609,11 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
       const Product next = tall ? product(prob(x, ld, P, lda, a.no, a.ni, n), sx, sA, l.next)
                                 : product(prob(P, lda, x, ld, a.no, a.ni, n), sA, sx, l.next);
       if (s + 1 < a.steps) {
-        const typename EpNext<T>::Args en{x, X[~s & 1], ld, sx, (float)a.a};
+        const typename EpNext<T>::Args en{x, X[~s & 1], ld, sx, (float)a.a, 1.f / A_UP};
         e = tall ? launch_product<T, false, false, false, EpNext<T>>(next, en) : launch_product<T, false, true, false, EpNext<T>>(next, en);
       } else {
         const typename EpUpdate<T, TI>::Args eu{x, ld, sx, a.r ? (const TI*)a.r + from : nullptr, (TI*)a.W + from, size,
-                                                (float)a.a, (float)(a.alpha * down), (float)a.beta};
+                                                (float)a.a, 1.f / A_UP, (float)(a.alpha * down), (float)a.beta};
         e = tall ? launch_product<T, false, false, false, EpUpdate<T, TI>>(next, eu)
                  : launch_product<T, false, true, false, EpUpdate<T, TI>>(next, eu);
       }
