@@ -526,7 +526,7 @@ typedef struct {
 } lp_orth;
 
 /* Workspace bytes of lp_orth_update; 0 for an invalid update. It holds X twice, A and b A + c A^2 of as many
- * matrices as 128 MiB hold (at least one), and the partial sums of split products. */
+ * matrices as 1 GiB holds (at least one), and the partial sums of split products. */
 size_t lp_orth_workspace_bytes(const lp_orth* orth);
 
 /* The update. g, r, W [N][no][ni]; m, mo [N][no][ni] fp32: m' goes to mo, which may be m. Without mo (m NULL

@@ -128,9 +128,18 @@ GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad) {
   return l;
 }
 
-// Matrices are taken a chunk at a time, whose X, A and P stay in the last cache (256 MB) and of which there are enough to
-// fill the card with tiles.
-constexpr size_t ORTH_CHUNK = (size_t)128 << 20;
+// Matrices are taken a chunk at a time, whose X, A and P take ORTH_CHUNK at most: enough that launches and their uneven
+// ends do not count (2048 of 220 x 220 f32: 7.2 ms by 64 MiB, 6.2 by 128, which the last cache would hold, 5.4 by 512, 5.0).
+constexpr size_t ORTH_CHUNK = (size_t)1 << 30;
+
+// A symmetric product over rows, tiles of 192 where they are estimated faster: n = 4096 has 253 of them (136 of 256, 528
+// of 128), one for every CU.
+static mm::Plan sym_plan(size_t e, int n, int k, int batch, bool duo) {
+  const mm::Plan p = mm::plan_of(e, n, n, k, batch, true, duo);
+  const int tm = mm::ceil_div(n, 192);
+  const double us = mm::ceil_div(k * (long)e, 128) * (double)mm::ceil_div((long)batch * tm * (tm + 1) / 2, 256) * (duo ? 1.6 : 1.1);
+  return us < p.us ? mm::Plan{192, 1, tm, tm, us} : p;
+}
 
 OrthLayout orth_layout(int dtype, int N, int no, int ni) {
   const size_t e = esize(dtype);  // (of the products: f16 for both 16-bit types)
@@ -146,8 +155,8 @@ OrthLayout orth_layout(int dtype, int N, int no, int ni) {
   const size_t x = (size_t)no * l.ld * e, a = (size_t)n * l.lda * e;
   l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a)), 1), 16384));
   l.parts = (int)std::min<size_t>(((size_t)no * ni + 4095) / 4096, 2048);
-  l.gram = mm::plan_of(e, n, n, k, l.chunk, true, duo);
-  l.poly = mm::plan_of(e, n, n, n, l.chunk, true, duo);
+  l.gram = no > ni ? mm::plan_of(e, n, n, k, l.chunk, true, duo) : sym_plan(e, n, k, l.chunk, duo);
+  l.poly = sym_plan(e, n, n, l.chunk, duo);
   l.next = mm::plan_of(e, no, ni, n, l.chunk, false, duo);
   const auto part = [&](const mm::Plan& p, bool sym) {
     return p.splits > 1 ? (size_t)l.chunk * p.splits * tiles_of(p, sym) * p.tile * p.tile * 4 : 0;

@@ -14,6 +14,7 @@ namespace mm {
 // the kernel of one row, one_features() features a tile) and splits of the contraction.
 struct Plan {
   int tile, splits, tm, tn;
+  double us = 0;  // estimated time
   size_t part_bytes() const { return splits > 1 ? (size_t)splits * tm * tn * tile * tile * 4 : 0; }
 };
 }  // namespace mm

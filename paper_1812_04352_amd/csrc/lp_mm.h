@@ -1229,6 +1229,9 @@ typedef Shape<64, 64, 2, 2, 128, 4, 2> Tile64;  // (eight stages are no faster: 
 typedef Shape<256, 256, 2, 4, 128, 2, 1> Tile256f;  // float: two steps a stage; bound by the split's vector instructions
 typedef Shape<128, 128, 2, 2, 128, 2, 1> Tile128f;
 typedef Shape<64, 64, 2, 2, 128, 4, 1> Tile64f;
+// between: symmetric results whose tiles of 256 leave much of the card idle (both operands in rows)
+typedef Shape<192, 192, 2, 3, 128, 2, 2> Tile192;
+typedef Shape<192, 192, 2, 3, 128, 2, 1> Tile192d;
 // of a pair of arrays in rows: 32 features of each, a wave holds both products of its rows
 typedef Shape<64, 64, 2, 1, 128, 4, 2> Tile64p;
 typedef Shape<64, 64, 2, 1, 128, 4, 1> Tile64pf;
@@ -1265,7 +1268,7 @@ inline Plan plan_of(size_t esz, long M, long N, long K, long batch = 1, bool sym
       if (splits > 1) t += 3.0 + 2.0 * splits * M * tn * tile * 4 * (sym ? 0.5 : 1.0) * batch / 3e6;
       if (t < least) {
         least = t;
-        best = Plan{tile, splits, (int)tm, (int)tn};
+        best = Plan{tile, splits, (int)tm, (int)tn, t};
       }
     }
   }

@@ -541,9 +541,9 @@ hipError_t launch_shape(Product w, const typename E::Args& ea) {
   p.tm = w.pl.tm, p.tn = w.pl.tn;
   p.kper = std::max(1, mm::ceil_div(mm::ceil_div(p.K, BK), w.pl.splits)) * BK;
   const unsigned tiles = (unsigned)tiles_of(w.pl, SYM);
-  if (S::BM == 256 || w.pl.splits == 1) {
+  if (S::BM > 128 || w.pl.splits == 1) {
     k_bmm<T, S, AT, BT, E><<<dim3(tiles, 1, (unsigned)w.batch), S::NT, 0, w.st>>>(p, w.sa, w.sb, ea);
-  } else if constexpr (S::BM < 256) {
+  } else if constexpr (S::BM <= 128) {
     typedef ShapeOf<mm::Shape<S::BM, S::BN, S::WGM, S::WGN, 128, 2, 2>, SYM> SF;
     k_bmm<T, S, AT, BT, EpPart><<<dim3(tiles, (unsigned)w.pl.splits, (unsigned)w.batch), S::NT, 0, w.st>>>(p, w.sa, w.sb, {w.part});
     k_bfinish<SF, E><<<dim3(tiles, 1, (unsigned)w.batch), S::NT, 0, w.st>>>(p, w.part, w.pl.splits, ea);
@@ -553,6 +553,9 @@ hipError_t launch_shape(Product w, const typename E::Args& ea) {
 
 template <typename T, bool AT, bool BT, bool SYM, class E>
 hipError_t launch_product(const Product& w, const typename E::Args& ea) {
+  if constexpr (SYM && !AT && !BT) {
+    if (w.pl.tile == 192) return launch_shape<T, std::conditional_t<sizeof(T) == 2, mm::Tile192, mm::Tile192d>, AT, BT, SYM, E>(w, ea);
+  }
   if constexpr (sizeof(T) == 2) {
     if (w.pl.tile == 256) return launch_shape<T, mm::Tile256, AT, BT, SYM, E>(w, ea);
     if (w.pl.tile == 128) return launch_shape<T, mm::Tile128, AT, BT, SYM, E>(w, ea);

@@ -194,7 +194,7 @@ def test_orth_workspaces(dtype):
         # (X, A and their like in rows of up to 128 bytes more; at most 32 sums of whole tiles of 128 for each product)
         rows = held + 2 * 128 * (no + n) + 8 * 128
         parts = 128 * max((n + 128) ** 2, (no + 128) * (ni + 128))
-        assert all_ <= max(rows, 2 ** 27 + 16384 * 1024 + rows) + min(N, max(1, 2 ** 27 // held)) * parts + 4096, (N, no, ni, all_)
+        assert all_ <= max(rows, 2 ** 30 + 16384 * 1024 + rows) + min(N, max(1, 2 ** 30 // held)) * parts + 4096, (N, no, ni, all_)
     assert seen > 60
 
 

@@ -71,7 +71,7 @@ def test_plain_orthogonalisation(dtype, shape):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("shape", [(1, 2304, 2048), (1, 2048, 2304), (1, 4096, 512)])
+@pytest.mark.parametrize("shape", [(1, 2304, 2048), (1, 2048, 2304), (1, 4096, 512), (1, 1500, 1600), (3, 1000, 1008)])
 def test_large(dtype, shape):
     g = gradients(5, dtype, *shape)
     s = K.Orth(dtype, *shape)
@@ -82,9 +82,10 @@ def test_large(dtype, shape):
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_batches_of_several_chunks(dtype):
     """More matrices than the workspace holds at once; each is treated by itself."""
-    N, no, ni = (2200, 70, 66) if dtype == "f32" else (4300, 70, 66)
+    N, no, ni = (6100, 250, 66) if dtype == "f32" else (12200, 250, 66)
     g = gradients(6, dtype, 64, no, ni)
     s = K.Orth(dtype, N, no, ni, steps=3)
+    assert L.lp_orth_workspace_bytes(L.orth(dtype, 2 * N, no, ni)) < 1.1 * L.lp_orth_workspace_bytes(s.od)
     one = K.Orth(dtype, 64, no, ni, steps=3)
     few = g.cuda()
     W = s(few.repeat(-(-N // 64), 1, 1)[:N].contiguous(), None, None, None, 1.0)
