@@ -58,6 +58,24 @@ struct Piece {
   }
 };
 
+// The wave's sum of a value in every lane: neighbours within rows of 16 lanes by data-parallel moves, whose
+// latency is a vector instruction's, then the four rows' sums in order.
+__device__ __forceinline__ float wave_sum(float v) {
+#ifdef __HIP_DEVICE_COMPILE__
+#define LP_ADD_MOVED(ctrl) v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, 0xf, 0xf, true))
+  LP_ADD_MOVED(0xb1);   // quad_perm 1, 0, 3, 2
+  LP_ADD_MOVED(0x4e);   // quad_perm 2, 3, 0, 1
+  LP_ADD_MOVED(0x141);  // the other quad of eight lanes: row_half_mirror
+  LP_ADD_MOVED(0x140);  // the other half of sixteen: row_mirror
+#undef LP_ADD_MOVED
+  float r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 16 * i));
+  v = (r[0] + r[1]) + (r[2] + r[3]);
+#endif
+  return v;
+}
+
 // Sums of two values over a group of TPR threads, the same in all of them. Groups wider than a wave
 // exchange through the LDS: `at` alternates between its two halves, so that one barrier a sum is enough
 // (a wave that writes a half again has passed the barrier behind which all have read it).
@@ -67,10 +85,15 @@ struct GroupSum {
   float2 (*lds)[NT / 64];
   int at = 0;
   __device__ __forceinline__ float2 operator()(float2 s) {
+    if constexpr (TPR < 64) {
 #pragma unroll
-    for (int o = (TPR < 64 ? TPR : 64) / 2; o > 0; o >>= 1) {
-      s.x += __shfl_xor(s.x, o, 64);
-      s.y += __shfl_xor(s.y, o, 64);
+      for (int o = TPR / 2; o > 0; o >>= 1) {
+        s.x += __shfl_xor(s.x, o, 64);
+        s.y += __shfl_xor(s.y, o, 64);
+      }
+    } else {
+      s.x = wave_sum(s.x);
+      s.y = wave_sum(s.y);
     }
     if constexpr (TPR > 64) {
       const int wave = threadIdx.x >> 6;
@@ -176,65 +199,87 @@ __device__ __forceinline__ void add_groups(const float (&acc)[C][16 / sizeof(T)]
   }
 }
 
-template <typename T, int TPR, int C>
+// FULL: q = TPR C V, no piece behind the row's end. The next round's rows are requested before this one's sums (one
+// piece a thread: registers), so that a workgroup a CU keeps memory busy.
+template <typename T, int TPR, int C, bool FULL>
 __global__ __launch_bounds__(NT_B) void k_backward(BackArgs a) {
   typedef Piece<T, TPR, C> P;
   constexpr int V = P::V, G = NT_B / TPR;
+  constexpr bool AHEAD = C == 1;
   __shared__ float2 lds[2][NT_B / 64];
   __shared__ __attribute__((aligned(16))) float sums[G == 1 ? 4 : NT_B * C * V];
   GroupSum<TPR, NT_B> sum{lds};
-  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, q = a.q;
-  const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = static_cast<const T*>(a.dr);
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, q = FULL ? TPR * C * V : a.q;
+  const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = a.dx ? static_cast<const T*>(a.dr) : nullptr;
   T* dx = static_cast<T*>(a.dx);
-  P ga;
-  if (a.gamma) ga.load(static_cast<const T*>(a.gamma), t, q);
+  float ga[C][V];
+  {
+    P p;
+    if (a.gamma) p.load(static_cast<const T*>(a.gamma), t, q);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < V; ++k) ga[c][k] = a.gamma ? (float)p.v[c][k] : 1.f;
+  }
   const float n = (float)q;
   float dg[C][V] = {}, db[C][V] = {};
   const long r1 = min((long)a.B, (long)(blockIdx.x + 1) * a.rows);
-  for (long r0 = (long)blockIdx.x * a.rows; r0 < r1; r0 += G) {  // (the same rounds for every thread)
+  struct {
+    P x, d, r;
+  } now, next;
+  const auto load = [&](auto& to, long r) {
+    const long at = min(r, r1 - 1) * q;
+    to.x.load(x + at, t, q);
+    to.d.load(dy + at, t, q);
+    if (dr) to.r.load(dr + at, t, q);
+  };
+  long r0 = (long)blockIdx.x * a.rows;
+  if (AHEAD && r0 < r1) load(now, r0 + g);
+  for (; r0 < r1; r0 += G) {  // (the same rounds for every thread)
     const long r = r0 + g;
-    const bool on = r < r1;
-    P px, pd, pr;
-    px.load(x + min(r, r1 - 1) * q, t, q);
-    pd.load(dy + min(r, r1 - 1) * q, t, q);
-    if (dr && dx) pr.load(dr + min(r, r1 - 1) * q, t, q);
+    if constexpr (AHEAD) {
+      if (r0 + G < r1) load(next, r + G);
+    } else {
+      load(now, r);
+    }
     float2 s = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        s.x += (float)px.v[c][k];
-        s.y = a.gamma ? fmaf((float)pd.v[c][k], (float)ga.v[c][k], s.y) : s.y + (float)pd.v[c][k];
+        s.x += (float)now.x.v[c][k];
+        s.y = fmaf((float)now.d.v[c][k], ga[c][k], s.y);
       }
     s = sum(s);
     const float mean = s.x / n, m1 = s.y / n;
     s = {0.f, 0.f};
+    float d[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        const float d = P::first(t, c) + k < q ? (float)px.v[c][k] - mean : 0.f;
-        const float gk = a.gamma ? (float)pd.v[c][k] * (float)ga.v[c][k] : (float)pd.v[c][k];
-        s.x = fmaf(d, d, s.x);
-        s.y = fmaf(gk, d, s.y);
+        d[c][k] = FULL || P::first(t, c) + k < q ? (float)now.x.v[c][k] - mean : 0.f;
+        s.x = fmaf(d[c][k], d[c][k], s.x);
+        s.y = fmaf((float)now.d.v[c][k] * ga[c][k], d[c][k], s.y);
       }
     s = sum(s);
     const float rstd = 1.f / sqrtf(s.x / n + a.eps), m2 = s.y / n * rstd;
-    if (!on) continue;
+    if (r < r1) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      float f[V];
+      for (int c = 0; c < C; ++c) {
+        float f[V];
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const float d = (float)pd.v[c][k], xh = ((float)px.v[c][k] - mean) * rstd;
-        const float gk = a.gamma ? d * (float)ga.v[c][k] : d;
-        f[k] = rstd * (gk - m1 - xh * m2);
-        if (dr && dx) f[k] += (float)pr.v[c][k];
-        dg[c][k] = fmaf(d, xh, dg[c][k]);
-        db[c][k] += d;
+        for (int k = 0; k < V; ++k) {
+          const float dk = (float)now.d.v[c][k], xh = d[c][k] * rstd;
+          f[k] = rstd * (dk * ga[c][k] - m1 - xh * m2);
+          if (dr) f[k] += (float)now.r.v[c][k];
+          dg[c][k] = fmaf(dk, xh, dg[c][k]);
+          db[c][k] += dk;
+        }
+        if (dx) P::store(dx + r * q, t, q, c, f);
       }
-      if (dx) P::store(dx + r * q, t, q, c, f);
     }
+    if constexpr (AHEAD) now = next;
   }
   float* part = a.part ? a.part + (size_t)blockIdx.x * 2 * q : nullptr;
   if (a.dgamma) add_groups<T, TPR, C>(dg, sums, q, static_cast<T*>(a.dgamma), part);
@@ -359,29 +404,23 @@ struct Group {
   int tpr, c;
 };
 
-inline Group forward_group(size_t esz, int B, int q) {
-  const int v = 16 / (int)esz, pieces = mm::ceil_div(q, v);
-  for (int tpr : {4, 8, 16, 32, 64})
-    if (pieces <= tpr) return {tpr, 1};
-  if (B >= 1024) {  // enough rows for a wave each
-    for (int c : {2, 4, 8})
-      if (pieces <= 64 * c) return {64, c};
-  }
-  for (int c : {1, 2, 4, 8})
-    if (pieces <= 256 * c) return {256, c};
-  return pieces <= 1024 * 8 ? Group{1024, 8} : Group{0, 0};
-}
-
-inline Group backward_group(size_t esz, int q) {
+inline Group forward_group(size_t esz, int q) {
   const int v = 16 / (int)esz, pieces = mm::ceil_div(q, v);
   for (int tpr : {4, 8, 16, 32, 64})
     if (pieces <= tpr) return {tpr, 1};
   if (pieces <= 128) return {64, 2};
-  for (int c : {1, 2})
+  for (int c : {1, 2, 4})
     if (pieces <= 256 * c) return {256, c};
-  for (int c : {1, 2})
+  for (int c : {2, 4})
     if (pieces <= 1024 * c) return {1024, c};
   return {0, 0};
+}
+
+inline Group backward_group(size_t esz, int q) {
+  const int v = 16 / (int)esz, pieces = mm::ceil_div(q, v);
+  for (int tpr : {4, 8, 16, 32, 64, 128, 256, 512, 1024})
+    if (pieces <= tpr) return {tpr, 1};
+  return pieces <= 2048 ? Group{1024, 2} : Group{0, 0};
 }
 
 // Rows of a backward workgroup
@@ -401,11 +440,11 @@ hipError_t forward_g(const NormArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t forward_t(const NormArgs& a, hipStream_t st) {
-  const Group g = forward_group(sizeof(T), a.B, a.q);
+  const Group g = forward_group(sizeof(T), a.q);
 #define LP_CASE(TPR, C) \
   if (g.tpr == TPR && g.c == C) return forward_g<T, TPR, C>(a, st);
-  LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(64, 2) LP_CASE(64, 4) LP_CASE(64, 8)
-  LP_CASE(256, 1) LP_CASE(256, 2) LP_CASE(256, 4) LP_CASE(256, 8) LP_CASE(1024, 8)
+  LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(64, 2) LP_CASE(256, 1) LP_CASE(256, 2)
+  LP_CASE(256, 4) LP_CASE(1024, 2) LP_CASE(1024, 4)
 #undef LP_CASE
   k_forward_long<T><<<(unsigned)std::min(a.B, 2048), 1024, 0, st>>>((const T*)a.x, (const T*)a.gamma, (const T*)a.beta, (T*)a.y, a.B,
                                                                   a.q, (float)a.eps);
@@ -421,9 +460,13 @@ hipError_t backward_t(const NormArgs& a, hipStream_t st) {
              a.B, a.q, l.rows, (float)a.eps};
   const Group g = backward_group(sizeof(T), a.q);
   if (g.tpr) {
-#define LP_CASE(TPR, C) \
-  if (g.tpr == TPR && g.c == C) k_backward<T, TPR, C><<<(unsigned)l.groups, NT_B, 0, st>>>(b);
-    LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(64, 2) LP_CASE(256, 1) LP_CASE(256, 2)
+    const bool full = a.q == g.tpr * g.c * (16 / (int)sizeof(T));
+#define LP_CASE(TPR, C)                                                                                      \
+  if (g.tpr == TPR && g.c == C) {                                                                            \
+    if (full) k_backward<T, TPR, C, true><<<(unsigned)l.groups, NT_B, 0, st>>>(b);                           \
+    else k_backward<T, TPR, C, false><<<(unsigned)l.groups, NT_B, 0, st>>>(b);                               \
+  }
+    LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(128, 1) LP_CASE(256, 1) LP_CASE(512, 1)
     LP_CASE(1024, 1) LP_CASE(1024, 2)
 #undef LP_CASE
   } else {
