@@ -104,18 +104,45 @@ struct Parts {
 
 namespace lp {
 
+// dx and dz^T x as one launch where both take the smallest tiles and contract over at most BOTH_STAGES stages, microseconds
+// of the whole way back against a launch each (and one more for a split): bf16 320 x 60 -> 384 18.0 (20.1), 209 x 649 -> 649
+// 22.7 (28.3), 2000 x 256 -> 700 21.1 (28.7), f32 1000 x 220 -> 587 (38 stages) 49.5 (50.8); longer ones are better split: f32
+// 1000 x 100 -> 900 (57 stages) 57.6 (45.8), 600 x 512 -> 1024 (64) 75.2 (65.4).
+constexpr int BOTH_STAGES = 40;
+
+// The pair's plan. Its smallest tile (two waves, 32 features of each array) takes 0.30 us a stage alone on a CU and 0.45 beside
+// another (floats 0.75, 1.15), no less than its weights' reading takes; joining a split 5 us: 24 x 2048 -> 5120 f16
+// 14.2 us whole, 17.2, 21.8 and 28.1 in two, four and eight; 2 x 4096 -> 4096 bf16 22.9, 23.1, 24.3, 35.3.
+static mm::Plan pair_plan(size_t e, int B, int ni, int no) {
+  mm::Plan p = mm::plan_of(e, B, 2L * no, ni);
+  if (p.tile != 64) return p;
+  const int steps = mm::ceil_div(ni * (long)e, mm::STAGE_BYTES);
+  const double one = e == 2 ? 0.30 : 0.75, two = e == 2 ? 0.45 : 1.15, read = 2.0 * no * ni * e / 4.9e6;
+  double least = 1e30;
+  for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    if (splits > 1 && steps < 4 * splits) break;
+    const long n = mm::ceil_div((long)p.tm * p.tn * splits, 256);
+    double t = std::max(read, mm::ceil_div(steps, splits) * ((n / 2) * two + (n % 2) * one));
+    if (splits > 1) t += 5.0 + 2.0 * splits * B * p.tn * 64 * 4 / 3e6;
+    if (t < least) least = t, p.splits = splits;
+  }
+  return p;
+}
+
 GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad) {
   const size_t e = esize(dtype), row = mm::padded(e, ni) * e;
   const int two = 2 * mm::ceil_div(no, mm::PAIR_BLOCK) * mm::PAIR_BLOCK;
   GatedLayout l{};
   // (a pair's tile holds half a tile's features of each: the tiles of a product of 2 no features)
-  l.z = mm::plan_of(e, B, 2L * no, ni);
+  l.z = pair_plan(e, B, ni, no);
   if (B == 1 && !grad) l.z = mm::Plan{1, 1, 1, mm::ceil_div(no, mm::one_features(2L * no) / 2)};
   size_t part = l.z.part_bytes();
   Parts p;
   if (grad) {
     l.zx = mm::plan_of(e, B, ni, two);
     l.zw = mm::plan_of(e, two, ni, B);
+    const double stages = mm::ceil_div((long)std::max(two, B) * (long)e, mm::STAGE_BYTES);
+    l.both = l.zx.tile == 64 && l.zw.tile == 64 && stages <= BOTH_STAGES;
     part = std::max({part, l.zx.part_bytes(), l.zw.part_bytes()});
     // (and the layer itself, whose plan differs for one row only and then has no sums to join)
     l.dz = p.take((size_t)B * two * e);

@@ -38,8 +38,32 @@ __device__ __forceinline__ float logistic(float z) {
   }
 }
 
-// s(z) and s'(z). gelu is z times the normal distribution function, by erfc so that its tail keeps
-// its relative accuracy. A NaN stays one.
+// The standard normal distribution function of z and its density's exponential e = exp(-z^2 / 2). erfc, not erf, so that
+// the tail keeps its relative accuracy; of the 16-bit types by a polynomial in t = 1 / (1 + 0.425 |x|), x = z / sqrt 2,
+// fitted to exp(x^2) erfc(x) in relative error over all x >= 0 (1.2e-7; 5.3e-7 evaluated in fp32): the device library's
+// erfc took half of the few-token case's second launch.
+template <typename T>
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  if constexpr (sizeof(T) == 2) {
+    e = __builtin_amdgcn_exp2f(-0.7213475204444817f * z * z);
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.425f * 0.7071067811865476f * fabsf(z));
+    float p = 0.07218405604362488f;
+    p = fmaf(p, t, -0.3160977065563202f);
+    p = fmaf(p, t, 0.4126853942871094f);
+    p = fmaf(p, t, -0.10791664570569992f);
+    p = fmaf(p, t, 0.2575562298297882f);
+    p = fmaf(p, t, 0.199957013130188f);
+    p = fmaf(p, t, 0.2419607788324356f);
+    p = fmaf(p, t, 0.2396707832813263f);
+    const float tail = 0.5f * p * t * e;
+    return z > 0.f ? 1.f - tail : tail;
+  } else {
+    e = expf(-0.5f * z * z);
+    return 0.5f * erfcf(-0.7071067811865476f * z);
+  }
+}
+
+// s(z) and s'(z). gelu is z times the normal distribution function. A NaN stays one.
 template <typename T, int ACT>
 __device__ __forceinline__ void gate(float z, float& s, float& ds) {
   if constexpr (ACT == ACT_SILU) {
@@ -47,9 +71,10 @@ __device__ __forceinline__ void gate(float z, float& s, float& ds) {
     s = z * t;
     ds = t * (1.f + z * (1.f - t));
   } else if constexpr (ACT == ACT_GELU) {
-    const float cdf = 0.5f * erfcf(-0.7071067811865476f * z);
+    float e;
+    const float cdf = normal_cdf<T>(z, e);
     s = z * cdf;
-    ds = cdf + z * (0.3989422804014327f * expf(-0.5f * z * z));
+    ds = cdf + z * (0.3989422804014327f * e);
   } else {
     s = wide::sigma<T, ACT>(z);
     ds = wide::dsigma<T, ACT>(z);
@@ -193,6 +218,18 @@ struct EpPairRows {
   }
 };
 
+// dx and dz^T x, neither of which needs the other, as one launch, the longer contraction's tiles first
+template <typename T, class S1, class S2, class E1, class E2>
+__global__ __launch_bounds__(S1::NT, S1::WAVES) void k_both(mm::Prob p1, typename E1::Args e1, mm::Prob p2, typename E2::Args e2) {
+  static_assert(S1::NT == S2::NT && sizeof(mm::Stages<S1>) == sizeof(mm::Stages<S2>), "the same workgroups");
+  __shared__ mm::Stages<S1> stages;
+  const int n1 = p1.tm * p1.tn, n2 = p2.tm * p2.tn, id = blockIdx.x;
+  const bool swap = p2.K > p1.K;
+  const int b1 = swap ? n2 : 0, b2 = swap ? 0 : n1;  // where each product's workgroups begin
+  if (id >= b1 && id < b1 + n1) mm::mm_tile<T, S1, false, true, E1>(p1, e1, id - b1, stages);
+  else mm::mm_tile<T, S2, true, true, E2>(p2, e2, id - b2, reinterpret_cast<mm::Stages<S2>&>(stages));
+}
+
 inline mm::Prob prob(const void* A, long lda, const void* B, const void* B2, long ldb, int M, int N, int K, int kw) {
   mm::Prob p{A, B, lda, ldb, M, N, K, nullptr, 0, 0, 0, 0, 0};
   p.B2 = B2;
@@ -248,12 +285,25 @@ hipError_t backward_t(const GatedArgs& a, hipStream_t st) {
     e = mm::launch_mm<T, false, false, EpGatedGrad<T>, mm::PAIR_ROWS>(
         prob(o.x, o.ldx, o.Wg, o.Wu, o.ldw, a.B, a.no, a.ni, 0), eg, l.z, part, st);
   }
+  const mm::Prob px = prob(dz, two, o.Wg, o.Wu, o.ldw, a.B, a.ni, two, a.no), pw = prob(dz, two, o.x, nullptr, o.ldx, two, a.ni, a.B, 0);
+  const typename EpOut<T>::Args ex{(T*)a.dx};
+  const typename EpPairRows<T>::Args ew{{(T*)a.dWg, (T*)a.dWu}, a.no};
+  const bool weights = a.dWg || a.dWu;
+  if (e == hipSuccess && l.both && a.B && a.dx && weights) {
+    typedef std::conditional_t<sizeof(T) == 2, mm::Tile64, mm::Tile64f> S;
+    const auto whole = [](mm::Prob p) {
+      p.tm = mm::ceil_div(p.M, S::BM), p.tn = mm::ceil_div(p.N, S::BN);
+      p.kper = mm::ceil_div(p.K * (long)sizeof(T), mm::STAGE_BYTES) * (mm::STAGE_BYTES / (int)sizeof(T));
+      return p;
+    };
+    const mm::Prob x = whole(px), w2 = whole(pw);
+    k_both<T, mm::Paired<S, mm::PAIR_COLS>, S, EpOut<T>, EpPairRows<T>>
+        <<<(unsigned)(x.tm * x.tn + w2.tm * w2.tn), S::NT, 0, st>>>(x, ex, w2, ew);
+    return hipGetLastError();
+  }
   if (e == hipSuccess && a.B && a.dx)
-    e = mm::launch_mm<T, false, true, EpOut<T>, mm::PAIR_COLS>(prob(dz, two, o.Wg, o.Wu, o.ldw, a.B, a.ni, two, a.no),
-                                                               {(T*)a.dx}, l.zx, part, st);
-  if (e == hipSuccess && (a.dWg || a.dWu))
-    e = mm::launch_mm<T, true, true, EpPairRows<T>>(prob(dz, two, o.x, nullptr, o.ldx, two, a.ni, a.B, 0),
-                                                    {{(T*)a.dWg, (T*)a.dWu}, a.no}, l.zw, part, st);
+    e = mm::launch_mm<T, false, true, EpOut<T>, mm::PAIR_COLS>(px, ex, l.zx, part, st);
+  if (e == hipSuccess && weights) e = mm::launch_mm<T, true, true, EpPairRows<T>>(pw, ew, l.zw, part, st);
   return e;
 }
 

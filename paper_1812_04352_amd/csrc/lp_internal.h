@@ -357,6 +357,7 @@ struct GatedArgs {
 struct GatedLayout {
   size_t dz, x, Wg, Wu, part, total;
   mm::Plan z, zx, zw;  // the pair x Wg^T, x Wu^T, and dz W, dz^T x
+  bool both;           // the last two run as one launch of the smallest tiles
 };
 GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad);
 

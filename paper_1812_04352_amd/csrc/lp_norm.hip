@@ -20,8 +20,10 @@ namespace norm {
 
 using mm::GVec;
 
-constexpr int NT_F = 256;   // threads of a forward workgroup (more where a row takes more)
-constexpr int NT_B = 1024;  // and of a backward one: few rows of partial sums
+// Threads of a workgroup whose groups have TPR each: whole groups, about 256 forward and about 1024 back, where every
+// workgroup leaves a row of partial sums.
+constexpr int threads_forward(int tpr) { return tpr > 256 ? tpr : 256 / tpr * tpr; }
+constexpr int threads_back(int tpr) { return 1024 / tpr * tpr; }
 
 // A thread's pieces of a row: features (c TPR + t) V .. of the group's thread t
 template <typename T, int TPR, int C>
@@ -30,17 +32,47 @@ struct Piece {
   typedef typename GVec<T, V>::type Vec;
   Vec v[C];
   static __device__ __forceinline__ int first(int t, int c) { return (c * TPR + t) * V; }
-  // zeros behind the row's end
+  // Whole pieces: one that the row's end cuts is read from V values before that end, and those behind it from there too
+  // (so that no lane branches and nothing waits for the load); cut() makes them what they stand for.
   __device__ __forceinline__ void load(const T* row, int t, int q) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int n = first(t, c);
-      if (n + V <= q) {
-        v[c] = *reinterpret_cast<const Vec*>(row + n);
+      if (q >= V) {
+        v[c] = *reinterpret_cast<const Vec*>(row + min(first(t, c), q - V));
       } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k) v[c][k] = n + k < q ? row[n + k] : (T)0.f;
+        for (int k = 0; k < V; ++k) v[c][k] = first(t, c) + k < q ? row[first(t, c) + k] : (T)0.f;
       }
+    }
+  }
+  // What follows converts the values again: kept as floats from pass to pass they would not fit the registers.
+  __device__ __forceinline__ void forget() {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+      u32x4 x = __builtin_bit_cast(u32x4, v[c]);
+      asm volatile("" : "+v"(x));
+      v[c] = __builtin_bit_cast(Vec, x);
+    }
+#endif
+  }
+  // zeros behind the row's end
+  __device__ __forceinline__ void cut(int t, int q) {
+    if (q < V) return;
+    const int bits = (V - q % V) % V * 8 * (int)sizeof(T);  // of the values before the cut piece
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+      const int n = first(t, c);
+      const u64x2 x = __builtin_bit_cast(u64x2, v[c]);
+      u64x2 y = {0, 0};
+      if (bits >= 64) y[0] = x[1] >> (bits - 64);
+      else if (bits > 0) y[0] = x[0] >> bits | x[1] << (64 - bits), y[1] = x[1] >> bits;
+      const bool whole = n + V <= q, none = n >= q;
+      y[0] = whole ? x[0] : none ? 0 : y[0];
+      y[1] = whole ? x[1] : none ? 0 : y[1];
+      v[c] = __builtin_bit_cast(Vec, y);
     }
   }
   static __device__ __forceinline__ void store(T* row, int t, int q, int c, const float (&f)[V]) {
@@ -117,13 +149,14 @@ __global__ __launch_bounds__(NT) void k_forward(const T* x, const T* gamma, cons
   GroupSum<TPR, NT> sum{lds};
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
   P ga, be;
-  if (gamma) ga.load(gamma, t, q);
-  if (beta) be.load(beta, t, q);
+  if (gamma) ga.load(gamma, t, q), ga.cut(t, q);
+  if (beta) be.load(beta, t, q), be.cut(t, q);
   const float n = (float)q;
   for (long r0 = (long)blockIdx.x * G; r0 < B; r0 += (long)gridDim.x * G) {  // (the same rounds for every thread)
     const long r = r0 + g;
     P p;
     p.load(x + min(r, (long)B - 1) * q, t, q);
+    p.cut(t, q);
     float2 s = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -167,7 +200,7 @@ struct BackArgs {
 template <typename T, int TPR, int C>
 __device__ __forceinline__ void add_groups(const float (&acc)[C][16 / sizeof(T)], float* lds, int q, T* out, float* part) {
   typedef Piece<T, TPR, C> P;
-  constexpr int V = P::V, G = NT_B / TPR, ROW = TPR * C * V;
+  constexpr int V = P::V, NT = threads_back(TPR), G = NT / TPR, ROW = TPR * C * V;
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
   if constexpr (G == 1) {
 #pragma unroll
@@ -189,7 +222,7 @@ __device__ __forceinline__ void add_groups(const float (&acc)[C][16 / sizeof(T)]
       for (int k = 0; k < V; k += 4)
         *reinterpret_cast<float4*>(lds + g * ROW + P::first(t, c) + k) = make_float4(acc[c][k], acc[c][k + 1], acc[c][k + 2], acc[c][k + 3]);
     __syncthreads();
-    for (int n = threadIdx.x; n < q; n += NT_B) {
+    for (int n = threadIdx.x; n < q; n += NT) {
       float s = lds[n];
 #pragma unroll
       for (int i = 1; i < G; ++i) s += lds[i * ROW + n];
@@ -202,25 +235,22 @@ __device__ __forceinline__ void add_groups(const float (&acc)[C][16 / sizeof(T)]
 // FULL: q = TPR C V, no piece behind the row's end. The next round's rows are requested before this one's sums (one
 // piece a thread: registers), so that a workgroup a CU keeps memory busy.
 template <typename T, int TPR, int C, bool FULL>
-__global__ __launch_bounds__(NT_B) void k_backward(BackArgs a) {
+__global__ __launch_bounds__(threads_back(TPR)) void k_backward(BackArgs a) {
   typedef Piece<T, TPR, C> P;
-  constexpr int V = P::V, G = NT_B / TPR;
+  constexpr int V = P::V, NT = threads_back(TPR), G = NT / TPR;
   constexpr bool AHEAD = C == 1;
-  __shared__ float2 lds[2][NT_B / 64];
-  __shared__ __attribute__((aligned(16))) float sums[G == 1 ? 4 : NT_B * C * V];
-  GroupSum<TPR, NT_B> sum{lds};
+  __shared__ float2 lds[2][NT / 64];
+  __shared__ __attribute__((aligned(16))) float sums[G == 1 ? 4 : NT * C * V];
+  GroupSum<TPR, NT> sum{lds};
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, q = FULL ? TPR * C * V : a.q;
   const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = a.dx ? static_cast<const T*>(a.dr) : nullptr;
   T* dx = static_cast<T*>(a.dx);
-  float ga[C][V];
-  {
-    P p;
-    if (a.gamma) p.load(static_cast<const T*>(a.gamma), t, q);
+  P ga;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+  for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int k = 0; k < V; ++k) ga[c][k] = a.gamma ? (float)p.v[c][k] : 1.f;
-  }
+    for (int k = 0; k < V; ++k) ga.v[c][k] = (T)1.f;
+  if (a.gamma) ga.load(static_cast<const T*>(a.gamma), t, q), ga.cut(t, q);
   const float n = (float)q;
   float dg[C][V] = {}, db[C][V] = {};
   const long r1 = min((long)a.B, (long)(blockIdx.x + 1) * a.rows);
@@ -242,36 +272,41 @@ __global__ __launch_bounds__(NT_B) void k_backward(BackArgs a) {
     } else {
       load(now, r);
     }
+    if constexpr (!FULL) now.x.cut(t, q), now.d.cut(t, q);  // (dr's values behind the end are not used, those of a cut piece are)
+    if constexpr (!FULL) {
+      if (dr) now.r.cut(t, q);
+    }
     float2 s = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         s.x += (float)now.x.v[c][k];
-        s.y = fmaf((float)now.d.v[c][k], ga[c][k], s.y);
+        s.y = fmaf((float)now.d.v[c][k], (float)ga.v[c][k], s.y);
       }
     s = sum(s);
     const float mean = s.x / n, m1 = s.y / n;
     s = {0.f, 0.f};
-    float d[C][V];
+    if constexpr (!AHEAD) now.x.forget(), now.d.forget(), ga.forget();
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        d[c][k] = FULL || P::first(t, c) + k < q ? (float)now.x.v[c][k] - mean : 0.f;
-        s.x = fmaf(d[c][k], d[c][k], s.x);
-        s.y = fmaf((float)now.d.v[c][k] * ga[c][k], d[c][k], s.y);
+        const float d = FULL || P::first(t, c) + k < q ? (float)now.x.v[c][k] - mean : 0.f;
+        s.x = fmaf(d, d, s.x);
+        s.y = fmaf((float)now.d.v[c][k] * (float)ga.v[c][k], d, s.y);
       }
     s = sum(s);
     const float rstd = 1.f / sqrtf(s.x / n + a.eps), m2 = s.y / n * rstd;
+    if constexpr (!AHEAD) now.x.forget(), now.d.forget(), ga.forget();
     if (r < r1) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         float f[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float dk = (float)now.d.v[c][k], xh = d[c][k] * rstd;
-          f[k] = rstd * (dk * ga[c][k] - m1 - xh * m2);
+          const float dk = (float)now.d.v[c][k], xh = ((float)now.x.v[c][k] - mean) * rstd;
+          f[k] = rstd * (dk * (float)ga.v[c][k] - m1 - xh * m2);
           if (dr) f[k] += (float)now.r.v[c][k];
           dg[c][k] = fmaf(dk, xh, dg[c][k]);
           db[c][k] += dk;
@@ -404,23 +439,30 @@ struct Group {
   int tpr, c;
 };
 
+#define LP_FORWARD_GROUPS(CASE)                                                                                        \
+  CASE(4, 1) CASE(8, 1) CASE(16, 1) CASE(32, 1) CASE(64, 1) CASE(64, 2) CASE(64, 3) CASE(64, 4) CASE(128, 3) CASE(256, 2) \
+  CASE(256, 3) CASE(256, 4) CASE(512, 3) CASE(1024, 2) CASE(1024, 3) CASE(1024, 4)
+#define LP_BACKWARD_GROUPS(CASE)                                                                                   \
+  CASE(4, 1) CASE(8, 1) CASE(16, 1) CASE(32, 1) CASE(64, 1) CASE(128, 1) CASE(192, 1) CASE(256, 1) CASE(320, 1) \
+  CASE(384, 1) CASE(512, 1) CASE(768, 1) CASE(1024, 1) CASE(1024, 2)
+
+// The first group of the list (by its pieces) that holds the row
 inline Group forward_group(size_t esz, int q) {
-  const int v = 16 / (int)esz, pieces = mm::ceil_div(q, v);
-  for (int tpr : {4, 8, 16, 32, 64})
-    if (pieces <= tpr) return {tpr, 1};
-  if (pieces <= 128) return {64, 2};
-  for (int c : {1, 2, 4})
-    if (pieces <= 256 * c) return {256, c};
-  for (int c : {2, 4})
-    if (pieces <= 1024 * c) return {1024, c};
+  const int pieces = mm::ceil_div(q * (long)esz, 16);
+#define LP_CASE(TPR, C) \
+  if (pieces <= TPR * C) return {TPR, C};
+  LP_FORWARD_GROUPS(LP_CASE)
+#undef LP_CASE
   return {0, 0};
 }
 
 inline Group backward_group(size_t esz, int q) {
-  const int v = 16 / (int)esz, pieces = mm::ceil_div(q, v);
-  for (int tpr : {4, 8, 16, 32, 64, 128, 256, 512, 1024})
-    if (pieces <= tpr) return {tpr, 1};
-  return pieces <= 2048 ? Group{1024, 2} : Group{0, 0};
+  const int pieces = mm::ceil_div(q * (long)esz, 16);
+#define LP_CASE(TPR, C) \
+  if (pieces <= TPR * C) return {TPR, C};
+  LP_BACKWARD_GROUPS(LP_CASE)
+#undef LP_CASE
+  return {0, 0};
 }
 
 // Rows of a backward workgroup
@@ -432,7 +474,7 @@ inline int backward_rows(int groups, int B) {
 
 template <typename T, int TPR, int C>
 hipError_t forward_g(const NormArgs& a, hipStream_t st) {
-  constexpr int NT = TPR > NT_F ? TPR : NT_F, G = NT / TPR;
+  constexpr int NT = threads_forward(TPR), G = NT / TPR;
   const unsigned grid = (unsigned)std::min<long>(mm::ceil_div(a.B, G), 4096);
   k_forward<T, TPR, C, NT><<<grid, NT, 0, st>>>((const T*)a.x, (const T*)a.gamma, (const T*)a.beta, (T*)a.y, a.B, a.q, (float)a.eps);
   return hipGetLastError();
@@ -443,8 +485,7 @@ hipError_t forward_t(const NormArgs& a, hipStream_t st) {
   const Group g = forward_group(sizeof(T), a.q);
 #define LP_CASE(TPR, C) \
   if (g.tpr == TPR && g.c == C) return forward_g<T, TPR, C>(a, st);
-  LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(64, 2) LP_CASE(256, 1) LP_CASE(256, 2)
-  LP_CASE(256, 4) LP_CASE(1024, 2) LP_CASE(1024, 4)
+  LP_FORWARD_GROUPS(LP_CASE)
 #undef LP_CASE
   k_forward_long<T><<<(unsigned)std::min(a.B, 2048), 1024, 0, st>>>((const T*)a.x, (const T*)a.gamma, (const T*)a.beta, (T*)a.y, a.B,
                                                                   a.q, (float)a.eps);
@@ -461,13 +502,12 @@ hipError_t backward_t(const NormArgs& a, hipStream_t st) {
   const Group g = backward_group(sizeof(T), a.q);
   if (g.tpr) {
     const bool full = a.q == g.tpr * g.c * (16 / (int)sizeof(T));
-#define LP_CASE(TPR, C)                                                                                      \
-  if (g.tpr == TPR && g.c == C) {                                                                            \
-    if (full) k_backward<T, TPR, C, true><<<(unsigned)l.groups, NT_B, 0, st>>>(b);                           \
-    else k_backward<T, TPR, C, false><<<(unsigned)l.groups, NT_B, 0, st>>>(b);                               \
+#define LP_CASE(TPR, C)                                                                                \
+  if (g.tpr == TPR && g.c == C) {                                                                      \
+    if (full) k_backward<T, TPR, C, true><<<(unsigned)l.groups, threads_back(TPR), 0, st>>>(b);        \
+    else k_backward<T, TPR, C, false><<<(unsigned)l.groups, threads_back(TPR), 0, st>>>(b);            \
   }
-    LP_CASE(4, 1) LP_CASE(8, 1) LP_CASE(16, 1) LP_CASE(32, 1) LP_CASE(64, 1) LP_CASE(128, 1) LP_CASE(256, 1) LP_CASE(512, 1)
-    LP_CASE(1024, 1) LP_CASE(1024, 2)
+    LP_BACKWARD_GROUPS(LP_CASE)
 #undef LP_CASE
   } else {
     float2* stats = reinterpret_cast<float2*>(w + l.stats);
@@ -489,7 +529,7 @@ NormLayout norm_layout(int dtype, int B, int q) {
   const norm::Group g = norm::backward_group(dtype == 0 ? 4 : 2, q);
   NormLayout l{};
   if (g.tpr) {
-    l.rows = norm::backward_rows(norm::NT_B / g.tpr, B);
+    l.rows = norm::backward_rows(norm::threads_back(g.tpr) / g.tpr, B);
   } else {
     l.rows = std::min(2048, std::max(16, mm::ceil_div(B, 1024)));
     l.stats = ((size_t)B * 8 + 255) / 256 * 256;
