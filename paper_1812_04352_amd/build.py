@@ -48,9 +48,8 @@ SAN_FLAGS = ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-
              "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer",
              "-Xarch_host", "-shared-libasan"]
 # the translation units with host logic beyond launches
-SAN_SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_gated_bf16.hip", "lp_gated_f16.hip", "lp_gated_f32.hip",
-               "lp_orth_f16.hip", "lp_orth_f32.hip", "lp_norm.hip", "lp_step_host.cpp", "lp_block_host.cpp", "lp_host.cpp",
-               "lp_noalloc.hip"]
+SAN_SOURCES = ["lp_step_bf16.hip", "lp_step_f16.hip", "lp_step_f32.hip", "lp_norm.hip", "lp_step_host.cpp", "lp_block_host.cpp",
+               "lp_host.cpp", "lp_noalloc.hip"]
 SAN_OUT = os.path.join(OBJ, "liblp_san.so")
 
 
