@@ -470,9 +470,13 @@ __device__ __forceinline__ void wait_and_meet() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// id: the workgroup's index among the product's
-template <class S>
-__device__ __forceinline__ Place place(const Prob& p, int id, int wave, int& K) {
+// id: the workgroup's index among the product's. SCALAR: the tile's place is put into scalar registers by force: it comes
+// from divisions, which are made in vector registers, and beside a large epilogue the compiler may leave the
+// operands' addresses there too, of which no descriptor can be formed. (The compiler does not see the written-out
+// instruction's hazards: a wait state between a vector instruction's result and its reading, and five until a scalar that
+// it writes may be read by any other instruction.)
+template <class S, bool SCALAR = false>
+__device__ __forceinline__ Place place(const Prob& p, int id, int split, int wave, int& K) {
   Place c;
   K = p.K;
   c.M = p.M;
@@ -484,6 +488,13 @@ __device__ __forceinline__ Place place(const Prob& p, int id, int wave, int& K) 
   }
   if constexpr (S::SYM) tile_below(id, p.tm, c.mt, c.nt);
   else tile_of(id, p.tm, p.tn, c.mt, c.nt);
+#ifdef __HIP_DEVICE_COMPILE__
+  if constexpr (SCALAR) {
+    asm volatile("s_nop 1\n\tv_readfirstlane_b32 %0, %2\n\tv_readfirstlane_b32 %1, %3\n\ts_nop 4"
+                 : "=&s"(c.mt), "=&s"(c.nt)
+                 : "v"(c.mt), "v"(c.nt));
+  }
+#endif
   c.m0 = c.mt * S::BM;
   c.n0 = c.nt * S::BNO;
   c.lim = min(c.N, c.n0 + S::BNO);
@@ -492,7 +503,7 @@ __device__ __forceinline__ Place place(const Prob& p, int id, int wave, int& K) 
   c.wn = wave % S::WGN;
   c.mw = c.m0 + c.wm * (S::BM / S::WGM);
   c.nw = c.n0 + c.wn * (S::BNO / S::WGN);
-  c.split = blockIdx.y;
+  c.split = split;
   return c;
 }
 
@@ -503,7 +514,7 @@ struct Stages {
 };
 
 template <typename T, class S, bool AT, bool BT, class E>
-__device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& ea, int id, Stages<S>& stages) {
+__device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& ea, int id, Stages<S>& stages, int split = blockIdx.y) {
   constexpr int BM = S::BM, BN = S::BN, WGM = S::WGM, WGN = S::WGN, KB = S::KB, NS = S::NS, NT = S::NT;
   constexpr int FM = BM / WGM / 32, FN = BN / WGN / 32, GK = S::GK;
   constexpr int NG = KB / (16 * (int)sizeof(T)) / GK;
@@ -519,9 +530,9 @@ __device__ __forceinline__ void mm_tile(const Prob& p, const typename E::Args& e
   static_assert(epilogue_lds(WGM * WGN, BM, WGN) <= NS * (BM + BN) * KB, "the epilogue's LDS");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int K;
-  const Place c = place<S>(p, id, wave, K);
+  const Place c = place<S, std::is_same<T, Duo>::value || S::SYM || S::PAIR != PAIR_NONE>(p, id, split, wave, K);
   if (c.m0 >= c.M) return;
-  const int k0 = blockIdx.y * p.kper, k1 = min(K, k0 + p.kper);
+  const int k0 = split * p.kper, k1 = min(K, k0 + p.kper);
   const int steps = k1 > k0 ? (k1 - k0 + SA::BK - 1) / SA::BK : 0;
   const Reader<T, SA, KB, FM, AT> ra(c.wm * (BM / WGM), c.lane);
   // (of a pair in rows: the blocks of both halves, which lie BN / 2 rows apart)
@@ -751,12 +762,23 @@ struct BlockIO<Duo> {
     *reinterpret_cast<Quad*>(at) = h;
     *reinterpret_cast<Quad*>(at + 16) = l;
   }
-  static __device__ __forceinline__ void quads(const Duo* a, long ld, const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
+  struct Block {
+    Piece p[ITER];
+  };
+  static __device__ __forceinline__ Block fetch(const Duo* a, long ld, const Place& c, int i, int j) {
+    Block b;
 #pragma unroll
     for (int t = 0; t < ITER; ++t) {
       const int id = c.lane + 64 * t, m = min(c.mw + 32 * i + id / CPR, c.M - 1), n = c.nw + 32 * j + id % CPR * V;
-      *reinterpret_cast<Piece*>(buf + id / CPR * PITCH + id % CPR * 16) =
-          n < ld ? *reinterpret_cast<const Piece*>(a + (size_t)m * ld + n) : Piece{0.f, 0.f, 0.f, 0.f};
+      b.p[t] = *reinterpret_cast<const Piece*>(a + (size_t)m * ld + min((long)n, ld - V));  // (pieces behind a row: not used)
+    }
+    return b;
+  }
+  static __device__ __forceinline__ void quads(const Block& b, const Place& c, unsigned char* buf, f32x4 (&v)[4]) {
+#pragma unroll
+    for (int t = 0; t < ITER; ++t) {
+      const int id = c.lane + 64 * t;
+      *reinterpret_cast<Piece*>(buf + id / CPR * PITCH + id % CPR * 16) = b.p[t];
     }
     wave_in_order();
     const unsigned char* r = buf + (c.lane & 31) * PITCH + (c.lane >> 5) * 8;
@@ -825,12 +847,20 @@ struct Rows {
 
 template <bool WHOLE, int FM, int FN, bool AHEAD>
 struct Rows<WHOLE, Duo, FM, FN, AHEAD> {
+  typedef BlockIO<Duo> IO;
+  static constexpr bool NEXT = FM * FN <= 4;  // (larger tiles have no registers for it)
   const Duo* a;
   long ld;
-  __device__ __forceinline__ Rows(const Duo* a_, long ld_, const Place&) : a(a_), ld(ld_) {}
+  IO::Block next;
+  __device__ __forceinline__ Rows(const Duo* a_, long ld_, const Place& c) : a(a_), ld(ld_) {
+    if (NEXT && a) next = IO::fetch(a, ld, c, 0, 0);
+  }
   __device__ __forceinline__ void get(const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
     if (a) {
-      BlockIO<Duo>::quads(a, ld, c, i, j, buf, v);
+      const IO::Block b = NEXT ? next : IO::fetch(a, ld, c, i, j);
+      if (NEXT && i + 1 < FM) next = IO::fetch(a, ld, c, i + 1, j);
+      else if (NEXT && j + 1 < FN) next = IO::fetch(a, ld, c, 0, j + 1);
+      IO::quads(b, c, buf, v);
     } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = 0.f;
@@ -957,14 +987,15 @@ struct EpScale {
   }
 };
 
-// Adds the partial sums of a split contraction in order and runs the epilogue.
+// Adds the partial sums of a split contraction, a tile's from `first` on `step` tiles apart, in order and runs the epilogue.
 template <class S, class E>
-__device__ __forceinline__ void finish_tile(const Prob& p, const f32x4* part, int splits, const typename E::Args& ea) {
+__device__ __forceinline__ void finish_tile(const Prob& p, int id, const f32x4* part, size_t first, size_t step, int splits,
+                                            const typename E::Args& ea) {
   constexpr int WGM = S::WGM, WGN = S::WGN, FM = S::BM / WGM / 32, FN = S::BN / WGN / 32, Q = 4 * FM * FN;
   __shared__ __attribute__((aligned(16))) float lds[epilogue_lds(WGM * WGN, S::BM, WGN) / 4];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int K;
-  const Place c = place<S>(p, blockIdx.x, wave, K);
+  const Place c = place<S>(p, id, 0, wave, K);
   if (c.m0 >= c.M) return;
   f32x16 acc[FM][FN];
 #pragma unroll
@@ -973,7 +1004,7 @@ __device__ __forceinline__ void finish_tile(const Prob& p, const f32x4* part, in
     for (int j = 0; j < FN; ++j) acc[i][j] = 0.f;
 #pragma unroll 2
   for (int k = 0; k < splits; ++k) {
-    const f32x4* in = part + ((size_t)k * gridDim.x + blockIdx.x) * (Q * S::NT) + threadIdx.x;
+    const f32x4* in = part + (first + k * step) * (Q * S::NT) + threadIdx.x;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
       if (c.row(i) >= c.M) continue;
@@ -993,7 +1024,7 @@ __device__ __forceinline__ void finish_tile(const Prob& p, const f32x4* part, in
 
 template <class S, class E>
 __global__ __launch_bounds__(S::NT) void k_finish(Prob p, const f32x4* part, int splits, typename E::Args ea) {
-  finish_tile<S, E>(p, part, splits, ea);
+  finish_tile<S, E>(p, blockIdx.x, part, blockIdx.x, gridDim.x, splits, ea);
 }
 
 // A product of one row of A (both operands in rows): bound by reading B once. A workgroup takes NF

@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256) void k_scale(Momentum<TI, 8> u, int no, int ni
 // turned as it is read and written), and the LDS holds what the products read, X and then A and P in its place,
 // as the sum of two f16 values each (2^-22 relative): three instructions a product of two such values.
 //   wave (wi, wj): rows 32 wi .., of A and P columns 32 wj .., of X the blocks wj, wj + 2, .. of 32 columns.
-// 2048 of 64 x 64 f32 LP_SMALL_US us.
+// 2048 of 64 x 64 f32 74 us (2.3 TB/s of g, m, r in and m, W out; 384 us by a launch for every product).
 constexpr int SMALL_N = 64, SMALL_K = 256;
 
 struct Half2 {
@@ -237,42 +237,90 @@ struct SmallArgs {
   double eps, up;  // X is kept times up
 };
 
+// f(0) .. f(N - 1), the index a constant: registers have no other
+template <int N, typename F>
+__device__ __forceinline__ void blocks(F f) {
+  if constexpr (N > 0) {
+    blocks<N - 1>(f);
+    f(std::integral_constant<int, N - 1>{});
+  }
+}
+
 template <typename TI, int KB, bool TALL>
-__global__ __launch_bounds__(256) void k_small(Momentum<TI, TALL ? 1 : 4> u, const TI* r, TI* W, SmallArgs a) {
+__global__ __launch_bounds__(256) void k_small(Momentum<TI, 4> u, const TI* r, TI* W, SmallArgs a) {
   typedef SmallLds<KB> Lds;
   __shared__ Lds lds;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 1, wj = wave & 1;
   const int n = TALL ? a.ni : a.no, k = TALL ? a.no : a.ni, m = 32 * wi + (lane & 31);
   const size_t base = (size_t)blockIdx.x * a.no * a.ni;
-  // f(t, e, at, w): w values at index `at`, the elements e .. of block t
-  const auto each = [&](auto f) {
+  // Block t of an array [no][ni], zeros behind the matrix (loads without a branch: those are of its first value), and back.
+  // Pieces of four values of a wide matrix whose rows are such pieces.
+  const bool pieces = !TALL && k % 4 == 0;
+  const auto fetch = [&](auto* p, int t) {
+    p += base;
+    int ni = a.ni;
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("" : "+s"(ni));  // the indices are formed anew each time: kept, they would not fit the registers
+#endif
+    f32x16 v;
 #pragma unroll
-    for (int t = 0; t < KB; ++t)
+    for (int q = 0; q < 4; ++q) {
+      const int c = 32 * (wj + 2 * t) + 8 * q + 4 * (lane >> 5);
+      if (pieces) {
+        const bool in = m < n && c < k;
+        const auto y = *reinterpret_cast<const typename GVec<std::remove_cv_t<std::remove_pointer_t<decltype(p)>>, 4>::type*>(p + (in ? m * ni + c : 0));
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = 32 * (wj + 2 * t) + 8 * q + 4 * (lane >> 5);
-        if constexpr (TALL) {
+        for (int e = 0; e < 4; ++e) v[4 * q + e] = in ? (float)y[e] : 0.f;
+      } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (m < n && c + e < k) f(t, 4 * q + e, base + (size_t)(c + e) * a.ni + m, 1);
-        } else {
-          if (m < n && c < k) f(t, 4 * q, base + (size_t)m * a.ni + c, min(4, k - c));
+        for (int e = 0; e < 4; ++e) {
+          const bool in = m < n && c + e < k;
+          const float y = (float)p[in ? (TALL ? (c + e) * ni + m : m * ni + c + e) : 0];
+          v[4 * q + e] = in ? y : 0.f;
         }
       }
-  };
-  constexpr int V = TALL ? 1 : 4;
-  f32x16 x[KB];
-#pragma unroll
-  for (int t = 0; t < KB; ++t) x[t] = 0.f;
-  double s = 0.0;
-  each([&](int t, int e, size_t at, int w) {
-    float v[V];
-    u.update(at, w, v);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (i < w) x[t][e + i] = v[i];
-      if (i < w) s += (double)v[i] * (double)v[i];
     }
+    return v;
+  };
+  const auto store = [&](auto* p, int t, const f32x16& v) {
+    typedef std::remove_pointer_t<decltype(p)> TO;
+    p += base;
+    int ni = a.ni;
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("" : "+s"(ni));
+#endif
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int c = 32 * (wj + 2 * t) + 8 * q + 4 * (lane >> 5);
+      if (pieces) {
+        typename GVec<TO, 4>::type y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = (TO)v[4 * q + e];
+        if (m < n && c < k) *reinterpret_cast<typename GVec<TO, 4>::type*>(p + m * ni + c) = y;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (m < n && c + e < k) p[TALL ? (c + e) * ni + m : m * ni + c + e] = (TO)v[4 * q + e];
+      }
+    }
+  };
+  f32x16 x[KB];
+  double s = 0.0;
+  blocks<KB>([&](auto t) {
+    x[t] = fetch(u.g, t);
+    if (u.mo) {
+      f32x16 mo = x[t];
+      if (u.m) {
+        const f32x16 old = fetch(u.m, t);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) mo[e] = fmaf(u.mu, old[e], mo[e]);
+      }
+      store(u.mo, t, mo);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[t][e] = u.nesterov ? fmaf(u.mu, mo[e], x[t][e]) : mo[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s += (double)x[t][e] * (double)x[t][e];
   });
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
@@ -316,21 +364,15 @@ __global__ __launch_bounds__(256) void k_small(Momentum<TI, TALL ? 1 : 4> u, con
     __syncthreads();  // and X and P
   }
   const float alpha = (float)(a.alpha / a.up);
-  each([&](int t, int e, size_t at, int w) {
-    float f[V];
-    if (r) u.get(r + at, w, f);
+  blocks<KB>([&](auto t) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = alpha * (i < w ? x[t][e + i] : 0.f) + (r ? a.beta * f[i] : 0.f);
-    if (w == V) {
-      typename GVec<TI, V>::type y;
+    for (int e = 0; e < 16; ++e) x[t][e] *= alpha;
+    if (r) {
+      const f32x16 old = fetch(r, t);
 #pragma unroll
-      for (int i = 0; i < V; ++i) y[i] = (TI)f[i];
-      *reinterpret_cast<typename GVec<TI, V>::type*>(W + at) = y;
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < w) W[at + i] = (TI)f[i];
+      for (int e = 0; e < 16; ++e) x[t][e] = fmaf(a.beta, old[e], x[t][e]);
     }
+    store(W, t, x[t]);
   });
 }
 
@@ -491,36 +533,68 @@ struct EpUpdate {
   }
 };
 
-// the partial sums of a split contraction
-struct EpPart : mm::EpRaw {
-  typedef mm::EpRaw::Args Args;
+// The partial sums of a split contraction, a workgroup's own place
+struct EpPart {
+  struct Args {
+    f32x4* part;
+  };
+  template <bool WHOLE, int FM, int FN, int WGM, int WGN>
+  static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float*) {
+    constexpr int NT = 64 * WGM * WGN;
+    f32x4* out = a.part + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      if (c.row(i) >= c.M) continue;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) out[((i * FN + j) * 4 + q) * NT] = mm::quad(acc[i][j], q);
+    }
+  }
 };
-template <class S>
-__device__ __forceinline__ mm::f32x4* part_of(mm::f32x4* part, int splits, int z) {
-  return part + (size_t)z * splits * gridDim.x * (S::BM * S::BN / 4);
+
+// A workgroup's matrix, tile and split. Workgroups go to the eight XCDs in turn, each with its own L2: of many matrices
+// each keeps its tiles on one of them, where they share its operands (grid: 8 times the splits, tiles, matrices by
+// eight); of few the tiles are spread over all (grid: tiles, splits, matrices; tile_of). (No division: the compiler makes
+// those in vector registers and leaves what follows from them there, where no descriptor can be formed.)
+constexpr int MANY = 64;
+struct Where {
+  int z, tile, tiles, split, splits;
+};
+__device__ __forceinline__ Where where(int batch) {
+  if (batch >= MANY)
+    return {(int)(blockIdx.x & 7) + 8 * (int)blockIdx.z, (int)blockIdx.y, (int)gridDim.y, (int)(blockIdx.x >> 3), (int)(gridDim.x >> 3)};
+  return {(int)blockIdx.z, (int)blockIdx.x, (int)gridDim.x, (int)blockIdx.y, (int)gridDim.y};
+}
+inline dim3 grid_of(int batch, int tiles, int splits) {
+  if (batch >= MANY) return dim3(8u * splits, tiles, mm::ceil_div(batch, 8));
+  return dim3(tiles, splits, batch);
 }
 
 template <class S> struct Symmetric : S { static constexpr bool SYM = true; };
 template <class S, bool SYM> using ShapeOf = std::conditional_t<SYM, Symmetric<S>, S>;
 
-// The products of a batch (grid z): operands' distances in bytes
+// The products of a batch: operands' distances in bytes
 template <typename T, class S, bool AT, bool BT, class E>
-__global__ __launch_bounds__(S::NT, S::WAVES) void k_bmm(mm::Prob p, size_t sa, size_t sb, typename E::Args ea) {
+__global__ __launch_bounds__(S::NT, S::WAVES) void k_bmm(mm::Prob p, int batch, size_t sa, size_t sb, typename E::Args ea) {
   __shared__ mm::Stages<S> stages;
-  const int z = blockIdx.z;
-  p.A = static_cast<const unsigned char*>(p.A) + z * sa;
-  p.B = static_cast<const unsigned char*>(p.B) + z * sb;
+  const Where w = where(batch);
+  if (w.z >= batch) return;
+  p.A = static_cast<const unsigned char*>(p.A) + w.z * sa;
+  p.B = static_cast<const unsigned char*>(p.B) + w.z * sb;
   if constexpr (std::is_same<E, EpPart>::value) {
-    ea.part = part_of<S>(ea.part, gridDim.y, z);
-    mm::mm_tile<T, S, AT, BT, E>(p, ea, blockIdx.x, stages);
+    ea.part += (((size_t)w.z * w.splits + w.split) * w.tiles + w.tile) * (S::BM * S::BN / 4);
+    mm::mm_tile<T, S, AT, BT, E>(p, ea, w.tile, stages, w.split);
   } else {
-    mm::mm_tile<T, S, AT, BT, E>(p, E::at(ea, z), blockIdx.x, stages);
+    mm::mm_tile<T, S, AT, BT, E>(p, E::at(ea, w.z), w.tile, stages, w.split);
   }
 }
 
 template <class S, class E>
-__global__ __launch_bounds__(S::NT) void k_bfinish(mm::Prob p, mm::f32x4* part, int splits, typename E::Args ea) {
-  mm::finish_tile<S, E>(p, part_of<S>(part, splits, blockIdx.z), splits, E::at(ea, blockIdx.z));
+__global__ __launch_bounds__(S::NT) void k_bfinish(mm::Prob p, int batch, const f32x4* part, int splits, typename E::Args ea) {
+  const Where w = where(batch);
+  if (w.z >= batch) return;
+  mm::finish_tile<S, E>(p, w.tile, part, (size_t)w.z * splits * w.tiles + w.tile, w.tiles, splits, E::at(ea, w.z));
 }
 
 // A product of the batch and how it runs
@@ -540,13 +614,13 @@ hipError_t launch_shape(Product w, const typename E::Args& ea) {
   mm::Prob& p = w.p;
   p.tm = w.pl.tm, p.tn = w.pl.tn;
   p.kper = std::max(1, mm::ceil_div(mm::ceil_div(p.K, BK), w.pl.splits)) * BK;
-  const unsigned tiles = (unsigned)tiles_of(w.pl, SYM);
+  const int tiles = (int)tiles_of(w.pl, SYM);
   if (S::BM > 128 || w.pl.splits == 1) {
-    k_bmm<T, S, AT, BT, E><<<dim3(tiles, 1, (unsigned)w.batch), S::NT, 0, w.st>>>(p, w.sa, w.sb, ea);
+    k_bmm<T, S, AT, BT, E><<<grid_of(w.batch, tiles, 1), S::NT, 0, w.st>>>(p, w.batch, w.sa, w.sb, ea);
   } else if constexpr (S::BM <= 128) {
     typedef ShapeOf<mm::Shape<S::BM, S::BN, S::WGM, S::WGN, 128, 2, 2>, SYM> SF;
-    k_bmm<T, S, AT, BT, EpPart><<<dim3(tiles, (unsigned)w.pl.splits, (unsigned)w.batch), S::NT, 0, w.st>>>(p, w.sa, w.sb, {w.part});
-    k_bfinish<SF, E><<<dim3(tiles, 1, (unsigned)w.batch), S::NT, 0, w.st>>>(p, w.part, w.pl.splits, ea);
+    k_bmm<T, S, AT, BT, EpPart><<<grid_of(w.batch, tiles, w.pl.splits), S::NT, 0, w.st>>>(p, w.batch, w.sa, w.sb, {w.part});
+    k_bfinish<SF, E><<<grid_of(w.batch, tiles, 1), S::NT, 0, w.st>>>(p, w.batch, w.part, w.pl.splits, ea);
   }
   return hipGetLastError();
 }
