@@ -9,7 +9,10 @@
 //              dzg and dzu lie side by side in blocks of PAIR_BLOCK features, dz [B][2 no32]: dx is then
 //              one contraction over both (the weights' rows taken from either array in turn), and
 //              dz^T x one product whose rows belong to dWg and dWu in turn.
-// Bound by the products: 4 B ni no operations forward, 12 B ni no back.
+// Bound by the products: 4 B ni no operations forward, 12 B ni no back: 8192 x 4096 -> 10240 bf16 1110 us forward (1.24
+// PFLOP/s) and 3404 back (1.21). One token reads both weights at 5.7 TB/s (29 us there); 24 x 2048 -> 5120 f16 take 12.9 us.
+// dz is rounded to the element type, which is what the next two products' matrix instructions take: the gradients'
+// error in bf16 grows by it from 0.0017 to 0.0023 of their norm.
 #pragma once
 
 #include <type_traits>

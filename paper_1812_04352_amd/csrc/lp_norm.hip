@@ -9,7 +9,9 @@
 //              A thread keeps the same features of all its rows, so it sums their dgamma and dbeta in
 //              registers; a workgroup adds its groups' in order and writes one row of partial sums, which a
 //              second kernel adds in fp64 (a single workgroup writes the gradients themselves).
-// Bound by memory. Rows that no group can hold are read again for every pass.
+// Bound by memory: 8192 x 4096 bf16 25 us forward (5.3 TB/s), 65 us back with dr (4.1; 62 in the kernel and 4.6 in the sum of
+// 256 rows of partial sums, one of each workgroup, of which there is one a CU; without the next rows requested ahead and with
+// sums by LDS exchanges 97). Rows that no group can hold are read again for every pass.
 #include <algorithm>
 
 #include "lp_internal.h"
