@@ -490,7 +490,8 @@ int32_t lp_gated_forward(const lp_gated* layer, const void* x, const void* Wg, c
                          size_t ws_bytes, void* stream);
 
 /* Gradients of the layer for dy [B][no], from its inputs (zg = x Wg^T and zu = x Wu^T are formed again):
- *   dzg = dy zu sigma'(zg),  dzu = dy sigma(zg)   (rounded to the dtype for the next products)
+ *   dzg = dy zu sigma'(zg),  dzu = dy sigma(zg)   (rounded to the dtype for the next products: with LP_F16
+ *                                                  they have to stay below 65504, scale a loss accordingly)
  *   dx  = dzg Wg + dzu Wu   [B][ni]   (one sum, rounded once)
  *   dWg = dzg^T x,  dWu = dzu^T x   [no][ni]
  * dx, dWg, dWu nullable: not wanted. Outputs must not alias inputs. */
@@ -504,7 +505,7 @@ int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, 
  *   m' = mu m + g,   v = m' (nesterov: g + mu m'),   X = v / (|v| + eps), |v| the root of the sum of squares,
  *   `steps` times   X <- a X + (b A + c A^2) X,  A = X X^T,
  *   W  = alpha X + beta r,
- * each matrix by itself. The iteration maps each singular value s of X to a s + b s^3 + c s^5 and keeps the
+ * each matrix by itself (one that holds a NaN or an infinity becomes NaN). The iteration maps each singular value s of X to a s + b s^3 + c s^5 and keeps the
  * singular vectors: with a, b, c = 3.4445, -4.7750, 2.0315 five steps bring those above 0.003 to between 0.7 and
  * 1.2, with 15/8, -10/8, 3/8 those near one converge to one.
  * fp32: the products' operands X, A and b A + c A^2 are kept as sums of two f16 values each (2^-22 relative).

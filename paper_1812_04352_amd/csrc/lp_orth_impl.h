@@ -382,12 +382,18 @@ template <typename TI, int KB>
 hipError_t small_t(const OrthArgs& a, hipStream_t st) {
   const double up = ldexp(1.0, (int)lround(0.5 * log2((double)a.no * a.ni)));
   const SmallArgs s{a.no, a.ni, a.steps, (float)a.a, (float)a.b, (float)a.c, (float)a.alpha, (float)a.beta, a.eps, up};
-  const TI *g = (const TI*)a.g, *r = (const TI*)a.r;
-  if (a.no > a.ni)
-    k_small<TI, KB, true><<<(unsigned)a.N, 256, 0, st>>>({g, a.m, a.mo, (float)a.mu, a.nesterov}, r, (TI*)a.W, s);
-  else
-    k_small<TI, KB, false><<<(unsigned)a.N, 256, 0, st>>>({g, a.m, a.mo, (float)a.mu, a.nesterov}, r, (TI*)a.W, s);
-  return hipGetLastError();
+  constexpr int MOST = 1 << 22;  // workgroups a launch (2^32 threads are too many)
+  for (int z0 = 0; z0 < a.N; z0 += MOST) {
+    const size_t from = (size_t)z0 * a.no * a.ni;
+    const unsigned grid = (unsigned)std::min(MOST, a.N - z0);
+    const Momentum<TI, 4> u{(const TI*)a.g + from, a.m ? a.m + from : nullptr, a.mo ? a.mo + from : nullptr, (float)a.mu, a.nesterov};
+    const TI* r = a.r ? (const TI*)a.r + from : nullptr;
+    if (a.no > a.ni) k_small<TI, KB, true><<<grid, 256, 0, st>>>(u, r, (TI*)a.W + from, s);
+    else k_small<TI, KB, false><<<grid, 256, 0, st>>>(u, r, (TI*)a.W + from, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // ---------------------------------------------------------------- products
