@@ -15,8 +15,8 @@
 // small singular values do, by a factor a a step: O is off by 1.2e-3 to 3e-3 of its norm for noise and noise with
 // a few strong directions, by 4e-2 (bf16: 0.3) where four directions exceed the noise a hundredfold.
 // Bound by the products: steps (3 n^2 k + n^3) operations, n the short and k the long side: 4096 x 4096 bf16 1514 us (0.91
-// PFLOP/s of those; a symmetric product 98 us, the other one 142), 2048 of 220 x 220 f32 4439 us (98 TFLOP/s: the
-// seven stages of a tile are short beside its first loads and its epilogue).
+// PFLOP/s of those; a symmetric product 98 us, the other one 142), 2048 of 220 x 220 f32 4439 us (98 TFLOP/s:
+// memory, 4.3 to 6.2 TB/s, since X, A and P pass through it for every product).
 #pragma once
 
 #include <math.h>

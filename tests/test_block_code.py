@@ -50,11 +50,11 @@ def test_written_out_reads_of_a_first_lane_wait(code, u):
     """The compiler does not see their hazards: a vector register may be read a wait state after a vector instruction
     wrote it, and the scalar that they write five later."""
     seen = 0
-    for text in re.findall(r";APP\n(.*?);NO_APP", code[u][0], re.S):
+    for text in re.findall(r"#ASMSTART\n(.*?);;#ASMEND", code[u][0], re.S):
         if "v_readfirstlane" not in text:
             continue
         seen += 1
-        names = [x.split()[:2] for x in text.replace(";;", "\n").split("\n") if x.split()]
+        names = [x.split()[:2] for x in text.split("\n") if x.split()]
         assert [n[0] for n in names] == ["s_nop", "v_readfirstlane_b32", "v_readfirstlane_b32", "s_nop"], text
         assert int(names[0][1]) >= 1 and int(names[3][1]) >= 4, text
     assert seen >= 10
