@@ -77,8 +77,12 @@ def build_sanitized(verbose: bool = True) -> str:
     """Build _build/liblp_san.so: the library with its host logic (argument
     checks, workspace layout, MGRIT schedule) compiled with AddressSanitizer and
     UndefinedBehaviorSanitizer; the kernel translation units are the ordinary
-    objects (built first if missing)."""
+    objects (built first if missing). A library newer than every source is taken as it is."""
     os.makedirs(os.path.join(OBJ, "san"), exist_ok=True)
+    include = os.path.join(ROOT, "include")
+    files = [__file__] + [os.path.join(d, f) for d in (CSRC, include) for f in os.listdir(d)]
+    if os.path.exists(SAN_OUT) and os.path.getmtime(SAN_OUT) > max(os.path.getmtime(f) for f in files):
+        return SAN_OUT
     with cf.ThreadPoolExecutor(max(1, min(6, os.cpu_count() or 1))) as ex:
         objs = list(ex.map(_sanitized_object, SOURCES))
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-Xarch_host", "-fsanitize=address",
