@@ -10,8 +10,7 @@
 //   A and P = b A + c A^2 are symmetric: only tiles on and below the diagonal are formed, and stored on both sides of
 //   it. a X is added in fp32 in the last product's epilogue, that of the last step updates W.
 // 16-bit gradients: X, A and P are kept in f16 whatever the gradient's type is. No singular value exceeds 1.3 or
-// so, so that A and P are in range, and X is kept times 2^shift, about the root of the long side, which brings
-// its values to the size of 1: f16 then rounds eight times finer than bf16 does. Rounding errors grow like the
+// so, so that A and P are in range: f16 then rounds eight times finer than bf16 does. Rounding errors grow like the
 // small singular values do, by a factor a a step: O is off by 1.2e-3 to 3e-3 of its norm for noise and noise with
 // a few strong directions, by 4e-2 (bf16: 0.3) where four directions exceed the noise a hundredfold.
 // Bound by the products: steps (3 n^2 k + n^3) operations, n the short and k the long side: 4096 x 4096 bf16 1514 us (0.91
@@ -35,8 +34,11 @@ using mm::f32x4;
 using mm::GVec;
 using mm::Place;
 
-constexpr float A_UP = 256.f;     // A and P are kept times this, X times 2^shift: small values stay normal f16 numbers
-constexpr int MOST_SHIFT = 13;  // (X's values are at most 1.3 2^13)
+// A and P are kept times A_UP, X times X_UP: as large as f16 holds where singular values stay below 3 (X 49152, P about
+// 53000), so that what is small beside a matrix's largest values keeps its bits. (X times the root of n k, which
+// brings the values of noise to 1: where a row, a column or a value of 220 x 220 f32 carries the norm, O was off by
+// 7e-6 to 1.1e-5 of its norm, now by 3e-7 to 1.4e-6.)
+constexpr float A_UP = 256.f, X_UP = 16384.f;
 
 // ---------------------------------------------------------------- v, its norm, and X
 
@@ -130,7 +132,7 @@ __device__ __forceinline__ void put_values(T* row, int c, const float (&v)[8]) {
   }
 }
 
-// X = v 2^shift / (|v| + eps) in rows of ld values, zeros behind the ni that count (grid y: the matrix)
+// X = v up / (|v| + eps) in rows of ld values, zeros behind the ni that count (grid y: the matrix)
 template <typename TI, typename T>
 __global__ __launch_bounds__(256) void k_scale(Momentum<TI, 8> u, int no, int ni, int ld, const double* part, int parts, double eps,
                                                double up, T* X) {
@@ -668,8 +670,7 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
   const bool tall = a.no > a.ni;
   const int n = std::min(a.no, a.ni), k = std::max(a.no, a.ni), ld = l.ld, lda = l.lda;
   const size_t size = (size_t)a.no * a.ni, sx = (size_t)a.no * ld, sA = (size_t)n * lda;
-  const int shift = std::min((int)lround(0.5 * log2((double)n * k)), MOST_SHIFT);
-  const float down = ldexpf(1.f, -shift);
+  constexpr float down = 1.f / X_UP;
   for (int z0 = 0; z0 < a.N; z0 += l.chunk) {
     const int batch = std::min(l.chunk, a.N - z0);
     const size_t from = z0 * size;
@@ -677,7 +678,7 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
     float* mo = a.mo ? a.mo + from : nullptr;
     const unsigned gx = (unsigned)std::min<size_t>((sx + 4095) / 4096, 2048);
     k_momentum<TI><<<dim3((unsigned)l.parts, (unsigned)batch), 256, 0, st>>>({g, a.m ? a.m + from : nullptr, mo, (float)a.mu, a.nesterov}, size, norms);
-    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>({g, nullptr, mo, (float)a.mu, a.nesterov}, a.no, a.ni, ld, norms, l.parts, a.eps, ldexp(1.0, shift), X[0]);
+    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>({g, nullptr, mo, (float)a.mu, a.nesterov}, a.no, a.ni, ld, norms, l.parts, a.eps, X_UP, X[0]);
     hipError_t e = hipGetLastError();
     for (int s = 0; s < a.steps && e == hipSuccess; ++s) {
       const T* x = X[s & 1];

@@ -250,3 +250,48 @@ class Orth:
         torch.cuda.synchronize()
         assert T.guarded(wf, W.numel())
         return W
+
+
+def two_parts(t, up):
+    """t times up as the sum of two f16 values."""
+    f = (t * up).float()
+    h = f.half()
+    return (h.double() + (f - h.float()).half().double()) / up
+
+
+def iterate_kept(v, steps, coeffs, eps, dtype, noise=E32, seed=0):
+    """The iteration in 64 bits with what the kernels round. Products' operands: X times 2^14 (of matrices of at most
+    64 x 256, about the root of their size), A and b A + c A^2 times 2^8, to two f16 parts (fp32, and those small
+    matrices in every type) or one. The X of a X is fp32 for small matrices. Every product is off by a step of fp32 of its row's and column's norms."""
+    a, b, c = coeffs
+    gen = torch.Generator(device="cpu").manual_seed(seed)
+    n, k = sorted(v.shape[1:])
+    small = n <= 64 and k <= 256
+    two = dtype == "f32" or small
+    up = 2.0 ** round(0.5 * math.log2(n * k)) if small else 2.0 ** 14
+    keep = two_parts if two else lambda t, f: (t * f).half().double() / f
+
+    def product(P, Q):
+        size = torch.linalg.vector_norm(P, dim=2)[:, :, None] * torch.linalg.vector_norm(Q, dim=1)[:, None, :]
+        u = 2 * torch.rand(size.shape, generator=gen, dtype=torch.float64).to(v.device) - 1
+        return torch.matmul(P, Q.contiguous()) + noise * u * size
+
+    X = v / (torch.linalg.vector_norm(v, dim=(1, 2), keepdim=True) + eps)
+    tall = v.shape[1] > v.shape[2]
+    X = X.transpose(1, 2).contiguous() if tall else X
+    for s in range(steps):
+        op = keep(X, up)
+        A = keep(product(op, op.transpose(1, 2)), 2.0 ** 8)
+        P = keep(b * A + c * product(A, A), 2.0 ** 8)
+        X = a * (X if small else op) + product(P, op)
+    return X.transpose(1, 2) if tall else X
+
+
+def orth_precise(W, r, O, E, dtype, what):
+    """W = O + r, r within a step of -O: W's own rounding is one of a difference, and what W and r leave of O is off
+    by no more than four times what the kernels' roundings cost in 64 bits (E: O with those), in every matrix's norm."""
+    off = W.to(O.device).double() - r.to(O.device).double() - O
+    own = T.half_step(dtype) * (O + r.to(O.device).double()).abs() + 3 * E32 * (O.abs() + r.to(O.device).double().abs()) + T.tiny(dtype)
+    norm = lambda t: torch.linalg.vector_norm(t, dim=(1, 2))
+    most = 4 * norm(E - O) + norm(own)
+    assert (norm(off) <= most).all(), (what, (norm(off) / norm(O)).tolist()[:4], (most / norm(O)).tolist()[:4])
