@@ -508,12 +508,11 @@ int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, 
  * each matrix by itself (one that holds a NaN or an infinity becomes NaN). The iteration maps each singular value s of X to a s + b s^3 + c s^5 and keeps the
  * singular vectors: with a, b, c = 3.4445, -4.7750, 2.0315 five steps bring those above 0.003 to between 0.7 and
  * 1.2, with 15/8, -10/8, 3/8 those near one converge to one.
- * fp32: the products' operands X, A and b A + c A^2 are kept as sums of two f16 values each (2^-22 relative).
- * 16-bit types: they are rounded to f16, or of matrices of at most 64 x 256 kept as such sums too. Powers of two keep
- * them in range, for which a, b, c have to keep singular values below about 3. A rounding error grows like a
- * small singular value does, by about a factor a a step: with the first coefficients and five steps X is off
- * by 1e-3 to 3e-3 of its norm on noise (fp32: 3e-6), more where a few directions exceed the others a
- * hundredfold (4e-2; 1e-4). */
+ * The products' operands X, A and b A + c A^2 are kept as sums of two f16 values each (2^-22 relative) with LP_F32 and
+ * for matrices of at most 64 x 256 of every type, else they are rounded to f16; what that rounds off X is kept for
+ * the sum a X + .. alone. Powers of two bring them to the top of f16's range, for which a, b, c have to keep singular
+ * values below about 3. With the first coefficients and five steps X is off by 4e-4 to 2e-3 of its norm by single f16
+ * values, by 3e-7 to 3e-6 by sums of two (1e-5 to 2e-5 where a few directions exceed the others a hundredfold and more). */
 typedef struct {
   int32_t abi_version;   /* must equal LP_ABI_VERSION */
   int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16: g, r and W; m is fp32 */
@@ -526,8 +525,8 @@ typedef struct {
   double mu;             /* finite in fp32 */
 } lp_orth;
 
-/* Workspace bytes of lp_orth_update; 0 for an invalid update. It holds X twice, A and b A + c A^2 of as many
- * matrices as 1 GiB holds (at least one), and the partial sums of split products. */
+/* Workspace bytes of lp_orth_update; 0 for an invalid update. It holds X twice (16-bit types: and what it
+ * rounds off), A and b A + c A^2 of as many matrices as 1 GiB holds (at least one), and the partial sums of split products. */
 size_t lp_orth_workspace_bytes(const lp_orth* orth);
 
 /* The update. g, r, W [N][no][ni]; m, mo [N][no][ni] fp32: m' goes to mo, which may be m. Without mo (m NULL

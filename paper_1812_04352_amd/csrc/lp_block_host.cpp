@@ -180,7 +180,7 @@ OrthLayout orth_layout(int dtype, int N, int no, int ni) {
   l.ld = (mm::padded(e, ni) + 7) / 8 * 8;
   l.lda = (mm::padded(e, n) + 7) / 8 * 8;
   const size_t x = (size_t)no * l.ld * e, a = (size_t)n * l.lda * e;
-  l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a)), 1), 16384));
+  l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a) + (duo ? 0 : x)), 1), 16384));
   l.parts = (int)std::min<size_t>(((size_t)no * ni + 4095) / 4096, 2048);
   l.gram = no > ni ? mm::plan_of(e, n, n, k, l.chunk, true, duo) : sym_plan(e, n, k, l.chunk, duo);
   l.poly = sym_plan(e, n, n, l.chunk, duo);
@@ -191,6 +191,7 @@ OrthLayout orth_layout(int dtype, int N, int no, int ni) {
   Parts p;
   l.norms = p.take((size_t)l.chunk * l.parts * 8);
   for (size_t& at : l.X) at = p.take(l.chunk * x);
+  if (!duo) l.lo = p.take(l.chunk * x);
   l.A = p.take(l.chunk * a);
   l.P = p.take(l.chunk * a);
   l.part = p.take(std::max({part(l.gram, true), part(l.poly, true), part(l.next, false)}));

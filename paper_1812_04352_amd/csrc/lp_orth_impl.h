@@ -9,10 +9,17 @@
 // noise (fp32 products: 2e-6). aX is added to the product in fp32.
 //   A and P = b A + c A^2 are symmetric: only tiles on and below the diagonal are formed, and stored on both sides of
 //   it. a X is added in fp32 in the last product's epilogue, that of the last step updates W.
-// 16-bit gradients: X, A and P are kept in f16 whatever the gradient's type is. No singular value exceeds 1.3 or
-// so, so that A and P are in range: f16 then rounds eight times finer than bf16 does. Rounding errors grow like the
-// small singular values do, by a factor a a step: O is off by 1.2e-3 to 3e-3 of its norm for noise and noise with
-// a few strong directions, by 4e-2 (bf16: 0.3) where four directions exceed the noise a hundredfold.
+// 16-bit gradients: the products' operands X, A and P are in f16 whatever the gradient's type is. No singular value
+// exceeds 1.3 or so, so that A and P are in range: f16 then rounds eight times finer than bf16 does. What rounding costs
+// is kept down in two ways.
+//   A rounding error of X grows like the small singular values do, by a factor a a step, where it is added to them, in
+//   a X: the X of a X keeps what f16 rounds off in an array of its own.
+//   In the last steps, where X is nearly orthogonal, P is nearly (b + c) I and a X + P X a small difference: they form
+//   (a + b + c) X + (P - (b + c) I) X, whose product is small and its rounding with it. (While singular values still
+//   differ much it would mix strong directions into small ones: the last two steps.)
+// O is off by 4e-4 to 1.1e-3 of its norm for noise, a few strong directions or singular values down to a thousandth
+// (by X in f16 alone and P as it is 1.4e-3 to 1.5e-2), by 1.3e-3 where four directions exceed the noise a hundredfold
+// (4e-2), by 2e-3 where single values do. It takes 6 % more time.
 // Bound by the products: steps (3 n^2 k + n^3) operations, n the short and k the long side: 4096 x 4096 bf16 1514 us (0.91
 // PFLOP/s of those; a symmetric product 98 us, the other one 142), 2048 of 220 x 220 f32 4439 us (98 TFLOP/s:
 // memory, 4.3 to 6.2 TB/s, since X, A and P pass through it for every product).
@@ -119,6 +126,9 @@ __global__ __launch_bounds__(256) void k_momentum(Momentum<TI, VV> u, size_t siz
   if (threadIdx.x == 0) part[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = ((sh[0] + sh[1]) + sh[2]) + sh[3];
 }
 
+// what f16 rounds off
+__device__ __forceinline__ float rest(float v) { return v - (float)(mm::f16)v; }
+
 template <typename T>
 __device__ __forceinline__ void put_values(T* row, int c, const float (&v)[8]) {
   if constexpr (std::is_same<T, mm::Duo>::value) {
@@ -132,10 +142,11 @@ __device__ __forceinline__ void put_values(T* row, int c, const float (&v)[8]) {
   }
 }
 
-// X = v up / (|v| + eps) in rows of ld values, zeros behind the ni that count (grid y: the matrix)
+// X = v up / (|v| + eps) in rows of ld values, zeros behind the ni that count (grid y: the matrix); lo (16-bit T): what it
+// rounds off
 template <typename TI, typename T>
 __global__ __launch_bounds__(256) void k_scale(Momentum<TI, 8> u, int no, int ni, int ld, const double* part, int parts, double eps,
-                                               double up, T* X) {
+                                               double up, T* X, T* lo) {
   __shared__ double sh;
   if (threadIdx.x < 64) {
     const double* p = part + (size_t)blockIdx.y * parts;
@@ -161,6 +172,11 @@ __global__ __launch_bounds__(256) void k_scale(Momentum<TI, 8> u, int no, int ni
       for (int k = 0; k < 8; ++k) v[k] = k < n ? (float)((double)v[k] * scale) : 0.f;
     }
     put_values(X + r * ld, c, v);
+    if constexpr (std::is_same<T, mm::f16>::value) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = rest(v[k]);
+      put_values(lo + ((size_t)blockIdx.y * no + r) * ld, c, v);
+    }
   }
 }
 
@@ -435,7 +451,7 @@ __device__ __forceinline__ void put_mirror(mm::Duo* a, long ld, const Place& c, 
   IO::flush(a, ld, c.nw + 32 * j, c.N, c.mw + 32 * i, c.lane, buf);
 }
 
-// f D + b A of a symmetric D, rows of ld values (A nullable)
+// f D + b A + d I of a symmetric D, rows of ld values (A nullable)
 template <typename T>
 struct EpSym {
   struct Args {
@@ -443,7 +459,7 @@ struct EpSym {
     T* out;
     int ld;
     size_t stride;  // of a matrix
-    float f, b;
+    float f, b, d;
   };
   static __device__ __forceinline__ Args at(Args a, int z) {
     if (a.A) a.A += z * a.stride;
@@ -465,52 +481,77 @@ struct EpSym {
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             v[q][k] = c.row(i) < c.M && (WHOLE || c.feature(j, q) + k < c.lim) ? a.f * acc[i][j][4 * q + k] + a.b * v[q][k] : 0.f;
+        if constexpr (std::is_same<T, mm::f16>::value) {
+          if (a.d != 0.f && c.mt == c.nt) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[q][k] += c.row(i) == c.feature(j, q) + k && c.row(i) < c.M ? a.d : 0.f;
+          }
+        }
         mm::put_rows<WHOLE>(a.out, a.ld, c.upto(a.ld), c, i, j, buf, v);
         if (c.mt != c.nt) put_mirror(a.out, a.ld, c, i, j, buf, v);
       }
   }
 };
 
-// a X + d D
+// a X + d D. f16: X is the sum of X and lo, and lo becomes what f16 rounds off the result.
 template <typename T>
 struct EpNext {
+  static constexpr bool LO = std::is_same<T, mm::f16>::value;
   struct Args {
     const T* X;
     T* out;
     int ld;
     size_t stride;
     float a, d;
+    T* lo;
   };
   static __device__ __forceinline__ Args at(Args a, int z) {
     a.X += z * a.stride;
     a.out += z * a.stride;
+    if constexpr (LO) a.lo += z * a.stride;
     return a;
   }
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     unsigned char* buf = mm::wave_lds(lds, c, WGN);
     mm::Rows<WHOLE, T, FM, FN> X(a.X, a.ld, c);
+    mm::Rows<WHOLE, T, FM, FN> lo(LO ? a.lo : nullptr, a.ld, c);
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        f32x4 v[4];
+        f32x4 v[4], w[4];
         X.get(c, i, j, buf, v);
+        if constexpr (LO) {
+          lo.get(c, i, j, buf, w);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] += w[q];
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             v[q][k] = WHOLE || c.feature(j, q) + k < c.lim ? a.a * v[q][k] + a.d * acc[i][j][4 * q + k] : 0.f;
         mm::put_rows<WHOLE>(a.out, a.ld, c.upto(a.ld), c, i, j, buf, v);
+        if constexpr (LO) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[q][k] = rest(v[q][k]);
+          mm::put_rows<WHOLE>(a.lo, a.ld, c.upto(a.ld), c, i, j, buf, v);
+        }
       }
   }
 };
 
-// W = alpha (a X + d D) + beta r, rows of N values (r nullable)
+// W = alpha (a X + d D) + beta r, rows of N values (r nullable). f16: X is the sum of X and lo.
 template <typename T, typename TO>
 struct EpUpdate {
+  static constexpr bool LO = std::is_same<T, mm::f16>::value;
   struct Args {
-    const T* X;
+    const T *X, *lo;
     int ld;
     size_t stride;   // of a matrix of X
     const TO* r;
@@ -520,6 +561,7 @@ struct EpUpdate {
   };
   static __device__ __forceinline__ Args at(Args a, int z) {
     a.X += z * a.stride;
+    if constexpr (LO) a.lo += z * a.stride;
     if (a.r) a.r += z * a.wstride;
     a.W += z * a.wstride;
     return a;
@@ -528,6 +570,7 @@ struct EpUpdate {
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     unsigned char* buf = mm::wave_lds(lds, c, WGN);
     mm::Rows<WHOLE, T, FM, FN> X(a.X, a.ld, c);
+    mm::Rows<WHOLE, T, FM, FN> lo(LO ? a.lo : nullptr, a.ld, c);
     mm::Rows<WHOLE, TO, FM, FN, false> r(a.r, c.N, c);
 #pragma unroll
     for (int j = 0; j < FN; ++j)
@@ -535,6 +578,11 @@ struct EpUpdate {
       for (int i = 0; i < FM; ++i) {
         f32x4 v[4], w[4];
         X.get(c, i, j, buf, v);
+        if constexpr (LO) {
+          lo.get(c, i, j, buf, w);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) v[q] += w[q];
+        }
         r.get(c, i, j, buf, w);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = (v[q] * a.a + mm::quad(acc[i][j], q) * a.d) * a.alpha + w[q] * a.beta;
@@ -667,6 +715,8 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
   double* norms = reinterpret_cast<double*>(w + l.norms);
   T* X[2] = {reinterpret_cast<T*>(w + l.X[0]), reinterpret_cast<T*>(w + l.X[1])};
   T *A = reinterpret_cast<T*>(w + l.A), *P = reinterpret_cast<T*>(w + l.P);
+  constexpr bool LO = std::is_same<T, mm::f16>::value;
+  T* lo = LO ? reinterpret_cast<T*>(w + l.lo) : nullptr;
   const bool tall = a.no > a.ni;
   const int n = std::min(a.no, a.ni), k = std::max(a.no, a.ni), ld = l.ld, lda = l.lda;
   const size_t size = (size_t)a.no * a.ni, sx = (size_t)a.no * ld, sA = (size_t)n * lda;
@@ -678,15 +728,18 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
     float* mo = a.mo ? a.mo + from : nullptr;
     const unsigned gx = (unsigned)std::min<size_t>((sx + 4095) / 4096, 2048);
     k_momentum<TI><<<dim3((unsigned)l.parts, (unsigned)batch), 256, 0, st>>>({g, a.m ? a.m + from : nullptr, mo, (float)a.mu, a.nesterov}, size, norms);
-    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>({g, nullptr, mo, (float)a.mu, a.nesterov}, a.no, a.ni, ld, norms, l.parts, a.eps, X_UP, X[0]);
+    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>({g, nullptr, mo, (float)a.mu, a.nesterov}, a.no, a.ni, ld, norms, l.parts, a.eps, X_UP, X[0], lo);
     hipError_t e = hipGetLastError();
     for (int s = 0; s < a.steps && e == hipSuccess; ++s) {
       const T* x = X[s & 1];
       const auto product = [&](const mm::Prob& p, size_t sa, size_t sb, const mm::Plan& pl) {
         return Product{p, sa * sizeof(T), sb * sizeof(T), pl, batch, reinterpret_cast<mm::f32x4*>(w + l.part), st};
       };
+      // what goes from P to a (its multiple of I has to be in f16's range too: far from it)
+      const double move = LO && s + 2 >= a.steps && fabs(a.b + a.c) <= 8 ? a.b + a.c : 0.0;
       // A, the scale of X taken out; P = b A + c A^2
-      const typename EpSym<T>::Args ea{nullptr, A, lda, sA, down * down * A_UP, 0.f}, ep{A, P, lda, sA, (float)a.c / A_UP, (float)a.b};
+      const typename EpSym<T>::Args ea{nullptr, A, lda, sA, down * down * A_UP, 0.f, 0.f},
+          ep{A, P, lda, sA, (float)a.c / A_UP, (float)a.b, (float)-move * A_UP};
       const Product gram = product(prob(x, ld, x, ld, n, n, k), sx, sx, l.gram);
       e = tall ? launch_product<T, true, true, true, EpSym<T>>(gram, ea) : launch_product<T, false, false, true, EpSym<T>>(gram, ea);
       if (e != hipSuccess) break;
@@ -695,11 +748,11 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
       const Product next = tall ? product(prob(x, ld, P, lda, a.no, a.ni, n), sx, sA, l.next)
                                 : product(prob(P, lda, x, ld, a.no, a.ni, n), sA, sx, l.next);
       if (s + 1 < a.steps) {
-        const typename EpNext<T>::Args en{x, X[~s & 1], ld, sx, (float)a.a, 1.f / A_UP};
+        const typename EpNext<T>::Args en{x, X[~s & 1], ld, sx, (float)(a.a + move), 1.f / A_UP, lo};
         e = tall ? launch_product<T, false, false, false, EpNext<T>>(next, en) : launch_product<T, false, true, false, EpNext<T>>(next, en);
       } else {
-        const typename EpUpdate<T, TI>::Args eu{x, ld, sx, a.r ? (const TI*)a.r + from : nullptr, (TI*)a.W + from, size,
-                                                (float)a.a, 1.f / A_UP, (float)(a.alpha * down), (float)a.beta};
+        const typename EpUpdate<T, TI>::Args eu{x, lo, ld, sx, a.r ? (const TI*)a.r + from : nullptr, (TI*)a.W + from, size,
+                                                (float)(a.a + move), 1.f / A_UP, (float)(a.alpha * down), (float)a.beta};
         e = tall ? launch_product<T, false, false, false, EpUpdate<T, TI>>(next, eu)
                  : launch_product<T, false, true, false, EpUpdate<T, TI>>(next, eu);
       }

@@ -262,7 +262,9 @@ def two_parts(t, up):
 def iterate_kept(v, steps, coeffs, eps, dtype, noise=E32, seed=0):
     """The iteration in 64 bits with what the kernels round. Products' operands: X times 2^14 (of matrices of at most
     64 x 256, about the root of their size), A and b A + c A^2 times 2^8, to two f16 parts (fp32, and those small
-    matrices in every type) or one. The X of a X is fp32 for small matrices. Every product is off by a step of fp32 of its row's and column's norms."""
+    matrices in every type) or one, of which b A + c A^2 without (b + c) I in the last two steps (where |b + c| is at
+    most 8). The X of a X: fp32 (small matrices), else two parts too. Every product is off by a step of fp32 of its
+    row's and column's norms."""
     a, b, c = coeffs
     gen = torch.Generator(device="cpu").manual_seed(seed)
     n, k = sorted(v.shape[1:])
@@ -270,6 +272,7 @@ def iterate_kept(v, steps, coeffs, eps, dtype, noise=E32, seed=0):
     two = dtype == "f32" or small
     up = 2.0 ** round(0.5 * math.log2(n * k)) if small else 2.0 ** 14
     keep = two_parts if two else lambda t, f: (t * f).half().double() / f
+    eye = torch.eye(n, dtype=torch.float64, device=v.device)
 
     def product(P, Q):
         size = torch.linalg.vector_norm(P, dim=2)[:, :, None] * torch.linalg.vector_norm(Q, dim=1)[:, None, :]
@@ -280,10 +283,11 @@ def iterate_kept(v, steps, coeffs, eps, dtype, noise=E32, seed=0):
     tall = v.shape[1] > v.shape[2]
     X = X.transpose(1, 2).contiguous() if tall else X
     for s in range(steps):
+        move = 0.0 if two or s + 2 < steps or abs(b + c) > 8 else b + c
         op = keep(X, up)
         A = keep(product(op, op.transpose(1, 2)), 2.0 ** 8)
-        P = keep(b * A + c * product(A, A), 2.0 ** 8)
-        X = a * (X if small else op) + product(P, op)
+        P = keep(b * A + c * product(A, A) - move * eye, 2.0 ** 8)
+        X = (a + move) * (X if small else two_parts(X, up)) + product(P, op)
     return X.transpose(1, 2) if tall else X
 
 
