@@ -446,11 +446,11 @@ typedef struct {
   int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16 */
   int32_t B;             /* rows, >= 0 (0: nothing to do; weight gradients are zero) */
   int32_t q;             /* features of a row, >= 1 */
-  double eps;            /* >= 0, finite in fp32 (0: a row of equal values gives NaN) */
+  double eps;            /* >= 0, finite in fp32 (0: a row of equal values has no norm, NaN as a rule) */
 } lp_norm;
 
-/* gamma (1 without it) and beta (0) nullable. y may be x. Statistics are fp32: the sum of (x - m)^2 has to
- * stay in its range. An infinity or a NaN makes its own row NaN. */
+/* gamma (1 without it) and beta (0) nullable. y may be x. Statistics are fp32, about the row's mean
+ * however far it lies from 0: the sum of (x - m)^2 has to stay in its range. An infinity or a NaN makes its own row NaN. */
 int32_t lp_norm_forward(const lp_norm* norm, const void* x, const void* gamma, const void* beta, void* y, void* stream);
 
 /* Workspace bytes of lp_norm_backward (partial sums of the weights' gradients); 0 for an invalid norm. */

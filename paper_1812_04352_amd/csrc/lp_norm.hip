@@ -5,10 +5,15 @@
 //   backward:  with g = gamma dy, xh = (x - mean) r, r = 1 / sqrt(var + eps), over a row's q features
 //                dx = r (g - mean g - xh mean(g xh)) (+ dr),  dgamma = sum_rows dy xh,  dbeta = sum_rows dy
 //              one read of x, dy (and dr), one write of dx: the statistics are formed again from the row at
-//              hand, in two rounds of exchanges (the sums of x and g, then of (x - mean)^2 and g (x - mean)).
+//              hand, in two rounds of exchanges (the sums of x and g, then of x - mean, its square and its product
+//              with g).
 //              A thread keeps the same features of all its rows, so it sums their dgamma and dbeta in
 //              registers; a workgroup adds its groups' in order and writes one row of partial sums, which a
 //              second kernel adds in fp64 (a single workgroup writes the gradients themselves).
+//   The first mean is rounded, and so is the sum that it comes from: a row's x - mean does not sum to 0, but to what that
+//   mean is off by. Its mean is taken off x - mean, and the square of it off the mean square, so that a row whose mean
+//   exceeds its spread by far loses nothing, and equal values leave 0 (without that a row of 223 values 3300 was off by
+//   hundredths).
 // Bound by memory: 8192 x 4096 bf16 25 us forward (5.3 TB/s), 65 us back with dr (4.1; 62 in the kernel and 4.6 in the sum of
 // 256 rows of partial sums, one of each workgroup, of which there is one a CU; without the next rows requested ahead and with
 // sums by LDS exchanges 97). Rows that no group can hold are read again for every pass.
@@ -110,44 +115,57 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// Sums of two values over a group of TPR threads, the same in all of them. Groups wider than a wave
+// Sums of up to three values over a group of TPR threads, the same in all of them. Groups wider than a wave
 // exchange through the LDS: `at` alternates between its two halves, so that one barrier a sum is enough
 // (a wave that writes a half again has passed the barrier behind which all have read it).
 template <int TPR, int NT>
 struct GroupSum {
   static constexpr int W = TPR / 64;  // waves of a group
-  float2 (*lds)[NT / 64];
+  typedef float Lds[2][NT / 64][3];
+  Lds& lds;
   int at = 0;
-  __device__ __forceinline__ float2 operator()(float2 s) {
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&s)[N]) {
     if constexpr (TPR < 64) {
 #pragma unroll
-      for (int o = TPR / 2; o > 0; o >>= 1) {
-        s.x += __shfl_xor(s.x, o, 64);
-        s.y += __shfl_xor(s.y, o, 64);
-      }
+      for (int o = TPR / 2; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] += __shfl_xor(s[i], o, 64);
     } else {
-      s.x = wave_sum(s.x);
-      s.y = wave_sum(s.y);
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
     }
     if constexpr (TPR > 64) {
       const int wave = threadIdx.x >> 6;
-      if ((threadIdx.x & 63) == 0) lds[at][wave] = s;
-      __syncthreads();
-      const float2* g = lds[at] + wave / W * W;
-      s = g[0];
+      if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-      for (int w = 1; w < W; ++w) s.x += g[w].x, s.y += g[w].y;
+        for (int i = 0; i < N; ++i) lds[at][wave][i] = s[i];
+      }
+      __syncthreads();
+      const float(*g)[3] = lds[at] + wave / W * W;
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = g[0][i];
+      constexpr int AT_ONCE = N == 3 && W > 8 ? 3 : 15;  // (the widest groups lack the registers for three values of all)
+#pragma unroll AT_ONCE
+      for (int w = 1; w < W; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] += g[w][i];
       at ^= 1;
     }
-    return s;
   }
 };
+
+// The mean square of x - mean less the square of its mean, `off` (never below 0; a NaN stays one)
+__device__ __forceinline__ float variance(float square, float off) {
+  const float v = square - off * off;
+  return v < 0.f ? 0.f : v;
+}
 
 template <typename T, int TPR, int C, int NT>
 __global__ __launch_bounds__(NT) void k_forward(const T* x, const T* gamma, const T* beta, T* y, int B, int q, float eps) {
   typedef Piece<T, TPR, C> P;
   constexpr int V = P::V, G = NT / TPR;
-  __shared__ float2 lds[2][NT / 64];
+  __shared__ typename GroupSum<TPR, NT>::Lds lds;
   GroupSum<TPR, NT> sum{lds};
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
   P ga, be;
@@ -159,28 +177,31 @@ __global__ __launch_bounds__(NT) void k_forward(const T* x, const T* gamma, cons
     P p;
     p.load(x + min(r, (long)B - 1) * q, t, q);
     p.cut(t, q);
-    float2 s = {0.f, 0.f};
+    float s1[1] = {0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int k = 0; k < V; ++k) s.x += (float)p.v[c][k];
-    const float mean = sum(s).x / n;
-    s = {0.f, 0.f};
+      for (int k = 0; k < V; ++k) s1[0] += (float)p.v[c][k];
+    sum(s1);
+    const float mean = s1[0] / n;
+    float s2[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const float d = P::first(t, c) + k < q ? (float)p.v[c][k] - mean : 0.f;
-        s.x = fmaf(d, d, s.x);
+        s2[0] = fmaf(d, d, s2[0]);
+        s2[1] += d;
       }
-    const float rstd = 1.f / sqrtf(sum(s).x / n + eps);
+    sum(s2);
+    const float off = s2[1] / n, rstd = 1.f / sqrtf(variance(s2[0] / n, off) + eps);
     if (r >= B) continue;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       float f[V];
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        f[k] = ((float)p.v[c][k] - mean) * rstd;
+        f[k] = ((float)p.v[c][k] - mean - off) * rstd;
         if (gamma) f[k] *= (float)ga.v[c][k];
         if (beta) f[k] += (float)be.v[c][k];
       }
@@ -241,7 +262,7 @@ __global__ __launch_bounds__(threads_back(TPR)) void k_backward(BackArgs a) {
   typedef Piece<T, TPR, C> P;
   constexpr int V = P::V, NT = threads_back(TPR), G = NT / TPR;
   constexpr bool AHEAD = C == 1;
-  __shared__ float2 lds[2][NT / 64];
+  __shared__ typename GroupSum<TPR, NT>::Lds lds;
   __shared__ __attribute__((aligned(16))) float sums[G == 1 ? 4 : NT * C * V];
   GroupSum<TPR, NT> sum{lds};
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, q = FULL ? TPR * C * V : a.q;
@@ -278,28 +299,29 @@ __global__ __launch_bounds__(threads_back(TPR)) void k_backward(BackArgs a) {
     if constexpr (!FULL) {
       if (dr) now.r.cut(t, q);
     }
-    float2 s = {0.f, 0.f};
+    float s1[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
-        s.x += (float)now.x.v[c][k];
-        s.y = fmaf((float)now.d.v[c][k], (float)ga.v[c][k], s.y);
+        s1[0] += (float)now.x.v[c][k];
+        s1[1] = fmaf((float)now.d.v[c][k], (float)ga.v[c][k], s1[1]);
       }
-    s = sum(s);
-    const float mean = s.x / n, m1 = s.y / n;
-    s = {0.f, 0.f};
+    sum(s1);
+    const float mean = s1[0] / n, m1 = s1[1] / n;
+    float s2[3] = {0.f, 0.f, 0.f};
     if constexpr (!AHEAD) now.x.forget(), now.d.forget(), ga.forget();
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const float d = FULL || P::first(t, c) + k < q ? (float)now.x.v[c][k] - mean : 0.f;
-        s.x = fmaf(d, d, s.x);
-        s.y = fmaf((float)now.d.v[c][k] * (float)ga.v[c][k], d, s.y);
+        s2[0] = fmaf(d, d, s2[0]);
+        s2[1] += d;
+        s2[2] = fmaf((float)now.d.v[c][k] * (float)ga.v[c][k], d, s2[2]);
       }
-    s = sum(s);
-    const float rstd = 1.f / sqrtf(s.x / n + a.eps), m2 = s.y / n * rstd;
+    sum(s2);
+    const float off = s2[1] / n, rstd = 1.f / sqrtf(variance(s2[0] / n, off) + a.eps), m2 = (s2[2] / n - off * m1) * rstd;
     if constexpr (!AHEAD) now.x.forget(), now.d.forget(), ga.forget();
     if (r < r1) {
 #pragma unroll
@@ -307,7 +329,7 @@ __global__ __launch_bounds__(threads_back(TPR)) void k_backward(BackArgs a) {
         float f[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-          const float dk = (float)now.d.v[c][k], xh = ((float)now.x.v[c][k] - mean) * rstd;
+          const float dk = (float)now.d.v[c][k], xh = ((float)now.x.v[c][k] - mean - off) * rstd;
           f[k] = rstd * (dk * (float)ga.v[c][k] - m1 - xh * m2);
           if (dr) f[k] += (float)now.r.v[c][k];
           dg[c][k] = fmaf(dk, xh, dg[c][k]);
@@ -354,37 +376,46 @@ __global__ __launch_bounds__(1024) void k_sum(const float* part, int rows, int q
 
 // ---- rows that no group holds: every pass reads them again
 
-// mean and 1 / sqrt(var + eps) of a row, and with dy given the means of g and g xh, over a workgroup of 1024
+// A row's statistics: its first mean, what that is off by, 1 / sqrt(var + eps), and with dy the means of g and g xh
+struct LongStats {
+  float mean, off, rstd, m1, m2;
+  __device__ __forceinline__ float xh(float x) const { return (x - mean - off) * rstd; }
+};
+
+// over a workgroup of 1024
 template <typename T>
-__device__ __forceinline__ void long_stats(const T* x, const T* dy, const T* gamma, int q, float eps, GroupSum<1024, 1024>& sum,
-                                           float& mean, float& rstd, float& m1, float& m2) {
+__device__ __forceinline__ LongStats long_stats(const T* x, const T* dy, const T* gamma, int q, float eps, GroupSum<1024, 1024>& sum) {
   const float n = (float)q;
-  float2 s = {0.f, 0.f};
+  LongStats r;
+  float s1[2] = {0.f, 0.f};
   for (int i = threadIdx.x; i < q; i += 1024) {
-    s.x += (float)x[i];
-    if (dy) s.y += (gamma ? (float)gamma[i] : 1.f) * (float)dy[i];
+    s1[0] += (float)x[i];
+    if (dy) s1[1] += (gamma ? (float)gamma[i] : 1.f) * (float)dy[i];
   }
-  s = sum(s);
-  mean = s.x / n, m1 = s.y / n;
-  s = {0.f, 0.f};
+  sum(s1);
+  r.mean = s1[0] / n, r.m1 = s1[1] / n;
+  float s2[3] = {0.f, 0.f, 0.f};
   for (int i = threadIdx.x; i < q; i += 1024) {
-    const float d = (float)x[i] - mean;
-    s.x = fmaf(d, d, s.x);
-    if (dy) s.y = fmaf((gamma ? (float)gamma[i] : 1.f) * (float)dy[i], d, s.y);
+    const float d = (float)x[i] - r.mean;
+    s2[0] = fmaf(d, d, s2[0]);
+    s2[1] += d;
+    if (dy) s2[2] = fmaf((gamma ? (float)gamma[i] : 1.f) * (float)dy[i], d, s2[2]);
   }
-  s = sum(s);
-  rstd = 1.f / sqrtf(s.x / n + eps), m2 = s.y / n * rstd;
+  sum(s2);
+  r.off = s2[1] / n;
+  r.rstd = 1.f / sqrtf(variance(s2[0] / n, r.off) + eps);
+  r.m2 = (s2[2] / n - r.off * r.m1) * r.rstd;
+  return r;
 }
 
 template <typename T>
 __global__ __launch_bounds__(1024) void k_forward_long(const T* x, const T* gamma, const T* beta, T* y, int B, int q, float eps) {
-  __shared__ float2 lds[2][16];
+  __shared__ GroupSum<1024, 1024>::Lds lds;
   GroupSum<1024, 1024> sum{lds};
   for (long r = blockIdx.x; r < B; r += gridDim.x) {
-    float mean, rstd, m1, m2;
-    long_stats<T>(x + r * q, nullptr, nullptr, q, eps, sum, mean, rstd, m1, m2);
+    const LongStats s = long_stats<T>(x + r * q, nullptr, nullptr, q, eps, sum);
     for (int i = threadIdx.x; i < q; i += 1024) {
-      float f = ((float)x[r * q + i] - mean) * rstd;
+      float f = s.xh((float)x[r * q + i]);
       if (gamma) f *= (float)gamma[i];
       if (beta) f += (float)beta[i];
       y[r * q + i] = (T)f;
@@ -392,23 +423,21 @@ __global__ __launch_bounds__(1024) void k_forward_long(const T* x, const T* gamm
   }
 }
 
-// dx, and the statistics of every row (mean, rstd) for the weights' gradients
+// dx, and the statistics of every row (mean, off, rstd) for the weights' gradients
 template <typename T>
-__global__ __launch_bounds__(1024) void k_backward_long(BackArgs a, float2* stats) {
-  __shared__ float2 lds[2][16];
+__global__ __launch_bounds__(1024) void k_backward_long(BackArgs a, float4* stats) {
+  __shared__ GroupSum<1024, 1024>::Lds lds;
   GroupSum<1024, 1024> sum{lds};
   const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = static_cast<const T*>(a.dr);
   const T* gamma = static_cast<const T*>(a.gamma);
   T* dx = static_cast<T*>(a.dx);
   const int q = a.q;
   for (long r = blockIdx.x; r < a.B; r += gridDim.x) {
-    float mean, rstd, m1, m2;
-    long_stats<T>(x + r * q, dy + r * q, gamma, q, a.eps, sum, mean, rstd, m1, m2);
-    if (threadIdx.x == 0) stats[r] = {mean, rstd};
+    const LongStats s = long_stats<T>(x + r * q, dy + r * q, gamma, q, a.eps, sum);
+    if (threadIdx.x == 0) stats[r] = make_float4(s.mean, s.off, s.rstd, 0.f);
     if (!dx) continue;
     for (int i = threadIdx.x; i < q; i += 1024) {
-      const float xh = ((float)x[r * q + i] - mean) * rstd;
-      float f = rstd * ((gamma ? (float)gamma[i] : 1.f) * (float)dy[r * q + i] - m1 - xh * m2);
+      float f = s.rstd * ((gamma ? (float)gamma[i] : 1.f) * (float)dy[r * q + i] - s.m1 - s.xh((float)x[r * q + i]) * s.m2);
       if (dr) f += (float)dr[r * q + i];
       dx[r * q + i] = (T)f;
     }
@@ -417,16 +446,16 @@ __global__ __launch_bounds__(1024) void k_backward_long(BackArgs a, float2* stat
 
 // partial sums of dgamma and dbeta: a thread's feature over a run of rows (grid y)
 template <typename T>
-__global__ __launch_bounds__(256) void k_weights_long(BackArgs a, const float2* stats) {
+__global__ __launch_bounds__(256) void k_weights_long(BackArgs a, const float4* stats) {
   const int i = blockIdx.x * 256 + threadIdx.x, q = a.q;
   if (i >= q) return;
   const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy);
   float dg = 0.f, db = 0.f;
   const long r1 = min((long)a.B, (long)(blockIdx.y + 1) * a.rows);
   for (long r = (long)blockIdx.y * a.rows; r < r1; ++r) {
-    const float2 s = stats[r];
+    const float4 s = stats[r];
     const float d = (float)dy[r * q + i];
-    dg = fmaf(d, ((float)x[r * q + i] - s.x) * s.y, dg);
+    dg = fmaf(d, ((float)x[r * q + i] - s.x - s.y) * s.z, dg);
     db += d;
   }
   float* part = a.part + (size_t)blockIdx.y * 2 * q;
@@ -512,7 +541,7 @@ hipError_t backward_t(const NormArgs& a, hipStream_t st) {
     LP_BACKWARD_GROUPS(LP_CASE)
 #undef LP_CASE
   } else {
-    float2* stats = reinterpret_cast<float2*>(w + l.stats);
+    float4* stats = reinterpret_cast<float4*>(w + l.stats);
     b.part = reinterpret_cast<float*>(w + l.part);
     if (a.B) k_backward_long<T><<<(unsigned)std::min(a.B, 2048), 1024, 0, st>>>(b, stats);
     if (weights) k_weights_long<T><<<dim3((unsigned)mm::ceil_div(a.q, 256), (unsigned)l.groups), 256, 0, st>>>(b, stats);
@@ -534,7 +563,7 @@ NormLayout norm_layout(int dtype, int B, int q) {
     l.rows = norm::backward_rows(norm::threads_back(g.tpr) / g.tpr, B);
   } else {
     l.rows = std::min(2048, std::max(16, mm::ceil_div(B, 1024)));
-    l.stats = ((size_t)B * 8 + 255) / 256 * 256;
+    l.stats = ((size_t)B * 16 + 255) / 256 * 256;
   }
   l.groups = std::max(1, mm::ceil_div(B, l.rows));
   l.part = l.stats;  // (the rows' statistics come first)

@@ -299,3 +299,23 @@ def orth_precise(W, r, O, E, dtype, what):
     norm = lambda t: torch.linalg.vector_norm(t, dim=(1, 2))
     most = 4 * norm(E - O) + norm(own)
     assert (norm(off) <= most).all(), (what, (norm(off) / norm(O)).tolist()[:4], (most / norm(O)).tolist()[:4])
+
+
+def norm_stats_sharp(x, eps):
+    """norm_stats with a bound that does not grow with a row's mean: a first mean is off by D at most, the mean of what it
+    leaves, d + D, is taken off that, and its square off the mean square. (x less the first mean is exact where
+    both are near, else off by half a step of itself.)"""
+    x = x.double()
+    q = x.shape[1]
+    n = 84 + q / 1024
+    mean = x.mean(1, keepdim=True)
+    d = x - mean
+    D = n * E32 * x.abs().mean(1, keepdim=True)
+    left = d.abs() + D
+    ed = (n + 1) * E32 * left.mean(1, keepdim=True) + 2 * E32 * left
+    var = (d * d).mean(1, keepdim=True)
+    ev = (n + 4) * E32 * (left * left).mean(1, keepdim=True) + (2 * d.abs() * ed + ed * ed).mean(1, keepdim=True)
+    rstd = (var + eps) ** -0.5
+    er = rstd * (0.5 * ev / (var + eps) + 4 * E32)
+    xh = d * rstd
+    return xh, (ed * (rstd + er) + d.abs() * er + E32 * xh.abs()), rstd, er, n

@@ -166,3 +166,60 @@ def test_captured(dtype):
             torch.cuda.synchronize()
             for a, b in zip(outs, want):
                 assert torch.equal(a, b)
+
+
+# every way a row is held: lanes of a wave, waves, several pieces a thread, read again for each pass
+WIDTHS = [3, 20, 223, 257, 1111, 3000, 4096, 7001, 9000, 16384, 20001, 70001]
+
+
+@pytest.mark.parametrize("q", WIDTHS)
+def test_rows_of_equal_values(q):
+    """A sum of q equal values is rounded and so is its mean: what it is off by must not pass for a spread."""
+    values = [0.1, 0.7, 3.3, 3.3e3, -1.1e-3, 12345.678]
+    g = torch.Generator().manual_seed(q)
+    x = torch.tensor(values).repeat(5)[:, None].repeat(1, q)
+    gamma, beta = 1 + T.draw(g, (q,), "f32", 0.3), T.draw(g, (q,), "f32", 0.5)
+    dy, dr = T.draw(g, x.shape, "f32", 0.1), T.draw(g, x.shape, "f32", 0.1)
+    s = K.Norm("f32", *x.shape)
+    assert torch.equal(s.forward(T.gpu(x), T.gpu(gamma), T.gpu(beta)).cpu(), beta.expand(x.shape))
+    dx, dgamma, dbeta = s.backward(T.gpu(x), T.gpu(gamma), T.gpu(dy), T.gpu(dr))
+    assert not dgamma.any()
+    (r, e), _, (rb, eb) = K.norm_backward(x, gamma, dy, dr, 1e-5, "f32")
+    ga = (dy * gamma).double()  # dx = (g - mean g) / sqrt(eps) + dr
+    e = 400 * (84 + q / 1024) * K.E32 * (ga.abs().mean(1, keepdim=True) + ga.abs()) + 2 * K.E32 * dr.abs()
+    T.check(dx, r, e, "dx")
+    T.check(dbeta, rb, eb, "dbeta")
+
+
+@pytest.mark.parametrize("B", [1, 40])
+@pytest.mark.parametrize("q", WIDTHS)
+def test_means_far_beyond_the_spread(q, B, monkeypatch):
+    """Rows whose mean is 10^3 to 10^5 times their spread: held to a bound without the mean."""
+    monkeypatch.setattr(K, "norm_stats", K.norm_stats_sharp)
+    _, gamma, beta, dy, dr = inputs(q, "f32", B, q)
+    g = torch.Generator().manual_seed(q)
+    x = (torch.randn((B, q), generator=g) + torch.tensor([1e3, 1e4, -1e5, 3e4, 0.0])[torch.arange(B) % 5][:, None]).float()
+    s = K.Norm("f32", B, q)
+    T.check(s.forward(T.gpu(x), T.gpu(gamma), T.gpu(beta)), *K.norm_forward(x, gamma, beta, 1e-5, "f32"), "y")
+    got = s.backward(T.gpu(x), T.gpu(gamma), T.gpu(dy), T.gpu(dr))
+    for name, a, (r, e) in zip(("dx", "dgamma", "dbeta"), got, K.norm_backward(x, gamma, dy, dr, 1e-5, "f32")):
+        T.check(a, r, e, name)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_equal_values_without_eps(dtype):
+    """No spread and nothing added to it: NaN, and in the other rows nothing of it."""
+    B, q = 12, 223
+    x, gamma, beta, dy, _ = inputs(3, dtype, B, q)
+    x = (torch.randn((B, q), generator=torch.Generator().manual_seed(4)) * 0.5).to(x.dtype)
+    for i, v in ((1, 0.1), (4, 0.7), (7, 3.3), (11, 0.0)):
+        x[i] = v
+    rows = torch.ones(B, dtype=torch.bool)
+    rows[[1, 4, 7, 11]] = False
+    s = K.Norm(dtype, B, q, eps=0.0)
+    y = s.forward(T.gpu(x), T.gpu(gamma), T.gpu(beta)).cpu()
+    assert torch.isnan(y[~rows]).all()
+    T.check(y[rows], *K.norm_forward(x[rows], gamma, beta, 0.0, dtype), "y")
+    dx = s.backward(T.gpu(x), T.gpu(gamma), T.gpu(dy), None)[0].cpu()
+    assert torch.isnan(dx[~rows]).all()
+    T.check(dx[rows], *K.norm_backward(x[rows], gamma, dy[rows], None, 0.0, dtype)[0], "dx")
