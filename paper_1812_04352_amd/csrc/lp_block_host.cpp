@@ -104,11 +104,15 @@ struct Parts {
 
 namespace lp {
 
-// dx and dz^T x as one launch where both take the smallest tiles and contract over at most BOTH_STAGES stages, microseconds
-// of the whole way back against a launch each (and one more for a split): bf16 320 x 60 -> 384 18.0 (20.1), 209 x 649 -> 649
-// 22.7 (28.3), 2000 x 256 -> 700 21.1 (28.7), f32 1000 x 220 -> 587 (38 stages) 49.5 (50.8); longer ones are better split: f32
-// 1000 x 100 -> 900 (57 stages) 57.6 (45.8), 600 x 512 -> 1024 (64) 75.2 (65.4).
-constexpr int BOTH_STAGES = 40;
+// dx and dz^T x as one launch where both take the smallest tiles and contract over at most so many stages, unsplit; one side
+// alone is then unsplit too, so that its bits do not depend on what else is wanted. The whole way back against a launch
+// each, split as the plans are, microseconds by the longer contraction's stages.
+//   bf16: 21 (209 x 649 -> 649) 22.9 (25.3), 38 (1500 x 100 -> 1200) 30.1 (36.1), 57 (300 x 200 -> 1800) 24.6 (26.2), 72
+//         (4600 x 200 -> 700) 38.5 (43.6), 79 (400 x 300 -> 2500) 42.5 (38.0)
+//   f32:  20 (600 x 300 -> 300) 35.1 (41.7), 25 (800 x 100 -> 150) 30.7 (33.3), 26 (700 x 200 -> 400) 36.6 (40.0), 29
+//         (900 x 128 -> 200) 33.7 (34.5), 30 (250 x 300 -> 450) 41.5 (37.9), 32 (100 x 100 -> 500) 35.9 (28.2), 38
+//         (1000 x 220 -> 587) 47.8 (48.4); dx alone of the last two unsplit 36.1 (22.0) and 46.9 (32.0)
+constexpr int both_stages(size_t e) { return e == 2 ? 72 : 28; }
 
 // The pair's plan. Its smallest tile (two waves, 32 features of each array) takes 0.30 us a stage alone on a CU and 0.45 beside
 // another (floats 0.75, 1.15), no less than its weights' reading takes; joining a split 5 us: 24 x 2048 -> 5120 f16
@@ -142,7 +146,8 @@ GatedLayout gated_layout(int dtype, int B, int ni, int no, bool grad) {
     l.zx = mm::plan_of(e, B, ni, two);
     l.zw = mm::plan_of(e, two, ni, B);
     const double stages = mm::ceil_div((long)std::max(two, B) * (long)e, mm::STAGE_BYTES);
-    l.both = l.zx.tile == 64 && l.zw.tile == 64 && stages <= BOTH_STAGES;
+    l.both = l.zx.tile == 64 && l.zw.tile == 64 && stages <= both_stages(e);
+    if (l.both) l.zx.splits = l.zw.splits = 1;
     part = std::max({part, l.zx.part_bytes(), l.zw.part_bytes()});
     // (and the layer itself, whose plan differs for one row only and then has no sums to join)
     l.dz = p.take((size_t)B * two * e);

@@ -176,3 +176,15 @@ def test_captured_and_on_another_stream(dtype):
         torch.cuda.synchronize()
         for a, b in zip((y, dx, dWg, dWu), want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", [(1000, 220, 587), (209, 649, 649), (320, 60, 384), (2000, 256, 700), (600, 512, 1024), (40, 3000, 500), (700, 200, 400), (4600, 200, 700)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_bits_do_not_depend_on_what_else_is_wanted(dtype, shape):
+    """Sizes whose gradients come from one launch where both sides are wanted, and others."""
+    x, Wg, Wu, dy = (T.gpu(t) for t in inputs(29, dtype, *shape))
+    s = K.Gated(dtype, "silu", *shape)
+    full = s.backward(x, Wg, Wu, dy)
+    for want in ((True, False, False), (False, True, False), (False, False, True), (True, True, False), (False, True, True)):
+        for a, f, w in zip(s.backward(x, Wg, Wu, dy, want), full, want):
+            assert (a is None) if not w else torch.equal(a, f), want
