@@ -151,3 +151,17 @@ def test_captured(dtype):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(mo, want[0]) and torch.equal(W, want[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(70, 8, 5000), (67, 5000, 8), (130, 70, 1500), (64, 300, 20)])
+def test_large_batches_of_long_matrices(dtype, shape):
+    """Batches whose matrices are spread over the XCDs, with contractions that are split."""
+    g, m = gradients(9, dtype, *shape), gradients(10, "f32", *shape)
+    r = T.draw(torch.Generator().manual_seed(2), shape, dtype, 0.1)
+    s = K.Orth(dtype, *shape, mu=0.9, nesterov=True)
+    mo, mf = T.out(shape, torch.float32)
+    W = s(T.gpu(g), T.gpu(m), mo, T.gpu(r), -0.05, 0.99)
+    assert T.guarded(mf, mo.numel())
+    _, v = K.momentum(g, m, 0.9, True, dtype)
+    K.orth_check(W, v.cuda(), r, 5, Q, 1e-7, -0.05, 0.99, dtype, f"W {shape}")
