@@ -496,10 +496,14 @@ inline Group backward_group(size_t esz, int q) {
   return {0, 0};
 }
 
-// Rows of a backward workgroup
+// Rows of a backward workgroup: a round of its groups, more where 256 workgroups (one a CU, each with all the waves it can
+// hold) would not take all rows so. A round is a chain of load, two sums and store, longer than what the second kernel
+// takes for another row of partial sums; with at least one round (two, four), microseconds in a graph: 1000 x 220 f32 7.5
+// (8.8, 12.4), 64 x 4096 bf16 7.8 (9.2, 13.0), 512 x 4096 11.9 (11.5, 15.0), 8192 x 64 7.9 (8.6, 10.9), 2000 x 1111 f16 14.2
+// (14.2, 19.4); dx alone 4.0 (5.9, 9.8), 3.9 (5.8, 9.8), 4.5 (6.3, 10.3), 3.2 (4.5, 6.9), 8.6 (8.7, 14.3).
 inline int backward_rows(int groups, int B) {
-  const int most = 256;  // workgroups: one a CU, each with all the waves it can hold
-  const int rows = std::max(mm::ceil_div(B, most), 4 * groups);
+  const int most = 256;
+  const int rows = std::max(mm::ceil_div(B, most), groups);
   return mm::ceil_div(std::min(rows, 2048 * groups), groups) * groups;  // (at most 2048 rows in a sum of fp32)
 }
 
