@@ -490,8 +490,12 @@ int32_t lp_gated_forward(const lp_gated* layer, const void* x, const void* Wg, c
                          size_t ws_bytes, void* stream);
 
 /* Gradients of the layer for dy [B][no], from its inputs (zg = x Wg^T and zu = x Wu^T are formed again):
- *   dzg = dy zu sigma'(zg),  dzu = dy sigma(zg)   (rounded to the dtype for the next products: with LP_F16
- *                                                  they have to stay below 65504, scale a loss accordingly)
+ *   dzg = dy zu sigma'(zg),  dzu = dy sigma(zg)   (rounded to the dtype for the next products, as g of a step is:
+ *                                                  with LP_BF16 the gradients are off by 0.0023 of their norm,
+ *                                                  0.0017 of which is their own rounding; with LP_F16 dz has to
+ *                                                  stay below 65504, loses bits below 2^-14 and vanishes below
+ *                                                  2^-25, also where a sum of many such values would
+ *                                                  not: scale a loss accordingly)
  *   dx  = dzg Wg + dzu Wu   [B][ni]   (one sum, rounded once)
  *   dWg = dzg^T x,  dWu = dzu^T x   [no][ni]
  * dx, dWg, dWu nullable: not wanted. Outputs must not alias inputs. */

@@ -29,7 +29,8 @@ using mm::f32x4;
 using mm::Place;
 
 // The logistic function, by e = exp(-|z|), which does not overflow; on the hardware's exp2 and reciprocal for
-// the 16-bit types (relative error (|z| + 4) 2^-23 at most: that of the exponent, and a step each).
+// the 16-bit types (relative error (|z| + 4) 2^-23 at most: that of the exponent, and a step each; e is 0 where it
+// lies below 2^-126, beyond |z| = 87.3).
 template <typename T>
 __device__ __forceinline__ float logistic(float z) {
   if constexpr (sizeof(T) == 2) {

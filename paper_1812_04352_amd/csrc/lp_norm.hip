@@ -12,12 +12,16 @@
 //              second kernel adds in fp64 (a single workgroup writes the gradients themselves).
 //   The first mean is rounded, and so is the sum that it comes from: a row's x - mean does not sum to 0, but to what that
 //   mean is off by. Its mean is taken off x - mean, and the square of it off the mean square, so that a row whose mean
-//   exceeds its spread by far loses nothing, and equal values leave 0 (without that a row of 223 values 3300 was off by
-//   hundredths).
+//   exceeds its spread by far loses nothing, and equal values leave 0 (without that a row of 223 values 3300 in fp32
+//   was off by hundredths). bf16 rows that a group holds do not need it: where the mean exceeds the spread, the values
+//   are multiples of one step, 2^9 at most, and 2^15 of them sum exactly; the mean is then off by half an fp32 step,
+//   2^-17 of the values' own, and the spread is at least that by the root of q: off by 2^-9.5 of it at most. (It takes 1 to 6 % of
+//   the time back, 8192 x 4096 f32 97 -> 98 us, 20000 x 700 f32 49 -> 52, 5003 x 1111 f16 19.1 -> 20.2.)
 // Bound by memory: 8192 x 4096 bf16 25 us forward (5.3 TB/s), 65 us back with dr (4.1; 62 in the kernel and 4.6 in the sum of
 // 256 rows of partial sums, one of each workgroup, of which there is one a CU; without the next rows requested ahead and with
 // sums by LDS exchanges 97). Rows that no group can hold are read again for every pass.
 #include <algorithm>
+#include <type_traits>
 
 #include "lp_internal.h"
 #include "lp_mm.h"
@@ -97,9 +101,9 @@ struct Piece {
   }
 };
 
-// The wave's sum of a value in every lane: neighbours within rows of 16 lanes by data-parallel moves, whose
-// latency is a vector instruction's, then the four rows' sums in order.
-__device__ __forceinline__ float wave_sum(float v) {
+// A value's sum over rows of 16 lanes, the same in all of them, by data-parallel moves, whose latency is a vector
+// instruction's
+__device__ __forceinline__ float row_sum(float v) {
 #ifdef __HIP_DEVICE_COMPILE__
 #define LP_ADD_MOVED(ctrl) v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, 0xf, 0xf, true))
   LP_ADD_MOVED(0xb1);   // quad_perm 1, 0, 3, 2
@@ -107,6 +111,14 @@ __device__ __forceinline__ float wave_sum(float v) {
   LP_ADD_MOVED(0x141);  // the other quad of eight lanes: row_half_mirror
   LP_ADD_MOVED(0x140);  // the other half of sixteen: row_mirror
 #undef LP_ADD_MOVED
+#endif
+  return v;
+}
+
+// The wave's sum of a value in every lane: its four rows' sums in order
+__device__ __forceinline__ float wave_sum(float v) {
+  v = row_sum(v);
+#ifdef __HIP_DEVICE_COMPILE__
   float r[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 16 * i));
@@ -115,13 +127,15 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
-// Sums of up to three values over a group of TPR threads, the same in all of them. Groups wider than a wave
-// exchange through the LDS: `at` alternates between its two halves, so that one barrier a sum is enough
-// (a wave that writes a half again has passed the barrier behind which all have read it).
-template <int TPR, int NT>
+// Sums of up to M values (two or four) over a group of TPR threads, the same in all of them. Groups wider than a wave
+// exchange through the LDS, where every lane adds its group's waves in order; of many waves (M W > 16: 8192 x 4096 f32 back 98
+// us, 116 in order) every row of 16 lanes reads one a lane: `at` alternates between two halves, so that one barrier a sum is enough (a wave that writes a half
+// again has passed the barrier behind which all have read it).
+template <int TPR, int NT, int M>
 struct GroupSum {
   static constexpr int W = TPR / 64;  // waves of a group
-  typedef float Lds[2][NT / 64][3];
+  typedef float Values __attribute__((ext_vector_type(M)));
+  typedef Values Lds[2][NT / 64];
   Lds& lds;
   int at = 0;
   template <int N>
@@ -136,24 +150,33 @@ struct GroupSum {
       for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
     }
     if constexpr (TPR > 64) {
-      const int wave = threadIdx.x >> 6;
-      if ((threadIdx.x & 63) == 0) {
+      static_assert(W <= 16, "a row of lanes");
+      const int wave = threadIdx.x >> 6, w = threadIdx.x & 15;
+      Values v = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) lds[at][wave][i] = s[i];
-      }
+      for (int i = 0; i < N; ++i) v[i] = s[i];
+      if ((threadIdx.x & 63) == 0) lds[at][wave] = v;
       __syncthreads();
-      const float(*g)[3] = lds[at] + wave / W * W;
+      const Values* g = lds[at] + wave / W * W;
+      if constexpr (M * W > 16) {
+        v = g[min(w, W - 1)];
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[i] = g[0][i];
-      constexpr int AT_ONCE = N == 3 && W > 8 ? 3 : 15;  // (the widest groups lack the registers for three values of all)
-#pragma unroll AT_ONCE
-      for (int w = 1; w < W; ++w)
+        for (int i = 0; i < N; ++i) s[i] = row_sum(w < W ? v[i] : 0.f);
+      } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] += g[w][i];
+        for (int k = 0; k < W; ++k) {
+          v = g[k];
+#pragma unroll
+          for (int i = 0; i < N; ++i) s[i] = k ? s[i] + v[i] : v[i];
+        }
+      }
       at ^= 1;
     }
   }
 };
+
+// Values of this type are taken about the mean of x - mean
+template <typename T> constexpr bool CENTRE = !std::is_same<T, __bf16>::value;
 
 // The mean square of x - mean less the square of its mean, `off` (never below 0; a NaN stays one)
 __device__ __forceinline__ float variance(float square, float off) {
@@ -165,8 +188,9 @@ template <typename T, int TPR, int C, int NT>
 __global__ __launch_bounds__(NT) void k_forward(const T* x, const T* gamma, const T* beta, T* y, int B, int q, float eps) {
   typedef Piece<T, TPR, C> P;
   constexpr int V = P::V, G = NT / TPR;
-  __shared__ typename GroupSum<TPR, NT>::Lds lds;
-  GroupSum<TPR, NT> sum{lds};
+  typedef GroupSum<TPR, NT, 2> Sum;
+  __shared__ typename Sum::Lds lds;
+  Sum sum{lds};
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
   P ga, be;
   if (gamma) ga.load(gamma, t, q), ga.cut(t, q);
@@ -184,17 +208,19 @@ __global__ __launch_bounds__(NT) void k_forward(const T* x, const T* gamma, cons
       for (int k = 0; k < V; ++k) s1[0] += (float)p.v[c][k];
     sum(s1);
     const float mean = s1[0] / n;
-    float s2[2] = {0.f, 0.f};
+    float s2[CENTRE<T> ? 2 : 1] = {};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const float d = P::first(t, c) + k < q ? (float)p.v[c][k] - mean : 0.f;
         s2[0] = fmaf(d, d, s2[0]);
-        s2[1] += d;
+        if constexpr (CENTRE<T>) s2[1] += d;
       }
     sum(s2);
-    const float off = s2[1] / n, rstd = 1.f / sqrtf(variance(s2[0] / n, off) + eps);
+    float off = 0.f;
+    if constexpr (CENTRE<T>) off = s2[1] / n;
+    const float rstd = 1.f / sqrtf(variance(s2[0] / n, off) + eps);
     if (r >= B) continue;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -262,9 +288,10 @@ __global__ __launch_bounds__(threads_back(TPR)) void k_backward(BackArgs a) {
   typedef Piece<T, TPR, C> P;
   constexpr int V = P::V, NT = threads_back(TPR), G = NT / TPR;
   constexpr bool AHEAD = C == 1;
-  __shared__ typename GroupSum<TPR, NT>::Lds lds;
+  typedef GroupSum<TPR, NT, CENTRE<T> ? 4 : 2> Sum;
+  __shared__ typename Sum::Lds lds;
   __shared__ __attribute__((aligned(16))) float sums[G == 1 ? 4 : NT * C * V];
-  GroupSum<TPR, NT> sum{lds};
+  Sum sum{lds};
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, q = FULL ? TPR * C * V : a.q;
   const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = a.dx ? static_cast<const T*>(a.dr) : nullptr;
   T* dx = static_cast<T*>(a.dx);
@@ -309,7 +336,7 @@ __global__ __launch_bounds__(threads_back(TPR)) void k_backward(BackArgs a) {
       }
     sum(s1);
     const float mean = s1[0] / n, m1 = s1[1] / n;
-    float s2[3] = {0.f, 0.f, 0.f};
+    float s2[CENTRE<T> ? 3 : 2] = {};
     if constexpr (!AHEAD) now.x.forget(), now.d.forget(), ga.forget();
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -317,11 +344,13 @@ __global__ __launch_bounds__(threads_back(TPR)) void k_backward(BackArgs a) {
       for (int k = 0; k < V; ++k) {
         const float d = FULL || P::first(t, c) + k < q ? (float)now.x.v[c][k] - mean : 0.f;
         s2[0] = fmaf(d, d, s2[0]);
-        s2[1] += d;
-        s2[2] = fmaf((float)now.d.v[c][k] * (float)ga.v[c][k], d, s2[2]);
+        s2[1] = fmaf((float)now.d.v[c][k] * (float)ga.v[c][k], d, s2[1]);
+        if constexpr (CENTRE<T>) s2[2] += d;
       }
     sum(s2);
-    const float off = s2[1] / n, rstd = 1.f / sqrtf(variance(s2[0] / n, off) + a.eps), m2 = (s2[2] / n - off * m1) * rstd;
+    float off = 0.f;
+    if constexpr (CENTRE<T>) off = s2[2] / n;
+    const float rstd = 1.f / sqrtf(variance(s2[0] / n, off) + a.eps), m2 = (s2[1] / n - off * m1) * rstd;
     if constexpr (!AHEAD) now.x.forget(), now.d.forget(), ga.forget();
     if (r < r1) {
 #pragma unroll
@@ -376,6 +405,8 @@ __global__ __launch_bounds__(1024) void k_sum(const float* part, int rows, int q
 
 // ---- rows that no group holds: every pass reads them again
 
+typedef GroupSum<1024, 1024, 4> LongSum;
+
 // A row's statistics: its first mean, what that is off by, 1 / sqrt(var + eps), and with dy the means of g and g xh
 struct LongStats {
   float mean, off, rstd, m1, m2;
@@ -384,7 +415,7 @@ struct LongStats {
 
 // over a workgroup of 1024
 template <typename T>
-__device__ __forceinline__ LongStats long_stats(const T* x, const T* dy, const T* gamma, int q, float eps, GroupSum<1024, 1024>& sum) {
+__device__ __forceinline__ LongStats long_stats(const T* x, const T* dy, const T* gamma, int q, float eps, LongSum& sum) {
   const float n = (float)q;
   LongStats r;
   float s1[2] = {0.f, 0.f};
@@ -410,8 +441,8 @@ __device__ __forceinline__ LongStats long_stats(const T* x, const T* dy, const T
 
 template <typename T>
 __global__ __launch_bounds__(1024) void k_forward_long(const T* x, const T* gamma, const T* beta, T* y, int B, int q, float eps) {
-  __shared__ GroupSum<1024, 1024>::Lds lds;
-  GroupSum<1024, 1024> sum{lds};
+  __shared__ LongSum::Lds lds;
+  LongSum sum{lds};
   for (long r = blockIdx.x; r < B; r += gridDim.x) {
     const LongStats s = long_stats<T>(x + r * q, nullptr, nullptr, q, eps, sum);
     for (int i = threadIdx.x; i < q; i += 1024) {
@@ -426,8 +457,8 @@ __global__ __launch_bounds__(1024) void k_forward_long(const T* x, const T* gamm
 // dx, and the statistics of every row (mean, off, rstd) for the weights' gradients
 template <typename T>
 __global__ __launch_bounds__(1024) void k_backward_long(BackArgs a, float4* stats) {
-  __shared__ GroupSum<1024, 1024>::Lds lds;
-  GroupSum<1024, 1024> sum{lds};
+  __shared__ LongSum::Lds lds;
+  LongSum sum{lds};
   const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dr = static_cast<const T*>(a.dr);
   const T* gamma = static_cast<const T*>(a.gamma);
   T* dx = static_cast<T*>(a.dx);

@@ -223,3 +223,29 @@ def test_equal_values_without_eps(dtype):
     dx = s.backward(T.gpu(x), T.gpu(gamma), T.gpu(dy), None)[0].cpu()
     assert torch.isnan(dx[~rows]).all()
     T.check(dx[rows], *K.norm_backward(x[rows], gamma, dy[rows], None, 0.0, dtype)[0], "dx")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("q", WIDTHS)
+def test_rows_of_equal_16_bit_values(q, dtype):
+    """And rows of which a value or two differ by the last place, the least spread that the type has."""
+    g = torch.Generator().manual_seed(q)
+    x = torch.tensor([0.1, 0.7, 3.3, 3.3e3, -1.1e-3, 12345.678]).repeat(5)[:, None].repeat(1, q).to(T.DT[dtype])
+    gamma, beta = (1 + T.draw(g, (q,), "f32", 0.3)).to(x.dtype), T.draw(g, (q,), dtype, 0.5)
+    dy = T.draw(g, x.shape, dtype, 0.1)
+    s = K.Norm(dtype, *x.shape)
+    assert torch.equal(s.forward(T.gpu(x), T.gpu(gamma), T.gpu(beta)).cpu(), beta.expand(x.shape))
+    assert not s.backward(T.gpu(x), T.gpu(gamma), T.gpu(dy), None)[1].any()
+    step = (x.double().abs().log2().floor().exp2() * torch.finfo(x.dtype).eps).to(x.dtype)
+    x[:, 0] += step[:, 0]
+    x[3:, q // 2] -= step[3:, 0]
+    xd = x.double()
+    d = xd - xd.mean(1, keepdim=True)
+    rstd = ((d * d).mean(1, keepdim=True) + 1e-5) ** -0.5
+    ref = d * rstd * gamma.double() + beta.double()
+    # bf16 rows that a group holds (2^15 values forward): off by half an fp32 step of the mean; else by what sums of x - mean
+    # are; fp32 steps of the values, the type's half step
+    off = 2.0 ** -24 * xd.mean(1, keepdim=True).abs() if dtype == "bf16" and q <= 1 << 15 else 0.0
+    n = 84 + q / 1024
+    err = (off + (n + 2) * K.E32 * (d.abs().mean(1, keepdim=True) + d.abs())) * rstd * gamma.double().abs() + n * K.E32 * (ref.abs() + beta.double().abs())
+    T.check(s.forward(T.gpu(x), T.gpu(gamma), T.gpu(beta)), ref, err + T.half_step(dtype) * (ref.abs() + err) + T.tiny(dtype), "y")
