@@ -513,7 +513,7 @@ int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, 
  * singular vectors: with a, b, c = 3.4445, -4.7750, 2.0315 five steps bring those above 0.003 to between 0.7 and
  * 1.2, with 15/8, -10/8, 3/8 those near one converge to one.
  * The products' operands X, A and b A + c A^2 are kept as sums of two f16 values each (2^-22 relative) with LP_F32 and
- * for matrices of at most 64 x 256 of every type, else they are rounded to f16; what that rounds off X is kept for
+ * for matrices of at most 64 x 256 of every type, else they are rounded to f16; X keeps eight bits more for
  * the sum a X + .. alone. Powers of two bring them to the top of f16's range, for which a, b, c have to keep singular
  * values below about 3. With the first coefficients and five steps X is off by 4e-4 to 2e-3 of its norm by single f16
  * values, by 3e-7 to 3e-6 by sums of two (1e-5 to 2e-5 where a few directions exceed the others a hundredfold and more). */
@@ -529,8 +529,8 @@ typedef struct {
   double mu;             /* finite in fp32 */
 } lp_orth;
 
-/* Workspace bytes of lp_orth_update; 0 for an invalid update. It holds X twice (16-bit types: and what it
- * rounds off), A and b A + c A^2 of as many matrices as 1 GiB holds (at least one), and the partial sums of split products. */
+/* Workspace bytes of lp_orth_update; 0 for an invalid update. It holds X twice (of 16-bit types
+ * with eight bits more), A and b A + c A^2 of as many matrices as 1 GiB holds (at least one), and the partial sums of split products. */
 size_t lp_orth_workspace_bytes(const lp_orth* orth);
 
 /* The update. g, r, W [N][no][ni]; m, mo [N][no][ni] fp32: m' goes to mo, which may be m. Without mo (m NULL

@@ -184,8 +184,9 @@ OrthLayout orth_layout(int dtype, int N, int no, int ni) {
   const bool duo = dtype == LP_F32;
   l.ld = (mm::padded(e, ni) + 7) / 8 * 8;
   l.lda = (mm::padded(e, n) + 7) / 8 * 8;
-  const size_t x = (size_t)no * l.ld * e, a = (size_t)n * l.lda * e;
-  l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a) + (duo ? 0 : x)), 1), 16384));
+  l.ldlo = duo ? 0 : (l.ld + 15) / 16 * 16;
+  const size_t x = (size_t)no * l.ld * e, a = (size_t)n * l.lda * e, lo = (size_t)no * l.ldlo;
+  l.chunk = (int)std::min<size_t>(std::max(N, 1), std::min<size_t>(std::max<size_t>(ORTH_CHUNK / (2 * (x + a) + lo), 1), 16384));
   l.parts = (int)std::min<size_t>(((size_t)no * ni + 4095) / 4096, 2048);
   l.gram = no > ni ? mm::plan_of(e, n, n, k, l.chunk, true, duo) : sym_plan(e, n, k, l.chunk, duo);
   l.poly = sym_plan(e, n, n, l.chunk, duo);
@@ -196,7 +197,7 @@ OrthLayout orth_layout(int dtype, int N, int no, int ni) {
   Parts p;
   l.norms = p.take((size_t)l.chunk * l.parts * 8);
   for (size_t& at : l.X) at = p.take(l.chunk * x);
-  if (!duo) l.lo = p.take(l.chunk * x);
+  l.lo = p.take(l.chunk * lo);
   l.A = p.take(l.chunk * a);
   l.P = p.take(l.chunk * a);
   l.part = p.take(std::max({part(l.gram, true), part(l.poly, true), part(l.next, false)}));

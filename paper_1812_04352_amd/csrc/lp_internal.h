@@ -331,8 +331,8 @@ struct OrthArgs {
   void* ws;
 };
 struct OrthLayout {
-  size_t norms, X[2], lo, A, P, part, total;  // (lo: 16-bit types)
-  int ld, lda;            // rows of X and of A, P
+  size_t norms, X[2], lo, A, P, part, total;  // (lo: 16-bit types, what X rounds off)
+  int ld, lda, ldlo;      // rows of X, of A and P, and of lo
   int chunk, parts;       // matrices taken at a time; partial sums of a matrix's squares
   mm::Plan gram, poly, next;  // the products A, A^2 and P X
 };

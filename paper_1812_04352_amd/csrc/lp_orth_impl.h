@@ -13,13 +13,15 @@
 // exceeds 1.3 or so, so that A and P are in range: f16 then rounds eight times finer than bf16 does. What rounding costs
 // is kept down in two ways.
 //   A rounding error of X grows like the small singular values do, by a factor a a step, where it is added to them, in
-//   a X: the X of a X keeps what f16 rounds off in an array of its own.
-//   In the last steps, where X is nearly orthogonal, P is nearly (b + c) I and a X + P X a small difference: they form
+//   a X: the X of a X has 8 bits more, in an array of their own (2^-19 relative; an f16 more is no better), but for
+//   the last two steps, behind which little grows. It takes 4096 x 4096 bf16 3 % more time, 2048 of 220 x 220 10 % (2846
+//   -> 3124 us; by an f16 more in every step 3461).
+//   In those, where X is nearly orthogonal, P is nearly (b + c) I and a X + P X a small difference: they form
 //   (a + b + c) X + (P - (b + c) I) X, whose product is small and its rounding with it. (While singular values still
-//   differ much it would mix strong directions into small ones: the last two steps.)
-// O is off by 4e-4 to 1.1e-3 of its norm for noise, a few strong directions or singular values down to a thousandth
-// (by X in f16 alone and P as it is 1.4e-3 to 1.5e-2), by 1.3e-3 where four directions exceed the noise a hundredfold
-// (4e-2), by 2e-3 where single values do. It takes 6 % more time.
+//   differ much it would mix strong directions into small ones.)
+// O is off by 4e-4 to 1.3e-3 of its norm for noise, a few strong directions or singular values down to a thousandth
+// (by X in f16 alone and P as it is 1.4e-3 to 1.5e-2), by 1.6e-3 where four directions exceed the noise a hundredfold
+// (4e-2), by 2.2e-3 where single values do.
 // Bound by the products: steps (3 n^2 k + n^3) operations, n the short and k the long side: 4096 x 4096 bf16 1514 us (0.91
 // PFLOP/s of those; a symmetric product 98 us, the other one 142), 2048 of 220 x 220 f32 4439 us (98 TFLOP/s:
 // memory, 4.3 to 6.2 TB/s, since X, A and P pass through it for every product).
@@ -126,8 +128,17 @@ __global__ __launch_bounds__(256) void k_momentum(Momentum<TI, VV> u, size_t siz
   if (threadIdx.x == 0) part[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = ((sh[0] + sh[1]) + sh[2]) + sh[3];
 }
 
-// what f16 rounds off
-__device__ __forceinline__ float rest(float v) { return v - (float)(mm::f16)v; }
+// Eight bits more than f16's: what it rounds off v, in 256ths of its value's last place, and the value with that (2^e: the
+// place of a value h is 2^(e - 25), below 2^-14 that of 2^-14)
+__device__ __forceinline__ int place(float h) { return max((int)(__builtin_bit_cast(uint32_t, h) >> 23 & 255) - 112, 1); }
+__device__ __forceinline__ float rest(float v) {
+  const float h = (float)(mm::f16)v;
+  const float r = (v - h) * __builtin_bit_cast(float, (uint32_t)(127 + 33 - place(h)) << 23);
+  return fminf(fmaxf(rintf(r), -127.f), 127.f);  // (a NaN gives -127, with its h a NaN again)
+}
+__device__ __forceinline__ float with_rest(float h, float r) {
+  return fmaf(r, __builtin_bit_cast(float, (uint32_t)(127 - 33 + place(h)) << 23), h);
+}
 
 template <typename T>
 __device__ __forceinline__ void put_values(T* row, int c, const float (&v)[8]) {
@@ -142,11 +153,11 @@ __device__ __forceinline__ void put_values(T* row, int c, const float (&v)[8]) {
   }
 }
 
-// X = v up / (|v| + eps) in rows of ld values, zeros behind the ni that count (grid y: the matrix); lo (16-bit T): what it
-// rounds off
+// X = v up / (|v| + eps) in rows of ld values, zeros behind the ni that count (grid y: the matrix); lo (f16, nullable):
+// its rest
 template <typename TI, typename T>
 __global__ __launch_bounds__(256) void k_scale(Momentum<TI, 8> u, int no, int ni, int ld, const double* part, int parts, double eps,
-                                               double up, T* X, T* lo) {
+                                               double up, T* X, int8_t* lo, int ldlo) {
   __shared__ double sh;
   if (threadIdx.x < 64) {
     const double* p = part + (size_t)blockIdx.y * parts;
@@ -173,9 +184,12 @@ __global__ __launch_bounds__(256) void k_scale(Momentum<TI, 8> u, int no, int ni
     }
     put_values(X + r * ld, c, v);
     if constexpr (std::is_same<T, mm::f16>::value) {
+      if (lo) {
+        typename GVec<int8_t, 8>::type y;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = rest(v[k]);
-      put_values(lo + ((size_t)blockIdx.y * no + r) * ld, c, v);
+        for (int k = 0; k < 8; ++k) y[k] = (int8_t)rest(v[k]);
+        *reinterpret_cast<typename GVec<int8_t, 8>::type*>(lo + ((size_t)blockIdx.y * no + r) * ldlo + c) = y;
+      }
     }
   }
 }
@@ -495,7 +509,45 @@ struct EpSym {
   }
 };
 
-// a X + d D. f16: X is the sum of X and lo, and lo becomes what f16 rounds off the result.
+// The array of rests, rows of ld values in whole 16-byte pieces, as a lane's quads block by block (compare mm::Rows), and back
+template <int FM, int FN>
+struct RestRows {
+  typedef mm::BlockIO<int8_t> IO;
+  int8_t* a;
+  long ld;
+  typename IO::Block next;
+  __device__ __forceinline__ typename IO::Block fetch(const Place& c, int i, int j) const {
+    static_assert(IO::ITER == 1 && IO::CPR == 2 && IO::V == 16, "a lane's piece");
+    const int m = min(c.mw + 32 * i + c.lane / 2, c.M - 1), n = c.nw + 32 * j + c.lane % 2 * 16;
+    return {{*reinterpret_cast<const typename IO::LPiece*>(a + (size_t)m * ld + min((long)n, ld - 16))}};
+  }
+  __device__ __forceinline__ RestRows(int8_t* a_, long ld_, const Place& c) : a(a_), ld(ld_) {
+    if (a) next = fetch(c, 0, 0);
+  }
+  __device__ __forceinline__ void get(const Place& c, int i, int j, unsigned char* buf, f32x4 (&v)[4]) {
+    const typename IO::Block b = next;
+    if (i + 1 < FM) next = fetch(c, i + 1, j);
+    else if (j + 1 < FN) next = fetch(c, 0, j + 1);
+    IO::quads(b, buf, c, v);
+  }
+  __device__ __forceinline__ void put(const Place& c, int i, int j, unsigned char* buf, const f32x4 (&v)[4]) const {
+    unsigned char* w = buf + (c.lane & 31) * IO::PITCH + (c.lane >> 5) * 4;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      typename IO::Quad x;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = (int8_t)v[q][k];
+      *reinterpret_cast<typename IO::Quad*>(w + 8 * q) = x;
+    }
+    mm::wave_in_order();
+    const int m = c.mw + 32 * i + c.lane / 2, n = c.nw + 32 * j + c.lane % 2 * 16;
+    const auto x = *reinterpret_cast<const typename IO::LPiece*>(buf + c.lane / 2 * IO::PITCH + c.lane % 2 * 16);
+    if (m < c.M && n < ld) *reinterpret_cast<typename IO::LPiece*>(a + (size_t)m * ld + n) = x;
+    mm::wave_in_order();
+  }
+};
+
+// a X + d D. f16: lo (nullable) is the rest of X, and becomes that of the result (more: it will be asked for).
 template <typename T>
 struct EpNext {
   static constexpr bool LO = std::is_same<T, mm::f16>::value;
@@ -505,29 +557,35 @@ struct EpNext {
     int ld;
     size_t stride;
     float a, d;
-    T* lo;
+    int8_t* lo;
+    int ldlo;
+    size_t slo;
+    bool more;
   };
   static __device__ __forceinline__ Args at(Args a, int z) {
     a.X += z * a.stride;
     a.out += z * a.stride;
-    if constexpr (LO) a.lo += z * a.stride;
+    if (LO && a.lo) a.lo += z * a.slo;
     return a;
   }
   template <bool WHOLE, int FM, int FN, int WGM, int WGN>
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     unsigned char* buf = mm::wave_lds(lds, c, WGN);
     mm::Rows<WHOLE, T, FM, FN> X(a.X, a.ld, c);
-    mm::Rows<WHOLE, T, FM, FN> lo(LO ? a.lo : nullptr, a.ld, c);
+    RestRows<FM, FN> lo(LO ? a.lo : nullptr, a.ldlo, c);
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        f32x4 v[4], w[4];
+        f32x4 v[4];
         X.get(c, i, j, buf, v);
-        if constexpr (LO) {
+        if (LO && a.lo) {
+          f32x4 w[4];
           lo.get(c, i, j, buf, w);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] += w[q];
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[q][k] = with_rest(v[q][k], w[q][k]);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
@@ -535,23 +593,22 @@ struct EpNext {
           for (int k = 0; k < 4; ++k)
             v[q][k] = WHOLE || c.feature(j, q) + k < c.lim ? a.a * v[q][k] + a.d * acc[i][j][4 * q + k] : 0.f;
         mm::put_rows<WHOLE>(a.out, a.ld, c.upto(a.ld), c, i, j, buf, v);
-        if constexpr (LO) {
+        if (LO && a.more) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[q][k] = rest(v[q][k]);
-          mm::put_rows<WHOLE>(a.lo, a.ld, c.upto(a.ld), c, i, j, buf, v);
+          lo.put(c, i, j, buf, v);
         }
       }
   }
 };
 
-// W = alpha (a X + d D) + beta r, rows of N values (r nullable). f16: X is the sum of X and lo.
+// W = alpha (a X + d D) + beta r, rows of N values (r nullable)
 template <typename T, typename TO>
 struct EpUpdate {
-  static constexpr bool LO = std::is_same<T, mm::f16>::value;
   struct Args {
-    const T *X, *lo;
+    const T* X;
     int ld;
     size_t stride;   // of a matrix of X
     const TO* r;
@@ -561,7 +618,6 @@ struct EpUpdate {
   };
   static __device__ __forceinline__ Args at(Args a, int z) {
     a.X += z * a.stride;
-    if constexpr (LO) a.lo += z * a.stride;
     if (a.r) a.r += z * a.wstride;
     a.W += z * a.wstride;
     return a;
@@ -570,7 +626,6 @@ struct EpUpdate {
   static __device__ __forceinline__ void run(const Args& a, const Place& c, f32x16 (&acc)[FM][FN], float* lds) {
     unsigned char* buf = mm::wave_lds(lds, c, WGN);
     mm::Rows<WHOLE, T, FM, FN> X(a.X, a.ld, c);
-    mm::Rows<WHOLE, T, FM, FN> lo(LO ? a.lo : nullptr, a.ld, c);
     mm::Rows<WHOLE, TO, FM, FN, false> r(a.r, c.N, c);
 #pragma unroll
     for (int j = 0; j < FN; ++j)
@@ -578,11 +633,6 @@ struct EpUpdate {
       for (int i = 0; i < FM; ++i) {
         f32x4 v[4], w[4];
         X.get(c, i, j, buf, v);
-        if constexpr (LO) {
-          lo.get(c, i, j, buf, w);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) v[q] += w[q];
-        }
         r.get(c, i, j, buf, w);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = (v[q] * a.a + mm::quad(acc[i][j], q) * a.d) * a.alpha + w[q] * a.beta;
@@ -718,7 +768,7 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
   T* X[2] = {reinterpret_cast<T*>(w + l.X[0]), reinterpret_cast<T*>(w + l.X[1])};
   T *A = reinterpret_cast<T*>(w + l.A), *P = reinterpret_cast<T*>(w + l.P);
   constexpr bool LO = std::is_same<T, mm::f16>::value;
-  T* lo = LO ? reinterpret_cast<T*>(w + l.lo) : nullptr;
+  int8_t* lo = LO && a.steps > 2 ? reinterpret_cast<int8_t*>(w + l.lo) : nullptr;
   const bool tall = a.no > a.ni;
   const int n = std::min(a.no, a.ni), k = std::max(a.no, a.ni), ld = l.ld, lda = l.lda;
   const size_t size = (size_t)a.no * a.ni, sx = (size_t)a.no * ld, sA = (size_t)n * lda;
@@ -730,7 +780,7 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
     float* mo = a.mo ? a.mo + from : nullptr;
     const unsigned gx = (unsigned)std::min<size_t>((sx + 4095) / 4096, 2048);
     k_momentum<TI><<<dim3((unsigned)l.parts, (unsigned)batch), 256, 0, st>>>({g, a.m ? a.m + from : nullptr, mo, (float)a.mu, a.nesterov}, size, norms);
-    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>({g, nullptr, mo, (float)a.mu, a.nesterov}, a.no, a.ni, ld, norms, l.parts, a.eps, X_UP, X[0], lo);
+    k_scale<TI, T><<<dim3(gx, (unsigned)batch), 256, 0, st>>>({g, nullptr, mo, (float)a.mu, a.nesterov}, a.no, a.ni, ld, norms, l.parts, a.eps, X_UP, X[0], lo, l.ldlo);
     hipError_t e = hipGetLastError();
     for (int s = 0; s < a.steps && e == hipSuccess; ++s) {
       const T* x = X[s & 1];
@@ -750,10 +800,10 @@ hipError_t update_t(const OrthArgs& a, hipStream_t st) {
       const Product next = tall ? product(prob(x, ld, P, lda, a.no, a.ni, n), sx, sA, l.next)
                                 : product(prob(P, lda, x, ld, a.no, a.ni, n), sA, sx, l.next);
       if (s + 1 < a.steps) {
-        const typename EpNext<T>::Args en{x, X[~s & 1], ld, sx, (float)(a.a + move), 1.f / A_UP, lo};
+        const typename EpNext<T>::Args en{x, X[~s & 1], ld, sx, (float)(a.a + move), 1.f / A_UP, s + 2 < a.steps ? lo : nullptr, l.ldlo, (size_t)a.no * l.ldlo, LO && s + 3 < a.steps};
         e = tall ? launch_product<T, false, false, false, EpNext<T>>(next, en) : launch_product<T, false, true, false, EpNext<T>>(next, en);
       } else {
-        const typename EpUpdate<T, TI>::Args eu{x, lo, ld, sx, a.r ? (const TI*)a.r + from : nullptr, (TI*)a.W + from, size,
+        const typename EpUpdate<T, TI>::Args eu{x, ld, sx, a.r ? (const TI*)a.r + from : nullptr, (TI*)a.W + from, size,
                                                 (float)(a.a + move), 1.f / A_UP, (float)(a.alpha * down), (float)a.beta};
         e = tall ? launch_product<T, false, false, false, EpUpdate<T, TI>>(next, eu)
                  : launch_product<T, false, true, false, EpUpdate<T, TI>>(next, eu);

@@ -259,12 +259,19 @@ def two_parts(t, up):
     return (h.double() + (f - h.float()).half().double()) / up
 
 
+def rest(t, up):
+    """What f16 rounds off t times up, to 256ths of its last place."""
+    h = (t * up).half().double()
+    place = torch.exp2((torch.frexp(h)[1] - 11).clamp(min=-24).double()) / 256
+    return torch.round((t * up - h) / place).clamp(-127, 127) * place / up
+
+
 def iterate_kept(v, steps, coeffs, eps, dtype, noise=E32, seed=0):
     """The iteration in 64 bits with what the kernels round. Products' operands: X times 2^14 (of matrices of at most
     64 x 256, about the root of their size), A and b A + c A^2 times 2^8, to two f16 parts (fp32, and those small
     matrices in every type) or one, of which b A + c A^2 without (b + c) I in the last two steps (where |b + c| is at
-    most 8). The X of a X: fp32 (small matrices), else two parts too. Every product is off by a step of fp32 of its
-    row's and column's norms."""
+    most 8). The X of a X: fp32 (small matrices), two parts too, or eight bits more but for the last two steps. Every
+    product is off by a step of fp32 of its row's and column's norms."""
     a, b, c = coeffs
     gen = torch.Generator(device="cpu").manual_seed(seed)
     n, k = sorted(v.shape[1:])
@@ -287,7 +294,8 @@ def iterate_kept(v, steps, coeffs, eps, dtype, noise=E32, seed=0):
         op = keep(X, up)
         A = keep(product(op, op.transpose(1, 2)), 2.0 ** 8)
         P = keep(b * A + c * product(A, A) - move * eye, 2.0 ** 8)
-        X = (a + move) * (X if small else two_parts(X, up)) + product(P, op)
+        own = X if small else op if two or s + 2 >= steps else op + rest(X, up)
+        X = (a + move) * own + product(P, op)
     return X.transpose(1, 2) if tall else X
 
 
