@@ -515,8 +515,8 @@ int32_t lp_gated_backward(const lp_gated* layer, const void* x, const void* Wg, 
  * The products' operands X, A and b A + c A^2 are kept as sums of two f16 values each (2^-22 relative) with LP_F32 and
  * for matrices of at most 64 x 256 of every type, else they are rounded to f16; X keeps eight bits more for
  * the sum a X + .. alone. Powers of two bring them to the top of f16's range, for which a, b, c have to keep singular
- * values below about 3. With the first coefficients and five steps X is off by 4e-4 to 2e-3 of its norm by single f16
- * values, by 3e-7 to 3e-6 by sums of two (1e-5 to 2e-5 where a few directions exceed the others a hundredfold and more). */
+ * values below about 3. With the first coefficients and five steps X is off by 5e-4 to 2e-3 of its norm by single f16
+ * values, by 3e-7 to 3e-6 by sums of two (2e-5 to 6e-5 where a few directions exceed the others a hundredfold and more). */
 typedef struct {
   int32_t abi_version;   /* must equal LP_ABI_VERSION */
   int32_t dtype;         /* LP_F32 | LP_BF16 | LP_F16: g, r and W; m is fp32 */

@@ -9,8 +9,8 @@
 //              dzg and dzu lie side by side in blocks of PAIR_BLOCK features, dz [B][2 no32]: dx is then
 //              one contraction over both (the weights' rows taken from either array in turn), and
 //              dz^T x one product whose rows belong to dWg and dWu in turn.
-// Bound by the products: 4 B ni no operations forward, 12 B ni no back: 8192 x 4096 -> 10240 bf16 1110 us forward (1.24
-// PFLOP/s) and 3404 back (1.21). One token reads both weights at 5.7 TB/s (29 us there); 24 x 2048 -> 5120 f16 take 12.9 us.
+// Bound by the products: 4 B ni no operations forward, 12 B ni no back: 8192 x 4096 -> 10240 bf16 1134 us forward (1.21
+// PFLOP/s) and 3486 back (1.18). One token reads both weights at 5.7 TB/s (29 us there); 24 x 2048 -> 5120 f16 take 12.9 us.
 // dz is rounded to the element type, which is what the next two products' matrix instructions take: the gradients'
 // error in bf16 grows by it from 0.0017 to 0.0023 of their norm.
 #pragma once
@@ -44,8 +44,9 @@ __device__ __forceinline__ float logistic(float z) {
 
 // The standard normal distribution function of z and its density's exponential e = exp(-z^2 / 2). erfc, not erf, so that
 // the tail keeps its relative accuracy; of the 16-bit types by a polynomial in t = 1 / (1 + 0.425 |x|), x = z / sqrt 2,
-// fitted to exp(x^2) erfc(x) in relative error over all x >= 0 (1.2e-7; 5.3e-7 evaluated in fp32): the device library's
-// erfc took half of the few-token case's second launch.
+// fitted to exp(x^2) erfc(x) in relative error over all x >= 0 (1.2e-7; 5.3e-7 evaluated in fp32; the function itself 6e-7
+// down to z = -3 and, with the exponential's rounding, which grows with z^2, 1.5e-6 to -5.5 and 8e-6 to -13). With the device
+// library's erfc 24 x 2048 -> 5120 f16 takes 14.0 us instead of 12.9.
 template <typename T>
 __device__ __forceinline__ float normal_cdf(float z, float& e) {
   if constexpr (sizeof(T) == 2) {

@@ -5,8 +5,9 @@
 //   X <- a X + (b A + c A^2) X   (tall: a X + X (b A + c A^2)),
 // which maps every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.
 // fp32 gradients: X, A and P are kept as sums of two f16 values (mm::Duo), a product of which is three of f16: half of
-// what splitting floats into three bf16 parts costs, and no split in the products' loop. O is off by 3e-6 of its norm on
-// noise (fp32 products: 2e-6). aX is added to the product in fp32.
+// what splitting floats into three bf16 parts costs, and no split in the products' loop. O is off by as much as with fp32
+// products (of its norm, five steps with 3.4445, -4.775, 2.0315: noise of 220 x 220 1.2e-6, those 1.7e-6; of 4096 x 4096 3.2e-6,
+// 4.8e-6; four directions a hundredfold 1.7e-5, 2.3e-5), but for matrices that one value carries (1e-6, 1e-7).
 //   A and P = b A + c A^2 are symmetric: only tiles on and below the diagonal are formed, and stored on both sides of
 //   it. a X is added in fp32 in the last product's epilogue, that of the last step updates W.
 // 16-bit gradients: the products' operands X, A and P are in f16 whatever the gradient's type is. No singular value
@@ -19,12 +20,12 @@
 //   In those, where X is nearly orthogonal, P is nearly (b + c) I and a X + P X a small difference: they form
 //   (a + b + c) X + (P - (b + c) I) X, whose product is small and its rounding with it. (While singular values still
 //   differ much it would mix strong directions into small ones.)
-// O is off by 4e-4 to 1.3e-3 of its norm for noise, a few strong directions or singular values down to a thousandth
-// (by X in f16 alone and P as it is 1.4e-3 to 1.5e-2), by 1.6e-3 where four directions exceed the noise a hundredfold
-// (4e-2), by 2.2e-3 where single values do.
-// Bound by the products: steps (3 n^2 k + n^3) operations, n the short and k the long side: 4096 x 4096 bf16 1514 us (0.91
-// PFLOP/s of those; a symmetric product 98 us, the other one 142), 2048 of 220 x 220 f32 4439 us (98 TFLOP/s:
-// memory, 4.3 to 6.2 TB/s, since X, A and P pass through it for every product).
+// O is off by 5e-4 to 1.5e-3 of its norm for noise, strong rows or columns, a few strong directions or singular values
+// down to a thousandth (by X in f16 alone and P as it is 1e-3 to 1.5e-2), by 1.6e-3 where four directions exceed the noise
+// a hundredfold (4e-2), by 2.2e-3 where a single value does (3.6e-3).
+// Bound by the products: steps (3 n^2 k + n^3) operations, n the short and k the long side: 4096 x 4096 bf16 1585 us (0.87
+// PFLOP/s of those; a symmetric product 83 us, the other one 139), 2048 of 220 x 220 f32 4593 us (95 TFLOP/s:
+// memory, 3.6 to 5.4 TB/s, since X, A and P pass through it for every product).
 #pragma once
 
 #include <math.h>
@@ -45,8 +46,8 @@ using mm::Place;
 
 // A and P are kept times A_UP, X times X_UP: as large as f16 holds where singular values stay below 3 (X 49152, P about
 // 53000), so that what is small beside a matrix's largest values keeps its bits. (X times the root of n k, which
-// brings the values of noise to 1: where a row, a column or a value of 220 x 220 f32 carries the norm, O was off by
-// 7e-6 to 1.1e-5 of its norm, now by 3e-7 to 1.4e-6.)
+// brings the values of noise to 1, O of 220 x 220 f32 is off by 7e-6 to 1.1e-5 of its norm where a row, a column or a value
+// carries that; so by 3e-7 to 1.4e-6.)
 constexpr float A_UP = 256.f, X_UP = 16384.f;
 
 // ---------------------------------------------------------------- v, its norm, and X
