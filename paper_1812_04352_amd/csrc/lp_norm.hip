@@ -15,8 +15,8 @@
 //   exceeds its spread by far loses nothing, and equal values leave 0 (without that a row of 223 values 3300 in fp32
 //   was off by hundredths). bf16 rows that a group holds do not need it: where the mean exceeds the spread, the values
 //   are multiples of one step, 2^9 at most, and 2^15 of them sum exactly; the mean is then off by half an fp32 step,
-//   2^-17 of the values' own, and the spread is at least that by the root of q: off by 2^-9.5 of it at most. (It takes 1 to 8 % of
-//   the time back, 8192 x 4096 f32 97 -> 98 us, 20000 x 700 f32 49 -> 52, 5003 x 1111 f16 19.1 -> 20.5.)
+//   2^-17 of the values' own, and the spread is at least that by the root of q: off by 2^-9.5 of it at most. (It takes
+//   1 to 8 % of the time back, 8192 x 4096 f32 97 -> 98 us, 20000 x 700 f32 49 -> 52, 5003 x 1111 f16 19.1 -> 20.5.)
 // Bound by memory: 8192 x 4096 bf16 24 us forward (5.6 TB/s), 64 us back with dr (4.2; the sum of 256 rows of partial sums,
 // one of each workgroup, of which there is one a CU, 4.7 of them; without the next rows requested ahead and with sums by
 // LDS exchanges 97). Rows that no group can hold are read again for every pass.
@@ -128,9 +128,9 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // Sums of up to M values (two or four) over a group of TPR threads, the same in all of them. Groups wider than a wave
-// exchange through the LDS, where every lane adds its group's waves in order; of many waves (M W > 16: 8192 x 4096 f32 back 98
-// us, 116 in order) every row of 16 lanes reads one a lane: `at` alternates between two halves, so that one barrier a sum is enough (a wave that writes a half
-// again has passed the barrier behind which all have read it).
+// exchange through the LDS, where every lane adds its group's waves in order; of many waves (M W > 16: 8192 x 4096 f32
+// back 98 us, 116 in order) every row of 16 lanes reads one a lane. `at` alternates between two halves, so that one
+// barrier a sum is enough (a wave that writes a half again has passed the barrier behind which all have read it).
 template <int TPR, int NT, int M>
 struct GroupSum {
   static constexpr int W = TPR / 64;  // waves of a group
